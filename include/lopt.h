@@ -251,8 +251,79 @@ lopt_status lopt_profile_enable(lopt_ctx* ctx, int on);
 lopt_status lopt_profile_read(lopt_ctx* ctx, double* ms_per_pass, uint64_t* n_steps);
 const char* lopt_pass_name(int pass);
 
+/* ---- The rest of the training loop around lopt_step: from the last hidden state to the gradients and the loss value that
+ * the step takes. These calls take no context and keep nothing between calls: every argument that is not marked _host is
+ * DEVICE memory owned by the caller, every call may run on any host thread and any stream, allocates nothing and can be
+ * captured into a HIP graph (with host arrays read while it is captured). They launch on the current device, to which
+ * `hip_stream` has to belong. Arrays need the alignment of their elements only; `ld_*` are distances between rows in elements. A
+ * workspace holds nothing that survives a call and needs no initial contents; 16-byte alignment. Inputs and outputs may not
+ * overlap unless it is said. Sums, statistics and norms are formed in 32 bits or more whatever the arrays' type, outputs
+ * are rounded once. Results are deterministic. A count of zero rows or tensors is a valid call. After a status other than
+ * LOPT_OK lopt_last_error(NULL) on the same thread has the message, and nothing was launched unless it is LOPT_EHIP. */
+typedef enum { LOPT_F32 = 0, LOPT_BF16 = 1, LOPT_F16 = 2 } lopt_type;
+
+/* Global gradient norm over a list of n tensors, and clipping:
+ *   norm = sqrt(sum over all elements of g^2),   c = min(1, max_norm / (norm + LOPT_CLIP_EPS)),   out = c g
+ * (the sum in 64 bits: no square overflows or vanishes). counts_host[n]: elements of each tensor, >= 0, in any number below 2^40;
+ * grads_host[n], out_host[n]: device pointers (null where the count is 0); types_host[n], out_types_host[n]: lopt_type of each.
+ * out_host null: the norm alone, nothing is scaled. out_host[i] may be grads_host[i] if its type is the same: gradients are
+ * clipped in place, and nothing is written where c is 1. norm: one float, not null.
+ * A norm that is NaN makes c and every output NaN; an infinite norm makes finite gradients 0 and infinite ones NaN.
+ * max_norm >= 0; +infinity: c = 1 for any finite norm.
+ * Errors: LOPT_EINVAL (null, type, alignment, max_norm, workspace too small), LOPT_ESHAPE (count), LOPT_EHIP. */
+#define LOPT_CLIP_EPS 1e-6f
+size_t lopt_clip_workspace(size_t n, const int64_t* counts_host);
+lopt_status lopt_clip_grads(size_t n, const int64_t* counts_host, const void* const* grads_host,
+                            const uint32_t* types_host, void* const* out_host, const uint32_t* out_types_host,
+                            float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Layer norm of `rows` rows of `cols` >= 1 elements of `type`:
+ *   mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),  y = (x - mean) rstd weight + bias
+ * weight, bias: `cols` elements of `weight_type`, each may be null (1 and 0). mean, rstd: `rows` floats for the backward pass, each may
+ * be null. y may be x (with the same ld). eps >= 0, finite.
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, cols or ld out of range; cols <= 2^31 - 1), LOPT_EHIP. */
+lopt_status lopt_layer_norm(const void* x, int64_t ld_x, const void* weight, const void* bias, void* y, int64_t ld_y,
+                            float* mean, float* rstd, int64_t rows, int64_t cols, float eps, uint32_t type,
+                            uint32_t weight_type, void* hip_stream);
+
+/* Its gradient. With xh = (x - mean) rstd and a = dy weight:
+ *   dx = rstd (a - sum(a) / cols - xh sum(a xh) / cols),   dweight = sum over rows of dy xh,   dbias = sum over rows of dy
+ * mean, rstd: as the forward pass left them. weight may be null (1). dx, dweight and dbias may be null (not wanted). dx may be
+ * dy or x (with the same ld). workspace: lopt_layer_norm_workspace bytes, may be null where that is 0.
+ * With zero rows dweight and dbias are 0. Errors: as lopt_layer_norm. */
+size_t lopt_layer_norm_workspace(int64_t rows, int64_t cols);
+lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight,
+                                     const float* mean, const float* rstd, void* dx, int64_t ld_dx, void* dweight,
+                                     void* dbias, int64_t rows, int64_t cols, uint32_t type, uint32_t weight_type,
+                                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Log probabilities under softmax(scale x) of each row x of `vocab` >= 1 logits: with m = max x, z = scale (x - m), S = sum e^z
+ *   logp = z[target] - ln S,   entropy = ln S - sum(e^z z) / S,   stats = (m, ln S) for the backward pass
+ *   top_logp, top_index [rows x top]: the `top` largest logits in order, the lowest index first among equals
+ * targets[rows], or null with logp null. A target equal to ignore_index gives logp 0; any other outside [0, vocab) gives NaN.
+ * Every output but stats may be null; top <= min(vocab, LOPT_TOP_MAX), top_logp and top_index go together. scale > 0, finite.
+ * Logits of -infinity are masked: probability 0. A row that is masked whole has stats (-infinity, -infinity), logp -infinity,
+ * entropy 0 and top alternatives -infinity in the order of their indices. A row with a NaN or +infinity has NaN for its logp,
+ * entropy and ln S and for every top_logp; its alternatives are ordered with NaN above +infinity.
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, vocab or ld out of range; vocab <= 2^31 - 1), LOPT_EHIP. */
+#define LOPT_TOP_MAX 32
+size_t lopt_token_logprobs_workspace(int64_t rows, int64_t vocab, uint32_t top);
+lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* targets, int64_t rows, int64_t vocab,
+                                uint32_t type, float scale, int64_t ignore_index, uint32_t top, float* logp, float* entropy,
+                                float* stats, float* top_logp, int64_t* top_index, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
+
+/* Their gradient: with p = e^(z - ln S), g = dlogp (0 where the target is ignored) and h = dentropy
+ *   dlogits = scale (g (1 at the target, else 0) - g p - h p (ln p + entropy))
+ * dlogp or dentropy may be null (0); targets may be null with dlogp, entropy with dentropy. The gradient of a row that is masked whole is 0;
+ * that of a row with a NaN, +infinity or a target out of range is NaN. dlogits may be logits (with the same ld). */
+lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const int64_t* targets, const float* stats,
+                                         const float* entropy, const float* dlogp, const float* dentropy, void* dlogits,
+                                         int64_t ld_d, int64_t rows, int64_t vocab, uint32_t type, float scale,
+                                         int64_t ignore_index, void* hip_stream);
+
 /* Message for the last non-OK status returned through this context ("" if none). With a
- * null ctx: the message of the last failed lopt_create / lopt_default_config on this thread. */
+ * null ctx: the message of the last failed call without a context on this thread. */
 const char* lopt_last_error(const lopt_ctx* ctx);
 
 #ifdef __cplusplus

@@ -20,7 +20,10 @@ STATIC_SCRATCH_BYTES = 64 << 20
 EXPORTS = ["lopt_default_config", "lopt_weights_count", "lopt_create", "lopt_destroy", "lopt_state_bytes",
            "lopt_init_state", "lopt_step", "lopt_step_static", "lopt_set_loss", "lopt_stats_offsets",
            "lopt_last_error",
-           "lopt_profile_enable", "lopt_profile_read", "lopt_pass_name"]
+           "lopt_profile_enable", "lopt_profile_read", "lopt_pass_name",
+           "lopt_clip_workspace", "lopt_clip_grads", "lopt_layer_norm", "lopt_layer_norm_workspace",
+           "lopt_layer_norm_backward", "lopt_token_logprobs_workspace", "lopt_token_logprobs",
+           "lopt_token_logprobs_backward"]
 
 
 class LoptError(RuntimeError):
@@ -85,6 +88,23 @@ def lib() -> C.CDLL:
     L.lopt_profile_read.restype = C.c_int
     L.lopt_pass_name.argtypes = [C.c_int]
     L.lopt_pass_name.restype = C.c_char_p
+    i64, u32, f32 = C.c_int64, C.c_uint32, C.c_float
+    L.lopt_clip_workspace.argtypes = [sz, vp]
+    L.lopt_clip_workspace.restype = sz
+    L.lopt_clip_grads.argtypes = [sz, vp, vp, vp, vp, vp, f32, vp, vp, sz, vp]
+    L.lopt_clip_grads.restype = C.c_int
+    L.lopt_layer_norm.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, f32, u32, u32, vp]
+    L.lopt_layer_norm.restype = C.c_int
+    L.lopt_layer_norm_workspace.argtypes = [i64, i64]
+    L.lopt_layer_norm_workspace.restype = sz
+    L.lopt_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i64, i64, u32, u32, vp, sz, vp]
+    L.lopt_layer_norm_backward.restype = C.c_int
+    L.lopt_token_logprobs_workspace.argtypes = [i64, i64, u32]
+    L.lopt_token_logprobs_workspace.restype = sz
+    L.lopt_token_logprobs.argtypes = [vp, i64, vp, i64, i64, u32, f32, i64, u32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.lopt_token_logprobs.restype = C.c_int
+    L.lopt_token_logprobs_backward.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, u32, f32, i64, vp]
+    L.lopt_token_logprobs_backward.restype = C.c_int
     L.lopt_last_error.argtypes = [vp]
     L.lopt_last_error.restype = C.c_char_p
     _lib = L

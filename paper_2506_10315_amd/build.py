@@ -22,6 +22,9 @@ UNITS = [
     ("lopt_apply_f16s.hip", "apply_f16s", []),
     ("lopt_apply_velo4.hip", "apply_velo4", []),
     ("lopt_apply_fc4x.hip", "apply_fc4x", []),
+    ("lopt_clip.hip", "clip", []),
+    ("lopt_layer_norm.hip", "layer_norm", []),
+    ("lopt_logprobs.hip", "logprobs", []),
 ]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

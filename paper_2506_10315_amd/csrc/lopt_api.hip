@@ -3,6 +3,7 @@
 #include <atomic>
 #include <cfloat>
 #include <cmath>
+#include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -131,6 +132,21 @@ std::vector<float> equilibrate_small_fc(const float* w, int H) {
 }
 
 }  // namespace
+
+// Status of a call without a context. The message may be lost where there is no memory for it; nothing throws.
+lopt_status lopt::fail_call(lopt_status st, const char* fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    g_last_error = buf;
+  } catch (...) {
+    g_last_error.clear();
+  }
+  return st;
+}
 
 struct lopt_ctx {
   lopt_config cfg;

@@ -172,4 +172,7 @@ void launch_apply_velo4(const Launch&, const StepArgs&, bool update_state, hipSt
 // feats not null: no k_finalize has run, every workgroup forms its tensor's scales and first layer (Plan::fold_finalize)
 void launch_apply_f16s(const Launch&, const StepArgs&, const WeightsDev&, const StepFeats* feats, bool update_state, hipStream_t);
 
+// Calls without a context (include/lopt.h): keeps the message for lopt_last_error(NULL), returns `st`.
+lopt_status fail_call(lopt_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
 }  // namespace lopt

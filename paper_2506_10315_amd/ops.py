@@ -1,0 +1,304 @@
+"""The operators of a training loop around the optimizer step, on torch tensors: layer norm, token log probabilities with
+entropy and top alternatives, their gradients, and clipping by the global gradient norm.
+
+Nothing numerical happens here: every function checks its tensors, allocates outputs and workspace, and hands pointers to the
+call of the same name in include/lopt.h (formulas, masks and special values are described there) on the current stream.
+Tensors are CUDA tensors of float32, bfloat16 or float16; `layer_norm` and `token_logprobs` take part in autograd, the
+`*_forward` and `*_backward` functions are the passes by themselves."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Iterable, List, NamedTuple, Optional, Sequence, Tuple, Union
+
+import torch
+
+from .binding import _check, lib
+
+__all__ = ["clip_grads", "clip_grad_norm_", "grad_norm", "layer_norm", "layer_norm_forward", "layer_norm_backward",
+           "TokenLogprobs", "token_logprobs", "token_logprobs_forward", "token_logprobs_backward", "TOP_MAX"]
+
+TOP_MAX = 32          # LOPT_TOP_MAX
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # lopt_type
+
+
+def _type(name: str, t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not a CUDA tensor")
+    k = _TYPES.get(t.dtype)
+    if k is None:
+        raise ValueError(f"{name} is of {t.dtype}; float32, bfloat16 or float16 is needed")
+    return k
+
+
+def _expect(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape) -> torch.Tensor:
+    """`t` on `like`'s device with this type and shape, contiguous (copied where it is not)."""
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}; {tuple(shape)} of {dtype} is needed")
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _matrix(name: str, t: torch.Tensor) -> Tuple[torch.Tensor, int, int, int]:
+    """(tensor, rows, columns, elements from row to row) of `t` seen as rows of its last dimension. A 2-D tensor keeps its row
+    stride; any other layout whose rows are not evenly spaced runs of adjacent elements is copied."""
+    if t.dim() == 0:
+        raise ValueError(f"{name} has no dimension")
+    cols = t.shape[-1]
+    if cols == 0:
+        raise ValueError(f"{name} has rows of no elements")
+    if not t.is_contiguous():
+        if t.dim() == 2 and (t.stride(1) == 1 or cols == 1):
+            return t, t.shape[0], cols, t.stride(0)
+        t = t.contiguous()
+    return t, t.numel() // cols, cols, cols
+
+
+def _run(fn, device: torch.device, *args):
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, torch.cuda.current_stream().cuda_stream)
+    if status:
+        _check(status)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(nbytes: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+# ---------------------------------------------------------------------------------------------- gradient norm and clipping
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether the elements fill one run of memory, in any order of the dimensions."""
+    if t.is_contiguous():
+        return True
+    run = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != run:
+            return False
+        run *= size
+    return True
+
+
+def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], max_norm: float) -> torch.Tensor:
+    n = len(grads)
+    if n == 0:
+        raise ValueError("no gradients")
+    device = grads[0].device
+    for name, ts in (("grads", grads), ("out", out or ())):
+        for t in ts:
+            if t.device != device or not t.is_cuda or t.dtype not in _TYPES or t.layout != torch.strided:
+                raise ValueError(f"{name}: CUDA tensors of float32, bfloat16 or float16 on one device are needed, not "
+                                 f"{t.dtype} on {t.device}")
+            if not _dense(t):
+                raise ValueError(f"{name}: a tensor of strides {t.stride()} does not fill one run of memory")
+    if out is not None:
+        if len(out) != n:
+            raise ValueError(f"{len(out)} outputs for {n} gradients")
+        for g, o in zip(grads, out):
+            if g.shape != o.shape or (g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous())):
+                raise ValueError("an output's shape or strides are not its gradient's")
+    counts = (C.c_int64 * n)(*[g.numel() for g in grads])
+    gp = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
+    gt = (C.c_uint32 * n)(*[_TYPES[g.dtype] for g in grads])
+    op = ot = None
+    if out is not None:
+        op = (C.c_void_p * n)(*[o.data_ptr() for o in out])
+        ot = (C.c_uint32 * n)(*[_TYPES[o.dtype] for o in out])
+    L = lib()
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    ws = _workspace(L.lopt_clip_workspace(n, counts), device)
+    _run(L.lopt_clip_grads, device, n, counts, gp, gt, op, ot, float(max_norm), norm.data_ptr(), _ptr(ws), ws.numel())
+    return norm
+
+
+@torch.no_grad()
+def grad_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
+    """The Euclidean norm of all elements of all tensors: a float32 tensor without dimensions, on their device."""
+    return _clip(list(grads), None, 0.0)
+
+
+@torch.no_grad()
+def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
+               out: Optional[Sequence[torch.Tensor]] = None) -> Tuple[List[torch.Tensor], torch.Tensor]:
+    """(clipped gradients, norm before clipping): every gradient times min(1, max_norm / (norm + 1e-6)). `out` receives
+    them, in float32 or any type this module takes; by default new float32 tensors, which is what LearnedOptimizer.step takes.
+    The gradients stay as they are."""
+    grads = list(grads)
+    out = [torch.empty_like(g, dtype=torch.float32) for g in grads] if out is None else list(out)
+    return out, _clip(grads, out, max_norm)
+
+
+@torch.no_grad()
+def clip_grad_norm_(parameters: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float) -> torch.Tensor:
+    """Clips the `.grad` of the parameters in place and returns the norm before. Parameters without a gradient are
+    skipped."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
+    grads = [p.grad for p in parameters if p.grad is not None]
+    return _clip(grads, grads, max_norm)
+
+
+# ---------------------------------------------------------------------------------------------- layer norm
+
+def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                       eps: float = 1e-5) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(y, mean, rstd) over the last dimension of `x`; y has x's type, mean and rstd are float32 of x's other dimensions."""
+    kind = _type("x", x)
+    x2, rows, cols, ld = _matrix("x", x)
+    wtype = None
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            if wtype is not None and t.dtype != wtype:
+                raise ValueError(f"bias is of {t.dtype}, weight of {wtype}")
+            wtype = t.dtype
+            _type(name, t)
+    if weight is not None:
+        weight = _expect("weight", weight, x, wtype, (cols,))
+    if bias is not None:
+        bias = _expect("bias", bias, x, wtype, (cols,))
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+    mean, rstd = stats[0], stats[1]
+    _run(lib().lopt_layer_norm, x.device, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(),
+         rows, cols, eps, kind, _TYPES[wtype] if wtype is not None else 0)
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                        need: Tuple[bool, bool, bool] = (True, True, True), bias_type: Optional[torch.dtype] = None):
+    """(dx, dweight, dbias) of layer_norm_forward; `need` says which are wanted, the others are None. dweight and dbias have the
+    weight's type (without a weight bias_type, by default float32)."""
+    kind = _type("x", x)
+    x2, rows, cols, ld = _matrix("x", x)
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
+        raise ValueError(f"dy is {tuple(dy.shape)} of {dy.dtype} on {dy.device}; x is {tuple(x.shape)} of {x.dtype} on {x.device}")
+    dy2, _, _, ld_dy = _matrix("dy", dy)
+    wtype = weight.dtype if weight is not None else bias_type or torch.float32
+    if wtype not in _TYPES:
+        raise ValueError(f"weights of {wtype}; float32, bfloat16 or float16 is needed")
+    if weight is not None:
+        weight = _expect("weight", weight, x, wtype, (cols,))
+    mean = _expect("mean", mean, x, torch.float32, x.shape[:-1])
+    rstd = _expect("rstd", rstd, x, torch.float32, x.shape[:-1])
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
+    dw = torch.empty(cols, dtype=wtype, device=x.device) if need[1] else None
+    db = torch.empty(cols, dtype=wtype, device=x.device) if need[2] else None
+    L = lib()
+    ws = _workspace(L.lopt_layer_norm_workspace(rows, cols), x.device) if need[1] or need[2] else None
+    _run(L.lopt_layer_norm_backward, x.device, dy2.data_ptr(), ld_dy, x2.data_ptr(), ld, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx), cols,
+         _ptr(dw), _ptr(db), rows, cols, kind, _TYPES[wtype], _ptr(ws), 0 if ws is None else ws.numel())
+    return dx, dw, db
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = layer_norm_forward(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.bias_type = None if bias is None else bias.dtype
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = layer_norm_backward(dy, x, weight, mean, rstd, ctx.needs_input_grad[:3], ctx.bias_type)
+        return dx, dw, db, None
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
+    """Layer norm over the last dimension, with gradients for x, weight and bias."""
+    return _LayerNorm.apply(x, weight, bias, eps)
+
+
+# ---------------------------------------------------------------------------------------------- token log probabilities
+
+class TokenLogprobs(NamedTuple):
+    logp: Optional[torch.Tensor]        # of the given tokens; 0 where ignored
+    entropy: Optional[torch.Tensor]
+    top_logp: Optional[torch.Tensor]    # [..., top], best first
+    top_index: Optional[torch.Tensor]   # int64
+    stats: torch.Tensor                 # [..., 2]: largest logit and ln sum e^z, for the backward pass
+
+
+def token_logprobs_forward(logits: torch.Tensor, targets: Optional[torch.Tensor], scale: float = 1.0, top: int = 0, ignore_index: int = -100,
+                           entropy: bool = True) -> TokenLogprobs:
+    """Log probabilities of `targets` (int64, logits.shape[:-1]; None: not wanted) under softmax(scale * logits), the entropy
+    and the `top` best alternatives of every row."""
+    kind = _type("logits", logits)
+    x, rows, vocab, ld = _matrix("logits", logits)
+    shape = logits.shape[:-1]
+    if targets is not None:
+        targets = _expect("targets", targets, logits, torch.int64, shape)
+    if not 0 <= top <= min(vocab, TOP_MAX):
+        raise ValueError(f"top={top} outside [0, {min(vocab, TOP_MAX)}]")
+    dev = logits.device
+    logp = torch.empty(shape, dtype=torch.float32, device=dev) if targets is not None else None
+    ent = torch.empty(shape, dtype=torch.float32, device=dev) if entropy else None
+    stats = torch.empty(shape + (2,), dtype=torch.float32, device=dev)
+    top_logp = torch.empty(shape + (top,), dtype=torch.float32, device=dev) if top else None
+    top_index = torch.empty(shape + (top,), dtype=torch.int64, device=dev) if top else None
+    L = lib()
+    ws = _workspace(L.lopt_token_logprobs_workspace(rows, vocab, top), dev)
+    _run(L.lopt_token_logprobs, dev, x.data_ptr(), ld, _ptr(targets), rows, vocab, kind, scale, ignore_index, top, _ptr(logp), _ptr(ent), stats.data_ptr(),
+         _ptr(top_logp), _ptr(top_index), _ptr(ws), 0 if ws is None else ws.numel())
+    return TokenLogprobs(logp, ent, top_logp, top_index, stats)
+
+
+def token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, entropy: Optional[torch.Tensor],
+                            dlogp: Optional[torch.Tensor], dentropy: Optional[torch.Tensor] = None, scale: float = 1.0,
+                            ignore_index: int = -100) -> torch.Tensor:
+    """The logits' gradient from those of logp and entropy (either may be None), in the logits' type. `stats` and `entropy` are
+    the forward pass's; `entropy` is needed with `dentropy` only, `targets` with `dlogp` only."""
+    kind = _type("logits", logits)
+    x, rows, vocab, ld = _matrix("logits", logits)
+    shape = logits.shape[:-1]
+    stats = _expect("stats", stats, logits, torch.float32, shape + (2,))
+    if dlogp is not None:
+        dlogp = _expect("dlogp", dlogp, logits, torch.float32, shape)
+        if targets is None:
+            raise ValueError("dlogp without targets")
+        targets = _expect("targets", targets, logits, torch.int64, shape)
+    if dentropy is not None:
+        dentropy = _expect("dentropy", dentropy, logits, torch.float32, shape)
+        if entropy is None:
+            raise ValueError("dentropy without entropy")
+        entropy = _expect("entropy", entropy, logits, torch.float32, shape)
+    dx = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _run(lib().lopt_token_logprobs_backward, logits.device, x.data_ptr(), ld, _ptr(targets), stats.data_ptr(), _ptr(entropy), _ptr(dlogp), _ptr(dentropy),
+         dx.data_ptr(), vocab, rows, vocab, kind, scale, ignore_index)
+    return dx
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, scale, top, ignore_index):
+        r = token_logprobs_forward(logits, targets, scale, top, ignore_index)
+        ctx.save_for_backward(logits, targets, r.stats, r.entropy)
+        ctx.scale, ctx.ignore_index = scale, ignore_index
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*[t for t in (r.top_logp, r.top_index, r.stats) if t is not None])
+        return r.logp, r.entropy, r.top_logp, r.top_index, r.stats
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogp, dentropy, *_):
+        if dlogp is None and dentropy is None:
+            return None, None, None, None, None
+        logits, targets, stats, entropy = ctx.saved_tensors
+        dx = token_logprobs_backward(logits, targets, stats, entropy, dlogp, dentropy, ctx.scale, ctx.ignore_index)
+        return dx, None, None, None, None
+
+
+def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], scale: float = 1.0, top: int = 0,
+                   ignore_index: int = -100) -> TokenLogprobs:
+    """token_logprobs_forward with gradients for the logits from logp and entropy. The mean of -logp over the tokens that are
+    not ignored is the loss that LearnedOptTorch.step takes."""
+    return TokenLogprobs(*_TokenLogprobs.apply(logits, targets, scale, top, ignore_index))

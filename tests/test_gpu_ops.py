@@ -1,0 +1,789 @@
+"""The training-loop operators (layer norm, token log probabilities, gradient clipping) against their formulas in float64
+on the host, through the torch functions and through the C boundary.
+
+Tolerances are bounds derived from the order of the operations, not fitted: `U` is the unit roundoff of float32, in which the
+kernels sum, `depth(n)` the longest chain of additions that any of n terms goes through (lanes add up to 32 + n / 256 terms one
+after the other, and the tree over lanes, wavefronts and pieces of a row has fewer than 24 levels), and every output gets its type's own rounding."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = ["fp32", "bf16", "fp16"]
+ROUND = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+TINY = {"fp32": 2.0 ** -149, "bf16": 2.0 ** -133, "fp16": 2.0 ** -24}     # smallest subnormal
+
+
+def depth(n):
+    return 56 + n // 256
+
+
+def tt(kind):
+    import torch
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[kind]
+
+
+def ops():
+    import paper_2506_10315_amd as P
+    return P.ops
+
+
+def dev(a, kind):
+    """float array -> GPU tensor of `kind`; the values that it holds, in float64."""
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(tt(kind))
+    return t.to("cuda:0"), t.double().numpy()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(got, want, tol, what):
+    got = host(got) if not isinstance(got, np.ndarray) else got
+    assert got.shape == want.shape, what
+    if want.dtype == np.float64:   # a result beyond float32's range is an infinity there
+        want = np.where(np.abs(want) > 3.4028235677973366e38, np.copysign(np.inf, want), want)
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    with np.errstate(invalid="ignore"):
+        bad = ~same & ~(np.abs(got - want) <= tol)
+    if bad.any():
+        i = tuple(int(v) for v in np.argwhere(bad)[0])
+        t = np.broadcast_to(tol, want.shape)[i]
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.size} off, first at {i}: {got[i]!r}, expected {want[i]!r} +- {t!r}")
+
+
+# ---------------------------------------------------------------------------------------------- gradient norm and clipping
+
+def clip_case(grads, max_norm):
+    norm = math.sqrt(sum(float((g * g).sum()) for g in grads))
+    with np.errstate(invalid="ignore", over="ignore"):
+        c = min(1.0, max_norm / (norm + 1e-6)) if not math.isnan(norm) else math.nan
+    return norm, c
+
+
+CLIP_LISTS = {
+    "one": [(1,)],
+    "empty tensors": [(0,), (5,), (3, 0), (1,)],
+    "toy": [(256, 256), (256,), (64, 256)],
+    "odd": [(7, 13), (16384,), (16385,), (3,), (127, 129), (1, 1), (65537,)],
+    "many": [(1 + 37 * i % 61,) for i in range(700)],
+    "one large": [(1531, 3001)],
+}
+
+
+@pytest.mark.parametrize("out_kind", ["same", "fp32"])
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("name", list(CLIP_LISTS))
+def test_clip(name, kind, out_kind):
+    r = np.random.default_rng(len(name))
+    pairs = [dev(r.standard_normal(s) * 10.0 ** r.uniform(-3, 0), kind) for s in CLIP_LISTS[name]]
+    grads = [a for _, a in pairs]
+    norm0, _ = clip_case(grads, 1.0)
+    ok = kind if out_kind == "same" else "fp32"
+    for max_norm in (0.37 * norm0, 2.0 * norm0, math.inf, 0.0):
+        norm, c = clip_case(grads, max_norm)
+        import torch
+        out = [torch.empty_like(t, dtype=tt(ok)) for t, _ in pairs]
+        res, n = ops().clip_grads([t for t, _ in pairs], max_norm, out=out)
+        close(n, np.array(norm), 2 * U * norm, "norm")
+        for i, (o, g) in enumerate(zip(res, grads)):
+            assert o is out[i]
+            close(o, c * g, (6 * U + ROUND[ok]) * abs(c * g) + TINY[ok], f"tensor {i}")
+        assert [np.array_equal(host(t), a) for t, a in pairs] == [True] * len(pairs)
+    close(ops().grad_norm([t for t, _ in pairs]), np.array(norm0), 2 * U * norm0, "norm alone")
+
+
+def test_clip_mixed_types_views_and_layouts():
+    import torch
+    r = np.random.default_rng(3)
+    ts, vals = [], []
+    for i, kind in enumerate(["fp32", "bf16", "fp16", "bf16", "fp32", "fp16"]):
+        t, a = dev(r.standard_normal(20011), kind)
+        ts.append(t[i + 1:20000 + i])          # starts off every grid
+        vals.append(a[i + 1:20000 + i])
+    t, a = dev(r.standard_normal((33, 17)), "fp32")
+    ts.append(t.t())                            # dense, other order of dimensions
+    vals.append(a.T)
+    norm, c = clip_case(vals, 1.5)
+    res, n = ops().clip_grads(ts, 1.5)
+    close(n, np.array(norm), 2 * U * norm, "norm")
+    for i, (o, v) in enumerate(zip(res, vals)):
+        assert o.dtype == torch.float32 and o.stride() == ts[i].stride()
+        close(o, c * v, 6 * U * abs(c * v), f"tensor {i}")
+    # outputs whose offset is not the input's
+    buf = torch.full((20000 * 6 + 1,), 7.0, device="cuda:0")
+    outs = [buf[20000 * i + 1:20000 * i + 20000] for i in range(6)]
+    ops().clip_grads(ts[:6], 1.5, out=outs)
+    _, c = clip_case(vals[:6], 1.5)
+    for i in range(6):
+        close(outs[i], c * vals[i], 6 * U * abs(c * vals[i]), f"view {i}")
+        assert float(buf[20000 * i]) == 7.0
+    assert float(buf[-1]) == 7.0
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_clip_in_place(kind):
+    import torch
+    r = np.random.default_rng(5)
+    params, vals = [], []
+    for s in [(300, 257), (65,), (1,), (0,)]:
+        p = torch.nn.Parameter(torch.zeros(s, device="cuda:0", dtype=tt(kind)))
+        p.grad, a = dev(r.standard_normal(s), kind)
+        params.append(p)
+        vals.append(a)
+    params.append(torch.nn.Parameter(torch.zeros(3, device="cuda:0")))   # no gradient
+    norm, c = clip_case(vals, 2.5)
+    n = ops().clip_grad_norm_(params, 2.5)
+    close(n, np.array(norm), 2 * U * norm, "norm")
+    for p, a in zip(params, vals):
+        close(p.grad, c * a, (6 * U + ROUND[kind]) * abs(c * a) + TINY[kind], "gradient")
+    before = [p.grad.clone() for p in params[:-1]]
+    ops().clip_grad_norm_(params, 1e9)
+    assert all(torch.equal(a, p.grad) for a, p in zip(before, params))
+    assert params[-1].grad is None
+
+
+def test_clip_special_values():
+    import torch
+    f = lambda *v: torch.tensor(v, device="cuda:0")
+    big = f(3e38, -3e38, 1e-30)                       # squares beyond float32
+    (o,), n = ops().clip_grads([big], 1.0)
+    assert float(n) == pytest.approx(math.sqrt(2) * 3e38 if math.sqrt(2) * 3e38 < 3.4028235e38 else math.inf)
+    (o,), n = ops().clip_grads([f(3e30, -4e30)], 1.0)
+    close(n, np.array(5e30), 1e24, "norm")
+    close(o, np.array([0.6, -0.8]), 1e-6, "large")
+    (o,), n = ops().clip_grads([f(3e-30, 4e-30)], 1.0)   # squares below float32
+    close(n, np.array(5e-30), 1e-36, "norm")
+    assert o.tolist() == f(3e-30, 4e-30).tolist()
+    (o,), n = ops().clip_grads([f(0.0, -0.0)], 0.0)
+    assert float(n) == 0.0 and o.tolist() == [0.0, 0.0]
+    (a, b), n = ops().clip_grads([f(1.0, math.nan), f(2.0)], 1.0)
+    assert math.isnan(float(n)) and bool(torch.isnan(a).all()) and bool(torch.isnan(b).all())
+    (a, b), n = ops().clip_grads([f(1.0, math.inf), f(2.0)], 1.0)
+    assert float(n) == math.inf and a[0] == 0 and bool(torch.isnan(a[1])) and b[0] == 0
+
+
+def test_clip_more_than_32_bits_of_elements():
+    import torch
+    n = (1 << 31) + 70001
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda:0")
+    g[5] = 3.0
+    g[-1] = 4.0
+    g[1 << 31] = 12.0
+    norm = ops().clip_grad_norm_([_param(g)], 6.5)
+    assert float(norm) == 13.0
+    want = (torch.tensor([3.0, 12.0, 4.0]) * float(np.float32(6.5) / (np.float32(13.0) + np.float32(1e-6)))).bfloat16()
+    assert torch.equal(torch.stack([g[5], g[1 << 31], g[-1]]).cpu(), want)
+    assert int((g != 0).sum()) == 3
+
+
+def _param(g):
+    class P:   # what clip_grad_norm_ looks at
+        grad = g
+    return P
+
+
+# ---------------------------------------------------------------------------------------------- layer norm
+
+def norm_exact(x, w, b, eps):
+    mean = x.mean(1)
+    d = x - mean[:, None]
+    var = (d * d).mean(1)
+    rstd = 1.0 / np.sqrt(var + eps)
+    xh = d * rstd[:, None]
+    y = xh * (1.0 if w is None else w) + (0.0 if b is None else b)
+    return y, mean, rstd, xh, var
+
+
+def norm_tolerance(x, w, b, eps, kind):
+    """Bounds of the forward pass for (y, mean, rstd)."""
+    y, mean, rstd, xh, var = norm_exact(x, w, b, eps)
+    D = depth(x.shape[1])
+    dm = (D + 1) * U * np.abs(x).mean(1) + U * np.abs(mean)
+    rel = 0.5 * ((D + 6) * U + (dm * dm) / (var + eps)) + 3 * U
+    w_ = 1.0 if w is None else np.abs(w)
+    dxh = rstd[:, None] * (dm[:, None] + U * np.abs(x - mean[:, None])) + np.abs(xh) * (rel[:, None] + 3 * U)
+    ty = 1.01 * (w_ * dxh + 3 * U * (np.abs(xh) * w_ + (0 if b is None else np.abs(b)))) + ROUND[kind] * np.abs(y) * 1.01 + TINY[kind]
+    return ty, 1.01 * dm + TINY["fp32"], 1.01 * rel * rstd
+
+
+NORM_SHAPES = [(1, 1), (3, 1), (2, 2), (5, 7), (1, 16), (33, 17), (9, 63), (4, 64), (13, 65), (7, 100), (21, 127), (3, 257), (1, 1024), (70, 768),
+               (5, 1023), (11, 1531), (3, 2049), (2, 4097), (2, 8200), (2, 16384), (1, 33000), (2, 70001), (600, 48), (2500, 5)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+def test_layer_norm_forward(rows, cols, kind):
+    r = np.random.default_rng(rows * 1000 + cols)
+    x, xv = dev(r.standard_normal((rows, cols)) * np.exp(r.standard_normal((rows, 1))) + r.standard_normal((rows, 1)), kind)
+    for wkind, have_w, have_b in (("fp32", True, True), (kind, True, False), ("bf16", False, True), ("fp32", False, False)):
+        w, wv = dev(1 + 0.3 * r.standard_normal(cols), wkind) if have_w else (None, None)
+        b, bv = dev(0.3 * r.standard_normal(cols), wkind) if have_b else (None, None)
+        y, mean, rstd = ops().layer_norm_forward(x, w, b, eps=1e-5)
+        want = norm_exact(xv, wv, bv, float(np.float32(1e-5)))
+        tol = norm_tolerance(xv, wv, bv, float(np.float32(1e-5)), kind)
+        for got, a, t, what in zip((y, mean, rstd), want, tol, ("y", "mean", "rstd")):
+            close(got, a, t, f"{what} weights {wkind} {have_w} {have_b}")
+
+
+def test_layer_norm_forward_strides_offsets_and_margins():
+    import torch
+    from paper_2506_10315_amd import binding as B
+    r = np.random.default_rng(8)
+    for kind in TYPES:
+        for cols, ld in ((100, 107), (768, 771), (1531, 1600), (8, 9)):
+            x, xv = dev(r.standard_normal((12, ld)), kind)
+            for off in (0, 1, 3):
+                c = cols - 5
+                want = norm_exact(xv[:, off:off + c], None, None, 0.0)
+                tol = norm_tolerance(xv[:, off:off + c], None, None, 0.0, kind)
+                y, mean, rstd = ops().layer_norm_forward(x[:, off:off + c], eps=0.0)
+                close(y, want[0], tol[0], "view")
+                # an output with margins, rows `ld + 2` apart
+                buf = torch.full((12, ld + 2), 3.0, dtype=tt(kind), device="cuda:0")
+                es = buf.element_size()
+                st = B.lib().lopt_layer_norm(x.data_ptr() + off * es, ld, None, None, buf.data_ptr() + 2 * es, ld + 2, None, None, 12, c, 0.0,
+                                             B_type(kind), 0, torch.cuda.current_stream().cuda_stream)
+                assert st == 0
+                close(buf[:, 2:2 + c], want[0], tol[0], "margins")
+                assert bool((buf[:, :2] == 3).all()) and bool((buf[:, 2 + c:] == 3).all())
+    # three dimensions, transposed: copied
+    x, xv = dev(r.standard_normal((4, 5, 36)), "fp32")
+    y, mean, rstd = ops().layer_norm_forward(x.transpose(0, 1))
+    xt = np.ascontiguousarray(xv.transpose(1, 0, 2))
+    close(y.reshape(20, 36), norm_exact(xt.reshape(20, 36), None, None, 1e-5)[0], norm_tolerance(xt.reshape(20, 36), None, None, 1e-5, "fp32")[0], "transposed")
+    assert mean.shape == (5, 4)
+
+
+def B_type(kind):
+    return TYPES.index(kind)
+
+
+def test_layer_norm_special_rows():
+    import torch
+    x = torch.randn(6, 300, device="cuda:0")
+    x[1] = 5.0                      # no spread: rstd = 1/sqrt(eps)
+    x[2, 7] = math.nan
+    x[3, 7] = math.inf
+    x[4] = 0.0
+    y, mean, rstd = ops().layer_norm_forward(x, eps=1e-5)
+    assert bool((y[1] == 0).all()) and float(mean[1]) == 5.0 and float(rstd[1]) == pytest.approx(1e-5 ** -0.5, rel=1e-6)
+    assert bool(torch.isnan(y[2]).all()) and bool(torch.isnan(y[3]).all())
+    assert bool((y[4] == 0).all())
+    assert bool(torch.isfinite(y[[0, 5]]).all())
+    # a large common offset costs no more than the rounding of the mean
+    z = (torch.randn(4, 1000) + 1000.0).cuda()
+    xv = host(z)
+    y, mean, rstd = ops().layer_norm_forward(z)
+    tol = norm_tolerance(xv, None, None, 1e-5, "fp32")
+    close(y, norm_exact(xv, None, None, 1e-5)[0], tol[0], "offset")
+    close(rstd, norm_exact(xv, None, None, 1e-5)[2], tol[2], "offset rstd")
+
+
+def test_layer_norm_zero_rows():
+    import torch
+    y, mean, rstd = ops().layer_norm_forward(torch.empty(0, 64, device="cuda:0"))
+    assert y.shape == (0, 64) and mean.shape == (0,)
+    dx, dw, db = ops().layer_norm_backward(y, y, torch.ones(64, device="cuda:0"), mean, rstd)
+    assert dx.shape == (0, 64) and dw.tolist() == [0.0] * 64 and db.tolist() == [0.0] * 64
+
+
+def norm_back_exact(dy, x, w, mean, rstd):
+    xh = (x - mean[:, None]) * rstd[:, None]
+    a = dy * (1.0 if w is None else w)
+    m1, m2 = a.mean(1), (a * xh).mean(1)
+    dx = rstd[:, None] * (a - m1[:, None] - xh * m2[:, None])
+    return dx, (dy * xh).sum(0), dy.sum(0), xh, a, m1, m2
+
+
+def norm_back_tolerance(dy, x, w, mean, rstd, kind, wkind):
+    dx, dw, db, xh, a, m1, m2 = norm_back_exact(dy, x, w, mean, rstd)
+    n = x.shape[1]
+    D = depth(n)
+    d1 = (D + 3) * U * np.abs(a).mean(1)
+    d2 = (D + 6) * U * np.abs(a * xh).mean(1)
+    tx = rstd[:, None] * (5 * U * np.abs(a) + 3 * U * np.abs(m1)[:, None] + 8 * U * np.abs(xh * m2[:, None]) + d1[:, None] + np.abs(xh) * d2[:, None])
+    # a lane adds at most 144 rows one after the other (lists of up to 30 000 rows), then the tree
+    Dr = min(x.shape[0], 144) + 24
+    tw = (Dr + 5) * U * np.abs(dy * xh).sum(0)
+    tb = (Dr + 2) * U * np.abs(dy).sum(0)
+    return (1.01 * tx + 1.01 * ROUND[kind] * np.abs(dx) + TINY[kind], 1.01 * tw + 1.01 * ROUND[wkind] * np.abs(dw) + TINY[wkind],
+            1.01 * tb + 1.01 * ROUND[wkind] * np.abs(db) + TINY[wkind])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES + [(3000, 96), (1301, 333), (9000, 8)])
+def test_layer_norm_backward(rows, cols, kind):
+    import torch
+    r = np.random.default_rng(rows * 1000 + cols)
+    x, xv = dev(r.standard_normal((rows, cols)) * np.exp(r.standard_normal((rows, 1))) + r.standard_normal((rows, 1)), kind)
+    dy, dyv = dev(r.standard_normal((rows, cols)), kind)
+    mean = torch.from_numpy(xv.mean(1).astype(np.float32)).cuda()
+    rstd = torch.from_numpy((1 / np.sqrt(xv.var(1) + 1e-5)).astype(np.float32)).cuda()
+    mv, rv = host(mean), host(rstd)
+    for wkind, have_w in (("fp32", True), (kind, True), ("fp32", False)):
+        w, wv = dev(1 + 0.3 * r.standard_normal(cols), wkind) if have_w else (None, None)
+        got = ops().layer_norm_backward(dy, x, w, mean, rstd)
+        want = norm_back_exact(dyv, xv, wv, mv, rv)
+        tol = norm_back_tolerance(dyv, xv, wv, mv, rv, kind, wkind)
+        for g, a, t, what in zip(got, want, tol, ("dx", "dw", "db")):
+            close(g, a, t, f"{what} weights {wkind} {have_w}")
+        again = ops().layer_norm_backward(dy, x, w, mean, rstd)
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+        for need in ((True, False, False), (False, True, False), (False, False, True)):
+            part = ops().layer_norm_backward(dy, x, w, mean, rstd, need=need)
+            for k in range(3):
+                assert (part[k] is None) == (not need[k])
+                assert part[k] is None or torch.equal(part[k], got[k])
+
+
+def test_layer_norm_backward_strides_and_margins():
+    import torch
+    from paper_2506_10315_amd import binding as B
+    r = np.random.default_rng(11)
+    for kind in TYPES:
+        for cols, off, ld in ((95, 1, 107), (768, 3, 771), (1526, 2, 1600), (4, 1, 9)):
+            x, xv = dev(r.standard_normal((40, ld)), kind)
+            dy, dyv = dev(r.standard_normal((40, ld + 1)), kind)
+            xs, dys = xv[:, off:off + cols], dyv[:, :cols]
+            mean = torch.from_numpy(xs.mean(1).astype(np.float32)).cuda()
+            rstd = torch.from_numpy((1 / np.sqrt(xs.var(1) + 1e-5)).astype(np.float32)).cuda()
+            want = norm_back_exact(dys, xs, None, host(mean), host(rstd))
+            tol = norm_back_tolerance(dys, xs, None, host(mean), host(rstd), kind, "fp32")
+            got = ops().layer_norm_backward(dy[:, :cols], x[:, off:off + cols], None, mean, rstd)
+            for k in range(3):
+                close(got[k], want[k], tol[k], f"view {k}")
+            buf = torch.full((40, ld + 2), 3.0, dtype=tt(kind), device="cuda:0")
+            es = buf.element_size()
+            st = B.lib().lopt_layer_norm_backward(dy.data_ptr(), ld + 1, x.data_ptr() + off * es, ld, None, mean.data_ptr(), rstd.data_ptr(),
+                                                  buf.data_ptr() + 2 * es, ld + 2, None, None, 40, cols, B_type(kind), 0, None, 0,
+                                                  torch.cuda.current_stream().cuda_stream)
+            assert st == 0
+            close(buf[:, 2:2 + cols], want[0], tol[0], "margins")
+            assert bool((buf[:, :2] == 3).all()) and bool((buf[:, 2 + cols:] == 3).all())
+            # in place of dy, with the weights' gradient from the values before
+            dyc = dy[:, :cols].contiguous()
+            dw = torch.empty(cols, device="cuda:0")
+            need = B.lib().lopt_layer_norm_workspace(40, cols)
+            ws = torch.empty(need, dtype=torch.uint8, device="cuda:0")
+            xc = x[:, off:off + cols].contiguous()
+            st = B.lib().lopt_layer_norm_backward(dyc.data_ptr(), cols, xc.data_ptr(), cols, None, mean.data_ptr(), rstd.data_ptr(), dyc.data_ptr(), cols,
+                                                  dw.data_ptr(), None, 40, cols, B_type(kind), 0, ws.data_ptr(), need,
+                                                  torch.cuda.current_stream().cuda_stream)
+            assert st == 0
+            close(dyc, want[0], tol[0], "in place")
+            close(dw, want[1], tol[1], "in place dw")
+    # a gradient that is broadcast over the rows
+    x, xv = dev(r.standard_normal((6, 50)), "fp32")
+    y, mean, rstd = ops().layer_norm_forward(x)
+    row, rowv = dev(r.standard_normal(50), "fp32")
+    dx, dw, db = ops().layer_norm_backward(row.expand(6, 50), x, None, mean, rstd)
+    want = norm_back_exact(np.broadcast_to(rowv, (6, 50)), xv, None, host(mean), host(rstd))
+    tol = norm_back_tolerance(np.broadcast_to(rowv, (6, 50)), xv, None, host(mean), host(rstd), "fp32", "fp32")
+    close(dx, want[0], tol[0], "broadcast dx")
+    close(db, want[2], tol[2], "broadcast db")
+
+
+def test_layer_norm_autograd_against_differences():
+    import torch
+    r = np.random.default_rng(21)
+    x, xv = dev(r.standard_normal((9, 37)), "fp32")
+    w, wv = dev(1 + 0.3 * r.standard_normal(37), "fp32")
+    b, bv = dev(0.3 * r.standard_normal(37), "fp32")
+    c, cv = dev(r.standard_normal((9, 37)), "fp32")
+    for t in (x, w, b):
+        t.requires_grad_()
+    (ops().layer_norm(x, w, b) * c).sum().backward()
+    eps = float(np.float32(1e-5))
+    loss = lambda a, s, o: float((norm_exact(a, s, o, eps)[0] * cv).sum())
+    h = 1e-5
+    for t, v, which in ((x, xv, 0), (w, wv, 1), (b, bv, 2)):
+        for _ in range(8):
+            d = r.standard_normal(v.shape)
+            args = [xv, wv, bv]
+            args[which] = v + h * d
+            up = loss(*args)
+            args[which] = v - h * d
+            slope = (up - loss(*args)) / (2 * h)
+            got = float((host(t.grad) * d).sum())
+            scale = float(np.abs(host(t.grad) * d).sum())
+            # differences: h^2 times a third derivative of order one, 2^-52 / h of the loss; gradient: a chain of
+            # about 37 + 24 sums of terms as large as the outcome, thrice (mean, spread, the backward sums)
+            assert abs(got - slope) <= 1e-8 * scale + 1e-8 + 3 * depth(37) * U * 4 * scale, (which, got, slope)
+
+
+# ---------------------------------------------------------------------------------------------- token log probabilities
+
+def logp_exact(x, target, scale, ignore=-100):
+    """Row by row from the definition; x float64 [rows, vocab]."""
+    rows, vocab = x.shape
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        m = np.fmax.reduce(x, axis=1)
+        base = np.where(m == -np.inf, 0.0, m)
+        z = scale * (x - base[:, None])
+        e = np.exp(z)
+        S = e.sum(1)
+        ls = np.log(S)
+        H = np.where(S == 0, 0.0, ls - np.where(e == 0, 0.0, e * z).sum(1) / S)
+        lp = np.where(S[:, None] == 0, -np.inf, z - ls[:, None])
+        at = np.full(rows, np.nan)
+        if target is not None:
+            for i, t in enumerate(target):
+                if t == ignore:
+                    at[i] = 0.0
+                elif 0 <= t < vocab:
+                    at[i] = lp[i, t]
+    # NaN above everything, the lowest index first among equals
+    key = np.where(np.isnan(x), np.inf, x)
+    order = np.stack([np.lexsort((np.arange(vocab), -key[i], ~np.isnan(x[i]))) for i in range(rows)]) if rows else np.zeros((0, vocab), int)
+    return at, H, np.stack([m, ls], 1), lp, order, z
+
+
+def logp_tolerance(x, scale):
+    """Bounds for (ln S, entropy, and logp as a function of z)."""
+    _, H, st, lp, _, z = logp_exact(x, None, scale)
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        p = np.exp(lp)
+        az = np.where(p > 0, np.abs(z), 0.0)
+        ez, ez2 = (p * az).sum(1), (p * az * az).sum(1)
+        D = depth(x.shape[1])
+        dS = U * (D + 5 + 5 * ez)
+        dlog = dS + 3 * U * np.abs(st[:, 1]) + TINY["fp32"]
+        dH = dlog + U * ((D + 8) * ez + 5 * ez2) + ez * dS + 3 * U * (np.abs(st[:, 1]) + ez)
+    clean = lambda v: np.where(np.isfinite(v), 1.01 * v, 0.0)
+    dz = np.where(np.isfinite(z), 5 * U * np.abs(z), 0.0)
+    tl = clean(dlog)[:, None] + dz + 3 * U * np.where(np.isfinite(lp), np.abs(lp), 0.0)
+    return clean(dlog), clean(dH), tl
+
+
+def logits_case(rows, vocab, seed, masked=0.0, spread=3.0):
+    r = np.random.default_rng(seed)
+    x = (spread * r.standard_normal((rows, vocab))).astype(np.float32)
+    t = r.integers(0, vocab, rows)
+    x[np.arange(rows), t] += 4.0
+    if masked:
+        x[r.random(x.shape) < masked] = -np.inf
+    return x, t
+
+
+def check_logp(x, kind, t, scale=1.0, top=0, ignore=-100, what=""):
+    import torch
+    xt, xv = (x, host(x)) if isinstance(x, torch.Tensor) else dev(x, kind)
+    tt_ = torch.from_numpy(np.asarray(t, dtype=np.int64)).cuda()
+    got = ops().token_logprobs_forward(xt, tt_, scale=scale, top=top, ignore_index=ignore)
+    s = float(np.float32(scale))
+    at, H, st, lp, order, _ = logp_exact(xv, t, s, ignore)
+    dlog, dH, tl = logp_tolerance(xv, s)
+    rows = np.arange(len(t))
+    ok = (np.asarray(t) >= 0) & (np.asarray(t) < xv.shape[1])
+    tat = np.where(ok, tl[rows, np.where(ok, t, 0)], 0.0)
+    close(got.logp, at, tat, what + " logp")
+    close(got.entropy, H, dH, what + " entropy")
+    nan = np.isnan(st[:, 1])
+    assert np.array_equal(host(got.stats)[~nan, 0], st[~nan, 0]), what + " largest logit"
+    close(got.stats[:, 1], st[:, 1], dlog, what + " ln S")
+    if top:
+        assert np.array_equal(got.top_index.cpu().numpy(), order[:, :top]), what + " alternatives"
+        close(got.top_logp, np.take_along_axis(lp, order[:, :top], 1), np.take_along_axis(tl, order[:, :top], 1), what + " top_logp")
+    return xt, xv, got
+
+
+LOGP_SHAPES = [(1, 1), (4, 2), (3, 7), (5, 63), (2, 64), (9, 65), (17, 100), (3, 255), (2, 257), (7, 1000), (2, 2047), (3, 2049), (5, 4099), (2, 8192),
+               (2, 8193), (1, 32000), (3, 50257), (1, 131073), (300, 33)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab", LOGP_SHAPES)
+def test_token_logprobs_forward(rows, vocab, kind):
+    for top, masked, scale in ((0, 0.0, 1.0), (min(5, vocab), 0.4, 1.25), (min(32, vocab), 0.0, 0.5), (1, 0.9, 1.0)):
+        x, t = logits_case(rows, vocab, rows * 7 + vocab + top, masked)
+        t[::3] = -100
+        check_logp(x, kind, t, scale, top, what=f"top {top} masked {masked}")
+
+
+def test_token_logprobs_ties_and_orders():
+    vocab = 20000
+    for kind in TYPES:
+        for name, row in (("equal", np.zeros(vocab)), ("rising", np.arange(vocab) / 512.0), ("falling", -np.arange(vocab) / 512.0),
+                          ("few values", np.arange(vocab) % 3.0), ("zeros of both signs", np.where(np.arange(vocab) % 2, 0.0, -0.0)),
+                          ("alternatives at the end", np.where(np.arange(vocab) >= vocab - 40, 1.0, 0.0)),
+                          ("lowest value", np.full(vocab, -3.3895314e38 if kind != "fp16" else -65504.0)),
+                          ("one allowed", np.where(np.arange(vocab) == 777, 0.5, -np.inf)),
+                          ("masked whole", np.full(vocab, -np.inf)),
+                          ("lowest value as mask", np.where(np.arange(vocab) % 5 == 1, np.arange(vocab) % 11, -3.3895314e38 if kind != "fp16" else -65504.0))):
+            for scale in (1.0, 2.0):
+                check_logp(np.stack([row, row[::-1]]), kind, np.array([777, 3]), scale, 32, what=f"{name} {kind}")
+
+
+def test_token_logprobs_special_rows_and_targets():
+    import torch
+    x, t = logits_case(12, 5000, 5)
+    x[1, 17] = np.nan
+    x[2, 40] = np.inf
+    x[3, :] = -np.inf
+    x[4, t[4]] = -np.inf            # the target itself is masked
+    x[5, [3, 4]] = np.nan
+    x[6, :] = np.nan
+    t[7], t[8], t[9] = -100, 5000, -1
+    _, _, got = check_logp(x, "fp32", t, top=6)
+    lp = host(got.logp)
+    assert np.isnan(lp[[1, 2, 5, 6, 8, 9]]).all() and lp[3] == -np.inf and lp[4] == -np.inf and lp[7] == 0
+    assert host(got.entropy)[3] == 0
+    _, _, got = check_logp(x, "bf16", t, top=6, ignore=-1)
+    assert host(got.logp)[9] == 0 and np.isnan(host(got.logp)[7])
+    r = ops().token_logprobs_forward(torch.zeros(0, 10, device="cuda:0"), torch.zeros(0, dtype=torch.int64, device="cuda:0"), top=3)
+    assert r.logp.shape == (0,) and r.top_index.shape == (0, 3)
+    r = ops().token_logprobs_forward(torch.zeros(2, 10, device="cuda:0"), None, entropy=False)
+    assert r.logp is None and r.entropy is None and float(r.stats[0, 1]) == pytest.approx(math.log(10))
+
+
+def test_token_logprobs_strides_and_dimensions():
+    import torch
+    x, _ = logits_case(14, 3007, 9)
+    t = np.arange(14) * 100
+    for kind in TYPES:
+        full, _ = dev(x, kind)
+        for off, vocab in ((0, 3000), (1, 2999), (3, 2001), (5, 100)):
+            check_logp(full[:, off:off + vocab], kind, t % vocab, top=7, what=f"{kind} {off}")
+    a = full.view(2, 7, 3007)
+    r = ops().token_logprobs_forward(a, torch.zeros(2, 7, dtype=torch.int64, device="cuda:0"), top=2)
+    b = ops().token_logprobs_forward(full, torch.zeros(14, dtype=torch.int64, device="cuda:0"), top=2)
+    assert r.logp.shape == (2, 7) and r.top_index.shape == (2, 7, 2) and r.stats.shape == (2, 7, 2)
+    assert torch.equal(r.logp.flatten(), b.logp) and torch.equal(r.top_index.flatten(), b.top_index.flatten())
+    one = ops().token_logprobs_forward(full[3], torch.tensor(5, device="cuda:0"), top=2)
+    assert one.logp.shape == () and one.top_index.tolist() == b.top_index[3].tolist()
+
+
+def logp_back_exact(x, t, stats, H, g, h, scale, ignore=-100):
+    rows, vocab = x.shape
+    with np.errstate(invalid="ignore", over="ignore"):
+        lp = scale * (x - stats[:, :1]) - stats[:, 1:]
+        p = np.exp(lp)
+        inner = np.where(p == 0, 0.0, p * (lp + H[:, None]))
+        gg = np.zeros(rows) if g is None else np.where(t == ignore, 0.0, g)
+        d = -gg[:, None] * p - (0.0 if h is None else h[:, None] * inner)
+        for i in range(rows):
+            if g is not None and t[i] != ignore:
+                if 0 <= t[i] < vocab:
+                    d[i, t[i]] += gg[i]
+                else:
+                    d[i] = np.nan
+            if stats[i, 1] == -np.inf:
+                d[i] = 0.0 if not np.isnan(d[i]).all() or 0 <= t[i] < vocab or t[i] == ignore else np.nan
+        return scale * d, lp, p, gg
+
+
+def check_back(x, kind, t, scale, g, h, ignore=-100, what=""):
+    """x: array, or a (tensor, values) pair."""
+    import torch
+    xt, xv = x if isinstance(x, tuple) else dev(x, kind)
+    tgt = torch.from_numpy(np.asarray(t, dtype=np.int64)).cuda()
+    _, H, st, _, _, _ = logp_exact(xv, t, scale, ignore)
+    ten = lambda a: None if a is None else torch.from_numpy(np.asarray(a, dtype=np.float32)).cuda()
+    s_, h_, g_, hh = ten(st), ten(H), ten(g), ten(h)
+    dx = ops().token_logprobs_backward(xt, tgt if g is not None else None, s_, h_ if h is not None else None, g_, hh, scale=scale, ignore_index=ignore)
+    f = lambda a: None if a is None else host(a)
+    want, lp, p, gg = logp_back_exact(xv, np.asarray(t), f(s_), f(h_), f(g_), f(hh), scale, ignore)
+    with np.errstate(invalid="ignore"):
+        z = np.where(p > 0, scale * (xv - f(s_)[:, :1]), 0.0)
+        l = np.where(p > 0, lp, 0.0)
+        r = U * (5 * np.abs(z) + 4 * np.abs(l) + 6)
+        tol = np.abs(gg)[:, None] * p * (r + 4 * U)
+        if h is not None:
+            hv, Hv = np.abs(f(hh))[:, None], f(h_)[:, None]
+            tol = tol + hv * p * (np.abs(l + Hv) * (r + 5 * U) + U * (5 * np.abs(z) + 3 * np.abs(l) + 2 * np.abs(Hv)))
+        tol = 1.01 * scale * tol + (3 * U + 1.01 * ROUND[kind]) * np.abs(want) + 2 * TINY[kind]
+        rows = np.arange(len(t))
+        ok = (np.asarray(t) >= 0) & (np.asarray(t) < xv.shape[1])
+        tol[rows[ok], np.asarray(t)[ok]] += scale * 4 * U * np.abs(gg[ok])
+    # below float32's normal range e^z may be flushed
+    tol = np.where(np.isnan(tol), 0.0, tol) + 2.0 ** -126 * scale * 100 * (np.abs(gg)[:, None] + (0 if h is None else np.abs(f(hh))[:, None]))
+    close(dx, want, tol, what)
+    return xt, tgt, s_, h_, g_, hh, dx
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab", LOGP_SHAPES)
+def test_token_logprobs_backward(rows, vocab, kind):
+    r = np.random.default_rng(rows + vocab)
+    for masked, scale, use_g, use_h in ((0.0, 1.0, True, True), (0.5, 1.25, True, False), (0.3, 0.5, False, True)):
+        x, t = logits_case(rows, vocab, rows * 3 + vocab, masked)
+        t[1::3] = -100
+        check_back(x, kind, t, scale, r.standard_normal(rows) if use_g else None, r.standard_normal(rows) if use_h else None,
+                   what=f"masked {masked} g {use_g} h {use_h}")
+
+
+def test_token_logprobs_backward_special_rows_strides_and_margins():
+    import torch
+    from paper_2506_10315_amd import binding as B
+    x, t = logits_case(12, 3007, 5)
+    x[1, 17] = np.nan
+    x[2, 40] = np.inf
+    x[3, :] = -np.inf
+    x[4, t[4]] = -np.inf
+    t[7], t[8], t[9] = -100, 3007, -1
+    g, h = np.linspace(-1, 1, 12), np.linspace(0.5, -0.2, 12)
+    for kind in TYPES:
+        out = check_back(x, kind, t, 1.0, g, h, what=kind)
+        dx = host(out[-1])
+        assert np.isnan(dx[[1, 2, 8, 9]]).all() and (dx[3] == 0).all() and np.isfinite(dx[[0, 4, 5, 6, 7, 10, 11]]).all()
+        for off, vocab in ((0, 3000), (1, 2999), (3, 2001), (2, 100)):
+            xs, ts = logits_case(12, 3007, 6)
+            full, fv = dev(xs, kind)
+            view, vv = full[:, off:off + vocab], fv[:, off:off + vocab]
+            tg = np.arange(12) * 8
+            _, tgt, st, ent, g_, h_, dx = check_back((view, vv), kind, tg, 1.0, g, h, what=f"{kind} {off}")
+            buf = torch.full((12, 3010), 3.0, dtype=tt(kind), device="cuda:0")
+            es = buf.element_size()
+            status = B.lib().lopt_token_logprobs_backward(view.data_ptr(), 3007, tgt.data_ptr(), st.data_ptr(), ent.data_ptr(), g_.data_ptr(), h_.data_ptr(),
+                                                          buf.data_ptr() + 2 * es, 3010, 12, vocab, B_type(kind), 1.0, -100,
+                                                          torch.cuda.current_stream().cuda_stream)
+            assert status == 0
+            assert torch.equal(buf[:, 2:2 + vocab], dx)
+            assert bool((buf[:, :2] == 3).all()) and bool((buf[:, 2 + vocab:] == 3).all())
+            # in place
+            status = B.lib().lopt_token_logprobs_backward(full.data_ptr() + off * es, 3007, tgt.data_ptr(), st.data_ptr(), ent.data_ptr(), g_.data_ptr(),
+                                                          h_.data_ptr(), full.data_ptr() + off * es, 3007, 12, vocab, B_type(kind), 1.0, -100,
+                                                          torch.cuda.current_stream().cuda_stream)
+            assert status == 0 and torch.equal(full[:, off:off + vocab], dx)
+
+
+def test_token_logprobs_autograd_against_differences():
+    import torch
+    r = np.random.default_rng(31)
+    x, t = logits_case(7, 53, 12)
+    t[2] = -100
+    c, k = r.standard_normal(7), r.standard_normal(7)
+    xt, xv = dev(x, "fp32")
+    xt.requires_grad_()
+    out = ops().token_logprobs(xt, torch.from_numpy(t).cuda(), scale=1.25, top=3)
+    assert not out.top_logp.requires_grad and not out.stats.requires_grad
+    (out.logp * torch.from_numpy(c).float().cuda() + out.entropy * torch.from_numpy(k).float().cuda()).sum().backward()
+    c32, k32 = np.float32(c).astype(float), np.float32(k).astype(float)
+    def loss(a):
+        at, H, _, _, _, _ = logp_exact(a, t, 1.25)
+        return float((at * c32 + H * k32).sum())
+    hstep = 1e-5
+    for _ in range(16):
+        d = r.standard_normal(xv.shape)
+        slope = (loss(xv + hstep * d) - loss(xv - hstep * d)) / (2 * hstep)
+        got = float((host(xt.grad) * d).sum())
+        scale = float(np.abs(host(xt.grad) * d).sum())
+        # differences as for the layer norm; gradient: e^z with |z| up to 30, and the forward pass's ln S and entropy
+        assert abs(got - slope) <= 1e-8 * scale + 1e-8 + 1.25 * (depth(53) + 200) * U * (scale + np.abs(d).max() * (np.abs(c).sum() + np.abs(k).sum())), (got, slope)
+    # one output's gradient alone, and none
+    xt.grad = None
+    out = ops().token_logprobs(xt, None)
+    out.entropy.sum().backward()
+    assert bool(torch.isfinite(xt.grad).all())
+
+
+# ---------------------------------------------------------------------------------------------- what a program does around them
+
+def test_rows_beyond_32_bits_of_offset():
+    import torch
+    ld = (1 << 31) + 8
+    buf = torch.zeros(2 * ld, dtype=torch.bfloat16, device="cuda:0")
+    x = buf.as_strided((2, 999), (ld, 1))
+    r = np.random.default_rng(2)
+    v, vv = dev(3 * r.standard_normal((2, 999)), "bf16")
+    x.copy_(v)
+    got = ops().token_logprobs_forward(x, torch.tensor([5, 700], device="cuda:0"), top=4)
+    want = ops().token_logprobs_forward(v, torch.tensor([5, 700], device="cuda:0"), top=4)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    y, mean, rstd = ops().layer_norm_forward(x)
+    y2, mean2, rstd2 = ops().layer_norm_forward(v)
+    assert torch.equal(y, y2) and torch.equal(mean, mean2) and torch.equal(rstd, rstd2)
+    a = ops().layer_norm_backward(x, x, None, mean, rstd)
+    b = ops().layer_norm_backward(v, v, None, mean, rstd)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    g = torch.tensor([1.0, -2.0], device="cuda:0")
+    assert torch.equal(ops().token_logprobs_backward(x, torch.tensor([5, 700], device="cuda:0"), got.stats, got.entropy, g, g),
+                       ops().token_logprobs_backward(v, torch.tensor([5, 700], device="cuda:0"), got.stats, got.entropy, g, g))
+
+
+def _training_pass(x, w, b, head, t):
+    """Layer norm, head, loss, their gradients, clipping: everything that the captured graph below holds."""
+    import torch
+    o = ops()
+    y, mean, rstd = o.layer_norm_forward(x, w, b)
+    logits = y @ head
+    r = o.token_logprobs_forward(logits, t, top=3)
+    g = torch.full_like(r.logp, -1.0 / t.numel())
+    dlogits = o.token_logprobs_backward(logits, t, r.stats, r.entropy, g, g)
+    dx, dw, db = o.layer_norm_backward(dlogits @ head.t().contiguous(), x, w, mean, rstd)
+    out, norm = o.clip_grads([dx, dw, db], 0.01)
+    return [y, logits, r.logp, r.entropy, r.top_logp, r.top_index, dlogits, dx, dw, db, norm, *out]
+
+
+def _pass_inputs():
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(4)
+    n = lambda *s: torch.randn(*s, device="cuda:0", generator=gen)
+    return n(96, 200), 1 + 0.1 * n(200), 0.1 * n(200), n(200, 777), torch.randint(0, 777, (96,), device="cuda:0", generator=gen)
+
+
+def test_operators_on_another_stream_and_twice_the_same():
+    import torch
+    args = _pass_inputs()
+    a = _training_pass(*args)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        b = _training_pass(*args)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_operators_in_a_captured_graph():
+    import torch
+    x, w, b, head, t = _pass_inputs()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        _training_pass(x, w, b, head, t)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _training_pass(x, w, b, head, t)
+    for k in range(4):
+        x.copy_(torch.roll(x, k + 1, 0) * 1.1)
+        t.copy_(torch.roll(t, 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = _training_pass(x, w, b, head, t)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k
+
+
+def test_functions_refuse_what_they_cannot_take():
+    import torch
+    o = ops()
+    x = torch.randn(4, 8, device="cuda:0")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda:0")
+    for call in (lambda: o.layer_norm_forward(x.cpu()), lambda: o.layer_norm_forward(x.double()), lambda: o.layer_norm_forward(x[:, :0]),
+                 lambda: o.layer_norm_forward(torch.tensor(1.0, device="cuda:0")), lambda: o.layer_norm_forward(x, x[0, :7]),
+                 lambda: o.layer_norm_forward(x, x[0].cpu()), lambda: o.layer_norm_forward(x, x[0], x[0].half()),
+                 lambda: o.layer_norm_backward(x.half(), x, None, x[:, 0], x[:, 0]), lambda: o.layer_norm_backward(x[:3], x, None, x[:, 0], x[:, 0]),
+                 lambda: o.layer_norm_backward(x, x, None, x[:3, 0], x[:, 0]),
+                 lambda: o.token_logprobs_forward(x, t.int()), lambda: o.token_logprobs_forward(x, t[:3]), lambda: o.token_logprobs_forward(x, t, top=9),
+                 lambda: o.token_logprobs_forward(x.double(), t), lambda: o.token_logprobs_forward(torch.randn(2, 50, device="cuda:0"), t[:2], top=33),
+                 lambda: o.token_logprobs_forward(x, t.cpu()), lambda: o.token_logprobs_backward(x, None, torch.zeros(4, 2, device="cuda:0"), None, x[:, 0]),
+                 lambda: o.token_logprobs_backward(x, t, torch.zeros(4, 2, device="cuda:0"), None, None, x[:, 0]),
+                 lambda: o.token_logprobs_backward(x, t, torch.zeros(4, 3, device="cuda:0"), None, x[:, 0]),
+                 lambda: o.clip_grads([], 1.0), lambda: o.clip_grads([x.double()], 1.0), lambda: o.clip_grads([x[:, :5]], 1.0),
+                 lambda: o.clip_grads([x.cpu()], 1.0), lambda: o.clip_grads([x], 1.0, out=[]), lambda: o.clip_grads([x], 1.0, out=[x.t().contiguous()]),
+                 lambda: o.clip_grads([x], 1.0, out=[torch.empty(8, 4, device="cuda:0").t()]), lambda: o.clip_grads([x[0].expand(4, 8)], 1.0)):
+        with pytest.raises(ValueError):
+            call()
+    from paper_2506_10315_amd import LoptError
+    for call in (lambda: o.layer_norm_forward(x, eps=-1.0), lambda: o.token_logprobs_forward(x, t, scale=0.0),
+                 lambda: o.token_logprobs_forward(x, t, scale=math.nan), lambda: o.clip_grads([x], -1.0), lambda: o.clip_grads([x], math.nan)):
+        with pytest.raises(LoptError):
+            call()
