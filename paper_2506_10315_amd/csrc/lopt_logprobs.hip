@@ -1,4 +1,5 @@
 // Log probabilities of given tokens with entropy and top alternatives, and their gradient.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 
@@ -9,74 +10,294 @@ namespace {
 
 // The order of the alternatives as one number: larger logit first, NaN above all, +0 and -0 alike, lower index first among equals.
 // No element's number is 0 or all ones.
-__device__ __forceinline__ uint64_t rank_key(float x, uint32_t index) {
-  uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
-  u = x != x ? 0xfffffffeu : u & 0x80000000u ? ~u : u | 0x80000000u;
-  return (uint64_t)u << 32 | (0xffffffffu - index);
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
+  return x != x ? 0xfffffffeu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint64_t rank_key(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (0xffffffffu - index); }
+__device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
+__device__ __forceinline__ float key_value(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-__device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t* red) {
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)v, d);
-    v = o > v ? o : v;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  for (int i = 0; i < kBlock / kWave; ++i) v = red[i] > v ? red[i] : v;
-  return v;
+// Running softmax sums of some logits x: base = the largest of them (-FLT_MAX where all are -infinity), s = sum e^(c (x - base)),
+// h = sum e^(c (x - base)) (x - base). c = scale / ln 2 goes into the hardware's 2^x; x - base is formed before it is scaled, so that large
+// logits lose nothing and a scale never makes a finite difference infinite twice. A masked logit has x - base = -infinity and
+// e = 0; its term of h is 0 because the difference is held to -FLT_MAX.
+struct Soft { float base, s, h; };
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// a's sums seen from a larger base.
+__device__ __forceinline__ Soft rebase(Soft a, float base, float c) {
+  const float diff = fmaxf(a.base - base, -FLT_MAX);
+  const float f = exp2_hw((a.base - base) * c), fs = f * a.s;   // NaN where both are +infinity
+  return Soft{base, fs, f * a.h + fs * diff};
+}
+__device__ __forceinline__ Soft wave_join(Soft a, float c) {
+  a = rebase(a, wave_max(a.base), c);
+  return Soft{a.base, wave_sum(a.s), wave_sum(a.h)};
 }
 
-// One workgroup a row; an alternative is the largest key below the one before it.
+struct Outputs {
+  float* logp;
+  float* entropy;
+  float* stats;
+  float* top_logp;
+  int64_t* top_index;
+};
+struct Target { int64_t t; float x; };
+
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_logprobs(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int vocab, float scale,
-                                                     int64_t ignore, int top, float* __restrict__ logp, float* __restrict__ entropy,
-                                                     float* __restrict__ stats, float* __restrict__ top_logp, int64_t* __restrict__ top_index) {
-  __shared__ float red[4];
-  __shared__ uint64_t redk[4];
-  const int64_t r = blockIdx.x;
-  const T* xr = x + r * ld;
-  float m = -INFINITY;
-  for (int64_t i = threadIdx.x; i < vocab; i += kBlock) m = fmaxf(m, to_f32(xr[i]));
-  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float base = m == -INFINITY ? 0.f : m;
-  float s = 0.f, h = 0.f;
-  for (int64_t i = threadIdx.x; i < vocab; i += kBlock) {
-    const float z = scale * (to_f32(xr[i]) - base), e = expf(z);
-    s += e;
-    h += e * fmaxf(z, -FLT_MAX);
+__device__ __forceinline__ Target load_target(const T* row, const int64_t* targets, int64_t r, int vocab) {
+  Target g{-1, 0.f};
+  if (targets) {
+    g.t = targets[r];
+    if (g.t >= 0 && g.t < vocab) g.x = to_f32(row[g.t]);
   }
-  s = block_sum<4>(s, red);
-  h = block_sum<4>(h, red);
-  const bool empty = s == 0.f;
-  const float log_s = logf(s);
-  if (threadIdx.x == 0) {
-    if (logp) {
-      const int64_t t = targets[r];
+  return g;
+}
+
+// A row's outputs from its sums. Lane k of the wavefront holds the key of alternative k.
+__device__ __forceinline__ void write_row(const Outputs& o, int64_t r, int lane, Soft a, Target g, int vocab, float scale, int64_t ignore, int top, uint64_t key) {
+  const bool empty = a.s == 0.f;
+  const float log_s = logf(a.s);
+  if (lane == 0) {
+    if (o.logp) {
       float v = NAN;
-      if (t == ignore) v = 0.f;
-      else if (t >= 0 && t < vocab) v = empty ? -INFINITY : scale * (to_f32(xr[t]) - base) - log_s;
-      logp[r] = v;
+      if (g.t == ignore) v = 0.f;
+      else if (g.t >= 0 && g.t < vocab) v = empty ? -INFINITY : scale * (g.x - a.base) - log_s;
+      o.logp[r] = v;
     }
-    if (entropy) entropy[r] = empty ? 0.f : log_s - h / s;
-    stats[2 * r] = m;
-    stats[2 * r + 1] = log_s;
+    if (o.entropy) o.entropy[r] = empty ? 0.f : log_s - scale * (a.h / a.s);
+    o.stats[2 * r] = empty ? -INFINITY : a.base;
+    o.stats[2 * r + 1] = log_s;
   }
-  uint64_t before = ~(uint64_t)0;
-  for (int k = 0; k < top; ++k) {
-    uint64_t best = 0;
-    for (int64_t i = threadIdx.x; i < vocab; i += kBlock) {
-      const uint64_t key = rank_key(to_f32(xr[i]), (uint32_t)i);
-      if (key < before && key > best) best = key;
+  if (lane < top) {
+    o.top_index[r * top + lane] = key_index(key);
+    o.top_logp[r * top + lane] = empty ? -INFINITY : scale * (key_value(key) - a.base) - log_s;
+  }
+}
+
+// A wavefront takes 2048 logits of a row at a time, 32 a lane in accesses of 16 bytes. The access that would pass the row's end
+// is moved back to end with it, and the elements that the lane before has are masked.
+constexpr int kPiece = 2048;
+template <typename T>
+struct Piece {
+  static constexpr int V = Pack<T>::n, N = 32 / V;
+  typedef typename Pack<T>::type pack;
+  pack raw[N];
+  __device__ __forceinline__ static uint32_t place(uint32_t first, int j) { return first + (j * kWave + (threadIdx.x & 63)) * V; }
+  __device__ __forceinline__ void load(const T* row, uint32_t first, uint32_t n) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (first + j * kWave * V >= n) break;
+      const uint32_t at = place(first, j);
+      if (n >= (uint32_t)V) {
+        raw[j] = *(const pack*)(row + min(at, n - V));
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) raw[j][e] = at + e < n ? row[at + e] : (T)-INFINITY;
+      }
     }
-    before = best = block_max(best, redk);
-    const uint32_t at = 0xffffffffu - (uint32_t)best;
-    if (threadIdx.x == 0) {
-      top_index[r * top + k] = at;
-      top_logp[r * top + k] = empty ? -INFINITY : scale * (to_f32(xr[at]) - base) - log_s;
+  }
+  // Index of an element, and whether it is this lane's.
+  __device__ __forceinline__ static uint32_t index(uint32_t first, int i, uint32_t n) {
+    const uint32_t at = place(first, i / V);
+    return (n >= (uint32_t)V ? min(at, n - V) : at) + i % V;
+  }
+  __device__ __forceinline__ static bool mine(uint32_t first, int i, uint32_t n) {
+    const uint32_t k = index(first, i, n);
+    return k >= place(first, i / V) && k < n;
+  }
+  __device__ __forceinline__ void unpack(float (&x)[32], uint32_t first, uint32_t n) const {
+    if (first + kPiece <= n) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = to_f32(raw[i / V][i % V]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      x[i] = -INFINITY;
+      if (first + i / V * kWave * V < n && mine(first, i, n)) x[i] = to_f32(raw[i / V][i % V]);
+    }
+  }
+};
+
+__device__ __forceinline__ void add_piece(Soft& a, const float (&x)[32], float c, bool first) {
+  float base = a.base;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) base = fmaxf(base, x[i]);
+  if (first) a.base = base;
+  else a = rebase(a, base, c);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const float d = x[i] - base, e = exp2_hw(d * c);
+    a.s += e;
+    a.h += e * fmaxf(d, -FLT_MAX);
+  }
+}
+
+// The `top` largest keys of a piece in order, key k in lane k (0: there are fewer). The `top` lanes with the largest maxima hold them all: the top-th
+// of these maxima is a bound below which nothing counts, and at most 32 elements of each of these lanes pass it. They are gathered in `list`
+// (room for 32 top keys) and put in order by counting how many are larger.
+template <typename T>
+__device__ __forceinline__ uint64_t piece_top(const float (&x)[32], uint32_t first, uint32_t n, int top, uint64_t* list) {
+  const int lane = threadIdx.x & 63;
+  uint32_t ord[32], hi = 0, at = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    ord[i] = Piece<T>::mine(first, i, n) ? order_of(x[i]) : 0;
+    if (ord[i] > hi) {   // in the order of the indices: the first among equals stays
+      hi = ord[i];
+      at = Piece<T>::index(first, i, n);
+    }
+  }
+  const uint64_t best = hi ? rank_key(hi, at) : 0;
+  int rank = 0;
+#pragma unroll
+  for (int l = 0; l < kWave; ++l) rank += readlane(best, l) > best;
+  const uint64_t who = __ballot(rank == top - 1);
+  const uint64_t bound = who ? readlane(best, __builtin_ctzll(who)) : 0;
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint64_t key = rank_key(ord[i], Piece<T>::index(first, i, n));
+    const bool pass = ord[i] && key >= bound;
+    const uint64_t mask = __ballot(pass);
+    if (pass) list[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
+    count += __popcll(mask);
+  }
+  wave_sync();
+  uint64_t out = 0;
+  for (int c = 0; c < count; c += kWave) {
+    const uint64_t key = c + lane < count ? list[c + lane] : 0;
+    int above = 0;
+    for (int k = 0; k < count; ++k) above += list[k] > key;
+    // hand the key to the lane of its rank
+    for (int k = 0; k < top; ++k) {
+      const uint64_t has = __ballot(c + lane < count && above == k);
+      if (has) {
+        const uint64_t v = readlane(key, __builtin_ctzll(has));
+        if (lane == k) out = v;
+      }
+    }
+  }
+  wave_sync();
+  return out;
+}
+
+// How a row is shared out: `segments` of `pieces` pieces, a wavefront each; a row of one segment is finished by that wavefront, more are
+// joined 64 at a time by k_logprobs_join. Alternatives are found piece by piece.
+struct RowPlan {
+  int64_t pieces, segments;
+};
+inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
+  const int64_t all = (vocab + kPiece - 1) / kPiece;
+  if (top) return RowPlan{1, all};
+  int64_t per = rows * all / 16384;
+  per = per < 1 ? 1 : per > 8 ? 8 : per;
+  const int64_t segments = (all + per - 1) / per;
+  return RowPlan{(all + segments - 1) / segments, segments};
+}
+
+// Workspace of one level of segments: the keys, then the sums.
+inline size_t level_bytes(int64_t rows, int64_t segments, uint32_t top) {
+  return (size_t)rows * (size_t)segments * (top * sizeof(uint64_t) + 3 * sizeof(float)) + 15 & ~(size_t)15;
+}
+
+// One wavefront a segment: a workgroup takes four rows where they have one segment, else four segments of a row.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kBlock) void k_logprobs(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
+                                                     int64_t ignore, int top, Outputs o, int64_t segments, uint32_t pieces, float* __restrict__ part,
+                                                     uint64_t* __restrict__ keys) {
+  extern __shared__ uint64_t lists[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float c = fminf(scale * kLog2e, FLT_MAX);
+  const bool whole = segments == 1;
+  for (int64_t b = blockIdx.x;; b += gridDim.x) {
+    const int64_t r = whole ? b * 4 + wave : b;
+    if (r >= rows) break;
+    const T* row = x + r * ld;
+    for (int64_t seg = whole ? 0 : (int64_t)blockIdx.y * 4 + wave; seg < segments; seg += (int64_t)gridDim.y * 4) {
+      const uint32_t first = (uint32_t)(seg * pieces) * (uint32_t)kPiece;
+      const uint32_t end = min((uint64_t)first + (uint64_t)pieces * kPiece, (uint64_t)vocab);
+      Target g{};
+      if (whole) g = load_target(row, targets, r, vocab);
+      Soft a{-FLT_MAX, 0.f, 0.f};
+      Piece<T> p;
+      p.load(row, first, vocab);
+      uint64_t key = 0;
+      float v[32];
+      if (TOP) {
+        p.unpack(v, first, vocab);
+        add_piece(a, v, c, true);
+        key = piece_top<T>(v, first, vocab, top, lists + wave * 32 * top);
+      } else {
+        for (uint32_t f = first; f < end; f += kPiece) {
+          Piece<T> next;
+          if (f + kPiece < end) next.load(row, f + kPiece, vocab);
+          p.unpack(v, f, vocab);
+          add_piece(a, v, c, f == first);
+          p = next;
+        }
+      }
+      a = wave_join(a, c);
+      if (whole) {
+        write_row(o, r, lane, a, g, vocab, scale, ignore, top, key);
+      } else {
+        const int64_t at = r * segments + seg;
+        if (lane < 3) part[3 * at + lane] = lane == 0 ? a.base : lane == 1 ? a.s : a.h;
+        if (TOP && lane < top) keys[at * top + lane] = key;
+      }
+    }
+  }
+}
+
+// Joins up to 64 neighbouring segments of a row, one wavefront: the sums lane by lane, the ordered lists of alternatives by taking the largest head
+// `top` times. `last`: all of the row's are here, and its outputs are written; else one segment of the next level is.
+template <typename T>
+__global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
+                                                         int64_t ignore, int top, Outputs o, int64_t segments, const float* __restrict__ part,
+                                                         const uint64_t* __restrict__ keys, float* __restrict__ part_out, uint64_t* __restrict__ keys_out) {
+  extern __shared__ uint64_t lists[];
+  const int lane = threadIdx.x;
+  const float c = fminf(scale * kLog2e, FLT_MAX);
+  const int64_t groups = (segments + kWave - 1) / kWave;
+  const bool last = groups == 1;
+  for (int64_t unit = blockIdx.x; unit < rows * groups; unit += gridDim.x) {
+    const int64_t r = unit / groups, group = unit - r * groups, at = r * segments + group * kWave;
+    const int count = (int)min(segments - group * kWave, (int64_t)kWave);
+    Target g{};
+    if (last) g = load_target(x + r * ld, targets, r, vocab);
+    Soft a{-FLT_MAX, 0.f, 0.f};
+    if (lane < count) a = Soft{part[3 * (at + lane)], part[3 * (at + lane) + 1], part[3 * (at + lane) + 2]};
+    uint64_t key = 0;
+    if (top) {
+      for (int i = lane; i < count * top; i += kWave) lists[i] = keys[at * top + i];
+      wave_sync();
+      int next = 1;
+      uint64_t head = lane < count ? lists[lane * top] : 0;
+      for (int k = 0; k < top; ++k) {
+        const uint32_t hi = wave_max((uint32_t)(head >> 32));
+        const uint32_t lo = wave_max((uint32_t)(head >> 32) == hi ? (uint32_t)head : 0u);
+        const uint64_t best = (uint64_t)hi << 32 | lo;
+        if (lane == k) key = best;
+        if (head == best) {
+          head = lane < count && next < top ? lists[lane * top + next] : 0;
+          ++next;
+        }
+      }
+      wave_sync();
+    }
+    a = wave_join(a, c);
+    if (last) {
+      write_row(o, r, lane, a, g, vocab, scale, ignore, top, key);
+    } else {
+      if (lane < 3) part_out[3 * unit + lane] = lane == 0 ? a.base : lane == 1 ? a.s : a.h;
+      if (lane < top) keys_out[unit * top + lane] = key;
     }
   }
 }
@@ -109,8 +330,11 @@ using namespace lopt;
 extern "C" {
 
 size_t lopt_token_logprobs_workspace(int64_t rows, int64_t vocab, uint32_t top) {
-  (void)rows, (void)vocab, (void)top;
-  return 0;
+  if (rows <= 0 || vocab <= 0 || rows > 0x7fffffffLL || vocab > 0x7fffffffLL || top > LOPT_TOP_MAX) return 0;
+  size_t bytes = 0;
+  for (int64_t segments = plan_rows(rows, vocab, top).segments; segments > 1; segments = (segments + kWave - 1) / kWave)
+    bytes += level_bytes(rows, segments, top);
+  return bytes;
 }
 
 static lopt_status check_logits(const void* logits, int64_t ld, int64_t rows, int64_t vocab, uint32_t type, float scale) {
@@ -134,10 +358,37 @@ lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* t
   LOPT_CHECK(check_array("top_index", top_index, 8, rows > 0 && top > 0));
   LOPT_CHECK(check_workspace(workspace, workspace_bytes, lopt_token_logprobs_workspace(rows, vocab, top)));
   if (rows == 0) return LOPT_OK;
+  const Outputs o{logp, entropy, stats, top_logp, top_index};
+  const RowPlan plan = plan_rows(rows, vocab, top);
+  const int64_t* tg = logp ? targets : nullptr;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  const int64_t blocks = plan.segments == 1 ? (rows + 3) / 4 : rows;
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20), plan.segments == 1 ? 1 : (unsigned)std::min<int64_t>((plan.segments + 3) / 4, 1024));
+  char* ws = (char*)workspace;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL(k_logprobs<T>, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, (int)vocab, scale,
-                       ignore_index, (int)top, logp, entropy, stats, top_logp, top_index);
+    const T* x = (const T*)logits;
+    const uint32_t n = (uint32_t)vocab;
+    uint64_t* keys = (uint64_t*)ws;
+    float* part = (float*)(ws + (size_t)rows * plan.segments * top * sizeof(uint64_t));
+    if (top)
+      hipLaunchKernelGGL((k_logprobs<T, true>), grid, dim3(kBlock), 4 * 32 * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index,
+                         (int)top, o, plan.segments, (uint32_t)plan.pieces, part, keys);
+    else
+      hipLaunchKernelGGL((k_logprobs<T, false>), grid, dim3(kBlock), 0, stream, x, ld, tg, rows, n, scale, ignore_index, 0, o, plan.segments,
+                         (uint32_t)plan.pieces, part, keys);
+    for (int64_t segments = plan.segments; segments > 1;) {
+      const int64_t groups = (segments + kWave - 1) / kWave;
+      char* above = (char*)keys + level_bytes(rows, segments, top);
+      uint64_t* keys_out = (uint64_t*)above;
+      float* part_out = (float*)(above + (size_t)rows * groups * top * sizeof(uint64_t));
+      hipLaunchKernelGGL(k_logprobs_join<T>, dim3((unsigned)std::min<int64_t>(rows * groups, 1 << 22)), dim3(kWave),
+                         std::min<int64_t>(segments, kWave) * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o,
+                         segments, (const float*)part, (const uint64_t*)keys, part_out, keys_out);
+      keys = keys_out;
+      part = part_out;
+      segments = groups;
+    }
   });
   return launch_status("lopt_token_logprobs");
 }

@@ -13,6 +13,12 @@ __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 template <typename T>
 __device__ __forceinline__ T from_f32(float v) { return (T)v; }   // round to nearest even
 
+// 16 bytes of consecutive elements, which may start at any element: the access needs no more than an element's alignment.
+template <typename T> struct Pack;
+template <> struct Pack<float> { static constexpr int n = 4; typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Pack<bf16_t> { static constexpr int n = 8; typedef bf16_t type __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Pack<f16_t> { static constexpr int n = 8; typedef f16_t type __attribute__((ext_vector_type(8), aligned(2))); };
+
 inline size_t type_bytes(uint32_t type) { return type == LOPT_F32 ? 4 : 2; }
 
 // Calls `f` with a value of the element type.
@@ -58,6 +64,37 @@ inline lopt_status launch_status(const char* what) {
     const lopt_status st_ = (call);             \
     if (st_ != LOPT_OK) return st_;             \
   } while (0)
+
+// Largest value over the 64 lanes of a wavefront; every lane gets it. NaN is passed over.
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  v = fmaxf(v, dpp_f<0x140>(v));
+  const float a = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 0));
+  const float b = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 16));
+  const float c = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 32));
+  const float d = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 48));
+  return fmaxf(fmaxf(a, b), fmaxf(c, d));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));
+  const uint32_t a = __builtin_amdgcn_readlane((int)v, 0), b = __builtin_amdgcn_readlane((int)v, 16);
+  const uint32_t c = __builtin_amdgcn_readlane((int)v, 32), d = __builtin_amdgcn_readlane((int)v, 48);
+  return max(max(a, b), max(c, d));
+}
+__device__ __forceinline__ uint64_t readlane(uint64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
+// What the lanes of this wavefront wrote to LDS before is there for all of them after.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // Sum over a workgroup of W wavefronts; every thread gets it. `red`: W values of LDS, free to use before and after.
 template <int W, typename V>
