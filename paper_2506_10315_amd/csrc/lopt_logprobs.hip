@@ -302,23 +302,67 @@ __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x
   }
 }
 
-template <typename T>
+// The gradient, element by element: a workgroup takes kBackPacks packs of 16 bytes a thread of one row. With A = scale (g + h entropy), B = scale h:
+//   dx = scale g [target] - p (A + B ln p)
+// where ln p = scale (x - m) - ln S. Elements behind the last whole pack of a row go one a thread.
+constexpr int kBackPacks = 4;
+template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld, const int64_t* __restrict__ targets, const float* __restrict__ stats,
                                                           const float* __restrict__ entropy, const float* __restrict__ dlogp,
-                                                          const float* __restrict__ dentropy, T* dx, int64_t ld_d, int vocab, float scale, int64_t ignore) {
-  const int64_t r = blockIdx.x;
-  const float m = stats[2 * r], log_s = stats[2 * r + 1];
-  const bool empty = log_s == -INFINITY;
-  const int64_t t = dlogp ? targets[r] : ignore;
-  float g = t == ignore ? 0.f : dlogp[r];
-  if (t != ignore && (t < 0 || t >= vocab)) g = NAN;
-  const float h = dentropy ? dentropy[r] : 0.f, ent = dentropy ? entropy[r] : 0.f;
-  for (int64_t i = threadIdx.x; i < vocab; i += kBlock) {
-    const float lp = fmaxf(scale * (to_f32(x[r * ld + i]) - m) - log_s, -FLT_MAX);
-    const float p = expf(lp);
-    float d = (i == t ? g : 0.f) - g * p - h * (p * (lp + ent));
-    d = empty ? g * 0.f : scale * d;
-    dx[r * ld_d + i] = from_f32<T>(d);
+                                                          const float* __restrict__ dentropy, T* dx, int64_t ld_d, int64_t rows, uint32_t vocab, float scale, int64_t ignore) {
+  typedef typename Pack<T>::type pack;
+  constexpr int V = Pack<T>::n;
+  constexpr uint32_t kSpan = kBackPacks * kBlock * V;
+  const uint32_t whole = vocab / V * V;
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* row = x + r * ld;
+    T* out = dx + r * ld_d;
+    const float m = stats[2 * r], log_s = stats[2 * r + 1];
+    const int64_t t = dlogp ? targets[r] : ignore;
+    float g = t == ignore ? 0.f : dlogp[r];
+    if (t != ignore && (t < 0 || t >= vocab)) g = NAN;
+    const float h = ENTROPY ? dentropy[r] : 0.f;
+    const float at_target = scale * g, A = scale * (g + (ENTROPY ? h * entropy[r] : 0.f)), B = scale * h;
+    const bool empty = log_s == -INFINITY;
+    const uint32_t at = t >= 0 && t < vocab ? (uint32_t)t : 0xffffffffu;
+    auto gradient = [&](float v) {
+      float lp = scale * (v - m) - log_s;
+      const float p = exp2_hw(lp * kLog2e);
+      if (ENTROPY) lp = fmaxf(lp, -1e4f);   // p is 0 there
+      const float d = -p * (ENTROPY ? A + B * lp : A);
+      return empty ? 0.f * A : d;
+    };
+    for (uint32_t first = blockIdx.y * kSpan; first < vocab; first += gridDim.y * kSpan) {
+      pack in[kBackPacks];
+#pragma unroll
+      for (int j = 0; j < kBackPacks; ++j) {
+        const uint32_t k = first + (j * kBlock + threadIdx.x) * V;
+        if (k < whole) in[j] = *(const pack*)(row + k);
+      }
+#pragma unroll
+      for (int j = 0; j < kBackPacks; ++j) {
+        const uint32_t k = first + (j * kBlock + threadIdx.x) * V;
+        if (k < whole) {
+          float d[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) d[e] = gradient(to_f32(in[j][e]));
+          if (at - k < (uint32_t)V) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (at == k + e) d[e] += empty ? 0.f : at_target;
+          }
+          pack o;
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[e] = from_f32<T>(d[e]);
+          *(pack*)(out + k) = o;
+        }
+      }
+      const uint32_t k = whole + threadIdx.x;
+      if (first + kSpan >= vocab && k < vocab) {
+        const float d = gradient(to_f32(row[k]));
+        out[k] = from_f32<T>(at == k && !empty ? d + at_target : d);
+      }
+    }
   }
 }
 
@@ -408,8 +452,14 @@ lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const i
   if (rows == 0) return LOPT_OK;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL(k_logprobs_back<T>, dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy,
-                       dlogp, dentropy, (T*)dlogits, ld_d, (int)vocab, scale, ignore_index);
+    constexpr int64_t kSpan = (int64_t)kBackPacks * kBlock * Pack<T>::n;
+    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20), (unsigned)std::min<int64_t>((vocab + kSpan - 1) / kSpan, 1024));
+    if (dentropy)
+      hipLaunchKernelGGL((k_logprobs_back<T, true>), grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp,
+                         dentropy, (T*)dlogits, ld_d, rows, (uint32_t)vocab, scale, ignore_index);
+    else
+      hipLaunchKernelGGL((k_logprobs_back<T, false>), grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp,
+                         dentropy, (T*)dlogits, ld_d, rows, (uint32_t)vocab, scale, ignore_index);
   });
   return launch_status("lopt_token_logprobs_backward");
 }
