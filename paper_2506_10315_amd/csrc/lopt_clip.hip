@@ -23,9 +23,6 @@ struct ClipBatch {
   int n;
 };
 
-__device__ __forceinline__ float load_as(const void* p, int64_t i, uint32_t type) {
-  return type == LOPT_F32 ? ((const float*)p)[i] : type == LOPT_BF16 ? to_f32(((const bf16_t*)p)[i]) : to_f32(((const f16_t*)p)[i]);
-}
 __device__ __forceinline__ void store_as(void* p, int64_t i, uint32_t type, float v) {
   if (type == LOPT_F32) ((float*)p)[i] = v;
   else if (type == LOPT_BF16) ((bf16_t*)p)[i] = from_f32<bf16_t>(v);

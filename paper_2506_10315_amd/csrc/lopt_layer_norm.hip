@@ -1,92 +1,375 @@
 // Layer norm and its gradient.
+#include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "lopt_ops.h"
 
 namespace lopt {
 namespace {
 
-// One workgroup a row: mean, then the squares of what is left, then the row again.
-template <typename T, typename W>
-__global__ __launch_bounds__(kBlock) void k_norm(const T* __restrict__ x, int64_t ld_x, const W* __restrict__ w, const W* __restrict__ b, T* y,
-                                                 int64_t ld_y, float* __restrict__ mean_out, float* __restrict__ rstd_out, int cols, float eps) {
-  __shared__ float red[4];
-  const int64_t r = blockIdx.x;
-  const T* xr = x + r * ld_x;
-  float s = 0.f;
-  for (int64_t i = threadIdx.x; i < cols; i += kBlock) s += to_f32(xr[i]);
-  const float mean = block_sum<4>(s, red) / (float)cols;
-  float v = 0.f;
-  for (int64_t i = threadIdx.x; i < cols; i += kBlock) {
-    const float d = to_f32(xr[i]) - mean;
-    v += d * d;
+// ---- rows that one group of G lanes holds in registers. G = 8, 16, 32, 64: several rows a workgroup; G = 256, 1024: a workgroup a row.
+template <int G> struct Group {
+  static constexpr int kThreads = G <= 64 ? kBlock : G, kRows = kThreads / G, kWaves = G <= 64 ? 1 : G / 64;
+};
+
+// Sum over a group; every lane of it gets the same. Groups of several wavefronts: `red` has kWaves floats that no other sum uses until
+// the group has passed another barrier.
+template <int G>
+__device__ __forceinline__ float group_sum(float v, float* red) {
+  if (G >= 64) {
+    v = wave_sum(v);
+    if (G > 64) {
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = red[0];
+#pragma unroll
+      for (int i = 1; i < Group<G>::kWaves; ++i) v += red[i];
+    }
+    return v;
   }
-  const float rstd = 1.f / sqrtf(block_sum<4>(v, red) / (float)cols + eps);
-  for (int64_t i = threadIdx.x; i < cols; i += kBlock) {
-    const float h = (to_f32(xr[i]) - mean) * rstd;
-    y[r * ld_y + i] = from_f32<T>(h * (w ? to_f32(w[i]) : 1.f) + (b ? to_f32(b[i]) : 0.f));
+  v += dpp_f<0xB1>(v);    // quad_perm [1,0,3,2]
+  v += dpp_f<0x4E>(v);    // quad_perm [2,3,0,1]
+  v += dpp_f<0x141>(v);   // row_half_mirror
+  if (G >= 16) v += dpp_f<0x140>(v);   // row_mirror
+  if (G >= 32) v += __shfl_xor(v, 16);
+  return v;
+}
+
+// A lane's share of a row: N packs of 16 bytes, G packs from one to the next. The pack that would pass the row's end is moved back to
+// end with it; its first `skip` elements are the lane's before, which sums pass over and stores write twice, the same. Rows shorter than a
+// pack (N = 0): one element a lane.
+template <typename T, int G, int N>
+struct Share {
+  static constexpr int V = N ? Pack<T>::n : 1, P = N ? N : 1, E = P * V;
+  uint32_t at[P];
+  int skip[P];
+  bool have[P];
+  __device__ __forceinline__ Share(uint32_t cols) {
+    const uint32_t lane = threadIdx.x & (G - 1);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const uint32_t k = (j * G + lane) * V;
+      have[j] = k < cols;
+      at[j] = min(k, cols - V);
+      skip[j] = have[j] ? (int)(k - at[j]) : V;
+    }
   }
-  if (threadIdx.x == 0) {
-    if (mean_out) mean_out[r] = mean;
-    if (rstd_out) rstd_out[r] = rstd;
+  __device__ __forceinline__ bool mine(int i) const { return i % V >= skip[i / V]; }
+};
+
+template <typename T, int G, int N>
+struct Row {
+  typedef Share<T, G, N> S;
+  typedef typename Pack<T>::type pack;
+  pack raw[N ? N : 1];
+  __device__ __forceinline__ void load(const T* row, const S& s) {
+#pragma unroll
+    for (int j = 0; j < S::P; ++j)
+      if (s.have[j]) {
+        if (N) raw[j] = *(const pack*)(row + s.at[j]);
+        else raw[j][0] = row[s.at[j]];
+      }
+  }
+  __device__ __forceinline__ float get(int i) const { return to_f32(raw[i / S::V][i % S::V]); }
+  __device__ __forceinline__ static void store(T* row, const S& s, int j, const float* v) {
+    if (!s.have[j]) return;
+    if (N) {
+      pack o;
+#pragma unroll
+      for (int e = 0; e < S::V; ++e) o[e] = from_f32<T>(v[e]);
+      *(pack*)(row + s.at[j]) = o;
+    } else {
+      row[s.at[j]] = from_f32<T>(v[0]);
+    }
+  }
+};
+
+// One pack of a lane's share of a weight or bias vector; `other` where there is none.
+template <typename W, int V>
+__device__ __forceinline__ void load_pack_as(const W* p, float* v) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = to_f32(p[e]);
+}
+template <typename S>
+__device__ __forceinline__ void load_vector(const void* p, uint32_t type, const S& s, int j, float other, float* v) {
+#pragma unroll
+  for (int e = 0; e < S::V; ++e) v[e] = other;
+  if (!p || !s.have[j]) return;
+  if (type == LOPT_F32) load_pack_as<float, S::V>((const float*)p + s.at[j], v);
+  else if (type == LOPT_BF16) load_pack_as<bf16_t, S::V>((const bf16_t*)p + s.at[j], v);
+  else load_pack_as<f16_t, S::V>((const f16_t*)p + s.at[j], v);
+}
+
+// Groups of 1024 have 128 registers a lane: they ask for nothing ahead and read the vectors again for every row.
+template <int G> constexpr bool kAhead = G < 1024;
+
+struct Vectors { const void* w; const void* b; uint32_t type; };
+
+// Every group takes rows a grid apart and asks for the next before it works on the one it has.
+template <typename T, int G, int N>
+__global__ __launch_bounds__(Group<G>::kThreads) void k_norm(const T* x, int64_t ld_x, Vectors wb, T* y, int64_t ld_y, float* __restrict__ mean_out,
+                                                             float* __restrict__ rstd_out, int64_t rows, uint32_t cols, float eps) {
+  typedef Share<T, G, N> S;
+  constexpr int E = S::E, V = S::V, kRows = Group<G>::kRows;
+  __shared__ float red[2][2][Group<G>::kWaves];
+  const S s(cols);
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+  Row<T, G, N> next;
+  if (kAhead<G> && r < rows) next.load(x + r * ld_x, s);
+  float w[E], b[E];
+  auto vectors = [&](int j) {
+    load_vector(wb.w, wb.type, s, j, 1.f, w + j * V);
+    load_vector(wb.b, wb.type, s, j, 0.f, b + j * V);
+  };
+  if (kAhead<G>) {
+#pragma unroll
+    for (int j = 0; j < S::P; ++j) vectors(j);
+  }
+  for (int odd = 0; r < rows; r += step, odd ^= 1) {
+    if (!kAhead<G>) next.load(x + r * ld_x, s);
+    const Row<T, G, N> row = next;
+    if (kAhead<G> && r + step < rows) next.load(x + (r + step) * ld_x, s);
+    float v[E], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      v[i] = row.get(i);
+      if (s.mine(i)) sum += v[i];
+    }
+    const float mean = group_sum<G>(sum, red[odd][0]) / (float)cols;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      v[i] -= mean;
+      if (s.mine(i)) sum += v[i] * v[i];
+    }
+    const float rstd = 1.f / sqrtf(group_sum<G>(sum, red[odd][1]) / (float)cols + eps);
+#pragma unroll
+    for (int j = 0; j < S::P; ++j) {
+      if (!kAhead<G>) vectors(j);
+#pragma unroll
+      for (int i = j * V; i < j * V + V; ++i) v[i] = v[i] * rstd * w[i] + b[i];
+      Row<T, G, N>::store(y + r * ld_y, s, j, v + j * V);
+    }
+    if (threadIdx.x % G == 0) {
+      if (mean_out) mean_out[r] = mean;
+      if (rstd_out) rstd_out[r] = rstd;
+    }
   }
 }
 
-constexpr int kSlab = 128;   // rows whose column sums one wavefront adds up
-
-// Partial sums of dy xh and dy over a slab of rows, a column a lane. Before dx, which may overwrite dy or x.
-template <typename T>
-__global__ __launch_bounds__(kWave) void k_norm_columns(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ x, int64_t ld_x,
-                                                        const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int cols,
-                                                        float* __restrict__ part) {
-  const int64_t c = (int64_t)blockIdx.x * kWave + threadIdx.x;
-  const int64_t r0 = (int64_t)blockIdx.y * kSlab, r1 = min(r0 + kSlab, (int64_t)rows);
-  if (c >= cols) return;
-  float sw = 0.f, sb = 0.f;
-  for (int64_t r = r0; r < r1; ++r) {
-    const float g = to_f32(dy[r * ld_dy + c]);
-    sw += g * ((to_f32(x[r * ld_x + c]) - mean[r]) * rstd[r]);
-    sb += g;
+// The gradient of the same rows. The columns' sums stay in each lane's registers over all of its rows; at the end the workgroup's groups add theirs
+// up in LDS, one after the other, and the workgroup writes one row of partial sums: part[block][2][cols].
+template <typename T, int G, int N>
+__global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const void* __restrict__ weight,
+                                                                  uint32_t weight_type, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                                                                  int64_t ld_dx, int64_t rows, uint32_t cols, float* __restrict__ part) {
+  typedef Share<T, G, N> S;
+  constexpr int E = S::E, kRows = Group<G>::kRows;
+  __shared__ float red[2][2][Group<G>::kWaves];
+  const S s(cols);
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+  Row<T, G, N> next_x, next_dy;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto ask = [&](int64_t q) {
+    next_x.load(x + q * ld_x, s);
+    next_dy.load(dy + q * ld_dy, s);
+    next_mean = mean[q];
+    next_rstd = rstd[q];
+  };
+  if (kAhead<G> && r < rows) ask(r);
+  float w[E], sw[E] = {}, sb[E] = {};
+#pragma unroll
+  for (int j = 0; j < S::P; ++j) load_vector(weight, weight_type, s, j, 1.f, w + j * S::V);
+  for (int odd = 0; r < rows; r += step, odd ^= 1) {
+    if (!kAhead<G>) ask(r);
+    const Row<T, G, N> rx = next_x, rdy = next_dy;
+    const float mu = next_mean, rs = next_rstd;
+    if (kAhead<G> && r + step < rows) ask(r + step);
+    float h[E], a[E], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float g = rdy.get(i);
+      h[i] = (rx.get(i) - mu) * rs;
+      a[i] = g * w[i];
+      sw[i] += g * h[i];
+      sb[i] += g;
+      if (s.mine(i)) {
+        s1 += a[i];
+        s2 += a[i] * h[i];
+      }
+    }
+    if (dx) {
+      const float m1 = group_sum<G>(s1, red[odd][0]) / (float)cols, m2 = group_sum<G>(s2, red[odd][1]) / (float)cols;
+#pragma unroll
+      for (int i = 0; i < E; ++i) a[i] = rs * (a[i] - m1 - h[i] * m2);
+#pragma unroll
+      for (int j = 0; j < S::P; ++j) Row<T, G, N>::store(dx + r * ld_dx, s, j, a + j * S::V);
+    }
   }
-  part[(int64_t)blockIdx.y * 2 * cols + c] = sw;
-  part[((int64_t)blockIdx.y * 2 + 1) * cols + c] = sb;
+  if (!part) return;
+  float* out = part + (int64_t)blockIdx.x * 2 * cols;
+  if (kRows == 1) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (s.mine(i)) {
+        out[s.at[i / S::V] + i % S::V] = sw[i];
+        out[cols + s.at[i / S::V] + i % S::V] = sb[i];
+      }
+    return;
+  }
+  __shared__ float sums[kRows == 1 ? 1 : 2][kRows == 1 ? 1 : G * E];
+  const int group = threadIdx.x / G, lane = threadIdx.x % G;
+  for (int k = 0; k < kRows; ++k) {
+    if (group == k) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        sums[0][i * G + lane] = k ? sums[0][i * G + lane] + sw[i] : sw[i];
+        sums[1][i * G + lane] = k ? sums[1][i * G + lane] + sb[i] : sb[i];
+      }
+    }
+    __syncthreads();
+  }
+  if (group == 0) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (s.mine(i)) {
+        out[s.at[i / S::V] + i % S::V] = sums[0][i * G + lane];
+        out[cols + s.at[i / S::V] + i % S::V] = sums[1][i * G + lane];
+      }
+  }
 }
 
+// The partial sums of `parts` workgroups, added up in double: a workgroup takes 32 columns of one of the two sums, 32 lanes a row of partial sums.
 template <typename W>
-__global__ __launch_bounds__(kWave) void k_norm_columns_sum(const float* __restrict__ part, int slabs, int cols, W* __restrict__ dw, W* __restrict__ db) {
-  const int64_t c = (int64_t)blockIdx.x * kWave + threadIdx.x;
+__global__ __launch_bounds__(1024) void k_norm_columns_sum(const float* __restrict__ part, int64_t parts, uint32_t cols, W* __restrict__ dw, W* __restrict__ db) {
+  __shared__ double sums[32][33];
+  const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
+  W* out = blockIdx.y ? db : dw;
+  if (!out) return;
+  const uint64_t c = (uint64_t)blockIdx.x * 32 + col;
+  double s = 0.0;
+  if (c < cols)
+    for (int64_t k = row; k < parts; k += 32) s += (double)part[(2 * k + blockIdx.y) * cols + c];
+  sums[row][col] = s;
+  __syncthreads();
+  if (row == 0 && c < cols) {
+    for (int i = 1; i < 32; ++i) s += sums[i][col];
+    out[c] = from_f32<W>((float)s);
+  }
+}
+
+// ---- rows too long for registers: the row is read again for every use
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_long(const T* x, int64_t ld_x, Vectors wb, T* y, int64_t ld_y, float* __restrict__ mean_out,
+                                                    float* __restrict__ rstd_out, int64_t rows, uint32_t cols, float eps) {
+  __shared__ float red[16];
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* xr = x + r * ld_x;
+    float s = 0.f;
+    for (uint32_t i = threadIdx.x; i < cols; i += 1024) s += to_f32(xr[i]);
+    const float mean = block_sum<16>(s, red) / (float)cols;
+    s = 0.f;
+    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
+      const float d = to_f32(xr[i]) - mean;
+      s += d * d;
+    }
+    const float rstd = 1.f / sqrtf(block_sum<16>(s, red) / (float)cols + eps);
+    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
+      const float h = (to_f32(xr[i]) - mean) * rstd;
+      y[r * ld_y + i] = from_f32<T>(h * (wb.w ? load_as(wb.w, i, wb.type) : 1.f) + (wb.b ? load_as(wb.b, i, wb.type) : 0.f));
+    }
+    if (threadIdx.x == 0) {
+      if (mean_out) mean_out[r] = mean;
+      if (rstd_out) rstd_out[r] = rstd;
+    }
+  }
+}
+
+constexpr int kSlab = 128;   // rows whose column sums one lane adds up
+
+// Partial sums of dy xh and dy over a slab of rows, a column a lane. Runs before dx, which may overwrite dy or x.
+template <typename T>
+__global__ __launch_bounds__(kWave) void k_norm_long_columns(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ x, int64_t ld_x,
+                                                             const float* __restrict__ mean, const float* __restrict__ rstd, int64_t rows, uint32_t cols,
+                                                             float* __restrict__ part) {
+  const uint32_t c = blockIdx.x * kWave + threadIdx.x;
   if (c >= cols) return;
-  double sw = 0.0, sb = 0.0;
-  for (int64_t k = 0; k < slabs; ++k) {
-    sw += part[k * 2 * cols + c];
-    sb += part[(k * 2 + 1) * cols + c];
-  }
-  if (dw) dw[c] = from_f32<W>((float)sw);
-  if (db) db[c] = from_f32<W>((float)sb);
-}
-
-template <typename T, typename W>
-__global__ __launch_bounds__(kBlock) void k_norm_rows(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const W* __restrict__ w,
-                                                      const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t ld_dx, int cols) {
-  __shared__ float red[4];
-  const int64_t r = blockIdx.x;
-  const float mu = mean[r], rs = rstd[r];
-  float s1 = 0.f, s2 = 0.f;
-  for (int64_t i = threadIdx.x; i < cols; i += kBlock) {
-    const float a = to_f32(dy[r * ld_dy + i]) * (w ? to_f32(w[i]) : 1.f);
-    s1 += a;
-    s2 += a * ((to_f32(x[r * ld_x + i]) - mu) * rs);
-  }
-  const float m1 = block_sum<4>(s1, red) / (float)cols;
-  const float m2 = block_sum<4>(s2, red) / (float)cols;
-  for (int64_t i = threadIdx.x; i < cols; i += kBlock) {
-    const float a = to_f32(dy[r * ld_dy + i]) * (w ? to_f32(w[i]) : 1.f);
-    const float h = (to_f32(x[r * ld_x + i]) - mu) * rs;
-    dx[r * ld_dx + i] = from_f32<T>(rs * (a - m1 - h * m2));
+  for (int64_t slab = blockIdx.y; slab * kSlab < rows; slab += gridDim.y) {
+    const int64_t r0 = slab * kSlab, r1 = min(r0 + kSlab, rows);
+    float sw = 0.f, sb = 0.f;
+    for (int64_t r = r0; r < r1; ++r) {
+      const float g = to_f32(dy[r * ld_dy + c]);
+      sw += g * ((to_f32(x[r * ld_x + c]) - mean[r]) * rstd[r]);
+      sb += g;
+    }
+    part[slab * 2 * cols + c] = sw;
+    part[(slab * 2 + 1) * cols + c] = sb;
   }
 }
 
-unsigned slabs_of(int64_t rows) { return (unsigned)((rows + kSlab - 1) / kSlab); }
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_long_rows(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const void* __restrict__ w, uint32_t weight_type,
+                                                         const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t ld_dx, int64_t rows,
+                                                         uint32_t cols) {
+  __shared__ float red[16];
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const float mu = mean[r], rs = rstd[r];
+    float s1 = 0.f, s2 = 0.f;
+    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
+      const float a = to_f32(dy[r * ld_dy + i]) * (w ? load_as(w, i, weight_type) : 1.f);
+      s1 += a;
+      s2 += a * ((to_f32(x[r * ld_x + i]) - mu) * rs);
+    }
+    const float m1 = block_sum<16>(s1, red) / (float)cols;
+    const float m2 = block_sum<16>(s2, red) / (float)cols;
+    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
+      const float a = to_f32(dy[r * ld_dy + i]) * (w ? load_as(w, i, weight_type) : 1.f);
+      const float h = (to_f32(x[r * ld_x + i]) - mu) * rs;
+      dx[r * ld_dx + i] = from_f32<T>(rs * (a - m1 - h * m2));
+    }
+  }
+}
+
+// Calls f(group size, packs) as integral constants for the smallest group that holds a row with at most `most` elements a lane; false
+// if none does.
+template <int V, int most, typename F>
+bool with_group(int64_t cols, F&& f) {
+  using std::integral_constant;
+  const int64_t packs = (cols + V - 1) / V;
+  auto take = [&](auto g, auto n) { f(g, n); return true; };
+  if (cols < V) return take(integral_constant<int, 8>{}, integral_constant<int, 0>{});
+  if (packs <= 8) return take(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  if (packs <= 16) return take(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (packs <= 32) return take(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  if (packs <= 64) return take(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (packs <= 128) return take(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  constexpr int N = most / V;
+  if (N >= 4 && packs <= 256) return take(integral_constant<int, 64>{}, integral_constant<int, N >= 4 ? 4 : 1>{});
+  if (N > 4 && packs <= 64 * N) return take(integral_constant<int, 64>{}, integral_constant<int, N>{});
+  if (packs <= 256 * N / 2) return take(integral_constant<int, 256>{}, integral_constant<int, N / 2>{});
+  if (packs <= 256 * N) return take(integral_constant<int, 256>{}, integral_constant<int, N>{});
+  if (packs <= 1024 * N / 2) return take(integral_constant<int, 1024>{}, integral_constant<int, N / 2>{});
+  if (packs <= 1024 * N) return take(integral_constant<int, 1024>{}, integral_constant<int, N>{});
+  return false;
+}
+// Elements a lane holds at most: forward the row and two vectors, backward two rows, one vector and two sums. 32 and 16 leave
+// every wavefront of a workgroup of 1024 the 128 registers that it can have.
+constexpr int kMostForward = 32, kMostBackward = 16;
+
+int64_t slabs_of(int64_t rows) { return (rows + kSlab - 1) / kSlab; }
+
+// Workgroups of the backward pass over rows in registers, at most this many: each writes one row of partial sums.
+constexpr int64_t kBackBlocks = 512;
+int64_t back_blocks(int64_t rows, int rows_a_block) { return std::min((rows + rows_a_block - 1) / rows_a_block, kBackBlocks); }
+template <int V>
+int64_t back_parts(int64_t rows, int64_t cols) {
+  int64_t parts = slabs_of(rows);
+  with_group<V, kMostBackward>(cols, [&](auto g, auto) { parts = back_blocks(rows, Group<decltype(g)::value>::kRows); });
+  return parts;
+}
 
 }  // namespace
 }  // namespace lopt
@@ -111,20 +394,26 @@ lopt_status lopt_layer_norm(const void* x, int64_t ld_x, const void* weight, con
   LOPT_CHECK(check_array("rstd", rstd, 4, false));
   if (rows == 0) return LOPT_OK;
   if (y == x && ld_y != ld_x && rows > 1) return fail_call(LOPT_EINVAL, "y is x, but ld_y is not ld_x");
+  const Vectors wb{weight, bias, weight_type};
   with_type(type, [&](auto t) {
-    with_type(weight_type, [&](auto u) {
-      using T = decltype(t);
-      using W = decltype(u);
-      hipLaunchKernelGGL((k_norm<T, W>), dim3((unsigned)rows), dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)x, ld_x, (const W*)weight,
-                         (const W*)bias, (T*)y, ld_y, mean, rstd, (int)cols, eps);
+    using T = decltype(t);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const bool held = with_group<Pack<T>::n, kMostForward>(cols, [&](auto g, auto n) {
+      constexpr int G = decltype(g)::value, N = decltype(n)::value;
+      const int64_t blocks = std::min<int64_t>((rows + Group<G>::kRows - 1) / Group<G>::kRows, G == 1024 ? 512 : 2048);
+      hipLaunchKernelGGL((k_norm<T, G, N>), dim3((unsigned)blocks), dim3(Group<G>::kThreads), 0, stream, (const T*)x, ld_x, wb, (T*)y, ld_y, mean, rstd,
+                         rows, (uint32_t)cols, eps);
     });
+    if (!held)
+      hipLaunchKernelGGL(k_norm_long<T>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(1024), 0, stream, (const T*)x, ld_x, wb, (T*)y, ld_y, mean,
+                         rstd, rows, (uint32_t)cols, eps);
   });
   return launch_status("lopt_layer_norm");
 }
 
 size_t lopt_layer_norm_workspace(int64_t rows, int64_t cols) {
-  if (rows <= 0 || cols <= 0) return 0;
-  return (size_t)slabs_of(rows) * 2 * (size_t)cols * sizeof(float);
+  if (rows <= 0 || cols <= 0 || rows > 0x7fffffffLL || cols > 0x7fffffffLL) return 0;
+  return (size_t)std::max(back_parts<4>(rows, cols), back_parts<8>(rows, cols)) * 2 * (size_t)cols * sizeof(float);
 }
 
 lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const float* mean,
@@ -151,22 +440,31 @@ lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
   if (rows == 0 && !columns) return LOPT_OK;
   hipStream_t stream = (hipStream_t)hip_stream;
   float* part = (float*)workspace;
+  const uint32_t n_cols = (uint32_t)cols;
   with_type(type, [&](auto t) {
-    with_type(weight_type, [&](auto u) {
-      using T = decltype(t);
-      using W = decltype(u);
-      const unsigned strips = (unsigned)((cols + kWave - 1) / kWave);
-      if (columns) {
-        if (rows > 0)
-          hipLaunchKernelGGL(k_norm_columns<T>, dim3(strips, slabs_of(rows)), dim3(kWave), 0, stream, (const T*)dy, ld_dy, (const T*)x, ld_x, mean, rstd,
-                             (int)rows, (int)cols, part);
-        hipLaunchKernelGGL(k_norm_columns_sum<W>, dim3(strips), dim3(kWave), 0, stream, (const float*)part, (int)slabs_of(rows), (int)cols,
-                           (W*)dweight, (W*)dbias);
+    using T = decltype(t);
+    int64_t parts = 0;
+    if (rows > 0) {
+      parts = back_parts<Pack<T>::n>(rows, cols);
+      const bool held = with_group<Pack<T>::n, kMostBackward>(cols, [&](auto g, auto n) {
+        constexpr int G = decltype(g)::value, N = decltype(n)::value;
+        hipLaunchKernelGGL((k_norm_back<T, G, N>), dim3((unsigned)parts), dim3(Group<G>::kThreads), 0, stream, (const T*)dy, ld_dy, (const T*)x, ld_x, weight,
+                           weight_type, mean, rstd, (T*)dx, ld_dx, rows, n_cols, columns ? part : nullptr);
+      });
+      if (!held) {
+        if (columns)
+          hipLaunchKernelGGL(k_norm_long_columns<T>, dim3((n_cols + kWave - 1) / kWave, (unsigned)std::min<int64_t>(parts, 1024)), dim3(kWave), 0, stream,
+                             (const T*)dy, ld_dy, (const T*)x, ld_x, mean, rstd, rows, n_cols, part);
+        if (dx)
+          hipLaunchKernelGGL(k_norm_long_rows<T>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(1024), 0, stream, (const T*)dy, ld_dy, (const T*)x, ld_x,
+                             weight, weight_type, mean, rstd, (T*)dx, ld_dx, rows, n_cols);
       }
-      if (dx && rows > 0)
-        hipLaunchKernelGGL((k_norm_rows<T, W>), dim3((unsigned)rows), dim3(kBlock), 0, stream, (const T*)dy, ld_dy, (const T*)x, ld_x, (const W*)weight,
-                           mean, rstd, (T*)dx, ld_dx, (int)cols);
-    });
+    }
+    if (columns)
+      with_type(weight_type, [&](auto u) {
+        using W = decltype(u);
+        hipLaunchKernelGGL(k_norm_columns_sum<W>, dim3((n_cols + 31) / 32, 2), dim3(1024), 0, stream, (const float*)part, parts, n_cols, (W*)dweight, (W*)dbias);
+      });
   });
   return launch_status("lopt_layer_norm_backward");
 }
