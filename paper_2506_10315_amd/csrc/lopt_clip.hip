@@ -1,6 +1,7 @@
 // Global gradient norm over a list of tensors, and clipping: norm = sqrt(sum g^2), out = min(1, max_norm / (norm + eps)) g.
 // Two sweeps over the list with the norm between them; the list travels in the kernels' arguments, so that a call uploads and keeps
 // nothing.
+#include <algorithm>
 #include <cmath>
 
 #include "lopt_ops.h"
@@ -8,8 +9,9 @@
 namespace lopt {
 namespace {
 
-constexpr int kChunk = 16384;     // elements one workgroup takes of one tensor
+constexpr int kChunk = 4096;      // elements of one tensor that a workgroup takes at a time: 16 a thread
 constexpr int kBatch = 160;       // tensors of one launch: 24 bytes each, within the 4 KB of kernel arguments
+constexpr int kGrid = 2048;       // workgroups that share out a list, eight a compute unit; each leaves one partial sum
 
 struct ClipTensor {
   const void* in;
@@ -21,61 +23,141 @@ struct ClipTensor {
 struct ClipBatch {
   ClipTensor t[kBatch];
   int n;
+  uint32_t chunks;     // of all of them
 };
 
-__device__ __forceinline__ void store_as(void* p, int64_t i, uint32_t type, float v) {
-  if (type == LOPT_F32) ((float*)p)[i] = v;
-  else if (type == LOPT_BF16) ((bf16_t*)p)[i] = from_f32<bf16_t>(v);
-  else ((f16_t*)p)[i] = from_f32<f16_t>(v);
-}
+// A workgroup's neighbouring chunks of the batch, and the tensor that the one at hand belongs to.
+struct Walk {
+  uint32_t begin, end;
+  int k;
+  __device__ __forceinline__ Walk(const ClipBatch& b, bool backwards) {
+    begin = (uint32_t)((uint64_t)b.chunks * blockIdx.x / gridDim.x);
+    end = (uint32_t)((uint64_t)b.chunks * (blockIdx.x + 1) / gridDim.x);
+    const uint32_t at = backwards ? end - 1 : begin;   // every workgroup has a chunk
+    k = __syncthreads_count(threadIdx.x < (unsigned)b.n && b.t[threadIdx.x].first <= at) - 1;
+  }
+  __device__ __forceinline__ void seek(const ClipBatch& b, uint32_t chunk) {
+    while (k + 1 < b.n && b.t[k + 1].first <= chunk) ++k;
+    while (b.t[k].first > chunk) --k;
+  }
+  __device__ __forceinline__ static int count(const ClipBatch& b, int k, uint32_t chunk) {
+    const uint32_t next = k + 1 == b.n ? b.chunks : b.t[k + 1].first;
+    return chunk + 1 == next ? (int)b.t[k].last + 1 : kChunk;
+  }
+};
 
-// Which tensor of the batch this workgroup's chunk belongs to, and the chunk's elements.
-struct Chunk { int tensor; int64_t at; int count; };
-__device__ __forceinline__ Chunk find_chunk(const ClipBatch& b) {
-  const int below = threadIdx.x < (unsigned)b.n ? b.t[threadIdx.x].first <= blockIdx.x : 0;
-  const int k = __syncthreads_count(below) - 1;
-  const uint32_t c = blockIdx.x - b.t[k].first;
-  const bool last = k + 1 == b.n ? blockIdx.x + 1 == gridDim.x : blockIdx.x + 1 == b.t[k + 1].first;
-  return Chunk{k, (int64_t)c * kChunk, last ? (int)b.t[k].last + 1 : kChunk};
+// A thread's 16 elements of a chunk of `count`, in groups of V neighbours, 256 V apart.
+template <typename T, int V>
+__device__ __forceinline__ void load_chunk(const T* p, int count, float (&v)[16]) {
+  typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+#pragma unroll
+  for (int j = 0; j < 16 / V; ++j) {
+    const int k = (j * kBlock + (int)threadIdx.x) * V;
+    if (k + V <= count) {
+      const vec x = *(const vec*)(p + k);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[j * V + e] = to_f32(x[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[j * V + e] = k + e < count ? to_f32(p[k + e]) : 0.f;
+    }
+  }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_chunk(T* p, int count, const float (&v)[16]) {
+  typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+#pragma unroll
+  for (int j = 0; j < 16 / V; ++j) {
+    const int k = (j * kBlock + (int)threadIdx.x) * V;
+    if (k + V <= count) {
+      vec x;
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] = from_f32<T>(v[j * V + e]);
+      *(vec*)(p + k) = x;
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (k + e < count) p[k + e] = from_f32<T>(v[j * V + e]);
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_chunk_as(const void* p, int64_t at, uint32_t type, int count, float (&v)[16]) {
+  if (type == LOPT_F32) load_chunk<float, V>((const float*)p + at, count, v);
+  else if (type == LOPT_BF16) load_chunk<bf16_t, V>((const bf16_t*)p + at, count, v);
+  else load_chunk<f16_t, V>((const f16_t*)p + at, count, v);
 }
 
 __global__ __launch_bounds__(kBlock) void k_clip_squares(const ClipBatch b, double* __restrict__ part) {
   __shared__ double red[4];
-  const Chunk c = find_chunk(b);
-  const uint32_t type = b.t[c.tensor].type;
+  Walk w(b, false);
   double s = 0.0;
-  for (int i = threadIdx.x; i < c.count; i += kBlock) {
-    const double g = (double)load_as(b.t[c.tensor].in, c.at + i, type);
-    s += g * g;
+  for (uint32_t c = w.begin; c < w.end; ++c) {
+    w.seek(b, c);
+    const int count = Walk::count(b, w.k, c);
+    const int64_t at = (int64_t)(c - b.t[w.k].first) * kChunk;
+    float v[16];
+    if (b.t[w.k].type == LOPT_F32) load_chunk<float, 4>((const float*)b.t[w.k].in + at, count, v);
+    else load_chunk_as<8>(b.t[w.k].in, at, b.t[w.k].type, count, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += (double)v[i] * (double)v[i];
   }
   s = block_sum<4>(s, red);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// norm[0] for the caller, coef[0] for the second sweep.
-__global__ __launch_bounds__(kBlock) void k_clip_norm(const double* __restrict__ part, int64_t n, float max_norm, float* __restrict__ norm,
-                                                      float* __restrict__ coef) {
-  __shared__ double red[4];
+// The norm from the partial sums of every launch of the first sweep, in every thread, and the factor.
+struct Norm { float norm, factor; };
+__device__ __forceinline__ Norm join_norm(const double* __restrict__ part, int parts, float max_norm, double* red) {
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += kBlock) s += part[i];
-  s = block_sum<4>(s, red);
-  if (threadIdx.x == 0) {
-    const float v = (float)sqrt(s);
-    norm[0] = v;
-    const float c = max_norm / (v + LOPT_CLIP_EPS);
-    coef[0] = c > 1.f ? 1.f : c;   // NaN stays
+  for (int i = threadIdx.x; i < parts; i += kBlock) s += part[i];
+  const float v = (float)sqrt(block_sum<4>(s, red));
+  const float c = max_norm / (v + LOPT_CLIP_EPS);
+  return Norm{v, c > 1.f ? 1.f : c};   // NaN stays
+}
+__global__ __launch_bounds__(kBlock) void k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm) {
+  __shared__ double red[4];
+  const Norm n = join_norm(part, parts, 0.f, red);
+  if (threadIdx.x == 0) norm[0] = n.norm;
+}
+
+// Every workgroup joins the partial sums for itself, which takes the place of a launch in between, and goes through its chunks from the last to
+// the first: what the first sweep read last is still in the Infinity Cache.
+__global__ __launch_bounds__(kBlock) void k_clip_scale(const ClipBatch b, const double* __restrict__ part, int parts, float max_norm, float* __restrict__ norm) {
+  __shared__ double red[4];
+  const Norm n = join_norm(part, parts, max_norm, red);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n.norm;
+  const float f = n.factor;
+  Walk w(b, true);
+  for (uint32_t c = w.end; c-- > w.begin;) {
+    w.seek(b, c);
+    const ClipTensor& t = b.t[w.k];
+    if (f == 1.f && t.in == t.out) continue;
+    const int count = Walk::count(b, w.k, c);
+    const int64_t at = (int64_t)(c - t.first) * kChunk;
+    float v[16];
+    if (t.type == LOPT_F32 && t.out_type == LOPT_F32) {
+      load_chunk<float, 4>((const float*)t.in + at, count, v);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] *= f;
+      store_chunk<float, 4>((float*)t.out + at, count, v);
+    } else {
+      load_chunk_as<8>(t.in, at, t.type, count, v);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] *= f;
+      if (t.out_type == LOPT_F32) store_chunk<float, 8>((float*)t.out + at, count, v);
+      else if (t.out_type == LOPT_BF16) store_chunk<bf16_t, 8>((bf16_t*)t.out + at, count, v);
+      else store_chunk<f16_t, 8>((f16_t*)t.out + at, count, v);
+    }
   }
 }
 
-__global__ __launch_bounds__(kBlock) void k_clip_scale(const ClipBatch b, const float* __restrict__ coef) {
-  const Chunk c = find_chunk(b);
-  const ClipTensor& t = b.t[c.tensor];
-  const float f = coef[0];
-  if (f == 1.f && t.in == t.out) return;
-  for (int i = threadIdx.x; i < c.count; i += kBlock) store_as(t.out, c.at + i, t.out_type, f * load_as(t.in, c.at + i, t.type));
-}
-
 int64_t chunks_of(int64_t count) { return (count + kChunk - 1) / kChunk; }
+// Workgroups of a launch that has `here` of the list's `all` chunks.
+int grid_of(int64_t here, int64_t all) { return (int)std::min<int64_t>(here, (here * kGrid + all - 1) / all); }
+// Partial sums of n tensors: kGrid and, for rounding up, one for every launch; no more than one a chunk. A launch ends after kBatch tensors, or
+// with more than 0.75 * 2^30 chunks.
+size_t most_parts(size_t n, int64_t chunks) { return (size_t)std::min<int64_t>(chunks, kGrid + (int64_t)((n + kBatch - 1) / kBatch) + (chunks >> 29)); }
 
 }  // namespace
 }  // namespace lopt
@@ -85,9 +167,9 @@ using namespace lopt;
 extern "C" {
 
 size_t lopt_clip_workspace(size_t n, const int64_t* counts) {
-  size_t chunks = 0;
-  for (size_t i = 0; counts && i < n; ++i) chunks += counts[i] > 0 ? (size_t)chunks_of(counts[i]) : 0;
-  return 16 + chunks * sizeof(double);
+  int64_t chunks = 0;
+  for (size_t i = 0; counts && i < n; ++i) chunks += counts[i] > 0 && counts[i] < (int64_t)1 << 40 ? chunks_of(counts[i]) : 0;
+  return std::max<size_t>(16, most_parts(n, chunks) * sizeof(double));
 }
 
 lopt_status lopt_clip_grads(size_t n, const int64_t* counts, const void* const* grads, const uint32_t* types, void* const* out,
@@ -109,32 +191,35 @@ lopt_status lopt_clip_grads(size_t n, const int64_t* counts, const void* const* 
     if (out && out[i] == grads[i] && types[i] != out_types[i]) return fail_call(LOPT_EINVAL, "tensor %zu: in place, but of another type", i);
     chunks += chunks_of(counts[i]);
   }
-  if (chunks >= (int64_t)1 << 31) return fail_call(LOPT_ESHAPE, "more than 2^45 elements");
-  LOPT_CHECK(check_workspace(workspace, workspace_bytes, 16 + (size_t)chunks * sizeof(double)));
+  LOPT_CHECK(check_workspace(workspace, workspace_bytes, std::max<size_t>(16, most_parts(n, chunks) * sizeof(double))));
   hipStream_t stream = (hipStream_t)hip_stream;
-  float* coef = (float*)workspace;
-  double* part = (double*)((char*)workspace + 16);
+  double* part = (double*)workspace;
+  int parts = 0;
   for (int pass = 0; pass < (out ? 2 : 1); ++pass) {
-    size_t i = 0;
-    int64_t done = 0;
-    while (i < n) {
+    for (size_t i = 0; i < n;) {
       ClipBatch b;
       b.n = 0;
       int64_t here = 0;
       for (; i < n && b.n < kBatch; ++i) {
         if (counts[i] == 0) continue;
         const int64_t c = chunks_of(counts[i]);
-        if (here > 0 && here + c > 0x7fffffff / kBlock) break;   // a grid's threads fit 31 bits
+        if (here + c > (int64_t)1 << 30) break;   // one tensor has 2^28 at most
         b.t[b.n++] = ClipTensor{grads[i], out ? out[i] : nullptr, (uint32_t)here, (uint32_t)(counts[i] - (c - 1) * kChunk - 1), types[i], out ? out_types[i] : 0};
         here += c;
       }
       if (!here) break;
-      if (pass == 0) hipLaunchKernelGGL(k_clip_squares, dim3((unsigned)here), dim3(kBlock), 0, stream, b, part + done);
-      else hipLaunchKernelGGL(k_clip_scale, dim3((unsigned)here), dim3(kBlock), 0, stream, b, (const float*)coef);
-      done += here;
+      b.chunks = (uint32_t)here;
+      const dim3 grid(grid_of(here, chunks));
+      if (pass == 0) {
+        hipLaunchKernelGGL(k_clip_squares, grid, dim3(kBlock), 0, stream, b, part + parts);
+        parts += grid.x;
+      } else {
+        hipLaunchKernelGGL(k_clip_scale, grid, dim3(kBlock), 0, stream, b, (const double*)part, parts, max_norm, norm);
+        norm = nullptr;   // the first launch writes it
+      }
     }
-    if (pass == 0) hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(kBlock), 0, stream, (const double*)part, chunks, max_norm, norm, coef);
   }
+  if (norm) hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(kBlock), 0, stream, (const double*)part, parts, norm);
   return launch_status("lopt_clip_grads");
 }
 
