@@ -8,6 +8,7 @@ Tensors are CUDA tensors of float32, bfloat16 or float16; `layer_norm` and `toke
 from __future__ import annotations
 
 import ctypes as C
+import operator
 from typing import Iterable, List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
@@ -54,12 +55,17 @@ def _matrix(name: str, t: torch.Tensor) -> Tuple[torch.Tensor, int, int, int]:
     return t, t.numel() // cols, cols, cols
 
 
+# the current stream's handle without the stream object, which costs more than the launch of a small kernel
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _run(fn, device: torch.device, *args):
-    if torch.cuda.current_device() == device.index:
-        status = fn(*args, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    if torch.cuda.current_device() == index:
+        status = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            status = fn(*args, torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
     if status:
         _check(status)
 
@@ -86,35 +92,51 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+def _clip_list(name: str, ts: Sequence[torch.Tensor], device: torch.device):
+    """(pointers, lopt_types, whether all are contiguous) of a list of tensors on `device`."""
+    for dev in set(map(_DEVICE, ts)):
+        if dev != device or dev.type != "cuda":
+            raise ValueError(f"{name}: a tensor on {dev}; all have to be on one CUDA device")
+    dtypes = list(map(_DTYPE, ts))
+    for k in set(dtypes):
+        if k not in _TYPES:
+            raise ValueError(f"{name}: a tensor of {k}; float32, bfloat16 or float16 is needed")
+    contiguous = all(map(torch.Tensor.is_contiguous, ts))
+    if not contiguous:
+        for t in ts:
+            if t.layout != torch.strided or not _dense(t):
+                raise ValueError(f"{name}: a tensor that does not fill one run of memory")
+    n = len(ts)
+    return (C.c_void_p * n)(*map(torch.Tensor.data_ptr, ts)), (C.c_uint32 * n)(*[_TYPES[k] for k in dtypes]), contiguous
+
+
+_DEVICE, _DTYPE, _SHAPE = operator.attrgetter("device"), operator.attrgetter("dtype"), operator.attrgetter("shape")
+
+
 def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], max_norm: float) -> torch.Tensor:
     n = len(grads)
     if n == 0:
         raise ValueError("no gradients")
     device = grads[0].device
-    for name, ts in (("grads", grads), ("out", out or ())):
-        for t in ts:
-            if t.device != device or not t.is_cuda or t.dtype not in _TYPES or t.layout != torch.strided:
-                raise ValueError(f"{name}: CUDA tensors of float32, bfloat16 or float16 on one device are needed, not "
-                                 f"{t.dtype} on {t.device}")
-            if not _dense(t):
-                raise ValueError(f"{name}: a tensor of strides {t.stride()} does not fill one run of memory")
-    if out is not None:
+    gp, gt, contiguous = _clip_list("grads", grads, device)
+    op = ot = None
+    if out is grads:
+        op, ot = gp, gt
+    elif out is not None:
         if len(out) != n:
             raise ValueError(f"{len(out)} outputs for {n} gradients")
-        for g, o in zip(grads, out):
-            if g.shape != o.shape or (g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous())):
-                raise ValueError("an output's shape or strides are not its gradient's")
-    counts = (C.c_int64 * n)(*[g.numel() for g in grads])
-    gp = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
-    gt = (C.c_uint32 * n)(*[_TYPES[g.dtype] for g in grads])
-    op = ot = None
-    if out is not None:
-        op = (C.c_void_p * n)(*[o.data_ptr() for o in out])
-        ot = (C.c_uint32 * n)(*[_TYPES[o.dtype] for o in out])
+        op, ot, out_contiguous = _clip_list("out", out, device)
+        if list(map(_SHAPE, grads)) != list(map(_SHAPE, out)):
+            raise ValueError("an output's shape is not its gradient's")
+        if not (contiguous and out_contiguous):
+            for g, o in zip(grads, out):
+                if g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous()):
+                    raise ValueError("an output's strides are not its gradient's")
+    counts = (C.c_int64 * n)(*map(torch.Tensor.numel, grads))
     L = lib()
     norm = torch.empty((), dtype=torch.float32, device=device)
-    ws = _workspace(L.lopt_clip_workspace(n, counts), device)
-    _run(L.lopt_clip_grads, device, n, counts, gp, gt, op, ot, float(max_norm), norm.data_ptr(), _ptr(ws), ws.numel())
+    ws = torch.empty(L.lopt_clip_workspace(n, counts), dtype=torch.uint8, device=device)
+    _run(L.lopt_clip_grads, device, n, counts, gp, gt, op, ot, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel())
     return norm
 
 
@@ -164,8 +186,8 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     if bias is not None:
         bias = _expect("bias", bias, x, wtype, (cols,))
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
-    mean, rstd = stats[0], stats[1]
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
     _run(lib().lopt_layer_norm, x.device, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(),
          rows, cols, eps, kind, _TYPES[wtype] if wtype is not None else 0)
     return y, mean, rstd
