@@ -251,8 +251,18 @@ __global__ __launch_bounds__(1024) void k_norm_columns_sum(const float* __restri
   if (!out) return;
   const uint64_t c = (uint64_t)blockIdx.x * 32 + col;
   double s = 0.0;
-  if (c < cols)
-    for (int64_t k = row; k < parts; k += 32) s += (double)part[(2 * k + blockIdx.y) * cols + c];
+  if (c < cols) {
+    const float* p = part + (uint64_t)blockIdx.y * cols + c;
+    int64_t k = row;
+    for (; k + 32 * 7 < parts; k += 32 * 8) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p[2 * (k + 32 * i) * cols];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += (double)v[i];
+    }
+    for (; k < parts; k += 32) s += (double)p[2 * k * cols];
+  }
   sums[row][col] = s;
   __syncthreads();
   if (row == 0 && c < cols) {

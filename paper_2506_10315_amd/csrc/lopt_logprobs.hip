@@ -10,9 +10,9 @@ namespace {
 
 // The order of the alternatives as one number: larger logit first, NaN above all, +0 and -0 alike, lower index first among equals.
 // No element's number is 0 or all ones.
-__device__ __forceinline__ uint32_t order_of(float x) {
+__device__ __forceinline__ uint32_t order_of(float x) {   // NaN: see piece_top
   const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
-  return x != x ? 0xfffffffeu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ uint64_t rank_key(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (0xffffffffu - index); }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
@@ -81,12 +81,11 @@ __device__ __forceinline__ void write_row(const Outputs& o, int64_t r, int lane,
   }
 }
 
-// A wavefront takes 2048 logits of a row at a time, 32 a lane in accesses of 16 bytes. The access that would pass the row's end
+// A wavefront takes a piece of a row at a time, E = 16 or 32 logits a lane in accesses of 16 bytes. The access that would pass the row's end
 // is moved back to end with it, and the elements that the lane before has are masked.
-constexpr int kPiece = 2048;
-template <typename T>
+template <typename T, int E>
 struct Piece {
-  static constexpr int V = Pack<T>::n, N = 32 / V;
+  static constexpr int V = Pack<T>::n, N = E / V, kSize = E * kWave;
   typedef typename Pack<T>::type pack;
   pack raw[N];
   __device__ __forceinline__ static uint32_t place(uint32_t first, int j) { return first + (j * kWave + (threadIdx.x & 63)) * V; }
@@ -112,95 +111,154 @@ struct Piece {
     const uint32_t k = index(first, i, n);
     return k >= place(first, i / V) && k < n;
   }
-  __device__ __forceinline__ void unpack(float (&x)[32], uint32_t first, uint32_t n) const {
-    if (first + kPiece <= n) {
+  __device__ __forceinline__ void unpack(float (&x)[E], uint32_t first, uint32_t n) const {
+    if (first + kSize <= n) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = to_f32(raw[i / V][i % V]);
+      for (int i = 0; i < E; ++i) x[i] = to_f32(raw[i / V][i % V]);
       return;
     }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (int i = 0; i < E; ++i) {
       x[i] = -INFINITY;
       if (first + i / V * kWave * V < n && mine(first, i, n)) x[i] = to_f32(raw[i / V][i % V]);
     }
   }
 };
 
-__device__ __forceinline__ void add_piece(Soft& a, const float (&x)[32], float c, bool first) {
+template <int E>
+__device__ __forceinline__ void add_piece(Soft& a, const float (&x)[E], float c, bool first) {
   float base = a.base;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) base = fmaxf(base, x[i]);
+  for (int i = 0; i < E; ++i) base = fmaxf(base, x[i]);
   if (first) a.base = base;
   else a = rebase(a, base, c);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
+  for (int i = 0; i < E; ++i) {
     const float d = x[i] - base, e = exp2_hw(d * c);
     a.s += e;
     a.h += e * fmaxf(d, -FLT_MAX);
   }
 }
 
-// The `top` largest keys of a piece in order, key k in lane k (0: there are fewer). The `top` lanes with the largest maxima hold them all: the top-th
-// of these maxima is a bound below which nothing counts, and at most 32 elements of each of these lanes pass it. They are gathered in `list`
-// (room for 32 top keys) and put in order by counting how many are larger.
-template <typename T>
-__device__ __forceinline__ uint64_t piece_top(const float (&x)[32], uint32_t first, uint32_t n, int top, uint64_t* list) {
-  const int lane = threadIdx.x & 63;
-  uint32_t ord[32], hi = 0, at = 0;
+// The largest number that at least `need` of the lanes' numbers reach; 0 if fewer than that are not 0.
+__device__ __forceinline__ uint32_t reached_by(uint32_t v, int need) {
+  int reach = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    ord[i] = Piece<T>::mine(first, i, n) ? order_of(x[i]) : 0;
-    if (ord[i] > hi) {   // in the order of the indices: the first among equals stays
-      hi = ord[i];
-      at = Piece<T>::index(first, i, n);
-    }
+  for (int l = 0; l < kWave; ++l) reach += (uint32_t)__builtin_amdgcn_readlane((int)v, l) >= v;
+  return wave_max(reach >= need ? v : 0u);
+}
+// Sum of the lanes' n (at most 63) before this one; `all`: of all lanes.
+__device__ __forceinline__ int count_before(int n, int* all) {
+  int before = 0, sum = 0;
+#pragma unroll
+  for (int b = 0; b < 6; ++b) {
+    const uint64_t mask = __ballot(n >> b & 1);
+    before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)) << b;
+    sum += __popcll(mask) << b;
   }
-  const uint64_t best = hi ? rank_key(hi, at) : 0;
-  int rank = 0;
-#pragma unroll
-  for (int l = 0; l < kWave; ++l) rank += readlane(best, l) > best;
-  const uint64_t who = __ballot(rank == top - 1);
-  const uint64_t bound = who ? readlane(best, __builtin_ctzll(who)) : 0;
-  int count = 0;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const uint64_t key = rank_key(ord[i], Piece<T>::index(first, i, n));
-    const bool pass = ord[i] && key >= bound;
-    const uint64_t mask = __ballot(pass);
-    if (pass) list[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
-    count += __popcll(mask);
+  *all = sum;
+  return before;
+}
+// The `top` largest of `count` different keys in order, key k in lane k (0: there are fewer): each goes to the place that the number of larger ones
+// names. `place`: room for `top` keys beside the list.
+__device__ __forceinline__ uint64_t in_order(const uint64_t* list, int count, int top, uint64_t* place) {
+  const int lane = threadIdx.x & 63;
+  if (count <= kWave) {
+    const uint64_t key = lane < count ? list[lane] : 0;
+    int above = 0;
+    for (int k = 0; k < count; ++k) above += readlane(key, k) > key;
+    if (lane < count && above < top) place[above] = key;
+  } else {
+    for (int c = lane; c < count; c += kWave) {
+      const uint64_t key = list[c];
+      int above = 0;
+      for (int k = 0; k < count; ++k) above += list[k] > key;
+      if (above < top) place[above] = key;
+    }
   }
   wave_sync();
-  uint64_t out = 0;
-  for (int c = 0; c < count; c += kWave) {
-    const uint64_t key = c + lane < count ? list[c + lane] : 0;
-    int above = 0;
-    for (int k = 0; k < count; ++k) above += list[k] > key;
-    // hand the key to the lane of its rank
-    for (int k = 0; k < top; ++k) {
-      const uint64_t has = __ballot(c + lane < count && above == k);
-      if (has) {
-        const uint64_t v = readlane(key, __builtin_ctzll(has));
-        if (lane == k) out = v;
-      }
-    }
-  }
+  const uint64_t out = lane < top && lane < count ? place[lane] : 0;
   wave_sync();
   return out;
+}
+
+// The `top` largest keys of a piece in order; `most` is the largest of the lane's logits (-FLT_MAX if all are masked). At least `top`
+// lanes' maxima reach `bound`, so nothing below it counts, and what lies above it belongs to fewer than `top` lanes. What equals it may be many
+// (masks, few different values): where the list does not hold them all, only the `top` of lowest index are taken.
+// `list`: room for (E + 2) top keys. `special`: there may be a NaN.
+template <typename T, int E>
+__device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, uint32_t first, uint32_t n, int top, bool special, uint64_t* list) {
+  typedef Piece<T, E> P;
+  const int room = E * top;
+  int pass = 0, count, at;
+  if (!special) {
+    const float bound = key_value((uint64_t)reached_by(order_of(most), top) << 32);
+#pragma unroll
+    for (int i = 0; i < E; ++i) pass += x[i] >= bound;
+    at = count_before(pass, &count);
+    if (count <= room && bound > -FLT_MAX) {   // no masked logit among them, nor one that is not this lane's
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (x[i] >= bound) list[at++] = rank_key(order_of(x[i]), P::index(first, i, n));
+      wave_sync();
+      return in_order(list, count, top, list + (E + 1) * top);
+    }
+  }
+  uint32_t ord[E], hi = 0;   // 0: not an element
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    ord[i] = x[i] != x[i] ? 0xfffffffeu : order_of(x[i]);
+    ord[i] = P::mine(first, i, n) ? ord[i] : 0;
+    hi = max(hi, ord[i]);
+  }
+  const uint32_t bound = max(reached_by(hi, top), 1u);
+  pass = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) pass += ord[i] > bound;
+  at = count_before(pass, &count);
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (ord[i] > bound) list[at++] = rank_key(ord[i], P::index(first, i, n));
+  int taken = 0;
+#pragma unroll
+  for (int j = 0; j < P::N; ++j) {   // in the order of the indices: packs, lanes, elements
+    pass = 0;
+#pragma unroll
+    for (int i = j * P::V; i < (j + 1) * P::V; ++i) pass += ord[i] == bound;
+    int all;
+    at = taken + count_before(pass, &all);
+#pragma unroll
+    for (int i = j * P::V; i < (j + 1) * P::V; ++i)
+      if (ord[i] == bound) {
+        if (at < top) list[count + at] = rank_key(ord[i], P::index(first, i, n));
+        ++at;
+      }
+    taken += all;
+  }
+  count += min(taken, top);
+  wave_sync();
+  return in_order(list, count, top, list + (E + 1) * top);
 }
 
 // How a row is shared out: `segments` of `pieces` pieces, a wavefront each; a row of one segment is finished by that wavefront, more are
 // joined 64 at a time by k_logprobs_join. Alternatives are found piece by piece.
 struct RowPlan {
+  int lane_elements;   // 16 or 32
   int64_t pieces, segments;
 };
+constexpr int64_t kFewPieces = 1024;
 inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
-  const int64_t all = (vocab + kPiece - 1) / kPiece;
-  if (top) return RowPlan{1, all};
+  const int64_t all = (vocab + 2047) / 2048;
+  if (top) {
+    // few rows: pieces of half the size, as long as one join takes them all
+    if (rows * all <= kFewPieces && all <= kWave / 2) return RowPlan{16, 1, (vocab + 1023) / 1024};
+    return RowPlan{32, 1, all};
+  }
   int64_t per = rows * all / 16384;
   per = per < 1 ? 1 : per > 8 ? 8 : per;
-  const int64_t segments = (all + per - 1) / per;
-  return RowPlan{(all + segments - 1) / segments, segments};
+  int64_t segments = (all + per - 1) / per;
+  if (segments > 1) segments = std::min((segments + 3) / 4 * 4, all);   // four a workgroup
+  return RowPlan{32, (all + segments - 1) / segments, segments};
 }
 
 // Workspace of one level of segments: the keys, then the sums.
@@ -209,10 +267,11 @@ inline size_t level_bytes(int64_t rows, int64_t segments, uint32_t top) {
 }
 
 // One wavefront a segment: a workgroup takes four rows where they have one segment, else four segments of a row.
-template <typename T, bool TOP>
+template <typename T, bool TOP, int E>
 __global__ __launch_bounds__(kBlock) void k_logprobs(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
                                                      int64_t ignore, int top, Outputs o, int64_t segments, uint32_t pieces, float* __restrict__ part,
                                                      uint64_t* __restrict__ keys) {
+  typedef Piece<T, E> P;
   extern __shared__ uint64_t lists[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = fminf(scale * kLog2e, FLT_MAX);
@@ -222,29 +281,31 @@ __global__ __launch_bounds__(kBlock) void k_logprobs(const T* __restrict__ x, in
     if (r >= rows) break;
     const T* row = x + r * ld;
     for (int64_t seg = whole ? 0 : (int64_t)blockIdx.y * 4 + wave; seg < segments; seg += (int64_t)gridDim.y * 4) {
-      const uint32_t first = (uint32_t)(seg * pieces) * (uint32_t)kPiece;
-      const uint32_t end = min((uint64_t)first + (uint64_t)pieces * kPiece, (uint64_t)vocab);
+      const uint32_t first = (uint32_t)(seg * pieces) * (uint32_t)P::kSize;
+      const uint32_t end = min((uint64_t)first + (uint64_t)pieces * P::kSize, (uint64_t)vocab);
+      Soft a{-FLT_MAX, 0.f, 0.f};
+      P p;
+      p.load(row, first, vocab);
       Target g{};
       if (whole) g = load_target(row, targets, r, vocab);
-      Soft a{-FLT_MAX, 0.f, 0.f};
-      Piece<T> p;
-      p.load(row, first, vocab);
       uint64_t key = 0;
-      float v[32];
+      float v[E];
       if (TOP) {
         p.unpack(v, first, vocab);
         add_piece(a, v, c, true);
-        key = piece_top<T>(v, first, vocab, top, lists + wave * 32 * top);
+        const float most = a.base;
+        a = wave_join(a, c);
+        key = piece_top<T, E>(v, most, first, vocab, top, a.s != a.s, lists + wave * (E + 2) * top);
       } else {
-        for (uint32_t f = first; f < end; f += kPiece) {
-          Piece<T> next;
-          if (f + kPiece < end) next.load(row, f + kPiece, vocab);
+        for (uint32_t f = first; f < end; f += P::kSize) {
+          P next;
+          if (f + P::kSize < end) next.load(row, f + P::kSize, vocab);
           p.unpack(v, f, vocab);
           add_piece(a, v, c, f == first);
           p = next;
         }
+        a = wave_join(a, c);
       }
-      a = wave_join(a, c);
       if (whole) {
         write_row(o, r, lane, a, g, vocab, scale, ignore, top, key);
       } else {
@@ -256,8 +317,8 @@ __global__ __launch_bounds__(kBlock) void k_logprobs(const T* __restrict__ x, in
   }
 }
 
-// Joins up to 64 neighbouring segments of a row, one wavefront: the sums lane by lane, the ordered lists of alternatives by taking the largest head
-// `top` times. `last`: all of the row's are here, and its outputs are written; else one segment of the next level is.
+// Joins up to 64 neighbouring segments of a row, one wavefront: the sums lane by lane, the ordered lists of alternatives by a bound
+// as in piece_top. `last`: all of the row's are here, and its outputs are written; else one segment of the next level is.
 template <typename T>
 __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
                                                          int64_t ignore, int top, Outputs o, int64_t segments, const float* __restrict__ part,
@@ -271,26 +332,25 @@ __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x
     const int64_t r = unit / groups, group = unit - r * groups, at = r * segments + group * kWave;
     const int count = (int)min(segments - group * kWave, (int64_t)kWave);
     Target g{};
-    if (last) g = load_target(x + r * ld, targets, r, vocab);
+    if (last && !top) g = load_target(x + r * ld, targets, r, vocab);
     Soft a{-FLT_MAX, 0.f, 0.f};
     if (lane < count) a = Soft{part[3 * (at + lane)], part[3 * (at + lane) + 1], part[3 * (at + lane) + 2]};
     uint64_t key = 0;
     if (top) {
+      uint64_t* list = lists + kWave * top;
       for (int i = lane; i < count * top; i += kWave) lists[i] = keys[at * top + i];
+      if (last) g = load_target(x + r * ld, targets, r, vocab);   // its two loads in a row run beside what follows
       wave_sync();
-      int next = 1;
-      uint64_t head = lane < count ? lists[lane * top] : 0;
-      for (int k = 0; k < top; ++k) {
-        const uint32_t hi = wave_max((uint32_t)(head >> 32));
-        const uint32_t lo = wave_max((uint32_t)(head >> 32) == hi ? (uint32_t)head : 0u);
-        const uint64_t best = (uint64_t)hi << 32 | lo;
-        if (lane == k) key = best;
-        if (head == best) {
-          head = lane < count && next < top ? lists[lane * top + next] : 0;
-          ++next;
-        }
-      }
+      // the lists are in order: where `need` of them reach a bound with their `deep`-th key, `top` keys do
+      const int deep = min((2 * top + count - 1) / count, top), need = (top + deep - 1) / deep;
+      const uint64_t bound = reached_by(lane < count ? (uint32_t)(lists[lane * top + deep - 1] >> 32) : 0u, need);
+      int pass = 0, all;
+      if (lane < count)
+        while (pass < top && lists[lane * top + pass] >> 32 >= max(bound, (uint64_t)1)) ++pass;
+      int to = count_before(pass, &all);
+      for (int k = 0; k < pass; ++k) list[to + k] = lists[lane * top + k];
       wave_sync();
+      key = in_order(list, all, top, lists);
     }
     a = wave_join(a, c);
     if (last) {
@@ -415,19 +475,20 @@ lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* t
     const uint32_t n = (uint32_t)vocab;
     uint64_t* keys = (uint64_t*)ws;
     float* part = (float*)(ws + (size_t)rows * plan.segments * top * sizeof(uint64_t));
-    if (top)
-      hipLaunchKernelGGL((k_logprobs<T, true>), grid, dim3(kBlock), 4 * 32 * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index,
-                         (int)top, o, plan.segments, (uint32_t)plan.pieces, part, keys);
-    else
-      hipLaunchKernelGGL((k_logprobs<T, false>), grid, dim3(kBlock), 0, stream, x, ld, tg, rows, n, scale, ignore_index, 0, o, plan.segments,
-                         (uint32_t)plan.pieces, part, keys);
+    auto launch = [&](auto kernel, size_t lds) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o, plan.segments, (uint32_t)plan.pieces, part, keys);
+    };
+    const size_t lds = 4 * (plan.lane_elements + 2) * top * sizeof(uint64_t);
+    if (!top) launch(k_logprobs<T, false, 32>, 0);
+    else if (plan.lane_elements == 16) launch(k_logprobs<T, true, 16>, lds);
+    else launch(k_logprobs<T, true, 32>, lds);
     for (int64_t segments = plan.segments; segments > 1;) {
       const int64_t groups = (segments + kWave - 1) / kWave;
       char* above = (char*)keys + level_bytes(rows, segments, top);
       uint64_t* keys_out = (uint64_t*)above;
       float* part_out = (float*)(above + (size_t)rows * groups * top * sizeof(uint64_t));
       hipLaunchKernelGGL(k_logprobs_join<T>, dim3((unsigned)std::min<int64_t>(rows * groups, 1 << 22)), dim3(kWave),
-                         std::min<int64_t>(segments, kWave) * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o,
+                         2 * kWave * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o,
                          segments, (const float*)part, (const uint64_t*)keys, part_out, keys_out);
       keys = keys_out;
       part = part_out;
