@@ -305,8 +305,9 @@ lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
  * Logits of -infinity are masked: probability 0. A row that is masked whole has stats (-infinity, -infinity), logp -infinity,
  * entropy 0 and top alternatives -infinity in the order of their indices. A row with a NaN or +infinity has NaN for its logp,
  * entropy and ln S and for every top_logp; its alternatives are ordered with NaN above +infinity.
- * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, vocab or ld out of range; vocab <= 2^31 - 1), LOPT_EHIP. */
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, vocab or ld out of range; vocab <= LOPT_VOCAB_MAX), LOPT_EHIP. */
 #define LOPT_TOP_MAX 32
+#define LOPT_VOCAB_MAX 0x7fff0000
 size_t lopt_token_logprobs_workspace(int64_t rows, int64_t vocab, uint32_t top);
 lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* targets, int64_t rows, int64_t vocab,
                                 uint32_t type, float scale, int64_t ignore_index, uint32_t top, float* logp, float* entropy,

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "lopt_ops.h"
 
@@ -21,24 +22,46 @@ __device__ __forceinline__ float key_value(uint64_t key) {
   return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-// Running softmax sums of some logits x: base = the largest of them (-FLT_MAX where all are -infinity), s = sum e^(c (x - base)),
-// h = sum e^(c (x - base)) (x - base). c = scale / ln 2 goes into the hardware's 2^x; x - base is formed before it is scaled, so that large
-// logits lose nothing and a scale never makes a finite difference infinite twice. A masked logit has x - base = -infinity and
-// e = 0; its term of h is 0 because the difference is held to -FLT_MAX.
-struct Soft { float base, s, h; };
-constexpr float kLog2e = 1.44269504088896341f;
+// Running softmax sums of some logits x. With c = scale / ln 2, the hardware's 2^x, m = the largest of them and b = m c rounded:
+//   s = sum 2^t,   h = sum 2^t t,   t = x c - b in one fused operation
+// b's own rounding, m c - b = delta, is the same for every logit of the row and is taken out of ln S at the end, so that large logits lose nothing:
+//   ln S = ln s - delta ln 2,   entropy = ln s - ln 2 h / s
+// which is one vector instruction a logit less than x - m, then times c. b stays within 1e30; a row whose largest logit lies beyond (masks of the type's lowest value on the whole row) is gone through again by
+// extreme_row.
+// A masked logit has t = -infinity and 2^t = 0; for the product t is held to a finite value.
+struct Soft { float m, s, h; };
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kMostBase = 1e30f;
 
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float base_of(float m, float c) { return fmaxf(m * c, -kMostBase); }
 
-// a's sums seen from a larger base.
-__device__ __forceinline__ Soft rebase(Soft a, float base, float c) {
-  const float diff = fmaxf(a.base - base, -FLT_MAX);
-  const float f = exp2_hw((a.base - base) * c), fs = f * a.s;   // NaN where both are +infinity
-  return Soft{base, fs, f * a.h + fs * diff};
+// a's sums seen from a larger m.
+__device__ __forceinline__ Soft rebase(Soft a, float m, float c) {
+  const float diff = base_of(a.m, c) - base_of(m, c), f = exp2_hw(diff), fs = f * a.s;
+  return Soft{m, fs, f * a.h + (fs == 0.f ? 0.f : fs * diff)};
 }
 __device__ __forceinline__ Soft wave_join(Soft a, float c) {
-  a = rebase(a, wave_max(a.base), c);
-  return Soft{a.base, wave_sum(a.s), wave_sum(a.h)};
+  a = rebase(a, wave_max(a.m), c);
+  return Soft{a.m, wave_sum(a.s), wave_sum(a.h)};
+}
+
+// The sums of a whole row by differences from its largest logit m, which may be as large as the type allows: for the few rows beyond kMostBase.
+template <typename T>
+__device__ Soft extreme_row(const T* row, uint32_t n, float m, float c) {
+  Soft a{m, 0.f, 0.f};
+  for (uint32_t i = threadIdx.x & 63; i < n; i += 8 * kWave) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = i + k * kWave < n ? to_f32(row[i + k * kWave]) : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float t = i + k * kWave < n ? (v[k] - m) * c : -INFINITY, e = exp2_hw(t);
+      a.s += e;
+      a.h += e * fmaxf(t, -FLT_MAX);
+    }
+  }
+  return Soft{m, wave_sum(a.s), wave_sum(a.h)};
 }
 
 struct Outputs {
@@ -61,82 +84,96 @@ __device__ __forceinline__ Target load_target(const T* row, const int64_t* targe
 }
 
 // A row's outputs from its sums. Lane k of the wavefront holds the key of alternative k.
-__device__ __forceinline__ void write_row(const Outputs& o, int64_t r, int lane, Soft a, Target g, int vocab, float scale, int64_t ignore, int top, uint64_t key) {
+template <typename T>
+__device__ __forceinline__ void write_row(const Outputs& o, int64_t r, const T* row, int lane, Soft a, float c, Target g, uint32_t vocab, float scale, int64_t ignore, int top,
+                                          uint64_t key) {
+  float delta = 0.f;
+  if (fabsf(a.m * c) < kMostBase) delta = __builtin_fmaf(a.m, c, -base_of(a.m, c));
+  else if (a.m != -INFINITY) a = extreme_row(row, vocab, a.m, c);
   const bool empty = a.s == 0.f;
-  const float log_s = logf(a.s);
+  const float ln_s = logf(a.s), log_s = ln_s - kLn2 * delta;
   if (lane == 0) {
     if (o.logp) {
       float v = NAN;
       if (g.t == ignore) v = 0.f;
-      else if (g.t >= 0 && g.t < vocab) v = empty ? -INFINITY : scale * (g.x - a.base) - log_s;
+      else if (g.t >= 0 && g.t < vocab) v = empty ? -INFINITY : scale * (g.x - a.m) - log_s;
       o.logp[r] = v;
     }
-    if (o.entropy) o.entropy[r] = empty ? 0.f : log_s - scale * (a.h / a.s);
-    o.stats[2 * r] = empty ? -INFINITY : a.base;
+    if (o.entropy) o.entropy[r] = empty ? 0.f : ln_s - kLn2 * (a.h / a.s);
+    o.stats[2 * r] = a.m;
     o.stats[2 * r + 1] = log_s;
   }
   if (lane < top) {
     o.top_index[r * top + lane] = key_index(key);
-    o.top_logp[r * top + lane] = empty ? -INFINITY : scale * (key_value(key) - a.base) - log_s;
+    o.top_logp[r * top + lane] = empty ? -INFINITY : scale * (key_value(key) - a.m) - log_s;
   }
 }
 
-// A wavefront takes a piece of a row at a time, E = 16 or 32 logits a lane in accesses of 16 bytes. The access that would pass the row's end
-// is moved back to end with it, and the elements that the lane before has are masked.
+// A wavefront takes a piece of a row at a time, E = 16 or 32 logits a lane in accesses of 16 bytes. Accesses are aligned: `off` elements ahead of the row
+// begin a pack of 16 bytes, and pieces and packs are counted from there (rows at odd elements of 16 bits: 4096x50257 98 us, 83 at 50258; counted from
+// their own start). The pack that would begin ahead of the row begins with it, the one that would pass the row's end ends
+// with it, and the elements that they share with the pack beside them are masked.
+template <typename T>
+__device__ __forceinline__ int pack_offset(const T* row, uint32_t n) {
+  return n >= (uint32_t)Pack<T>::n ? (int)((uintptr_t)row / sizeof(T) % Pack<T>::n) : 0;
+}
 template <typename T, int E>
 struct Piece {
   static constexpr int V = Pack<T>::n, N = E / V, kSize = E * kWave;
   typedef typename Pack<T>::type pack;
   pack raw[N];
-  __device__ __forceinline__ static uint32_t place(uint32_t first, int j) { return first + (j * kWave + (threadIdx.x & 63)) * V; }
-  __device__ __forceinline__ void load(const T* row, uint32_t first, uint32_t n) {
+  int first, off, n;
+  // Where the lane's pack j would begin, in elements of the row, and where it does.
+  __device__ __forceinline__ int place(int j) const { return first + (j * kWave + (int)(threadIdx.x & 63)) * V - off; }
+  __device__ __forceinline__ int begin(int j) const { return max(min(place(j), n - V), 0); }
+  __device__ __forceinline__ int index(int i) const { return begin(i / V) + i % V; }
+  // Whether an element is one, and this lane's.
+  __device__ __forceinline__ bool mine(int i) const {
+    const int p = place(i / V), k = index(i);
+    return k >= p && k < min(p + V, n);
+  }
+  __device__ __forceinline__ bool inside() const { return first >= off && first + kSize - off <= n; }
+  __device__ __forceinline__ void load(const T* row, int first_, int off_, int n_) {
+    first = first_, off = off_, n = n_;
+    if (n >= V) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) raw[j] = *(const pack*)(row + begin(j));
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) raw[i / V][i % V] = mine(i) ? row[index(i)] : (T)-INFINITY;
+    }
+  }
+  // Elements that are not the lane's become masked ones.
+  __device__ __forceinline__ void unpack(float (&x)[E]) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = to_f32(raw[i / V][i % V]);
+    if (inside()) return;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      if (first + j * kWave * V >= n) break;
-      const uint32_t at = place(first, j);
-      if (n >= (uint32_t)V) {
-        raw[j] = *(const pack*)(row + min(at, n - V));
-      } else {
+      const int low = place(j) - begin(j), high = min(low + V, n - begin(j));   // of the pack's elements, the lane's
 #pragma unroll
-        for (int e = 0; e < V; ++e) raw[j][e] = at + e < n ? row[at + e] : (T)-INFINITY;
-      }
-    }
-  }
-  // Index of an element, and whether it is this lane's.
-  __device__ __forceinline__ static uint32_t index(uint32_t first, int i, uint32_t n) {
-    const uint32_t at = place(first, i / V);
-    return (n >= (uint32_t)V ? min(at, n - V) : at) + i % V;
-  }
-  __device__ __forceinline__ static bool mine(uint32_t first, int i, uint32_t n) {
-    const uint32_t k = index(first, i, n);
-    return k >= place(first, i / V) && k < n;
-  }
-  __device__ __forceinline__ void unpack(float (&x)[E], uint32_t first, uint32_t n) const {
-    if (first + kSize <= n) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) x[i] = to_f32(raw[i / V][i % V]);
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      x[i] = -INFINITY;
-      if (first + i / V * kWave * V < n && mine(first, i, n)) x[i] = to_f32(raw[i / V][i % V]);
+      for (int e = 0; e < V; ++e) x[j * V + e] = e >= low && e < high ? x[j * V + e] : -INFINITY;
     }
   }
 };
 
 template <int E>
-__device__ __forceinline__ void add_piece(Soft& a, const float (&x)[E], float c, bool first) {
-  float base = a.base;
+__device__ __forceinline__ float most_of(const float (&x)[E]) {
+  float m = x[0];
 #pragma unroll
-  for (int i = 0; i < E; ++i) base = fmaxf(base, x[i]);
-  if (first) a.base = base;
-  else a = rebase(a, base, c);
+  for (int i = 1; i < E; ++i) m = fmaxf(m, x[i]);
+  return m;
+}
+template <int E>
+__device__ __forceinline__ void add_piece(Soft& a, const float (&x)[E], float most, float c) {
+  const float m = fmaxf(a.m, most);
+  a = rebase(a, m, c);
+  const float b = base_of(m, c);
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float d = x[i] - base, e = exp2_hw(d * c);
+    const float t = __builtin_fmaf(x[i], c, -b), e = exp2_hw(t);
     a.s += e;
-    a.h += e * fmaxf(d, -FLT_MAX);
+    a.h += e * fmaxf(t, -kMostBase);
   }
 }
 
@@ -147,11 +184,11 @@ __device__ __forceinline__ uint32_t reached_by(uint32_t v, int need) {
   for (int l = 0; l < kWave; ++l) reach += (uint32_t)__builtin_amdgcn_readlane((int)v, l) >= v;
   return wave_max(reach >= need ? v : 0u);
 }
-// Sum of the lanes' n (at most 63) before this one; `all`: of all lanes.
+// Sum of the lanes' n (at most 127) before this one; `all`: of all lanes.
 __device__ __forceinline__ int count_before(int n, int* all) {
   int before = 0, sum = 0;
 #pragma unroll
-  for (int b = 0; b < 6; ++b) {
+  for (int b = 0; b < 7; ++b) {
     const uint64_t mask = __ballot(n >> b & 1);
     before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)) << b;
     sum += __popcll(mask) << b;
@@ -159,35 +196,44 @@ __device__ __forceinline__ int count_before(int n, int* all) {
   *all = sum;
   return before;
 }
-// The `top` largest of `count` different keys in order, key k in lane k (0: there are fewer): each goes to the place that the number of larger ones
-// names. `place`: room for `top` keys beside the list.
+// The `top` largest of `count` different keys in order, key k in lane k (0: there are fewer). Up to 64 keys: each goes to the place that the number of
+// larger ones names (`place`: room for `top` keys beside the list); more: the largest is taken `top` times.
 __device__ __forceinline__ uint64_t in_order(const uint64_t* list, int count, int top, uint64_t* place) {
   const int lane = threadIdx.x & 63;
+  uint64_t out = 0;
   if (count <= kWave) {
     const uint64_t key = lane < count ? list[lane] : 0;
     int above = 0;
     for (int k = 0; k < count; ++k) above += readlane(key, k) > key;
     if (lane < count && above < top) place[above] = key;
+    wave_sync();
+    if (lane < top && lane < count) out = place[lane];
   } else {
-    for (int c = lane; c < count; c += kWave) {
-      const uint64_t key = list[c];
-      int above = 0;
-      for (int k = 0; k < count; ++k) above += list[k] > key;
-      if (above < top) place[above] = key;
+    auto largest = [&](uint64_t below) {
+      uint64_t best = 0;
+      for (int i = lane; i < count; i += kWave) {
+        const uint64_t key = list[i];
+        if (key < below && key > best) best = key;
+      }
+      return best;
+    };
+    uint64_t mine = largest(~(uint64_t)0);
+    for (int k = 0; k < top; ++k) {
+      const uint64_t best = wave_max(mine);
+      if (lane == k) out = best;
+      if (mine == best) mine = largest(best);
     }
   }
-  wave_sync();
-  const uint64_t out = lane < top && lane < count ? place[lane] : 0;
   wave_sync();
   return out;
 }
 
-// The `top` largest keys of a piece in order; `most` is the largest of the lane's logits (-FLT_MAX if all are masked). At least `top`
+// The `top` largest keys of a piece in order; `most` is the largest of the lane's logits. At least `top`
 // lanes' maxima reach `bound`, so nothing below it counts, and what lies above it belongs to fewer than `top` lanes. What equals it may be many
 // (masks, few different values): where the list does not hold them all, only the `top` of lowest index are taken.
 // `list`: room for (E + 2) top keys. `special`: there may be a NaN.
 template <typename T, int E>
-__device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, uint32_t first, uint32_t n, int top, bool special, uint64_t* list) {
+__device__ __forceinline__ uint64_t piece_top(const Piece<T, E>& p, const float (&x)[E], float most, int top, bool special, uint64_t* list) {
   typedef Piece<T, E> P;
   const int room = E * top;
   int pass = 0, count, at;
@@ -196,10 +242,10 @@ __device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, u
 #pragma unroll
     for (int i = 0; i < E; ++i) pass += x[i] >= bound;
     at = count_before(pass, &count);
-    if (count <= room && bound > -FLT_MAX) {   // no masked logit among them, nor one that is not this lane's
+    if (count <= room && bound > -INFINITY) {   // no masked logit among them, nor one that is not this lane's
 #pragma unroll
       for (int i = 0; i < E; ++i)
-        if (x[i] >= bound) list[at++] = rank_key(order_of(x[i]), P::index(first, i, n));
+        if (x[i] >= bound) list[at++] = rank_key(order_of(x[i]), (uint32_t)p.index(i));
       wave_sync();
       return in_order(list, count, top, list + (E + 1) * top);
     }
@@ -208,7 +254,7 @@ __device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, u
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     ord[i] = x[i] != x[i] ? 0xfffffffeu : order_of(x[i]);
-    ord[i] = P::mine(first, i, n) ? ord[i] : 0;
+    ord[i] = p.mine(i) ? ord[i] : 0;
     hi = max(hi, ord[i]);
   }
   const uint32_t bound = max(reached_by(hi, top), 1u);
@@ -218,7 +264,7 @@ __device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, u
   at = count_before(pass, &count);
 #pragma unroll
   for (int i = 0; i < E; ++i)
-    if (ord[i] > bound) list[at++] = rank_key(ord[i], P::index(first, i, n));
+    if (ord[i] > bound) list[at++] = rank_key(ord[i], (uint32_t)p.index(i));
   int taken = 0;
 #pragma unroll
   for (int j = 0; j < P::N; ++j) {   // in the order of the indices: packs, lanes, elements
@@ -230,7 +276,7 @@ __device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, u
 #pragma unroll
     for (int i = j * P::V; i < (j + 1) * P::V; ++i)
       if (ord[i] == bound) {
-        if (at < top) list[count + at] = rank_key(ord[i], P::index(first, i, n));
+        if (at < top) list[count + at] = rank_key(ord[i], (uint32_t)p.index(i));
         ++at;
       }
     taken += all;
@@ -240,25 +286,20 @@ __device__ __forceinline__ uint64_t piece_top(const float (&x)[E], float most, u
   return in_order(list, count, top, list + (E + 1) * top);
 }
 
-// How a row is shared out: `segments` of `pieces` pieces, a wavefront each; a row of one segment is finished by that wavefront, more are
-// joined 64 at a time by k_logprobs_join. Alternatives are found piece by piece.
-struct RowPlan {
-  int lane_elements;   // 16 or 32
-  int64_t pieces, segments;
-};
-constexpr int64_t kFewPieces = 1024;
-inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
-  const int64_t all = (vocab + 2047) / 2048;
-  if (top) {
-    // few rows: pieces of half the size, as long as one join takes them all
-    if (rows * all <= kFewPieces && all <= kWave / 2) return RowPlan{16, 1, (vocab + 1023) / 1024};
-    return RowPlan{32, 1, all};
-  }
-  int64_t per = rows * all / 16384;
-  per = per < 1 ? 1 : per > 8 ? 8 : per;
-  int64_t segments = (all + per - 1) / per;
-  if (segments > 1) segments = std::min((segments + 3) / 4 * 4, all);   // four a workgroup
-  return RowPlan{32, (all + segments - 1) / segments, segments};
+// The `top` largest of `count` lists of `top` ordered keys each, in order: a bound as in piece_top. `buffer`: room for count top keys. The
+// lists are overwritten.
+__device__ __forceinline__ uint64_t join_lists(uint64_t* lists, int count, int top, uint64_t* buffer) {
+  const int lane = threadIdx.x & 63;
+  // where `need` of the lists reach a bound with their `deep`-th key, `top` keys do
+  const int deep = min((2 * top + count - 1) / count, top), need = (top + deep - 1) / deep;
+  const uint32_t bound = max(reached_by(lane < count ? (uint32_t)(lists[lane * top + deep - 1] >> 32) : 0u, need), 1u);
+  int pass = 0, all;
+  if (lane < count)
+    while (pass < top && (uint32_t)(lists[lane * top + pass] >> 32) >= bound) ++pass;
+  const int to = count_before(pass, &all);
+  for (int k = 0; k < pass; ++k) buffer[to + k] = lists[lane * top + k];
+  wave_sync();
+  return in_order(buffer, all, top, lists);
 }
 
 // Workspace of one level of segments: the keys, then the sums.
@@ -266,59 +307,243 @@ inline size_t level_bytes(int64_t rows, int64_t segments, uint32_t top) {
   return (size_t)rows * (size_t)segments * (top * sizeof(uint64_t) + 3 * sizeof(float)) + 15 & ~(size_t)15;
 }
 
-// One wavefront a segment: a workgroup takes four rows where they have one segment, else four segments of a row.
+// Rows of one piece of 8, 16 or 32 logits a lane: a wavefront each.
 template <typename T, bool TOP, int E>
-__global__ __launch_bounds__(kBlock) void k_logprobs(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
-                                                     int64_t ignore, int top, Outputs o, int64_t segments, uint32_t pieces, float* __restrict__ part,
-                                                     uint64_t* __restrict__ keys) {
-  typedef Piece<T, E> P;
+__global__ __launch_bounds__(kBlock) void k_logprobs_short(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
+                                                           int64_t ignore, int top, Outputs o) {
   extern __shared__ uint64_t lists[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = fminf(scale * kLog2e, FLT_MAX);
-  const bool whole = segments == 1;
-  for (int64_t b = blockIdx.x;; b += gridDim.x) {
-    const int64_t r = whole ? b * 4 + wave : b;
-    if (r >= rows) break;
+  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < rows; r += (int64_t)gridDim.x * 4) {
     const T* row = x + r * ld;
-    for (int64_t seg = whole ? 0 : (int64_t)blockIdx.y * 4 + wave; seg < segments; seg += (int64_t)gridDim.y * 4) {
-      const uint32_t first = (uint32_t)(seg * pieces) * (uint32_t)P::kSize;
-      const uint32_t end = min((uint64_t)first + (uint64_t)pieces * P::kSize, (uint64_t)vocab);
-      Soft a{-FLT_MAX, 0.f, 0.f};
-      P p;
-      p.load(row, first, vocab);
-      Target g{};
-      if (whole) g = load_target(row, targets, r, vocab);
-      uint64_t key = 0;
+    Piece<T, E> p;
+    p.load(row, 0, pack_offset(row, vocab), vocab);
+    const Target g = load_target(row, targets, r, vocab);
+    float v[E];
+    p.unpack(v);
+    const float most = most_of(v);
+    Soft a{-INFINITY, 0.f, 0.f};
+    add_piece(a, v, most, c);
+    a = wave_join(a, c);
+    uint64_t key = 0;
+    if (TOP) key = piece_top(p, v, most, top, a.s != a.s, lists + wave * (E + 2) * top);
+    write_row(o, r, row, lane, a, c, g, vocab, scale, ignore, top, key);
+  }
+}
+
+// A workgroup a row, its wavefronts a piece each in turn; the first wavefront joins what they have.
+template <typename T, int E>
+__global__ __launch_bounds__(1024) void k_logprobs(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
+                                                   int64_t ignore, Outputs o) {
+  typedef Piece<T, E> P;
+  __shared__ Soft sums[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, step = waves * P::kSize;
+  const float c = fminf(scale * kLog2e, FLT_MAX);
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* row = x + r * ld;
+    const int off = pack_offset(row, vocab), end = (int)vocab + off;
+    P p;
+    p.load(row, wave * P::kSize, off, vocab);   // every wavefront has a piece
+    Target g{};
+    if (wave == 0) g = load_target(row, targets, r, vocab);
+    Soft a{-INFINITY, 0.f, 0.f};
+    for (int first = wave * P::kSize; first < end; first += step) {
       float v[E];
-      if (TOP) {
-        p.unpack(v, first, vocab);
-        add_piece(a, v, c, true);
-        const float most = a.base;
-        a = wave_join(a, c);
-        key = piece_top<T, E>(v, most, first, vocab, top, a.s != a.s, lists + wave * (E + 2) * top);
-      } else {
-        for (uint32_t f = first; f < end; f += P::kSize) {
-          P next;
-          if (f + P::kSize < end) next.load(row, f + P::kSize, vocab);
-          p.unpack(v, f, vocab);
-          add_piece(a, v, c, f == first);
-          p = next;
+      P next;
+      if (first + step < end) next.load(row, first + step, off, vocab);
+      p.unpack(v);
+      add_piece(a, v, most_of(v), c);
+      p = next;
+    }
+    a = wave_join(a, c);
+    if (lane == 0) sums[wave] = a;
+    __syncthreads();
+    if (wave == 0) {
+      a = wave_join(lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
+      write_row(o, r, row, lane, a, c, g, vocab, scale, ignore, 0, 0);
+    }
+    if (r + gridDim.x < rows) __syncthreads();
+  }
+}
+
+// The `top` largest of `count` >= top different keys in LDS, in order, by one wavefront. `buffer`: room for `count` keys.
+__device__ __forceinline__ uint64_t top_of_list(uint64_t* list, int count, int top, uint64_t* buffer) {
+  const int lane = threadIdx.x & 63;
+  if (count <= kWave) return in_order(list, count, top, buffer);
+  uint64_t best = 0;
+  for (int i = lane; i < count; i += kWave) best = max(best, list[i]);
+  const uint32_t bound = reached_by((uint32_t)(best >> 32), top);
+  int pass = 0, all;
+  for (int i = lane; i < count; i += kWave) pass += (uint32_t)(list[i] >> 32) >= bound;
+  int at = count_before(pass, &all);
+  for (int i = lane; i < count; i += kWave)
+    if ((uint32_t)(list[i] >> 32) >= bound) buffer[at++] = list[i];
+  wave_sync();
+  return in_order(buffer, all, top, list);
+}
+
+// The same with alternatives: the workgroup holds the whole row, E logits a lane. Every wavefront's lanes' maxima give a bound that `top` of them
+// reach; the largest of the wavefronts' bounds holds for the row. The few logits that reach it are gathered in LDS, and the first wavefront
+// puts them in order. Fewer than `top` logits that are not masked: all of them, then the masked ones of lowest index. More than the list holds (few
+// different values, masks of the type's lowest value): those above the bound, then of its equals those of lowest index; a wavefront's
+// logits are neighbours in the row. What is left, rows with a NaN among it, takes the largest key `top` times from memory.
+constexpr int kListed = 1024;
+template <typename T, int E>
+__global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
+                                                       int64_t ignore, int top, Outputs o) {
+  typedef Piece<T, E> P;
+  __shared__ Soft sums[16];
+  __shared__ uint32_t bounds[16];
+  __shared__ uint64_t heads[2][16], list[kListed + LOPT_TOP_MAX], buffer[kListed + LOPT_TOP_MAX];
+  __shared__ int listed[2], equals[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const float c = fminf(scale * kLog2e, FLT_MAX);
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* row = x + r * ld;
+    P p;
+    p.load(row, wave * P::kSize, pack_offset(row, vocab), vocab);
+    Target g{};
+    if (wave == 0) g = load_target(row, targets, r, vocab);
+    float v[E];
+    p.unpack(v);
+    const float most = most_of(v);
+    const uint32_t own = reached_by(order_of(most), top);
+    if (lane == 0) bounds[wave] = own;
+    if (threadIdx.x < 2) listed[threadIdx.x] = 0;
+    Soft a{-INFINITY, 0.f, 0.f};
+    add_piece(a, v, most, c);
+    a = wave_join(a, c);
+    if (lane == 0) sums[wave] = a;
+    __syncthreads();
+    const float bound = fmaxf(key_value((uint64_t)wave_max(lane < waves ? bounds[lane] : 0u) << 32), -FLT_MAX);   // masked logits do not reach it
+    a = wave_join(lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
+    const bool special = a.s != a.s;
+    auto gather = [&](auto passes, int* counter) {   // counts all, writes what the list holds
+      int pass = 0, all, from = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) pass += passes(v[i]);
+      int at = count_before(pass, &all);
+      if (!all) return;
+      if (lane == 0) from = atomicAdd(counter, all);
+      at += __builtin_amdgcn_readfirstlane(from);
+      if (at + pass > kListed) return;
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (passes(v[i])) list[at++] = rank_key(order_of(v[i]), (uint32_t)p.index(i));
+    };
+    gather([&](float y) { return y >= bound; }, &listed[0]);
+    __syncthreads();
+    int count = listed[0];
+    bool found = count <= kListed && !special;
+    if (!found && !special) {
+      int pass = 0, all, before = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) pass += v[i] == bound;
+      count_before(pass, &all);
+      if (lane == 0) equals[wave] = all;
+      gather([&](float y) { return y > bound; }, &listed[1]);
+      __syncthreads();
+      count = listed[1];
+      const int wanted = max(top - count, 0);
+      found = count <= kListed;
+      for (int w = 0; w < wave; ++w) before += equals[w];
+      if (found && before < wanted) {
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) {   // in the order of the indices: packs, lanes, elements
+          pass = 0;
+#pragma unroll
+          for (int i = j * P::V; i < (j + 1) * P::V; ++i) pass += v[i] == bound;
+          int at = before + count_before(pass, &all);
+          before += all;
+#pragma unroll
+          for (int i = j * P::V; i < (j + 1) * P::V; ++i)
+            if (v[i] == bound) {
+              if (at < wanted) list[count + at] = rank_key(order_of(v[i]), (uint32_t)p.index(i));
+              ++at;
+            }
         }
-        a = wave_join(a, c);
       }
-      if (whole) {
-        write_row(o, r, lane, a, g, vocab, scale, ignore, top, key);
-      } else {
-        const int64_t at = r * segments + seg;
-        if (lane < 3) part[3 * at + lane] = lane == 0 ? a.base : lane == 1 ? a.s : a.h;
-        if (TOP && lane < top) keys[at * top + lane] = key;
+      __syncthreads();
+      int have = 0;   // fewer than wanted where the bound keeps out masked logits
+      for (int w = 0; w < waves; ++w) have += equals[w];
+      count += min(wanted, have);
+    }
+    uint64_t key = 0;
+    if (found) {
+      if (wave == 0) {
+        key = count >= top ? top_of_list(list, count, top, buffer) : in_order(list, count, top, buffer);
+        if (count < top) {   // at most 31 are not masked: the first 64 hold enough that are
+          uint64_t masked = __ballot(lane < vocab && to_f32(row[min(lane, (int)vocab - 1)]) == -INFINITY);
+          if (lane >= count && lane < top) {
+            for (int k = count; k < lane; ++k) masked &= masked - 1;
+            key = rank_key(order_of(-INFINITY), __builtin_ctzll(masked));
+          }
+        }
       }
+    } else {
+      auto largest = [&](uint64_t below) {
+        uint64_t best = 0;
+        for (uint32_t i = threadIdx.x; i < vocab; i += blockDim.x) {
+          const float y = to_f32(row[i]);
+          const uint64_t k = rank_key(y != y ? 0xfffffffeu : order_of(y), i);
+          if (k < below && k > best) best = k;
+        }
+        return best;
+      };
+      uint64_t mine = largest(~(uint64_t)0);
+      for (int k = 0; k < top; ++k) {
+        const uint64_t own_best = wave_max(mine);
+        if (lane == 0) heads[k & 1][wave] = own_best;
+        __syncthreads();
+        uint64_t best = 0;
+        for (int w = 0; w < waves; ++w) best = max(best, heads[k & 1][w]);
+        if (lane == k) key = best;
+        if (mine == best) mine = largest(best);
+      }
+    }
+    if (wave == 0) write_row(o, r, row, lane, a, c, g, vocab, scale, ignore, top, key);
+    if (r + gridDim.x < rows) __syncthreads();
+  }
+}
+
+// The same where a row is too long for one workgroup: segments of `pieces` pieces, a wavefront each, joined 64 at a time by k_logprobs_join.
+// Alternatives: segments of one piece.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kBlock) void k_logprobs_split(const T* __restrict__ x, int64_t ld, int64_t rows, uint32_t vocab, float scale, int top, int64_t segments,
+                                                           uint32_t pieces, float* __restrict__ part, uint64_t* __restrict__ keys) {
+  typedef Piece<T, 32> P;
+  extern __shared__ uint64_t lists[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float c = fminf(scale * kLog2e, FLT_MAX);
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* row = x + r * ld;
+    const int off = pack_offset(row, vocab);
+    for (int64_t seg = (int64_t)blockIdx.y * 4 + wave; seg < segments; seg += (int64_t)gridDim.y * 4) {
+      const int64_t from = seg * pieces * P::kSize, to = min(from + (int64_t)pieces * P::kSize, (int64_t)vocab + off);
+      Soft a{-INFINITY, 0.f, 0.f};
+      uint64_t key = 0;
+      P p;
+      if (from < to) p.load(row, (int)from, off, vocab);
+      for (int64_t first = from; first < to; first += P::kSize) {
+        float v[32];
+        P next;
+        if (first + P::kSize < to) next.load(row, (int)first + P::kSize, off, vocab);
+        p.unpack(v);
+        const float most = most_of(v);
+        add_piece(a, v, most, c);
+        if (TOP) key = piece_top(p, v, most, top, __ballot(a.s != a.s) != 0, lists + wave * 34 * top);
+        p = next;
+      }
+      a = wave_join(a, c);
+      const int64_t at = r * segments + seg;
+      if (lane < 3) part[3 * at + lane] = lane == 0 ? a.m : lane == 1 ? a.s : a.h;
+      if (TOP && lane < top) keys[at * top + lane] = key;
     }
   }
 }
 
-// Joins up to 64 neighbouring segments of a row, one wavefront: the sums lane by lane, the ordered lists of alternatives by a bound
-// as in piece_top. `last`: all of the row's are here, and its outputs are written; else one segment of the next level is.
+// Joins up to 64 neighbouring segments of a row, one wavefront. `last`: all of the row's are here, and its outputs are written; else one
+// segment of the next level is.
 template <typename T>
 __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
                                                          int64_t ignore, int top, Outputs o, int64_t segments, const float* __restrict__ part,
@@ -331,49 +556,74 @@ __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x
   for (int64_t unit = blockIdx.x; unit < rows * groups; unit += gridDim.x) {
     const int64_t r = unit / groups, group = unit - r * groups, at = r * segments + group * kWave;
     const int count = (int)min(segments - group * kWave, (int64_t)kWave);
-    Target g{};
-    if (last && !top) g = load_target(x + r * ld, targets, r, vocab);
-    Soft a{-FLT_MAX, 0.f, 0.f};
+    Soft a{-INFINITY, 0.f, 0.f};
     if (lane < count) a = Soft{part[3 * (at + lane)], part[3 * (at + lane) + 1], part[3 * (at + lane) + 2]};
+    for (int i = lane; i < count * top; i += kWave) lists[i] = keys[at * top + i];
+    Target g{};
+    if (last) g = load_target(x + r * ld, targets, r, vocab);
     uint64_t key = 0;
     if (top) {
-      uint64_t* list = lists + kWave * top;
-      for (int i = lane; i < count * top; i += kWave) lists[i] = keys[at * top + i];
-      if (last) g = load_target(x + r * ld, targets, r, vocab);   // its two loads in a row run beside what follows
       wave_sync();
-      // the lists are in order: where `need` of them reach a bound with their `deep`-th key, `top` keys do
-      const int deep = min((2 * top + count - 1) / count, top), need = (top + deep - 1) / deep;
-      const uint64_t bound = reached_by(lane < count ? (uint32_t)(lists[lane * top + deep - 1] >> 32) : 0u, need);
-      int pass = 0, all;
-      if (lane < count)
-        while (pass < top && lists[lane * top + pass] >> 32 >= max(bound, (uint64_t)1)) ++pass;
-      int to = count_before(pass, &all);
-      for (int k = 0; k < pass; ++k) list[to + k] = lists[lane * top + k];
-      wave_sync();
-      key = in_order(list, all, top, lists);
+      key = join_lists(lists, count, top, lists + kWave * top);
     }
     a = wave_join(a, c);
     if (last) {
-      write_row(o, r, lane, a, g, vocab, scale, ignore, top, key);
+      write_row(o, r, x + r * ld, lane, a, c, g, vocab, scale, ignore, top, key);
     } else {
-      if (lane < 3) part_out[3 * unit + lane] = lane == 0 ? a.base : lane == 1 ? a.s : a.h;
+      if (lane < 3) part_out[3 * unit + lane] = lane == 0 ? a.m : lane == 1 ? a.s : a.h;
       if (lane < top) keys_out[unit * top + lane] = key;
     }
   }
 }
 
-// The gradient, element by element: a workgroup takes kBackPacks packs of 16 bytes a thread of one row. With A = scale (g + h entropy), B = scale h:
-//   dx = scale g [target] - p (A + B ln p)
-// where ln p = scale (x - m) - ln S. Elements behind the last whole pack of a row go one a thread.
+// Calls f(number of logits a lane, as an integral constant).
+template <typename F>
+inline void with_lane(int lane, F&& f) {
+  if (lane == 8) f(std::integral_constant<int, 8>{});
+  else if (lane == 16) f(std::integral_constant<int, 16>{});
+  else if (lane == 32) f(std::integral_constant<int, 32>{});
+  else f(std::integral_constant<int, 64>{});
+}
+
+// How rows are shared out. `lane`: logits a lane.
+enum RowForm { kRowWave, kRowBlock, kRowSplit };
+struct RowPlan {
+  RowForm form;
+  int lane, waves;
+  int64_t pieces, segments;   // kRowSplit
+};
+inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
+  const int64_t n = vocab + 7;   // a row counted from its pack
+  if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, 0, 0};
+  if (top) {
+    const int lane = n <= 16 * 1024 ? 16 : n <= 32 * 1024 ? 32 : 64;
+    if (n <= 64 * 1024) return RowPlan{kRowBlock, lane, (int)((n + lane * kWave - 1) / (lane * kWave)), 0, 0};
+    return RowPlan{kRowSplit, 32, 4, 1, (n + 2047) / 2048};
+  }
+  if (n <= 64 * 2048 || rows >= 256) {
+    // Wavefronts: one for about eight pieces up to four, and with fewer than 1024 rows as many as make 4096 in all, 16 a compute unit. us, pieces of 8 / 16
+    // / 32 logits a lane: 40000x2500 bf16 one wavefront 42 / 51 / 79; 16384x8191 one 49 / 50 / 59, two 48 / 52 / 66, four 53 / 57 / 78; 5200x32000 one 69 / 66 / 73, four
+    // 61 / 60 / 62; 4096x50257 one 100 / 86 / 84, four 82 / 77 / 79; 2048x50257 fp32 one 87 / 71 / 72, four 79 / 74 / 72.
+    const int lane = n <= 8 * 1024 + 7 ? 8 : 16;
+    const int64_t pieces = (vocab + lane * kWave - 1) / (lane * kWave), long_rows = std::clamp<int64_t>((pieces + 4) / 8, 1, 4);
+    return RowPlan{kRowBlock, lane, (int)std::max(long_rows, std::min<int64_t>({16, pieces, 4096 / rows})), 0, 0};
+  }
+  const int64_t pieces = (n + 2047) / 2048, per = std::clamp<int64_t>(rows * pieces / 16384, 1, 8);
+  return RowPlan{kRowSplit, 32, 4, per, (pieces + per - 1) / per};
+}
+
+// The gradient, element by element: a workgroup takes kBackPacks packs of 16 bytes a thread of one row, counted as in the forward pass from the pack in
+// which the gradient's row begins, so that stores are aligned (4096x50257 bf16, odd rows at odd elements: 184 -> 172 us); a logit's row at
+// another offset is read unaligned. Packs that reach out of the row go element by element.
+// With A = scale (g + h entropy), B = scale h:
+//   dx = scale g [target] - p (A + B ln p),   ln p = scale (x - m) - ln S
 constexpr int kBackPacks = 4;
 template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld, const int64_t* __restrict__ targets, const float* __restrict__ stats,
                                                           const float* __restrict__ entropy, const float* __restrict__ dlogp,
-                                                          const float* __restrict__ dentropy, T* dx, int64_t ld_d, int64_t rows, uint32_t vocab, float scale, int64_t ignore) {
+                                                          const float* __restrict__ dentropy, T* dx, int64_t ld_d, int64_t rows, int vocab, float scale, int64_t ignore) {
   typedef typename Pack<T>::type pack;
-  constexpr int V = Pack<T>::n;
-  constexpr uint32_t kSpan = kBackPacks * kBlock * V;
-  const uint32_t whole = vocab / V * V;
+  constexpr int V = Pack<T>::n, kSpan = kBackPacks * kBlock * V;
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* row = x + r * ld;
     T* out = dx + r * ld_d;
@@ -384,7 +634,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
     const float h = ENTROPY ? dentropy[r] : 0.f;
     const float at_target = scale * g, A = scale * (g + (ENTROPY ? h * entropy[r] : 0.f)), B = scale * h;
     const bool empty = log_s == -INFINITY;
-    const uint32_t at = t >= 0 && t < vocab ? (uint32_t)t : 0xffffffffu;
+    const int at = t != ignore && t >= 0 && t < vocab ? (int)t : -1;
     auto gradient = [&](float v) {
       float lp = scale * (v - m) - log_s;
       const float p = exp2_hw(lp * kLog2e);
@@ -392,21 +642,23 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
       const float d = -p * (ENTROPY ? A + B * lp : A);
       return empty ? 0.f * A : d;
     };
-    for (uint32_t first = blockIdx.y * kSpan; first < vocab; first += gridDim.y * kSpan) {
+    const int off = (int)((uintptr_t)out / sizeof(T) % V);
+    for (int64_t first = (int64_t)blockIdx.y * kSpan; first < (int64_t)vocab + off; first += (int64_t)gridDim.y * kSpan) {
+      const int begin = (int)first + (int)threadIdx.x * V - off;
       pack in[kBackPacks];
 #pragma unroll
       for (int j = 0; j < kBackPacks; ++j) {
-        const uint32_t k = first + (j * kBlock + threadIdx.x) * V;
-        if (k < whole) in[j] = *(const pack*)(row + k);
+        const int k = begin + j * kBlock * V;
+        if (k >= 0 && k <= vocab - V) in[j] = *(const pack*)(row + k);
       }
 #pragma unroll
       for (int j = 0; j < kBackPacks; ++j) {
-        const uint32_t k = first + (j * kBlock + threadIdx.x) * V;
-        if (k < whole) {
+        const int k = begin + j * kBlock * V;
+        if (k >= 0 && k <= vocab - V) {
           float d[V];
 #pragma unroll
           for (int e = 0; e < V; ++e) d[e] = gradient(to_f32(in[j][e]));
-          if (at - k < (uint32_t)V) {
+          if ((unsigned)(at - k) < (unsigned)V) {
 #pragma unroll
             for (int e = 0; e < V; ++e)
               if (at == k + e) d[e] += empty ? 0.f : at_target;
@@ -415,12 +667,12 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
 #pragma unroll
           for (int e = 0; e < V; ++e) o[e] = from_f32<T>(d[e]);
           *(pack*)(out + k) = o;
+        } else if (k > -V && k < vocab) {
+          for (int i = max(k, 0); i < min(k + V, vocab); ++i) {
+            const float d = gradient(to_f32(row[i]));
+            out[i] = from_f32<T>(at == i && !empty ? d + at_target : d);
+          }
         }
-      }
-      const uint32_t k = whole + threadIdx.x;
-      if (first + kSpan >= vocab && k < vocab) {
-        const float d = gradient(to_f32(row[k]));
-        out[k] = from_f32<T>(at == k && !empty ? d + at_target : d);
       }
     }
   }
@@ -435,15 +687,17 @@ extern "C" {
 
 size_t lopt_token_logprobs_workspace(int64_t rows, int64_t vocab, uint32_t top) {
   if (rows <= 0 || vocab <= 0 || rows > 0x7fffffffLL || vocab > 0x7fffffffLL || top > LOPT_TOP_MAX) return 0;
+  const RowPlan plan = plan_rows(rows, vocab, top);
   size_t bytes = 0;
-  for (int64_t segments = plan_rows(rows, vocab, top).segments; segments > 1; segments = (segments + kWave - 1) / kWave)
-    bytes += level_bytes(rows, segments, top);
+  if (plan.form == kRowSplit)
+    for (int64_t segments = plan.segments; segments > 1; segments = (segments + kWave - 1) / kWave) bytes += level_bytes(rows, segments, top);
   return bytes;
 }
 
 static lopt_status check_logits(const void* logits, int64_t ld, int64_t rows, int64_t vocab, uint32_t type, float scale) {
   LOPT_CHECK(check_type("type", type));
   LOPT_CHECK(check_matrix(rows, vocab, "vocab"));
+  if (vocab > LOPT_VOCAB_MAX) return fail_call(LOPT_ESHAPE, "vocab=%lld is above %d", (long long)vocab, LOPT_VOCAB_MAX);
   LOPT_CHECK(check_ld("ld", rows, vocab, ld, false));
   if (!(scale > 0.f) || std::isinf(scale)) return fail_call(LOPT_EINVAL, "scale must be finite and > 0");
   return check_array("logits", logits, type_bytes(type), rows > 0);
@@ -466,22 +720,40 @@ lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* t
   const RowPlan plan = plan_rows(rows, vocab, top);
   const int64_t* tg = logp ? targets : nullptr;
   hipStream_t stream = (hipStream_t)hip_stream;
-  const int64_t blocks = plan.segments == 1 ? (rows + 3) / 4 : rows;
-  const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20), plan.segments == 1 ? 1 : (unsigned)std::min<int64_t>((plan.segments + 3) / 4, 1024));
-  char* ws = (char*)workspace;
+  const unsigned blocks = (unsigned)std::min<int64_t>(plan.form == kRowWave ? (rows + 3) / 4 : rows, 1 << 20);
+  const uint32_t n = (uint32_t)vocab;
   with_type(type, [&](auto t) {
     using T = decltype(t);
     const T* x = (const T*)logits;
-    const uint32_t n = (uint32_t)vocab;
+    if (plan.form != kRowSplit) {
+      with_lane(plan.lane, [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        const dim3 block(plan.waves * kWave);
+        if constexpr (E <= 32)
+          if (plan.form == kRowWave) {
+            auto kernel = top ? k_logprobs_short<T, true, E> : k_logprobs_short<T, false, E>;
+            hipLaunchKernelGGL(kernel, dim3(blocks), block, plan.waves * (E + 2) * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
+            return;
+          }
+        if constexpr (E >= 16)
+          if (top) {
+            hipLaunchKernelGGL((k_logprobs_top<T, E>), dim3(blocks), block, 0, stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
+            return;
+          }
+        if constexpr (E <= 16) hipLaunchKernelGGL((k_logprobs<T, E>), dim3(blocks), block, 0, stream, x, ld, tg, rows, n, scale, ignore_index, o);
+      });
+      return;
+    }
+    char* ws = (char*)workspace;
     uint64_t* keys = (uint64_t*)ws;
     float* part = (float*)(ws + (size_t)rows * plan.segments * top * sizeof(uint64_t));
-    auto launch = [&](auto kernel, size_t lds) {
-      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), lds, stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o, plan.segments, (uint32_t)plan.pieces, part, keys);
-    };
-    const size_t lds = 4 * (plan.lane_elements + 2) * top * sizeof(uint64_t);
-    if (!top) launch(k_logprobs<T, false, 32>, 0);
-    else if (plan.lane_elements == 16) launch(k_logprobs<T, true, 16>, lds);
-    else launch(k_logprobs<T, true, 32>, lds);
+    const dim3 grid(blocks, (unsigned)std::min<int64_t>((plan.segments + 3) / 4, 1024));
+    if (top)
+      hipLaunchKernelGGL((k_logprobs_split<T, true>), grid, dim3(kBlock), 4 * 34 * top * sizeof(uint64_t), stream, x, ld, rows, n, scale, (int)top, plan.segments,
+                         (uint32_t)plan.pieces, part, keys);
+    else
+      hipLaunchKernelGGL((k_logprobs_split<T, false>), grid, dim3(kBlock), 0, stream, x, ld, rows, n, scale, 0, plan.segments, (uint32_t)plan.pieces, part,
+                         keys);
     for (int64_t segments = plan.segments; segments > 1;) {
       const int64_t groups = (segments + kWave - 1) / kWave;
       char* above = (char*)keys + level_bytes(rows, segments, top);
@@ -514,13 +786,13 @@ lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const i
   with_type(type, [&](auto t) {
     using T = decltype(t);
     constexpr int64_t kSpan = (int64_t)kBackPacks * kBlock * Pack<T>::n;
-    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20), (unsigned)std::min<int64_t>((vocab + kSpan - 1) / kSpan, 1024));
+    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20), (unsigned)std::min<int64_t>((vocab + Pack<T>::n - 1 + kSpan - 1) / kSpan, 1024));
     if (dentropy)
       hipLaunchKernelGGL((k_logprobs_back<T, true>), grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp,
-                         dentropy, (T*)dlogits, ld_d, rows, (uint32_t)vocab, scale, ignore_index);
+                         dentropy, (T*)dlogits, ld_d, rows, (int)vocab, scale, ignore_index);
     else
       hipLaunchKernelGGL((k_logprobs_back<T, false>), grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp,
-                         dentropy, (T*)dlogits, ld_d, rows, (uint32_t)vocab, scale, ignore_index);
+                         dentropy, (T*)dlogits, ld_d, rows, (int)vocab, scale, ignore_index);
   });
   return launch_status("lopt_token_logprobs_backward");
 }

@@ -90,6 +90,10 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   const uint32_t c = __builtin_amdgcn_readlane((int)v, 32), d = __builtin_amdgcn_readlane((int)v, 48);
   return max(max(a, b), max(c, d));
 }
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+  const uint32_t hi = wave_max((uint32_t)(v >> 32));
+  return (uint64_t)hi << 32 | wave_max((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+}
 __device__ __forceinline__ uint64_t readlane(uint64_t v, int lane) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
   return (uint64_t)hi << 32 | lo;
