@@ -36,8 +36,11 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
   return v;
 }
 
+// V floats that may start at any float.
+template <int V> struct FloatPack { typedef float type __attribute__((ext_vector_type(V), aligned(4))); };
+
 // A lane's share of a row: N packs of 16 bytes, G packs from one to the next. The pack that would pass the row's end is moved back to
-// end with it; its first `skip` elements are the lane's before, which sums pass over and stores write twice, the same. Rows shorter than a
+// end with it; its first `skip` elements are the lane's before. Rows shorter than a
 // pack (N = 0): one element a lane.
 template <typename T, int G, int N>
 struct Share {
@@ -50,12 +53,38 @@ struct Share {
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const uint32_t k = (j * G + lane) * V;
-      have[j] = k < cols;
-      at[j] = min(k, cols - V);
-      skip[j] = have[j] ? (int)(k - at[j]) : V;
+      const bool full = j < P / 2;   // with_group takes no more packs than it has to
+      have[j] = full || k < cols;
+      at[j] = full ? k : min(k, cols - V);
+      skip[j] = full ? 0 : have[j] ? (int)(k - at[j]) : V;
     }
   }
   __device__ __forceinline__ bool mine(int i) const { return i % V >= skip[i / V]; }
+  // The lane's columns of an array, written from v or added to it; `v` has its own at the same places.
+  __device__ __forceinline__ void write(float* a, const float (&v)[E]) const {
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      if (skip[j] == 0) {
+        typename FloatPack<V>::type o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = v[j * V + e];
+        *(typename FloatPack<V>::type*)(a + at[j]) = o;
+      } else if (have[j]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (e >= skip[j]) a[at[j] + e] = v[j * V + e];
+      }
+    }
+  }
+  __device__ __forceinline__ void add(const float* a, float (&v)[E]) const {
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+      if (have[j]) {
+        const typename FloatPack<V>::type o = *(const typename FloatPack<V>::type*)(a + at[j]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[j * V + e] = o[e] + v[j * V + e];
+      }
+  }
 };
 
 template <typename T, int G, int N>
@@ -65,16 +94,22 @@ struct Row {
   pack raw[N ? N : 1];
   __device__ __forceinline__ void load(const T* row, const S& s) {
 #pragma unroll
-    for (int j = 0; j < S::P; ++j)
+    for (int j = 0; j < S::P; ++j) {
+      raw[j] = pack{};
       if (s.have[j]) {
         if (N) raw[j] = *(const pack*)(row + s.at[j]);
         else raw[j][0] = row[s.at[j]];
       }
+    }
   }
   __device__ __forceinline__ float get(int i) const { return to_f32(raw[i / S::V][i % S::V]); }
   __device__ __forceinline__ static void store(T* row, const S& s, int j, const float* v) {
     if (!s.have[j]) return;
-    if (N) {
+    if (N && s.skip[j]) {
+#pragma unroll
+      for (int e = 0; e < S::V; ++e)
+        if (e >= s.skip[j]) row[s.at[j] + e] = from_f32<T>(v[e]);
+    } else if (N) {
       pack o;
 #pragma unroll
       for (int e = 0; e < S::V; ++e) o[e] = from_f32<T>(v[e]);
@@ -196,10 +231,9 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, i
       a[i] = g * w[i];
       sw[i] += g * h[i];
       sb[i] += g;
-      if (s.mine(i)) {
-        s1 += a[i];
-        s2 += a[i] * h[i];
-      }
+      const float am = s.mine(i) ? a[i] : 0.f;
+      s1 += am;
+      s2 += am * h[i];
     }
     if (dx) {
       const float m1 = group_sum<G>(s1, red[odd][0]) / (float)cols, m2 = group_sum<G>(s2, red[odd][1]) / (float)cols;
@@ -212,33 +246,26 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, i
   if (!part) return;
   float* out = part + (int64_t)blockIdx.x * 2 * cols;
   if (kRows == 1) {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (s.mine(i)) {
-        out[s.at[i / S::V] + i % S::V] = sw[i];
-        out[cols + s.at[i / S::V] + i % S::V] = sb[i];
-      }
+    s.write(out, sw);
+    s.write(out + cols, sb);
     return;
   }
-  __shared__ float sums[kRows == 1 ? 1 : 2][kRows == 1 ? 1 : G * E];
-  const int group = threadIdx.x / G, lane = threadIdx.x % G;
+  __shared__ __align__(16) float sums[2][kRows == 1 ? 4 : G * E];   // by column
+  const int group = threadIdx.x / G;
   for (int k = 0; k < kRows; ++k) {
     if (group == k) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        sums[0][i * G + lane] = k ? sums[0][i * G + lane] + sw[i] : sw[i];
-        sums[1][i * G + lane] = k ? sums[1][i * G + lane] + sb[i] : sb[i];
+      if (k) {
+        s.add(sums[0], sw);
+        s.add(sums[1], sb);
       }
+      s.write(sums[0], sw);
+      s.write(sums[1], sb);
     }
     __syncthreads();
   }
-  if (group == 0) {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (s.mine(i)) {
-        out[s.at[i / S::V] + i % S::V] = sums[0][i * G + lane];
-        out[cols + s.at[i / S::V] + i % S::V] = sums[1][i * G + lane];
-      }
+  for (uint32_t c = threadIdx.x; c < cols; c += Group<G>::kThreads) {
+    out[c] = sums[0][c];
+    out[cols + c] = sums[1][c];
   }
 }
 
@@ -344,7 +371,7 @@ __global__ __launch_bounds__(1024) void k_norm_long_rows(const T* dy, int64_t ld
 }
 
 // Calls f(group size, packs) as integral constants for the smallest group that holds a row with at most `most` elements a lane; false
-// if none does.
+// if none does. Of N >= 2 packs a lane the first N / 2 always lie in the row.
 template <int V, int most, typename F>
 bool with_group(int64_t cols, F&& f) {
   using std::integral_constant;
@@ -372,12 +399,12 @@ constexpr int kMostForward = 32, kMostBackward = 16;
 int64_t slabs_of(int64_t rows) { return (rows + kSlab - 1) / kSlab; }
 
 // Workgroups of the backward pass over rows in registers, at most this many: each writes one row of partial sums.
-constexpr int64_t kBackBlocks = 512;
-int64_t back_blocks(int64_t rows, int rows_a_block) { return std::min((rows + rows_a_block - 1) / rows_a_block, kBackBlocks); }
+template <int G>
+int64_t back_blocks(int64_t rows) { return std::min<int64_t>((rows + Group<G>::kRows - 1) / Group<G>::kRows, G == 1024 ? 256 : 512); }
 template <int V>
 int64_t back_parts(int64_t rows, int64_t cols) {
   int64_t parts = slabs_of(rows);
-  with_group<V, kMostBackward>(cols, [&](auto g, auto) { parts = back_blocks(rows, Group<decltype(g)::value>::kRows); });
+  with_group<V, kMostBackward>(cols, [&](auto g, auto) { parts = back_blocks<decltype(g)::value>(rows); });
   return parts;
 }
 

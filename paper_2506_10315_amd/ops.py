@@ -70,6 +70,11 @@ def _run(fn, device: torch.device, *args):
         _check(status)
 
 
+def _new(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of `t`'s shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -185,7 +190,7 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
         weight = _expect("weight", weight, x, wtype, (cols,))
     if bias is not None:
         bias = _expect("bias", bias, x, wtype, (cols,))
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _new(x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
     _run(lib().lopt_layer_norm, x.device, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(),
@@ -209,9 +214,12 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
         weight = _expect("weight", weight, x, wtype, (cols,))
     mean = _expect("mean", mean, x, torch.float32, x.shape[:-1])
     rstd = _expect("rstd", rstd, x, torch.float32, x.shape[:-1])
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
-    dw = torch.empty(cols, dtype=wtype, device=x.device) if need[1] else None
-    db = torch.empty(cols, dtype=wtype, device=x.device) if need[2] else None
+    dx = _new(x) if need[0] else None
+    dw = db = None
+    if need[1]:
+        dw = torch.empty_like(weight) if weight is not None else torch.empty(cols, dtype=wtype, device=x.device)
+    if need[2]:
+        db = torch.empty_like(dw) if dw is not None else torch.empty(cols, dtype=wtype, device=x.device)
     L = lib()
     ws = _workspace(L.lopt_layer_norm_workspace(rows, cols), x.device) if need[1] or need[2] else None
     _run(L.lopt_layer_norm_backward, x.device, dy2.data_ptr(), ld_dy, x2.data_ptr(), ld, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx), cols,
@@ -263,7 +271,9 @@ def token_logprobs_forward(logits: torch.Tensor, targets: Optional[torch.Tensor]
         raise ValueError(f"top={top} outside [0, {min(vocab, TOP_MAX)}]")
     dev = logits.device
     logp = torch.empty(shape, dtype=torch.float32, device=dev) if targets is not None else None
-    ent = torch.empty(shape, dtype=torch.float32, device=dev) if entropy else None
+    ent = None
+    if entropy:
+        ent = torch.empty_like(logp) if logp is not None else torch.empty(shape, dtype=torch.float32, device=dev)
     stats = torch.empty(shape + (2,), dtype=torch.float32, device=dev)
     top_logp = torch.empty(shape + (top,), dtype=torch.float32, device=dev) if top else None
     top_index = torch.empty(shape + (top,), dtype=torch.int64, device=dev) if top else None
@@ -293,7 +303,7 @@ def token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor
         if entropy is None:
             raise ValueError("dentropy without entropy")
         entropy = _expect("entropy", entropy, logits, torch.float32, shape)
-    dx = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    dx = _new(logits)
     _run(lib().lopt_token_logprobs_backward, logits.device, x.data_ptr(), ld, _ptr(targets), stats.data_ptr(), _ptr(entropy), _ptr(dlogp), _ptr(dentropy),
          dx.data_ptr(), vocab, rows, vocab, kind, scale, ignore_index)
     return dx
