@@ -47,14 +47,14 @@ struct Walk {
 };
 
 // A thread's 16 elements of a chunk of `count`, in groups of V neighbours, 256 V apart.
-template <typename T, int V>
+template <typename T, int V, bool NT>
 __device__ __forceinline__ void load_chunk(const T* p, int count, float (&v)[16]) {
   typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 #pragma unroll
   for (int j = 0; j < 16 / V; ++j) {
     const int k = (j * kBlock + (int)threadIdx.x) * V;
     if (k + V <= count) {
-      const vec x = *(const vec*)(p + k);
+      const vec x = NT ? __builtin_nontemporal_load((const vec*)(p + k)) : *(const vec*)(p + k);
 #pragma unroll
       for (int e = 0; e < V; ++e) v[j * V + e] = to_f32(x[e]);
     } else {
@@ -73,7 +73,7 @@ __device__ __forceinline__ void store_chunk(T* p, int count, const float (&v)[16
       vec x;
 #pragma unroll
       for (int e = 0; e < V; ++e) x[e] = from_f32<T>(v[j * V + e]);
-      *(vec*)(p + k) = x;
+      __builtin_nontemporal_store(x, (vec*)(p + k));
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e)
@@ -81,11 +81,11 @@ __device__ __forceinline__ void store_chunk(T* p, int count, const float (&v)[16
     }
   }
 }
-template <int V>
+template <int V, bool NT>
 __device__ __forceinline__ void load_chunk_as(const void* p, int64_t at, uint32_t type, int count, float (&v)[16]) {
-  if (type == LOPT_F32) load_chunk<float, V>((const float*)p + at, count, v);
-  else if (type == LOPT_BF16) load_chunk<bf16_t, V>((const bf16_t*)p + at, count, v);
-  else load_chunk<f16_t, V>((const f16_t*)p + at, count, v);
+  if (type == LOPT_F32) load_chunk<float, V, NT>((const float*)p + at, count, v);
+  else if (type == LOPT_BF16) load_chunk<bf16_t, V, NT>((const bf16_t*)p + at, count, v);
+  else load_chunk<f16_t, V, NT>((const f16_t*)p + at, count, v);
 }
 
 __global__ __launch_bounds__(kBlock) void k_clip_squares(const ClipBatch b, double* __restrict__ part) {
@@ -97,8 +97,8 @@ __global__ __launch_bounds__(kBlock) void k_clip_squares(const ClipBatch b, doub
     const int count = Walk::count(b, w.k, c);
     const int64_t at = (int64_t)(c - b.t[w.k].first) * kChunk;
     float v[16];
-    if (b.t[w.k].type == LOPT_F32) load_chunk<float, 4>((const float*)b.t[w.k].in + at, count, v);
-    else load_chunk_as<8>(b.t[w.k].in, at, b.t[w.k].type, count, v);
+    if (b.t[w.k].type == LOPT_F32) load_chunk<float, 4, false>((const float*)b.t[w.k].in + at, count, v);
+    else load_chunk_as<8, false>(b.t[w.k].in, at, b.t[w.k].type, count, v);
 #pragma unroll
     for (int i = 0; i < 16; ++i) s += (double)v[i] * (double)v[i];
   }
@@ -121,8 +121,23 @@ __global__ __launch_bounds__(kBlock) void k_clip_norm(const double* __restrict__
   if (threadIdx.x == 0) norm[0] = n.norm;
 }
 
+// V neighbours a lane: 16 bytes of the wider type, so that every access of a wavefront is one run of memory.
+template <int V>
+__device__ __forceinline__ void scale_chunk(const ClipTensor& t, int64_t at, int count, float f) {
+  float v[16];
+  load_chunk_as<V, true>(t.in, at, t.type, count, v);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] *= f;
+  if (t.out_type == LOPT_F32) store_chunk<float, V>((float*)t.out + at, count, v);
+  else if (t.out_type == LOPT_BF16) store_chunk<bf16_t, V>((bf16_t*)t.out + at, count, v);
+  else store_chunk<f16_t, V>((f16_t*)t.out + at, count, v);
+}
+
 // Every workgroup joins the partial sums for itself, which takes the place of a launch in between, and goes through its chunks from the last to
-// the first: what the first sweep read last is still in the Infinity Cache.
+// the first: what the first sweep read last is still in the Infinity Cache (355 M elements fp32 771 -> 747 us). That is also why the
+// first sweep's loads are ordinary ones, and this one's loads and stores nontemporal: what will not be read again pushes nothing out. us, ordinary / stores
+// nontemporal / stores and this sweep's loads / all: 86 M fp32 212 / 182 / 165 / 188, 54 M bf16 to fp32 105 / 79 / 74 / 93, 20 M bf16 31 / 28 / 26 / 31. Both sweeps
+// are bound by memory: 86 M fp32 are two reads and one write of 344 MB, 6.2 TB/s.
 __global__ __launch_bounds__(kBlock) void k_clip_scale(const ClipBatch b, const double* __restrict__ part, int parts, float max_norm, float* __restrict__ norm) {
   __shared__ double red[4];
   const Norm n = join_norm(part, parts, max_norm, red);
@@ -136,19 +151,8 @@ __global__ __launch_bounds__(kBlock) void k_clip_scale(const ClipBatch b, const 
     const int count = Walk::count(b, w.k, c);
     const int64_t at = (int64_t)(c - t.first) * kChunk;
     float v[16];
-    if (t.type == LOPT_F32 && t.out_type == LOPT_F32) {
-      load_chunk<float, 4>((const float*)t.in + at, count, v);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] *= f;
-      store_chunk<float, 4>((float*)t.out + at, count, v);
-    } else {
-      load_chunk_as<8>(t.in, at, t.type, count, v);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] *= f;
-      if (t.out_type == LOPT_F32) store_chunk<float, 8>((float*)t.out + at, count, v);
-      else if (t.out_type == LOPT_BF16) store_chunk<bf16_t, 8>((bf16_t*)t.out + at, count, v);
-      else store_chunk<f16_t, 8>((f16_t*)t.out + at, count, v);
-    }
+    if (t.type == LOPT_F32 || t.out_type == LOPT_F32) scale_chunk<4>(t, at, count, f);
+    else scale_chunk<8>(t, at, count, f);
   }
 }
 
