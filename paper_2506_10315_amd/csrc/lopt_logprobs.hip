@@ -612,19 +612,22 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
   return RowPlan{kRowSplit, 32, 4, per, (pieces + per - 1) / per};
 }
 
-// The gradient, element by element: a workgroup takes kBackPacks packs of 16 bytes a thread of one row, counted as in the forward pass from the pack in
-// which the gradient's row begins, so that stores are aligned (4096x50257 bf16, odd rows at odd elements: 184 -> 172 us); a logit's row at
-// another offset is read unaligned. Packs that reach out of the row go element by element.
-// With A = scale (g + h entropy), B = scale h:
+// The gradient, element by element. With A = scale (g + h entropy), B = scale h:
 //   dx = scale g [target] - p (A + B ln p),   ln p = scale (x - m) - ln S
+// Bound by memory: one read and one write of the logits. Groups of G lanes, 16 or 64 for short rows and the workgroup for others (65536x100 fp32 68 -> 16
+// us, 16384x1000 bf16 22 -> 15), take kBackPacks packs of 16 bytes a lane of a row, counted as in the forward pass from the pack in which the
+// gradient's row begins, so that stores are aligned (4096x50257 bf16, odd rows at odd elements: 184 -> 174 us); a logit's row at
+// another offset is read unaligned. Packs that reach out of the row go element by element. Accesses are nontemporal: nothing is read again here, and
+// what both arrays would push out of the caches is (256x50257 bf16 15 -> 12 us, 4096x32000 104 -> 96). us of 4096x50257 bf16 with 1, 2, 4, 8 packs: 176, 162, 160, 168.
 constexpr int kBackPacks = 4;
-template <typename T, bool ENTROPY>
+template <typename T, bool ENTROPY, int G>
 __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld, const int64_t* __restrict__ targets, const float* __restrict__ stats,
                                                           const float* __restrict__ entropy, const float* __restrict__ dlogp,
                                                           const float* __restrict__ dentropy, T* dx, int64_t ld_d, int64_t rows, int vocab, float scale, int64_t ignore) {
   typedef typename Pack<T>::type pack;
-  constexpr int V = Pack<T>::n, kSpan = kBackPacks * kBlock * V;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+  constexpr int V = Pack<T>::n, kSpan = kBackPacks * G * V, kRows = kBlock / G;
+  const int lane = threadIdx.x % G;
+  for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < rows; r += (int64_t)gridDim.x * kRows) {
     const T* row = x + r * ld;
     T* out = dx + r * ld_d;
     const float m = stats[2 * r], log_s = stats[2 * r + 1];
@@ -644,16 +647,16 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
     };
     const int off = (int)((uintptr_t)out / sizeof(T) % V);
     for (int64_t first = (int64_t)blockIdx.y * kSpan; first < (int64_t)vocab + off; first += (int64_t)gridDim.y * kSpan) {
-      const int begin = (int)first + (int)threadIdx.x * V - off;
+      const int begin = (int)first + lane * V - off;
       pack in[kBackPacks];
 #pragma unroll
       for (int j = 0; j < kBackPacks; ++j) {
-        const int k = begin + j * kBlock * V;
-        if (k >= 0 && k <= vocab - V) in[j] = *(const pack*)(row + k);
+        const int k = begin + j * G * V;
+        if (k >= 0 && k <= vocab - V) in[j] = __builtin_nontemporal_load((const pack*)(row + k));
       }
 #pragma unroll
       for (int j = 0; j < kBackPacks; ++j) {
-        const int k = begin + j * kBlock * V;
+        const int k = begin + j * G * V;
         if (k >= 0 && k <= vocab - V) {
           float d[V];
 #pragma unroll
@@ -666,7 +669,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
           pack o;
 #pragma unroll
           for (int e = 0; e < V; ++e) o[e] = from_f32<T>(d[e]);
-          *(pack*)(out + k) = o;
+          __builtin_nontemporal_store(o, (pack*)(out + k));
         } else if (k > -V && k < vocab) {
           for (int i = max(k, 0); i < min(k + V, vocab); ++i) {
             const float d = gradient(to_f32(row[i]));
@@ -785,14 +788,19 @@ lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const i
   if (rows == 0) return LOPT_OK;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    constexpr int64_t kSpan = (int64_t)kBackPacks * kBlock * Pack<T>::n;
-    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20), (unsigned)std::min<int64_t>((vocab + Pack<T>::n - 1 + kSpan - 1) / kSpan, 1024));
-    if (dentropy)
-      hipLaunchKernelGGL((k_logprobs_back<T, true>), grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp,
-                         dentropy, (T*)dlogits, ld_d, rows, (int)vocab, scale, ignore_index);
-    else
-      hipLaunchKernelGGL((k_logprobs_back<T, false>), grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp,
-                         dentropy, (T*)dlogits, ld_d, rows, (int)vocab, scale, ignore_index);
+    const int64_t packs = (vocab + 2 * Pack<T>::n - 2) / Pack<T>::n;   // that a row may touch
+    auto launch = [&](auto g) {
+      constexpr int G = decltype(g)::value;
+      // a rest of less than an eighth of a span goes to workgroups that have one (16384x8191 bf16 108 -> 96 us; rests of a quarter 18 -> 21)
+      const int64_t spans = (packs + kBackPacks * G - kBackPacks * G / 8) / (kBackPacks * G);
+      const dim3 grid((unsigned)std::min<int64_t>((rows + kBlock / G - 1) / (kBlock / G), 1 << 20), (unsigned)std::clamp<int64_t>(spans, 1, 1024));
+      auto kernel = dentropy ? k_logprobs_back<T, true, G> : k_logprobs_back<T, false, G>;
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp, dentropy, (T*)dlogits, ld_d,
+                         rows, (int)vocab, scale, ignore_index);
+    };
+    if (packs <= kBackPacks * 16) launch(std::integral_constant<int, 16>{});
+    else if (packs <= kBackPacks * 64) launch(std::integral_constant<int, 64>{});
+    else launch(std::integral_constant<int, kBlock>{});
   });
   return launch_status("lopt_token_logprobs_backward");
 }
