@@ -55,13 +55,14 @@ def _matrix(name: str, t: torch.Tensor) -> Tuple[torch.Tensor, int, int, int]:
     return t, t.numel() // cols, cols, cols
 
 
-# the current stream's handle without the stream object, which costs more than the launch of a small kernel
+# the current stream's handle and device without the objects around them, which cost as much as the launch of a small kernel
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _run(fn, device: torch.device, *args):
     index = device.index
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -145,13 +146,11 @@ def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], 
     return norm
 
 
-@torch.no_grad()
 def grad_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
     """The Euclidean norm of all elements of all tensors: a float32 tensor without dimensions, on their device."""
     return _clip(list(grads), None, 0.0)
 
 
-@torch.no_grad()
 def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
                out: Optional[Sequence[torch.Tensor]] = None) -> Tuple[List[torch.Tensor], torch.Tensor]:
     """(clipped gradients, norm before clipping): every gradient times min(1, max_norm / (norm + 1e-6)). `out` receives
@@ -162,7 +161,6 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
     return out, _clip(grads, out, max_norm)
 
 
-@torch.no_grad()
 def clip_grad_norm_(parameters: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float) -> torch.Tensor:
     """Clips the `.grad` of the parameters in place and returns the norm before. Parameters without a gradient are
     skipped."""

@@ -494,7 +494,7 @@ def check_logp(x, kind, t, scale=1.0, top=0, ignore=-100, what=""):
 
 
 LOGP_SHAPES = [(1, 1), (4, 2), (3, 7), (5, 63), (2, 64), (9, 65), (17, 100), (3, 255), (2, 257), (7, 1000), (2, 2047), (3, 2049), (5, 4099), (2, 8192),
-               (2, 8193), (1, 32000), (3, 50257), (1, 131073), (300, 33)]
+               (2, 8193), (1, 32000), (3, 50257), (1, 131073), (300, 33), (1100, 2100), (300, 5000), (4200, 2060)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -506,17 +506,19 @@ def test_token_logprobs_forward(rows, vocab, kind):
         check_logp(x, kind, t, scale, top, what=f"top {top} masked {masked}")
 
 
-def test_token_logprobs_ties_and_orders():
-    vocab = 20000
+@pytest.mark.parametrize("vocab", [900, 3000, 20000, 50257, 140000])
+def test_token_logprobs_ties_and_orders(vocab):
     for kind in TYPES:
         for name, row in (("equal", np.zeros(vocab)), ("rising", np.arange(vocab) / 512.0), ("falling", -np.arange(vocab) / 512.0),
-                          ("few values", np.arange(vocab) % 3.0), ("zeros of both signs", np.where(np.arange(vocab) % 2, 0.0, -0.0)),
+                          ("few values", np.arange(vocab) % 3.0), ("a ramp on a plateau", np.maximum(np.arange(vocab) - vocab + 30.0, 0)),
+                          ("forty allowed, a lane's", np.where(np.arange(vocab) % 512 == 8, np.arange(vocab) / 1024.0, -np.inf)),
+                          ("largest value", np.where(np.arange(vocab) % 7 == 3, 3.3895314e38 if kind != "fp16" else 65504.0, 0.0)), ("zeros of both signs", np.where(np.arange(vocab) % 2, 0.0, -0.0)),
                           ("alternatives at the end", np.where(np.arange(vocab) >= vocab - 40, 1.0, 0.0)),
                           ("lowest value", np.full(vocab, -3.3895314e38 if kind != "fp16" else -65504.0)),
                           ("one allowed", np.where(np.arange(vocab) == 777, 0.5, -np.inf)),
                           ("masked whole", np.full(vocab, -np.inf)),
                           ("lowest value as mask", np.where(np.arange(vocab) % 5 == 1, np.arange(vocab) % 11, -3.3895314e38 if kind != "fp16" else -65504.0))):
-            for scale in (1.0, 2.0):
+            for scale in (1.0, 2.0) if vocab < 30000 else (2.0,):
                 check_logp(np.stack([row, row[::-1]]), kind, np.array([777, 3]), scale, 32, what=f"{name} {kind}")
 
 
