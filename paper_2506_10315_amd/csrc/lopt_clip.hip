@@ -111,9 +111,8 @@ struct Norm { float norm, factor; };
 __device__ __forceinline__ Norm join_norm(const double* __restrict__ part, int parts, float max_norm, double* red) {
   double s = 0.0;
   for (int i = threadIdx.x; i < parts; i += kBlock) s += part[i];
-  const float v = (float)sqrt(block_sum<4>(s, red));
-  const float c = max_norm / (v + LOPT_CLIP_EPS);
-  return Norm{v, c > 1.f ? 1.f : c};   // NaN stays
+  const double v = sqrt(block_sum<4>(s, red)), c = (double)max_norm / (v + (double)LOPT_CLIP_EPS);
+  return Norm{(float)v, c > 1.0 ? 1.f : (float)c};   // NaN stays
 }
 __global__ __launch_bounds__(kBlock) void k_clip_norm(const double* __restrict__ part, int parts, float* __restrict__ norm) {
   __shared__ double red[4];

@@ -36,6 +36,31 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
   return v;
 }
 
+// Two at once: `red` has 2 kWaves floats.
+template <int G>
+__device__ __forceinline__ void group_sums(float& v, float& w, float* red) {
+  constexpr int W = Group<G>::kWaves;
+  if (W == 1) {
+    v = group_sum<G>(v, red);
+    w = group_sum<G>(w, red);
+    return;
+  }
+  v = wave_sum(v);
+  w = wave_sum(w);
+  if ((threadIdx.x & 63) == 0) {
+    red[threadIdx.x >> 6] = v;
+    red[W + (threadIdx.x >> 6)] = w;
+  }
+  __syncthreads();
+  v = red[0];
+  w = red[W];
+#pragma unroll
+  for (int i = 1; i < W; ++i) {
+    v += red[i];
+    w += red[W + i];
+  }
+}
+
 // V floats that may start at any float.
 template <int V> struct FloatPack { typedef float type __attribute__((ext_vector_type(V), aligned(4))); };
 
@@ -195,14 +220,14 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm(const T* x, int64_t
 }
 
 // The gradient of the same rows. The columns' sums stay in each lane's registers over all of its rows; at the end the workgroup's groups add theirs
-// up in LDS, one after the other, and the workgroup writes one row of partial sums: part[block][2][cols].
+// up through LDS, half to half, and the workgroup writes one row of partial sums: part[block][2][cols].
 template <typename T, int G, int N>
 __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const void* __restrict__ weight,
                                                                   uint32_t weight_type, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
                                                                   int64_t ld_dx, int64_t rows, uint32_t cols, float* __restrict__ part) {
   typedef Share<T, G, N> S;
   constexpr int E = S::E, kRows = Group<G>::kRows;
-  __shared__ float red[2][2][Group<G>::kWaves];
+  __shared__ float red[2][2 * Group<G>::kWaves];
   const S s(cols);
   const int64_t step = (int64_t)gridDim.x * kRows;
   int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
@@ -236,7 +261,8 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, i
       s2 += am * h[i];
     }
     if (dx) {
-      const float m1 = group_sum<G>(s1, red[odd][0]) / (float)cols, m2 = group_sum<G>(s2, red[odd][1]) / (float)cols;
+      group_sums<G>(s1, s2, red[odd]);
+      const float m1 = s1 / (float)cols, m2 = s2 / (float)cols;
 #pragma unroll
       for (int i = 0; i < E; ++i) a[i] = rs * (a[i] - m1 - h[i] * m2);
 #pragma unroll
@@ -245,27 +271,24 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, i
   }
   if (!part) return;
   float* out = part + (int64_t)blockIdx.x * 2 * cols;
-  if (kRows == 1) {
-    s.write(out, sw);
-    s.write(out + cols, sb);
-    return;
-  }
-  __shared__ __align__(16) float sums[2][kRows == 1 ? 4 : G * E];   // by column
+  __shared__ __align__(16) float sums[kRows == 1 ? 1 : kRows / 2][2][kRows == 1 ? 4 : G * E];   // by column
   const int group = threadIdx.x / G;
-  for (int k = 0; k < kRows; ++k) {
-    if (group == k) {
-      if (k) {
-        s.add(sums[0], sw);
-        s.add(sums[1], sb);
-      }
-      s.write(sums[0], sw);
-      s.write(sums[1], sb);
+#pragma unroll
+  for (int half = kRows / 2; half >= 1; half /= 2) {   // the upper half hands over to the lower
+    if (group >= half && group < 2 * half) {
+      s.write(sums[group - half][0], sw);
+      s.write(sums[group - half][1], sb);
+    }
+    __syncthreads();
+    if (group < half) {
+      s.add(sums[group][0], sw);
+      s.add(sums[group][1], sb);
     }
     __syncthreads();
   }
-  for (uint32_t c = threadIdx.x; c < cols; c += Group<G>::kThreads) {
-    out[c] = sums[0][c];
-    out[cols + c] = sums[1][c];
+  if (group == 0) {
+    s.write(out, sw);
+    s.write(out + cols, sb);
   }
 }
 

@@ -71,6 +71,11 @@ def _run(fn, device: torch.device, *args):
         _check(status)
 
 
+def _floats(rows: int, shape: torch.Size, device) -> torch.Tensor:
+    """float32 of `shape`, which has `rows` elements."""
+    return torch.empty(rows if len(shape) == 1 else shape, dtype=torch.float32, device=device)
+
+
 def _new(t: torch.Tensor) -> torch.Tensor:
     """A contiguous tensor of `t`'s shape and type."""
     return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
@@ -100,11 +105,11 @@ def _dense(t: torch.Tensor) -> bool:
 
 def _clip_list(name: str, ts: Sequence[torch.Tensor], device: torch.device):
     """(pointers, lopt_types, whether all are contiguous) of a list of tensors on `device`."""
-    for dev in set(map(_DEVICE, ts)):
-        if dev != device or dev.type != "cuda":
-            raise ValueError(f"{name}: a tensor on {dev}; all have to be on one CUDA device")
+    if set(map(torch.Tensor.get_device, ts)) != {device.index} or device.type != "cuda":
+        raise ValueError(f"{name}: all tensors have to be on one CUDA device")
     dtypes = list(map(_DTYPE, ts))
-    for k in set(dtypes):
+    kinds = set(dtypes)
+    for k in kinds:
         if k not in _TYPES:
             raise ValueError(f"{name}: a tensor of {k}; float32, bfloat16 or float16 is needed")
     contiguous = all(map(torch.Tensor.is_contiguous, ts))
@@ -113,10 +118,10 @@ def _clip_list(name: str, ts: Sequence[torch.Tensor], device: torch.device):
             if t.layout != torch.strided or not _dense(t):
                 raise ValueError(f"{name}: a tensor that does not fill one run of memory")
     n = len(ts)
-    return (C.c_void_p * n)(*map(torch.Tensor.data_ptr, ts)), (C.c_uint32 * n)(*[_TYPES[k] for k in dtypes]), contiguous
+    return (C.c_void_p * n)(*map(torch.Tensor.data_ptr, ts)), (C.c_uint32 * n)(*([_TYPES[dtypes[0]]] * n if len(kinds) == 1 else [_TYPES[k] for k in dtypes])), contiguous
 
 
-_DEVICE, _DTYPE, _SHAPE = operator.attrgetter("device"), operator.attrgetter("dtype"), operator.attrgetter("shape")
+_DTYPE, _SHAPE = operator.attrgetter("dtype"), operator.attrgetter("shape")
 
 
 def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], max_norm: float) -> torch.Tensor:
@@ -189,7 +194,7 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     if bias is not None:
         bias = _expect("bias", bias, x, wtype, (cols,))
     y = _new(x)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    mean = _floats(rows, x.shape[:-1], x.device)
     rstd = torch.empty_like(mean)
     _run(lib().lopt_layer_norm, x.device, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(),
          rows, cols, eps, kind, _TYPES[wtype] if wtype is not None else 0)
@@ -268,10 +273,10 @@ def token_logprobs_forward(logits: torch.Tensor, targets: Optional[torch.Tensor]
     if not 0 <= top <= min(vocab, TOP_MAX):
         raise ValueError(f"top={top} outside [0, {min(vocab, TOP_MAX)}]")
     dev = logits.device
-    logp = torch.empty(shape, dtype=torch.float32, device=dev) if targets is not None else None
+    logp = _floats(rows, shape, dev) if targets is not None else None
     ent = None
     if entropy:
-        ent = torch.empty_like(logp) if logp is not None else torch.empty(shape, dtype=torch.float32, device=dev)
+        ent = torch.empty_like(logp) if logp is not None else _floats(rows, shape, dev)
     stats = torch.empty(shape + (2,), dtype=torch.float32, device=dev)
     top_logp = torch.empty(shape + (top,), dtype=torch.float32, device=dev) if top else None
     top_index = torch.empty(shape + (top,), dtype=torch.int64, device=dev) if top else None

@@ -678,6 +678,17 @@ def test_token_logprobs_autograd_against_differences():
         scale = float(np.abs(host(xt.grad) * d).sum())
         # differences as for the layer norm; gradient: e^z with |z| up to 30, and the forward pass's ln S and entropy
         assert abs(got - slope) <= 1e-8 * scale + 1e-8 + 1.25 * (depth(53) + 200) * U * (scale + np.abs(d).max() * (np.abs(c).sum() + np.abs(k).sum())), (got, slope)
+    # logp may be changed in place, for any number of dimensions; the entropy belongs to the backward pass
+    for shape in ((7,), (1, 7), ()):
+        y = (xt[0] if shape == () else xt.view(shape + (53,))).detach().clone().requires_grad_()
+        out = ops().token_logprobs(y, torch.zeros(shape, dtype=torch.int64, device="cuda:0"))
+        out.logp.mul_(2.0)
+        (out.logp.sum() + out.entropy.sum()).backward()
+        assert out.logp.shape == shape and y.grad.shape == y.shape
+        out = ops().token_logprobs(y, torch.zeros(shape, dtype=torch.int64, device="cuda:0"))
+        out.entropy.add_(1.0)
+        with pytest.raises(RuntimeError):
+            out.entropy.sum().backward()
     # one output's gradient alone, and none
     xt.grad = None
     out = ops().token_logprobs(xt, None)
