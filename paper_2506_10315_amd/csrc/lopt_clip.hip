@@ -156,11 +156,13 @@ __global__ __launch_bounds__(kBlock) void k_clip_scale(const ClipBatch b, const 
 }
 
 int64_t chunks_of(int64_t count) { return (count + kChunk - 1) / kChunk; }
-// Workgroups of a launch that has `here` of the list's `all` chunks.
-int grid_of(int64_t here, int64_t all) { return (int)std::min<int64_t>(here, (here * kGrid + all - 1) / all); }
-// Partial sums of n tensors: kGrid and, for rounding up, one for every launch; no more than one a chunk. A launch ends after kBatch tensors, or
+// Workgroups of a launch that has `here` of the list's `all` chunks: its share of kGrid, but no fewer than kLeast (1346 M elements with 2000 tiny tensors,
+// twelve launches of those: 7.7 -> 3.6 ms).
+constexpr int kLeast = 128;
+int grid_of(int64_t here, int64_t all) { return (int)std::min<int64_t>(here, std::max<int64_t>((here * kGrid + all - 1) / all, kLeast)); }
+// Partial sums of n tensors at most: kGrid and, for rounding up, kLeast for every launch; no more than one a chunk. A launch ends after kBatch tensors, or
 // with more than 0.75 * 2^30 chunks.
-size_t most_parts(size_t n, int64_t chunks) { return (size_t)std::min<int64_t>(chunks, kGrid + (int64_t)((n + kBatch - 1) / kBatch) + (chunks >> 29)); }
+size_t most_parts(size_t n, int64_t chunks) { return (size_t)std::min<int64_t>(chunks, kGrid + kLeast * ((int64_t)((n + kBatch - 1) / kBatch) + (chunks >> 29))); }
 
 }  // namespace
 }  // namespace lopt

@@ -321,26 +321,78 @@ __global__ __launch_bounds__(1024) void k_norm_columns_sum(const float* __restri
   }
 }
 
-// ---- rows too long for registers: the row is read again for every use
+// ---- rows too long for registers: one workgroup a row, which reads it again (from L2) for every use
+// Calls f(first element, pack or element count) over a row: packs of 16 bytes, four in flight a thread, then what is left element by element.
+template <int V, typename F>
+__device__ __forceinline__ void along_row(uint32_t cols, F&& f) {
+  using std::integral_constant;
+  const uint32_t packs = cols / V;
+  uint32_t k = threadIdx.x;
+  for (; k + 3 * 1024 < packs; k += 4 * 1024) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f((k + j * 1024) * V, integral_constant<int, V>{});
+  }
+  for (; k < packs; k += 1024) f(k * V, integral_constant<int, V>{});
+  for (uint32_t i = packs * V + threadIdx.x; i < cols; i += 1024) f(i, integral_constant<int, 1>{});
+}
+template <typename T, int V>
+__device__ __forceinline__ void load_run(const T* p, float (&v)[V]) {
+  typedef T run __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  const run x = *(const run*)p;
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = to_f32(x[e]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_run(T* p, const float (&v)[V]) {
+  typedef T run __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  run x;
+#pragma unroll
+  for (int e = 0; e < V; ++e) x[e] = from_f32<T>(v[e]);
+  *(run*)p = x;
+}
+template <int V>
+__device__ __forceinline__ void load_run_as(const void* p, uint32_t i, uint32_t type, float other, float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = other;
+  if (!p) return;
+  if (type == LOPT_F32) load_run((const float*)p + i, v);
+  else if (type == LOPT_BF16) load_run((const bf16_t*)p + i, v);
+  else load_run((const f16_t*)p + i, v);
+}
+
 template <typename T>
 __global__ __launch_bounds__(1024) void k_norm_long(const T* x, int64_t ld_x, Vectors wb, T* y, int64_t ld_y, float* __restrict__ mean_out,
                                                     float* __restrict__ rstd_out, int64_t rows, uint32_t cols, float eps) {
+  constexpr int V = Pack<T>::n;
   __shared__ float red[16];
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* xr = x + r * ld_x;
     float s = 0.f;
-    for (uint32_t i = threadIdx.x; i < cols; i += 1024) s += to_f32(xr[i]);
+    along_row<V>(cols, [&](uint32_t i, auto n) {
+      float v[decltype(n)::value];
+      load_run(xr + i, v);
+#pragma unroll
+      for (float a : v) s += a;
+    });
     const float mean = block_sum<16>(s, red) / (float)cols;
     s = 0.f;
-    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
-      const float d = to_f32(xr[i]) - mean;
-      s += d * d;
-    }
+    along_row<V>(cols, [&](uint32_t i, auto n) {
+      float v[decltype(n)::value];
+      load_run(xr + i, v);
+#pragma unroll
+      for (float a : v) s += (a - mean) * (a - mean);
+    });
     const float rstd = 1.f / sqrtf(block_sum<16>(s, red) / (float)cols + eps);
-    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
-      const float h = (to_f32(xr[i]) - mean) * rstd;
-      y[r * ld_y + i] = from_f32<T>(h * (wb.w ? load_as(wb.w, i, wb.type) : 1.f) + (wb.b ? load_as(wb.b, i, wb.type) : 0.f));
-    }
+    along_row<V>(cols, [&](uint32_t i, auto n) {
+      constexpr int N = decltype(n)::value;
+      float v[N], w[N], b[N];
+      load_run(xr + i, v);
+      load_run_as(wb.w, i, wb.type, 1.f, w);
+      load_run_as(wb.b, i, wb.type, 0.f, b);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = (v[e] - mean) * rstd * w[e] + b[e];
+      store_run(y + r * ld_y + i, v);
+    });
     if (threadIdx.x == 0) {
       if (mean_out) mean_out[r] = mean;
       if (rstd_out) rstd_out[r] = rstd;
@@ -348,25 +400,34 @@ __global__ __launch_bounds__(1024) void k_norm_long(const T* x, int64_t ld_x, Ve
   }
 }
 
-constexpr int kSlab = 128;   // rows whose column sums one lane adds up
+constexpr int kSlab = 32;   // rows whose column sums one lane adds up
 
-// Partial sums of dy xh and dy over a slab of rows, a column a lane. Runs before dx, which may overwrite dy or x.
+// Partial sums of dy xh and dy over a slab of rows, a pack of columns a lane; the pack that would pass the row's end ends with it, and gives the columns that
+// it shares the same sums. Runs before dx, which may overwrite dy or x.
 template <typename T>
 __global__ __launch_bounds__(kWave) void k_norm_long_columns(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ x, int64_t ld_x,
                                                              const float* __restrict__ mean, const float* __restrict__ rstd, int64_t rows, uint32_t cols,
                                                              float* __restrict__ part) {
-  const uint32_t c = blockIdx.x * kWave + threadIdx.x;
-  if (c >= cols) return;
+  constexpr int V = Pack<T>::n;
+  const uint64_t k = ((uint64_t)blockIdx.x * kWave + threadIdx.x) * V;
+  if (k >= cols) return;
+  const uint32_t c = min((uint32_t)k, cols - V);
   for (int64_t slab = blockIdx.y; slab * kSlab < rows; slab += gridDim.y) {
     const int64_t r0 = slab * kSlab, r1 = min(r0 + kSlab, rows);
-    float sw = 0.f, sb = 0.f;
+    float sw[V] = {}, sb[V] = {};
+#pragma unroll 4
     for (int64_t r = r0; r < r1; ++r) {
-      const float g = to_f32(dy[r * ld_dy + c]);
-      sw += g * ((to_f32(x[r * ld_x + c]) - mean[r]) * rstd[r]);
-      sb += g;
+      float g[V], h[V];
+      load_run(dy + r * ld_dy + c, g);
+      load_run(x + r * ld_x + c, h);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        sw[e] += g[e] * ((h[e] - mean[r]) * rstd[r]);
+        sb[e] += g[e];
+      }
     }
-    part[slab * 2 * cols + c] = sw;
-    part[(slab * 2 + 1) * cols + c] = sb;
+    store_run(part + slab * 2 * cols + c, sw);
+    store_run(part + (slab * 2 + 1) * cols + c, sb);
   }
 }
 
@@ -374,22 +435,43 @@ template <typename T>
 __global__ __launch_bounds__(1024) void k_norm_long_rows(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const void* __restrict__ w, uint32_t weight_type,
                                                          const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t ld_dx, int64_t rows,
                                                          uint32_t cols) {
+  constexpr int V = Pack<T>::n;
   __shared__ float red[16];
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const float mu = mean[r], rs = rstd[r];
+    auto load = [&](uint32_t i, auto& a, auto& h) {
+      constexpr int N = sizeof(a) / sizeof(float);
+      float q[N];
+      load_run(dy + r * ld_dy + i, a);
+      load_run(x + r * ld_x + i, h);
+      load_run_as(w, i, weight_type, 1.f, q);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        a[e] *= q[e];
+        h[e] = (h[e] - mu) * rs;
+      }
+    };
     float s1 = 0.f, s2 = 0.f;
-    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
-      const float a = to_f32(dy[r * ld_dy + i]) * (w ? load_as(w, i, weight_type) : 1.f);
-      s1 += a;
-      s2 += a * ((to_f32(x[r * ld_x + i]) - mu) * rs);
-    }
+    along_row<V>(cols, [&](uint32_t i, auto n) {
+      constexpr int N = decltype(n)::value;
+      float a[N], h[N];
+      load(i, a, h);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        s1 += a[e];
+        s2 += a[e] * h[e];
+      }
+    });
     const float m1 = block_sum<16>(s1, red) / (float)cols;
     const float m2 = block_sum<16>(s2, red) / (float)cols;
-    for (uint32_t i = threadIdx.x; i < cols; i += 1024) {
-      const float a = to_f32(dy[r * ld_dy + i]) * (w ? load_as(w, i, weight_type) : 1.f);
-      const float h = (to_f32(x[r * ld_x + i]) - mu) * rs;
-      dx[r * ld_dx + i] = from_f32<T>(rs * (a - m1 - h * m2));
-    }
+    along_row<V>(cols, [&](uint32_t i, auto n) {
+      constexpr int N = decltype(n)::value;
+      float a[N], h[N];
+      load(i, a, h);
+#pragma unroll
+      for (int e = 0; e < N; ++e) a[e] = rs * (a[e] - m1 - h[e] * m2);
+      store_run(dx + r * ld_dx + i, a);
+    });
   }
 }
 
@@ -513,7 +595,7 @@ lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
       });
       if (!held) {
         if (columns)
-          hipLaunchKernelGGL(k_norm_long_columns<T>, dim3((n_cols + kWave - 1) / kWave, (unsigned)std::min<int64_t>(parts, 1024)), dim3(kWave), 0, stream,
+          hipLaunchKernelGGL(k_norm_long_columns<T>, dim3((n_cols / Pack<T>::n + kWave) / kWave, (unsigned)std::min<int64_t>(parts, 1024)), dim3(kWave), 0, stream,
                              (const T*)dy, ld_dy, (const T*)x, ld_x, mean, rstd, rows, n_cols, part);
         if (dx)
           hipLaunchKernelGGL(k_norm_long_rows<T>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(1024), 0, stream, (const T*)dy, ld_dy, (const T*)x, ld_x,

@@ -13,10 +13,6 @@ __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 template <typename T>
 __device__ __forceinline__ T from_f32(float v) { return (T)v; }   // round to nearest even
 
-__device__ __forceinline__ float load_as(const void* p, int64_t i, uint32_t type) {
-  return type == LOPT_F32 ? ((const float*)p)[i] : type == LOPT_BF16 ? to_f32(((const bf16_t*)p)[i]) : to_f32(((const f16_t*)p)[i]);
-}
-
 // 16 bytes of consecutive elements, which may start at any element: the access needs no more than an element's alignment.
 template <typename T> struct Pack;
 template <> struct Pack<float> { static constexpr int n = 4; typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
