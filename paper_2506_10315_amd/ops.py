@@ -7,8 +7,8 @@ Tensors are CUDA tensors of float32, bfloat16 or float16; `layer_norm` and `toke
 `*_forward` and `*_backward` functions are the passes by themselves."""
 from __future__ import annotations
 
-import ctypes as C
 import operator
+from array import array
 from typing import Iterable, List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
@@ -117,8 +117,8 @@ def _clip_list(name: str, ts: Sequence[torch.Tensor], device: torch.device):
         for t in ts:
             if t.layout != torch.strided or not _dense(t):
                 raise ValueError(f"{name}: a tensor that does not fill one run of memory")
-    n = len(ts)
-    return (C.c_void_p * n)(*map(torch.Tensor.data_ptr, ts)), (C.c_uint32 * n)(*([_TYPES[dtypes[0]]] * n if len(kinds) == 1 else [_TYPES[k] for k in dtypes])), contiguous
+    types = array("I", [_TYPES[dtypes[0]]]) * len(ts) if len(kinds) == 1 else array("I", [_TYPES[k] for k in dtypes])
+    return array("Q", map(torch.Tensor.data_ptr, ts)), types, contiguous
 
 
 _DTYPE, _SHAPE = operator.attrgetter("dtype"), operator.attrgetter("shape")
@@ -143,11 +143,13 @@ def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], 
             for g, o in zip(grads, out):
                 if g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous()):
                     raise ValueError("an output's strides are not its gradient's")
-    counts = (C.c_int64 * n)(*map(torch.Tensor.numel, grads))
+    counts = array("q", map(torch.Tensor.numel, grads))
+    at = [a and a.buffer_info()[0] for a in (counts, gp, gt, op, ot)]
     L = lib()
     norm = torch.empty((), dtype=torch.float32, device=device)
-    ws = torch.empty(L.lopt_clip_workspace(n, counts), dtype=torch.uint8, device=device)
-    _run(L.lopt_clip_grads, device, n, counts, gp, gt, op, ot, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel())
+    nbytes = L.lopt_clip_workspace(n, at[0])
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _run(L.lopt_clip_grads, device, n, *at, max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
     return norm
 
 
