@@ -522,6 +522,20 @@ def test_token_logprobs_ties_and_orders(vocab):
                 check_logp(np.stack([row, row[::-1]]), kind, np.array([777, 3]), scale, 32, what=f"{name} {kind}")
 
 
+@pytest.mark.parametrize("rows,vocab", [(4, 100), (3, 3000), (300, 5000), (2, 140000)])
+def test_token_logprobs_of_large_logits(rows, vocab):
+    """A common offset costs nothing beyond the logits' own rounding; the largest and smallest that the types hold stay right."""
+    for offset, scale in ((4096.0, 1.0), (-3.0e5, 1.25), (1e6, 0.5), (0.0, 1e-3), (0.0, 300.0)):
+        x, t = logits_case(rows, vocab, rows + vocab)
+        check_logp(x + np.float32(offset), "fp32", t, scale, 4, what=f"offset {offset} scale {scale}")
+    x, t = logits_case(rows, vocab, rows + vocab)
+    for value in (-1e31, 1e31, 3e38, -3e38):
+        y = x.copy()
+        y[::2] = value                 # rows of one value, beyond what the running sums' base may be
+        y[0, 1::3] = value / 2
+        check_logp(y, "fp32", t, 1.0, 4, what=f"{value}")
+
+
 def test_token_logprobs_special_rows_and_targets():
     import torch
     x, t = logits_case(12, 5000, 5)
