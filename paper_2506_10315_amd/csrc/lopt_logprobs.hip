@@ -601,7 +601,10 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
   const int64_t n = vocab + 7;   // a row counted from its pack
   if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, 0, 0};
   if (top) {
-    const int lane = n <= 16 * 1024 ? 16 : n <= 32 * 1024 ? 32 : 64;
+    // A wavefront's search costs about what 20 logits a lane do, whatever it holds; more wavefronts are done sooner. us with 16 / 32 / 64 logits a lane, bf16:
+    // 1x3000 5.1 / 6.0 / 7.9, 1024x8000 16.9 / 14.6 / 14.7, 1x16000 9.2 / 6.6 / 8.2, 1024x16000 30 / 20 / 18 (fp32 31 / 22 / 26), 256x32000 - / 11.8 / 11.9 (fp32
+    // 12.7 / 17.5), 1024x32000 - / 43 / 32.
+    const int lane = n <= 8 * 1024 ? 16 : n <= 16 * 1024 || (n <= 32 * 1024 && rows <= 256) ? 32 : 64;
     if (n <= 64 * 1024) return RowPlan{kRowBlock, lane, (int)((n + lane * kWave - 1) / (lane * kWave)), 0, 0};
     return RowPlan{kRowSplit, 32, 4, 1, (n + 2047) / 2048};
   }
