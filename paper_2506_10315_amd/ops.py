@@ -33,9 +33,9 @@ def _type(name: str, t: torch.Tensor) -> int:
 
 def _expect(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape) -> torch.Tensor:
     """`t` on `like`'s device with this type and shape, contiguous (copied where it is not)."""
-    if t.device != like.device:
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    if t.dtype != dtype or t.shape != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}; {tuple(shape)} of {dtype} is needed")
     return t if t.is_contiguous() else t.contiguous()
 
@@ -43,14 +43,15 @@ def _expect(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape) -> tor
 def _matrix(name: str, t: torch.Tensor) -> Tuple[torch.Tensor, int, int, int]:
     """(tensor, rows, columns, elements from row to row) of `t` seen as rows of its last dimension. A 2-D tensor keeps its row
     stride; any other layout whose rows are not evenly spaced runs of adjacent elements is copied."""
-    if t.dim() == 0:
+    shape = t.shape
+    if not shape:
         raise ValueError(f"{name} has no dimension")
-    cols = t.shape[-1]
+    cols = shape[-1]
     if cols == 0:
         raise ValueError(f"{name} has rows of no elements")
     if not t.is_contiguous():
-        if t.dim() == 2 and (t.stride(1) == 1 or cols == 1):
-            return t, t.shape[0], cols, t.stride(0)
+        if len(shape) == 2 and (t.stride(1) == 1 or cols == 1):
+            return t, shape[0], cols, t.stride(0)
         t = t.contiguous()
     return t, t.numel() // cols, cols, cols
 
@@ -60,8 +61,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _run(fn, device: torch.device, *args):
-    index = device.index
+def _run(fn, index: int, *args):
+    """The call on GPU `index`, on its current stream."""
     if _current_device() == index:
         status = fn(*args, _raw_stream(index))
     else:
@@ -74,6 +75,13 @@ def _run(fn, device: torch.device, *args):
 def _floats(rows: int, shape: torch.Size, device) -> torch.Tensor:
     """float32 of `shape`, which has `rows` elements."""
     return torch.empty(rows if len(shape) == 1 else shape, dtype=torch.float32, device=device)
+
+
+def _rows_of(rows: int, shape: torch.Size, n: int, dtype, device) -> torch.Tensor:
+    """`n` elements for each of the `rows` that `shape` has."""
+    if len(shape) == 1:
+        return torch.empty(rows, n, dtype=dtype, device=device)
+    return torch.empty(shape + (n,), dtype=dtype, device=device)
 
 
 def _new(t: torch.Tensor) -> torch.Tensor:
@@ -149,7 +157,7 @@ def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], 
     norm = torch.empty((), dtype=torch.float32, device=device)
     nbytes = L.lopt_clip_workspace(n, at[0])
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _run(L.lopt_clip_grads, device, n, *at, max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
+    _run(L.lopt_clip_grads, device.index, n, *at, max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
     return norm
 
 
@@ -184,22 +192,19 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     """(y, mean, rstd) over the last dimension of `x`; y has x's type, mean and rstd are float32 of x's other dimensions."""
     kind = _type("x", x)
     x2, rows, cols, ld = _matrix("x", x)
-    wtype = None
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None:
-            if wtype is not None and t.dtype != wtype:
-                raise ValueError(f"bias is of {t.dtype}, weight of {wtype}")
-            wtype = t.dtype
-            _type(name, t)
+    wtype = 0
     if weight is not None:
-        weight = _expect("weight", weight, x, wtype, (cols,))
+        wtype = _type("weight", weight)
+        weight = _expect("weight", weight, x, weight.dtype, (cols,))
     if bias is not None:
-        bias = _expect("bias", bias, x, wtype, (cols,))
+        if weight is None:
+            wtype = _type("bias", bias)
+        bias = _expect("bias", bias, x, bias.dtype if weight is None else weight.dtype, (cols,))
     y = _new(x)
     mean = _floats(rows, x.shape[:-1], x.device)
     rstd = torch.empty_like(mean)
-    _run(lib().lopt_layer_norm, x.device, x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(),
-         rows, cols, eps, kind, _TYPES[wtype] if wtype is not None else 0)
+    _run(lib().lopt_layer_norm, x.get_device(), x2.data_ptr(), ld, _ptr(weight), _ptr(bias), y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(),
+         rows, cols, eps, kind, wtype)
     return y, mean, rstd
 
 
@@ -209,7 +214,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     weight's type (without a weight bias_type, by default float32)."""
     kind = _type("x", x)
     x2, rows, cols, ld = _matrix("x", x)
-    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
+    if dy.shape != x.shape or dy.dtype is not x.dtype or dy.get_device() != x.get_device():
         raise ValueError(f"dy is {tuple(dy.shape)} of {dy.dtype} on {dy.device}; x is {tuple(x.shape)} of {x.dtype} on {x.device}")
     dy2, _, _, ld_dy = _matrix("dy", dy)
     wtype = weight.dtype if weight is not None else bias_type or torch.float32
@@ -217,8 +222,9 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
         raise ValueError(f"weights of {wtype}; float32, bfloat16 or float16 is needed")
     if weight is not None:
         weight = _expect("weight", weight, x, wtype, (cols,))
-    mean = _expect("mean", mean, x, torch.float32, x.shape[:-1])
-    rstd = _expect("rstd", rstd, x, torch.float32, x.shape[:-1])
+    shape = x.shape[:-1]
+    mean = _expect("mean", mean, x, torch.float32, shape)
+    rstd = _expect("rstd", rstd, x, torch.float32, shape)
     dx = _new(x) if need[0] else None
     dw = db = None
     if need[1]:
@@ -226,9 +232,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     if need[2]:
         db = torch.empty_like(dw) if dw is not None else torch.empty(cols, dtype=wtype, device=x.device)
     L = lib()
-    ws = _workspace(L.lopt_layer_norm_workspace(rows, cols), x.device) if need[1] or need[2] else None
-    _run(L.lopt_layer_norm_backward, x.device, dy2.data_ptr(), ld_dy, x2.data_ptr(), ld, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx), cols,
-         _ptr(dw), _ptr(db), rows, cols, kind, _TYPES[wtype], _ptr(ws), 0 if ws is None else ws.numel())
+    nbytes = L.lopt_layer_norm_workspace(rows, cols) if need[1] or need[2] else 0
+    ws = _workspace(nbytes, x.device)
+    _run(L.lopt_layer_norm_backward, x.get_device(), dy2.data_ptr(), ld_dy, x2.data_ptr(), ld, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx), cols,
+         _ptr(dw), _ptr(db), rows, cols, kind, _TYPES[wtype], _ptr(ws), nbytes)
     return dx, dw, db
 
 
@@ -279,13 +286,16 @@ def token_logprobs_forward(logits: torch.Tensor, targets: Optional[torch.Tensor]
     ent = None
     if entropy:
         ent = torch.empty_like(logp) if logp is not None else _floats(rows, shape, dev)
-    stats = torch.empty(shape + (2,), dtype=torch.float32, device=dev)
-    top_logp = torch.empty(shape + (top,), dtype=torch.float32, device=dev) if top else None
-    top_index = torch.empty(shape + (top,), dtype=torch.int64, device=dev) if top else None
+    stats = _rows_of(rows, shape, 2, torch.float32, dev)
+    top_logp = top_index = None
+    if top:
+        top_logp = _rows_of(rows, shape, top, torch.float32, dev)
+        top_index = torch.empty_like(top_logp, dtype=torch.int64)
     L = lib()
-    ws = _workspace(L.lopt_token_logprobs_workspace(rows, vocab, top), dev)
-    _run(L.lopt_token_logprobs, dev, x.data_ptr(), ld, _ptr(targets), rows, vocab, kind, scale, ignore_index, top, _ptr(logp), _ptr(ent), stats.data_ptr(),
-         _ptr(top_logp), _ptr(top_index), _ptr(ws), 0 if ws is None else ws.numel())
+    nbytes = L.lopt_token_logprobs_workspace(rows, vocab, top)
+    ws = _workspace(nbytes, dev)
+    _run(L.lopt_token_logprobs, dev.index, x.data_ptr(), ld, _ptr(targets), rows, vocab, kind, scale, ignore_index, top, _ptr(logp), _ptr(ent), stats.data_ptr(),
+         _ptr(top_logp), _ptr(top_index), _ptr(ws), nbytes)
     return TokenLogprobs(logp, ent, top_logp, top_index, stats)
 
 
@@ -309,7 +319,7 @@ def token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor
             raise ValueError("dentropy without entropy")
         entropy = _expect("entropy", entropy, logits, torch.float32, shape)
     dx = _new(logits)
-    _run(lib().lopt_token_logprobs_backward, logits.device, x.data_ptr(), ld, _ptr(targets), stats.data_ptr(), _ptr(entropy), _ptr(dlogp), _ptr(dentropy),
+    _run(lib().lopt_token_logprobs_backward, logits.get_device(), x.data_ptr(), ld, _ptr(targets), stats.data_ptr(), _ptr(entropy), _ptr(dlogp), _ptr(dentropy),
          dx.data_ptr(), vocab, rows, vocab, kind, scale, ignore_index)
     return dx
 
