@@ -178,12 +178,19 @@ __device__ __forceinline__ void add_piece(Soft& a, const float (&x)[E], float mo
   }
 }
 
-// The largest number that at least `need` of the lanes' numbers reach; 0 if fewer than that are not 0.
-__device__ __forceinline__ uint32_t reached_by(uint32_t v, int need) {
-  int reach = 0;
-#pragma unroll
-  for (int l = 0; l < kWave; ++l) reach += (uint32_t)__builtin_amdgcn_readlane((int)v, l) >= v;
-  return wave_max(reach >= need ? v : 0u);
+// The largest number that at least `need` of the lanes' numbers reach, bit by bit from the top; 0 if fewer than that are not 0. With fewer than 32 `bits`
+// what is left of it is 0, so that it is a little low: one vector instruction a bit.
+__device__ __forceinline__ uint32_t reached_by(uint32_t v, int need, int bits) {
+  uint32_t reached = 0;
+  for (int b = 31; b >= 32 - bits; --b) {
+    const uint32_t t = reached | 1u << b;
+    if (__popcll(__ballot(v >= t)) >= need) reached = t;
+  }
+  return reached;
+}
+constexpr int kBoundBits = 16;   // of a bound that may be low: sign, exponent, seven bits
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 // Sum of the lanes' n (at most 127) before this one; `all`: of all lanes.
 __device__ __forceinline__ int count_before(int n, int* all) {
@@ -191,7 +198,7 @@ __device__ __forceinline__ int count_before(int n, int* all) {
 #pragma unroll
   for (int b = 0; b < 7; ++b) {
     const uint64_t mask = __ballot(n >> b & 1);
-    before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)) << b;
+    before += lanes_before(mask) << b;
     sum += __popcll(mask) << b;
   }
   *all = sum;
@@ -229,9 +236,9 @@ __device__ __forceinline__ uint64_t in_order(const uint64_t* list, int count, in
   return out;
 }
 
-// The `top` largest keys of a piece in order; `most` is the largest of the lane's logits. At least `top`
-// lanes' maxima reach `bound`, so nothing below it counts, and what lies above it belongs to fewer than `top` lanes. What equals it may be many
-// (masks, few different values): where the list does not hold them all, only the `top` of lowest index are taken.
+// The `top` largest keys of a piece in order; `most` is the largest of the lane's logits. At least `top` lanes' maxima reach `bound`, so nothing below it
+// counts. Where the list does not hold what reaches it, or masked logits do, the bound is found to its last bit: what lies above it belongs to fewer than `top`
+// lanes, and of its equals, which may be many (masks, few different values), only the `top` of lowest index are taken.
 // `list`: room for (E + 2) top keys. `special`: there may be a NaN.
 template <typename T, int E>
 __device__ __forceinline__ uint64_t piece_top(const Piece<T, E>& p, const float (&x)[E], float most, int top, bool special, uint64_t* list) {
@@ -239,14 +246,21 @@ __device__ __forceinline__ uint64_t piece_top(const Piece<T, E>& p, const float 
   const int room = E * top;
   int pass = 0, count, at;
   if (!special) {
-    const float bound = key_value((uint64_t)reached_by(order_of(most), top) << 32);
+    const uint32_t reached = reached_by(order_of(most), top, kBoundBits);
+    const float bound = key_value((uint64_t)reached << 32);
+    count = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) pass += x[i] >= bound;
-    at = count_before(pass, &count);
-    if (count <= room && bound > -INFINITY) {   // no masked logit among them, nor one that is not this lane's
+    for (int i = 0; i < E; ++i) count += __popcll(__ballot(x[i] >= bound));
+    if (count <= room && reached > order_of(-INFINITY)) {   // no masked logit among them, nor one that is not this lane's
+      at = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (x[i] >= bound) list[at++] = rank_key(order_of(x[i]), (uint32_t)p.index(i));
+      for (int i = 0; i < E; ++i) {
+        const uint64_t mask = __ballot(x[i] >= bound);
+        if (mask) {
+          if (x[i] >= bound) list[at + lanes_before(mask)] = rank_key(order_of(x[i]), (uint32_t)p.index(i));
+          at += __popcll(mask);
+        }
+      }
       wave_sync();
       return in_order(list, count, top, list + (E + 1) * top);
     }
@@ -258,7 +272,7 @@ __device__ __forceinline__ uint64_t piece_top(const Piece<T, E>& p, const float 
     ord[i] = p.mine(i) ? ord[i] : 0;
     hi = max(hi, ord[i]);
   }
-  const uint32_t bound = max(reached_by(hi, top), 1u);
+  const uint32_t bound = max(reached_by(hi, top, 32), 1u);
   pass = 0;
 #pragma unroll
   for (int i = 0; i < E; ++i) pass += ord[i] > bound;
@@ -293,7 +307,7 @@ __device__ __forceinline__ uint64_t join_lists(uint64_t* lists, int count, int t
   const int lane = threadIdx.x & 63;
   // where `need` of the lists reach a bound with their `deep`-th key, `top` keys do
   const int deep = min((2 * top + count - 1) / count, top), need = (top + deep - 1) / deep;
-  const uint32_t bound = max(reached_by(lane < count ? (uint32_t)(lists[lane * top + deep - 1] >> 32) : 0u, need), 1u);
+  const uint32_t bound = max(reached_by(lane < count ? (uint32_t)(lists[lane * top + deep - 1] >> 32) : 0u, need, 32), 1u);
   int pass = 0, all;
   if (lane < count)
     while (pass < top && (uint32_t)(lists[lane * top + pass] >> 32) >= bound) ++pass;
@@ -375,7 +389,7 @@ __device__ __forceinline__ uint64_t top_of_list(uint64_t* list, int count, int t
   if (count <= kWave) return in_order(list, count, top, buffer);
   uint64_t best = 0;
   for (int i = lane; i < count; i += kWave) best = max(best, list[i]);
-  const uint32_t bound = reached_by((uint32_t)(best >> 32), top);
+  const uint32_t bound = reached_by((uint32_t)(best >> 32), top, 32);
   int pass = 0, all;
   for (int i = lane; i < count; i += kWave) pass += (uint32_t)(list[i] >> 32) >= bound;
   int at = count_before(pass, &all);
@@ -388,7 +402,7 @@ __device__ __forceinline__ uint64_t top_of_list(uint64_t* list, int count, int t
 // The same with alternatives: the workgroup holds the whole row, E logits a lane. Every wavefront's lanes' maxima give a bound that `top` of them
 // reach; the largest of the wavefronts' bounds holds for the row. The few logits that reach it are gathered in LDS, and the first wavefront
 // puts them in order. Fewer than `top` logits that are not masked: all of them, then the masked ones of lowest index. More than the list holds (few
-// different values, masks of the type's lowest value): those above the bound, then of its equals those of lowest index; a wavefront's
+// different values, masks of a low value): those above the bound, found to its last bit, then of its equals those of lowest index; a wavefront's
 // logits are neighbours in the row. What is left, rows with a NaN among it, takes the largest key `top` times from memory. Bound by vector issue and, for one
 // row, by one compute unit's: 1x50257 fp32 with 20 alternatives 16 us, 256x32000 bf16 with five 12.4, 1024x50257 bf16 with 20 72. One row spread over 13
 // workgroups that a second launch joins: 6.3 + 8.7 us, and a launch and a workspace more on the host (a call 23 us, so 17).
@@ -403,6 +417,10 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
   __shared__ int listed[2], equals[16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const float c = fminf(scale * kLog2e, FLT_MAX);
+  auto row_bound = [&] {   // masked logits do not reach it
+    const uint32_t b = wave_max(lane < waves ? bounds[lane] : 0u);
+    return b > order_of(-FLT_MAX) ? key_value((uint64_t)b << 32) : -FLT_MAX;
+  };
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* row = x + r * ld;
     P p;
@@ -412,7 +430,7 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
     float v[E];
     p.unpack(v);
     const float most = most_of(v);
-    const uint32_t own = reached_by(order_of(most), top);
+    const uint32_t own = reached_by(order_of(most), top, kBoundBits);
     if (lane == 0) bounds[wave] = own;
     if (threadIdx.x < 2) listed[threadIdx.x] = 0;
     Soft a{-INFINITY, 0.f, 0.f};
@@ -420,27 +438,35 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
     a = wave_join(a, c);
     if (lane == 0) sums[wave] = a;
     __syncthreads();
-    const float bound = fmaxf(key_value((uint64_t)wave_max(lane < waves ? bounds[lane] : 0u) << 32), -FLT_MAX);   // masked logits do not reach it
+    float bound = row_bound();
     a = wave_join(lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
     const bool special = a.s != a.s;
     auto gather = [&](auto passes, int* counter) {   // counts all, writes what the list holds
-      int pass = 0, all, from = 0;
+      int all = 0, from = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) pass += passes(v[i]);
-      int at = count_before(pass, &all);
+      for (int i = 0; i < E; ++i) all += __popcll(__ballot(passes(v[i])));
       if (!all) return;
       if (lane == 0) from = atomicAdd(counter, all);
-      at += __builtin_amdgcn_readfirstlane(from);
-      if (at + pass > kListed) return;
+      int at = __builtin_amdgcn_readfirstlane(from);
+      if (at + all > kListed) return;
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (passes(v[i])) list[at++] = rank_key(order_of(v[i]), (uint32_t)p.index(i));
+      for (int i = 0; i < E; ++i) {
+        const uint64_t mask = __ballot(passes(v[i]));
+        if (mask) {
+          if (passes(v[i])) list[at + lanes_before(mask)] = rank_key(order_of(v[i]), (uint32_t)p.index(i));
+          at += __popcll(mask);
+        }
+      }
     };
     gather([&](float y) { return y >= bound; }, &listed[0]);
     __syncthreads();
     int count = listed[0];
     bool found = count <= kListed && !special;
     if (!found && !special) {
+      const uint32_t exact = reached_by(order_of(most), top, 32);
+      if (lane == 0) bounds[wave] = exact;
+      __syncthreads();
+      bound = row_bound();
       int pass = 0, all, before = 0;
 #pragma unroll
       for (int i = 0; i < E; ++i) pass += v[i] == bound;
