@@ -133,7 +133,8 @@ struct Piece {
     const int p = place(i / V), k = index(i);
     return k >= p && k < min(p + V, n);
   }
-  __device__ __forceinline__ bool inside() const { return first >= off && first + kSize - off <= n; }
+  // Element of lane 0 that the wavefront's j-th packs begin with: below 0, they begin ahead of the row; n or above, they lie behind it.
+  __device__ __forceinline__ int from(int j) const { return first + j * kWave * V - off; }
   __device__ __forceinline__ void load(const T* row, int first_, int off_, int n_) {
     first = first_, off = off_, n = n_;
     if (n >= V) {
@@ -144,17 +145,35 @@ struct Piece {
       for (int i = 0; i < E; ++i) raw[i / V][i % V] = mine(i) ? row[index(i)] : (T)-INFINITY;
     }
   }
-  // Elements that are not the lane's become masked ones.
-  __device__ __forceinline__ void unpack(float (&x)[E]) const {
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = to_f32(raw[i / V][i % V]);
-    if (inside()) return;
+  // Elements that are not the lane's become masked ones, where they lie. Of a row's packs one wavefront's first and one's last are mixed.
+  __device__ __forceinline__ void mask() {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int low = place(j) - begin(j), high = min(low + V, n - begin(j));   // of the pack's elements, the lane's
+      if (from(j) >= 0 && from(j) + kWave * V <= n) continue;
+      if (from(j) >= n) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) x[j * V + e] = e >= low && e < high ? x[j * V + e] : -INFINITY;
+        for (int e = 0; e < V; ++e) raw[j][e] = (T)-INFINITY;
+      } else {
+        raw[j] = masked(raw[j], j);
+      }
     }
+  }
+  __device__ __forceinline__ pack masked(pack v, int j) const {
+    const int low = place(j) - begin(j), high = min(low + V, n - begin(j));   // of the pack's elements, the lane's
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = e >= low && e < high ? v[e] : (T)-INFINITY;
+    return v;
+  }
+  __device__ __forceinline__ void unpack(float (&x)[E]) {
+    mask();
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = to_f32(raw[i / V][i % V]);
+  }
+  // Pack j alone, read again (rows of a pack at least).
+  __device__ __forceinline__ void values(const T* row, int j, float (&x)[V]) const {
+    const pack v = masked(*(const pack*)(row + begin(j)), j);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = to_f32(v[e]);
   }
 };
 
@@ -389,7 +408,7 @@ __device__ __forceinline__ uint64_t top_of_list(uint64_t* list, int count, int t
   if (count <= kWave) return in_order(list, count, top, buffer);
   uint64_t best = 0;
   for (int i = lane; i < count; i += kWave) best = max(best, list[i]);
-  const uint32_t bound = reached_by((uint32_t)(best >> 32), top, 32);
+  const uint32_t bound = reached_by((uint32_t)(best >> 32), top, kBoundBits);
   int pass = 0, all;
   for (int i = lane; i < count; i += kWave) pass += (uint32_t)(list[i] >> 32) >= bound;
   int at = count_before(pass, &all);
@@ -441,24 +460,34 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
     float bound = row_bound();
     a = wave_join(lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
     const bool special = a.s != a.s;
-    auto gather = [&](auto passes, int* counter) {   // counts all, writes what the list holds
-      int all = 0, from = 0;
+    // Which logits reach the bound, a bit each: the sign of their distance, shifted in. There are few, and their values are read again.
+    constexpr int kBits = E < 32 ? E : 32, kWords = E / kBits;
+    uint32_t hits[kWords];
+    int pass = 0, all, at;
 #pragma unroll
-      for (int i = 0; i < E; ++i) all += __popcll(__ballot(passes(v[i])));
-      if (!all) return;
-      if (lane == 0) from = atomicAdd(counter, all);
-      int at = __builtin_amdgcn_readfirstlane(from);
-      if (at + all > kListed) return;
+    for (int w = 0; w < kWords; ++w) {
+      uint32_t below = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const uint64_t mask = __ballot(passes(v[i]));
-        if (mask) {
-          if (passes(v[i])) list[at + lanes_before(mask)] = rank_key(order_of(v[i]), (uint32_t)p.index(i));
-          at += __popcll(mask);
-        }
+      for (int i = 0; i < kBits; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[w * kBits + i] - bound), 31);
+      hits[w] = ~below << (32 - kBits);   // logit i of the word is bit 31 - i
+      pass += __popc(hits[w]);
+    }
+    at = count_before(pass, &all);
+    if (all) {
+      int begin = 0;
+      if (lane == 0) begin = atomicAdd(&listed[0], all);
+      begin = __builtin_amdgcn_readfirstlane(begin);
+      if (begin + all <= kListed) {
+        at += begin;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+          while (hits[w]) {
+            const int bit = __clz(hits[w]), k = p.index(w * kBits + bit);
+            hits[w] &= ~(0x80000000u >> bit);
+            list[at++] = rank_key(order_of(to_f32(row[k])), (uint32_t)k);
+          }
       }
-    };
-    gather([&](float y) { return y >= bound; }, &listed[0]);
+    }
     __syncthreads();
     int count = listed[0];
     bool found = count <= kListed && !special;
@@ -467,36 +496,56 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
       if (lane == 0) bounds[wave] = exact;
       __syncthreads();
       bound = row_bound();
-      int pass = 0, all, before = 0;
+      float y[P::V];
+      int above = 0, equal = 0, begin = 0;
+      for (int j = 0; j < P::N; ++j) {
+        p.values(row, j, y);
 #pragma unroll
-      for (int i = 0; i < E; ++i) pass += v[i] == bound;
-      count_before(pass, &all);
-      if (lane == 0) equals[wave] = all;
-      gather([&](float y) { return y > bound; }, &listed[1]);
+        for (int e = 0; e < P::V; ++e) {
+          above += __popcll(__ballot(y[e] > bound));
+          equal += __popcll(__ballot(y[e] == bound));
+        }
+      }
+      if (lane == 0) {
+        equals[wave] = equal;
+        begin = atomicAdd(&listed[1], above);
+      }
+      begin = __builtin_amdgcn_readfirstlane(begin);
+      if (begin + above <= kListed)
+        for (int j = 0; j < P::N; ++j) {
+          p.values(row, j, y);
+#pragma unroll
+          for (int e = 0; e < P::V; ++e) {
+            const uint64_t mask = __ballot(y[e] > bound);
+            if (y[e] > bound) list[begin + lanes_before(mask)] = rank_key(order_of(y[e]), (uint32_t)p.index(j * P::V + e));
+            begin += __popcll(mask);
+          }
+        }
       __syncthreads();
       count = listed[1];
-      const int wanted = max(top - count, 0);
       found = count <= kListed;
-      for (int w = 0; w < wave; ++w) before += equals[w];
-      if (found && before < wanted) {
-#pragma unroll
-        for (int j = 0; j < P::N; ++j) {   // in the order of the indices: packs, lanes, elements
+      const int wanted = max(top - count, 0);
+      int before = 0, have = 0;   // fewer than wanted where the bound keeps out masked logits
+      for (int w = 0; w < waves; ++w) {
+        before += w < wave ? equals[w] : 0;
+        have += equals[w];
+      }
+      if (found)
+        for (int j = 0; j < P::N && before < wanted; ++j) {   // in the order of the indices: packs, lanes, elements
+          p.values(row, j, y);
           pass = 0;
 #pragma unroll
-          for (int i = j * P::V; i < (j + 1) * P::V; ++i) pass += v[i] == bound;
-          int at = before + count_before(pass, &all);
+          for (int e = 0; e < P::V; ++e) pass += y[e] == bound;
+          at = before + count_before(pass, &all);
           before += all;
 #pragma unroll
-          for (int i = j * P::V; i < (j + 1) * P::V; ++i)
-            if (v[i] == bound) {
-              if (at < wanted) list[count + at] = rank_key(order_of(v[i]), (uint32_t)p.index(i));
+          for (int e = 0; e < P::V; ++e)
+            if (y[e] == bound) {
+              if (at < wanted) list[count + at] = rank_key(order_of(y[e]), (uint32_t)p.index(j * P::V + e));
               ++at;
             }
         }
-      }
       __syncthreads();
-      int have = 0;   // fewer than wanted where the bound keeps out masked logits
-      for (int w = 0; w < waves; ++w) have += equals[w];
       count += min(wanted, have);
     }
     uint64_t key = 0;
