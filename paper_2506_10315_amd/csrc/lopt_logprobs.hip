@@ -27,8 +27,8 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 //   s = sum 2^t,   h = sum 2^t t,   t = x c - b in one fused operation
 // b's own rounding, m c - b = delta, is the same for every logit of the row and is taken out of ln S at the end, so that large logits lose nothing:
 //   ln S = ln s - delta ln 2,   entropy = ln s - ln 2 h / s
-// which is one vector instruction a logit less than x - m, then times c. b stays within 1e30; a row whose largest logit lies beyond (masks of the type's lowest value on the whole row) is gone through again by
-// extreme_row.
+// which is one vector instruction a logit less than x - m, then times c. b stays within 1e30; a row whose largest logit lies beyond (masks of the type's
+// lowest value on the whole row) is summed again by extreme_sums.
 // A masked logit has t = -infinity and 2^t = 0; for the product t is held to a finite value.
 struct Soft { float m, s, h; };
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
@@ -47,21 +47,34 @@ __device__ __forceinline__ Soft wave_join(Soft a, float c) {
   return Soft{a.m, wave_sum(a.s), wave_sum(a.h)};
 }
 
-// The sums of a whole row by differences from its largest logit m, which may be as large as the type allows: for the few rows beyond kMostBase.
+// Rows whose largest logit m is finite, but beyond kMostBase times 1 / c: summed again by differences from m, which may be as large as the type allows. `at`:
+// the first logit of this lane, `step` from one to the next.
+__device__ __forceinline__ bool beyond(float m, float c) { return fabsf(m * c) >= kMostBase && m != -INFINITY; }
 template <typename T>
-__device__ Soft extreme_row(const T* row, uint32_t n, float m, float c) {
+__device__ Soft extreme_sums(const T* row, uint32_t n, float m, float c, uint32_t at, uint32_t step) {
   Soft a{m, 0.f, 0.f};
-  for (uint32_t i = threadIdx.x & 63; i < n; i += 8 * kWave) {
+  for (uint32_t i = at; i < n; i += 8 * step) {
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = i + k * kWave < n ? to_f32(row[i + k * kWave]) : -INFINITY;
+    for (int k = 0; k < 8; ++k) v[k] = i + k * step < n ? to_f32(row[i + k * step]) : -INFINITY;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float t = i + k * kWave < n ? (v[k] - m) * c : -INFINITY, e = exp2_hw(t);
+      const float t = i + k * step < n ? (v[k] - m) * c : -INFINITY, e = exp2_hw(t);
       a.s += e;
       a.h += e * fmaxf(t, -FLT_MAX);
     }
   }
+  return Soft{m, wave_sum(a.s), wave_sum(a.h)};
+}
+// By the whole workgroup; `sums`: what the wavefronts have, free for this on entry.
+template <typename T>
+__device__ Soft extreme_block(const T* row, uint32_t n, float m, float c, Soft* sums) {
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const Soft own = extreme_sums(row, n, m, c, threadIdx.x, blockDim.x);
+  __syncthreads();
+  if (lane == 0) sums[threadIdx.x >> 6] = own;
+  __syncthreads();
+  const Soft a = lane < waves ? sums[lane] : Soft{m, 0.f, 0.f};
   return Soft{m, wave_sum(a.s), wave_sum(a.h)};
 }
 
@@ -84,13 +97,9 @@ __device__ __forceinline__ Target load_target(const T* row, const int64_t* targe
   return g;
 }
 
-// A row's outputs from its sums. Lane k of the wavefront holds the key of alternative k.
-template <typename T>
-__device__ __forceinline__ void write_row(const Outputs& o, int64_t r, const T* row, int lane, Soft a, float c, Target g, uint32_t vocab, float scale, int64_t ignore, int top,
-                                          uint64_t key) {
-  float delta = 0.f;
-  if (fabsf(a.m * c) < kMostBase) delta = __builtin_fmaf(a.m, c, -base_of(a.m, c));
-  else if (a.m != -INFINITY) a = extreme_row(row, vocab, a.m, c);
+// A row's outputs from its sums, which are by differences where `beyond` says so. Lane k of the wavefront holds the key of alternative k.
+__device__ __forceinline__ void write_row(const Outputs& o, int64_t r, int lane, Soft a, float c, Target g, uint32_t vocab, float scale, int64_t ignore, int top, uint64_t key) {
+  const float delta = fabsf(a.m * c) < kMostBase ? __builtin_fmaf(a.m, c, -base_of(a.m, c)) : 0.f;
   const bool empty = a.s == 0.f;
   const float ln_s = logf(a.s), log_s = ln_s - kLn2 * delta;
   if (lane == 0) {
@@ -361,7 +370,8 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_short(const T* __restrict__
     a = wave_join(a, c);
     uint64_t key = 0;
     if (TOP) key = piece_top(p, v, most, top, a.s != a.s, lists + wave * (E + 2) * top);
-    write_row(o, r, row, lane, a, c, g, vocab, scale, ignore, top, key);
+    if (beyond(a.m, c)) a = extreme_sums(row, vocab, a.m, c, lane, kWave);
+    write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
   }
 }
 
@@ -394,10 +404,11 @@ __global__ __launch_bounds__(1024) void k_logprobs(const T* __restrict__ x, int6
     a = wave_join(a, c);
     if (lane == 0) sums[wave] = a;
     __syncthreads();
-    if (wave == 0) {
-      a = wave_join(lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
-      write_row(o, r, row, lane, a, c, g, vocab, scale, ignore, 0, 0);
-    }
+    a = lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f};
+    const float most = wave_max(a.m);
+    if (beyond(most, c)) a = extreme_block(row, vocab, most, c, sums);
+    else if (wave == 0) a = wave_join(a, c);
+    if (wave == 0) write_row(o, r, lane, a, c, g, vocab, scale, ignore, 0, 0);
     if (r + gridDim.x < rows) __syncthreads();
   }
 }
@@ -563,10 +574,15 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
     } else {
       auto largest = [&](uint64_t below) {
         uint64_t best = 0;
-        for (uint32_t i = threadIdx.x; i < vocab; i += blockDim.x) {
-          const float y = to_f32(row[i]);
-          const uint64_t k = rank_key(y != y ? 0xfffffffeu : order_of(y), i);
-          if (k < below && k > best) best = k;
+        for (uint32_t i = threadIdx.x; i < vocab; i += 8 * blockDim.x) {
+          float y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = to_f32(row[min(i + j * blockDim.x, vocab - 1)]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {   // the last logit may come more than once
+            const uint64_t k = rank_key(y[j] != y[j] ? 0xfffffffeu : order_of(y[j]), min(i + j * blockDim.x, vocab - 1));
+            if (k < below && k > best) best = k;
+          }
         }
         return best;
       };
@@ -581,7 +597,8 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
         if (mine == best) mine = largest(best);
       }
     }
-    if (wave == 0) write_row(o, r, row, lane, a, c, g, vocab, scale, ignore, top, key);
+    if (beyond(a.m, c)) a = extreme_block(row, vocab, a.m, c, sums);
+    if (wave == 0) write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
     if (r + gridDim.x < rows) __syncthreads();
   }
 }
@@ -648,7 +665,8 @@ __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x
     }
     a = wave_join(a, c);
     if (last) {
-      write_row(o, r, x + r * ld, lane, a, c, g, vocab, scale, ignore, top, key);
+      if (beyond(a.m, c)) a = extreme_sums(x + r * ld, vocab, a.m, c, lane, kWave);
+      write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
     } else {
       if (lane < 3) part_out[3 * unit + lane] = lane == 0 ? a.m : lane == 1 ? a.s : a.h;
       if (lane < top) keys_out[unit * top + lane] = key;
