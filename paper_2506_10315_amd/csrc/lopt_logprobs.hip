@@ -434,8 +434,8 @@ __device__ __forceinline__ uint64_t top_of_list(uint64_t* list, int count, int t
 // puts them in order. Fewer than `top` logits that are not masked: all of them, then the masked ones of lowest index. More than the list holds (few
 // different values, masks of a low value): those above the bound, found to its last bit, then of its equals those of lowest index; a wavefront's
 // logits are neighbours in the row. What is left, rows with a NaN among it, takes the largest key `top` times from memory. Bound by vector issue and, for one
-// row, by one compute unit's: 1x50257 fp32 with 20 alternatives 16 us, 256x32000 bf16 with five 12.4, 1024x50257 bf16 with 20 72. One row spread over 13
-// workgroups that a second launch joins: 6.3 + 8.7 us, and a launch and a workspace more on the host (a call 23 us, so 17).
+// row, by one compute unit's: 1x50257 fp32 with 20 alternatives 10.1 us, 256x32000 bf16 with five 9.0, 1024x50257 bf16 with 20 49. One row spread over 13
+// workgroups that a second launch joins: 6.3 + 8.7 us, and a launch and a workspace more on the host.
 constexpr int kListed = 1024;
 template <typename T, int E>
 __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
@@ -472,15 +472,15 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
     a = wave_join(lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
     const bool special = a.s != a.s;
     // Which logits reach the bound, a bit each: the sign of their distance, shifted in. There are few, and their values are read again.
-    constexpr int kBits = E < 32 ? E : 32, kWords = E / kBits;
+    constexpr int kWords = E / 32;
     uint32_t hits[kWords];
     int pass = 0, all, at;
 #pragma unroll
     for (int w = 0; w < kWords; ++w) {
       uint32_t below = 0;
 #pragma unroll
-      for (int i = 0; i < kBits; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[w * kBits + i] - bound), 31);
-      hits[w] = ~below << (32 - kBits);   // logit i of the word is bit 31 - i
+      for (int i = 0; i < 32; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[w * 32 + i] - bound), 31);
+      hits[w] = ~below;   // logit i of the word is bit 31 - i
       pass += __popc(hits[w]);
     }
     at = count_before(pass, &all);
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
           while (hits[w]) {
-            const int bit = __clz(hits[w]), k = p.index(w * kBits + bit);
+            const int bit = __clz(hits[w]), k = p.index(w * 32 + bit);
             hits[w] &= ~(0x80000000u >> bit);
             list[at++] = rank_key(order_of(to_f32(row[k])), (uint32_t)k);
           }
@@ -694,10 +694,10 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
   const int64_t n = vocab + 7;   // a row counted from its pack
   if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, 0, 0};
   if (top) {
-    // A wavefront's search costs about what 20 logits a lane do, whatever it holds; more wavefronts are done sooner. us with 16 / 32 / 64 logits a lane, bf16:
-    // 1x3000 5.1 / 6.0 / 7.9, 1024x8000 16.9 / 14.6 / 14.7, 1x16000 9.2 / 6.6 / 8.2, 1024x16000 30 / 20 / 18 (fp32 31 / 22 / 26), 256x32000 - / 11.8 / 11.9 (fp32
-    // 12.7 / 17.5), 1024x32000 - / 43 / 32.
-    const int lane = n <= 8 * 1024 ? 16 : n <= 16 * 1024 || (n <= 32 * 1024 && rows <= 256) ? 32 : 64;
+    // Fewer logits a lane are done sooner by a row alone, more cost less where rows queue for the units. us with 16 / 32 / 64 logits a lane: 1x3000 bf16
+    // 4.3 / 4.4 / 5.0, 256x8000 6.9 / 7.3 / 7.8, 1024x8000 13.1 / 10.4 / 10.0, 1x16000 8.0 / 6.5 / 6.5, 256x16000 9.1 / 7.3 / 8.5, 1024x16000 25 / 16.3 / 14.1
+    // (fp32 26 / 20.6 / 17.3), 1x32000 - / 8.6 / 7.7, 256x32000 - / 9.2 / 8.3 (fp32 - / 10.7 / 10.6), 1024x32000 - / 29 / 24 (fp32 - / 37 / 30).
+    const int lane = n <= 8 * 1024 || (n <= 16 * 1024 && rows <= 256) ? 32 : 64;
     if (n <= 64 * 1024) return RowPlan{kRowBlock, lane, (int)((n + lane * kWave - 1) / (lane * kWave)), 0, 0};
     return RowPlan{kRowSplit, 32, 4, 1, (n + 2047) / 2048};
   }
@@ -839,7 +839,7 @@ lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* t
             hipLaunchKernelGGL(kernel, dim3(blocks), block, plan.waves * (E + 2) * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
             return;
           }
-        if constexpr (E >= 16)
+        if constexpr (E >= 32)
           if (top) {
             hipLaunchKernelGGL((k_logprobs_top<T, E>), dim3(blocks), block, 0, stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
             return;
