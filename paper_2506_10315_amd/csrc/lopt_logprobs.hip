@@ -12,10 +12,11 @@ namespace {
 
 // The order of the alternatives as one number: larger logit first, NaN above all, +0 and -0 alike, lower index first among equals.
 // No element's number is 0 or all ones.
-__device__ __forceinline__ uint32_t order_of(float x) {   // NaN: see piece_top
+__device__ __forceinline__ uint32_t order_of(float x) {   // but for NaN
   const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ uint32_t full_order(float x) { return x != x ? 0xfffffffeu : order_of(x); }
 __device__ __forceinline__ uint64_t rank_key(uint32_t order, uint32_t index) { return (uint64_t)order << 32 | (0xffffffffu - index); }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 __device__ __forceinline__ float key_value(uint64_t key) {
@@ -220,11 +221,10 @@ constexpr int kBoundBits = 16;   // of a bound that may be low: sign, exponent, 
 __device__ __forceinline__ int lanes_before(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
-// Sum of the lanes' n (at most 127) before this one; `all`: of all lanes.
+// Sum of the lanes' n before this one, bit by bit (few are large); `all`: of all lanes.
 __device__ __forceinline__ int count_before(int n, int* all) {
   int before = 0, sum = 0;
-#pragma unroll
-  for (int b = 0; b < 7; ++b) {
+  for (int b = 0; __ballot(n >> b); ++b) {
     const uint64_t mask = __ballot(n >> b & 1);
     before += lanes_before(mask) << b;
     sum += __popcll(mask) << b;
@@ -264,23 +264,72 @@ __device__ __forceinline__ uint64_t in_order(const uint64_t* list, int count, in
   return out;
 }
 
-// The `top` largest keys of a piece in order; `most` is the largest of the lane's logits. At least `top` lanes' maxima reach `bound`, so nothing below it
-// counts. Where the list does not hold what reaches it, or masked logits do, the bound is found to its last bit: what lies above it belongs to fewer than `top`
-// lanes, and of its equals, which may be many (masks, few different values), only the `top` of lowest index are taken.
-// `list`: room for (E + 2) top keys. `special`: there may be a NaN.
+// The `top` largest keys of a piece in order, whatever its logits. At least `top` lanes' maxima reach a bound, which is found to its last bit: what lies above it
+// belongs to fewer than `top` lanes, and of its equals, which may be many (masks, few different values), only the `top` of lowest index are taken. The
+// values are read again, so that they take no registers. `list`: room for (E + 2) top keys.
 template <typename T, int E>
-__device__ __forceinline__ uint64_t piece_top(const Piece<T, E>& p, const float (&x)[E], float most, int top, bool special, uint64_t* list) {
+__device__ __forceinline__ uint64_t exact_top(const T* row, const Piece<T, E>& p, int top, uint64_t* list) {
   typedef Piece<T, E> P;
-  const int room = E * top;
-  int pass = 0, count, at;
-  if (!special) {
-    const uint32_t reached = reached_by(order_of(most), top, kBoundBits);
+  uint32_t ord[P::V], most = 0;   // 0: not an element
+  auto read = [&](int j) {
+    float y[P::V];
+    if (p.n >= P::V) p.values(row, j, y);
+#pragma unroll
+    for (int e = 0; e < P::V; ++e) {
+      const int i = j * P::V + e;
+      if (p.n < P::V) y[e] = to_f32(row[min(p.index(i), p.n - 1)]);
+      ord[e] = p.mine(i) ? full_order(y[e]) : 0;
+    }
+  };
+#pragma unroll 1
+  for (int j = 0; j < P::N; ++j) {
+    read(j);
+#pragma unroll
+    for (int e = 0; e < P::V; ++e) most = max(most, ord[e]);
+  }
+  const uint32_t bound = max(reached_by(most, top, 32), 1u);
+  int count = 0, taken = 0;
+#pragma unroll 1
+  for (int j = 0; j < P::N; ++j) {
+    read(j);
+#pragma unroll
+    for (int e = 0; e < P::V; ++e) {
+      const uint64_t mask = __ballot(ord[e] > bound);
+      if (ord[e] > bound) list[count + lanes_before(mask)] = rank_key(ord[e], (uint32_t)p.index(j * P::V + e));
+      count += __popcll(mask);
+    }
+  }
+#pragma unroll 1
+  for (int j = 0; j < P::N && taken < top; ++j) {   // in the order of the indices: packs, lanes, elements
+    read(j);
+    int pass = 0, all;
+#pragma unroll
+    for (int e = 0; e < P::V; ++e) pass += ord[e] == bound;
+    int at = taken + count_before(pass, &all);
+#pragma unroll
+    for (int e = 0; e < P::V; ++e)
+      if (ord[e] == bound) {
+        if (at < top) list[count + at] = rank_key(bound, (uint32_t)p.index(j * P::V + e));
+        ++at;
+      }
+    taken += all;
+  }
+  count += min(taken, top);
+  wave_sync();
+  return in_order(list, count, top, list + (E + 1) * top);
+}
+
+// The same from its values x, whose largest in the lane is `most`, by way of what reaches a bound that may be a little low; by exact_top where the list
+// does not hold that, or masked logits are among it. `special`: there may be a NaN.
+template <typename T, int E>
+__device__ __forceinline__ uint64_t piece_top(const T* row, const Piece<T, E>& p, const float (&x)[E], float most, int top, bool special, uint64_t* list) {
+  const uint32_t reached = reached_by(order_of(most), top, kBoundBits);
+  if (!special && reached > order_of(-INFINITY)) {   // no masked logit reaches it, nor one that is not this lane's
     const float bound = key_value((uint64_t)reached << 32);
-    count = 0;
+    int count = 0, at = 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) count += __popcll(__ballot(x[i] >= bound));
-    if (count <= room && reached > order_of(-INFINITY)) {   // no masked logit among them, nor one that is not this lane's
-      at = 0;
+    if (count <= E * top) {
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const uint64_t mask = __ballot(x[i] >= bound);
@@ -293,40 +342,7 @@ __device__ __forceinline__ uint64_t piece_top(const Piece<T, E>& p, const float 
       return in_order(list, count, top, list + (E + 1) * top);
     }
   }
-  uint32_t ord[E], hi = 0;   // 0: not an element
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    ord[i] = x[i] != x[i] ? 0xfffffffeu : order_of(x[i]);
-    ord[i] = p.mine(i) ? ord[i] : 0;
-    hi = max(hi, ord[i]);
-  }
-  const uint32_t bound = max(reached_by(hi, top, 32), 1u);
-  pass = 0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) pass += ord[i] > bound;
-  at = count_before(pass, &count);
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (ord[i] > bound) list[at++] = rank_key(ord[i], (uint32_t)p.index(i));
-  int taken = 0;
-#pragma unroll
-  for (int j = 0; j < P::N; ++j) {   // in the order of the indices: packs, lanes, elements
-    pass = 0;
-#pragma unroll
-    for (int i = j * P::V; i < (j + 1) * P::V; ++i) pass += ord[i] == bound;
-    int all;
-    at = taken + count_before(pass, &all);
-#pragma unroll
-    for (int i = j * P::V; i < (j + 1) * P::V; ++i)
-      if (ord[i] == bound) {
-        if (at < top) list[count + at] = rank_key(ord[i], (uint32_t)p.index(i));
-        ++at;
-      }
-    taken += all;
-  }
-  count += min(taken, top);
-  wave_sync();
-  return in_order(list, count, top, list + (E + 1) * top);
+  return exact_top(row, p, top, list);
 }
 
 // The `top` largest of `count` lists of `top` ordered keys each, in order: a bound as in piece_top. `buffer`: room for count top keys. The
@@ -369,7 +385,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_short(const T* __restrict__
     add_piece(a, v, most, c);
     a = wave_join(a, c);
     uint64_t key = 0;
-    if (TOP) key = piece_top(p, v, most, top, a.s != a.s, lists + wave * (E + 2) * top);
+    if (TOP) key = piece_top(row, p, v, most, top, a.s != a.s, lists + wave * (E + 2) * top);
     if (beyond(a.m, c)) a = extreme_sums(row, vocab, a.m, c, lane, kWave);
     write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
   }
@@ -434,7 +450,7 @@ __device__ __forceinline__ uint64_t top_of_list(uint64_t* list, int count, int t
 // puts them in order. Fewer than `top` logits that are not masked: all of them, then the masked ones of lowest index. More than the list holds (few
 // different values, masks of a low value): those above the bound, found to its last bit, then of its equals those of lowest index; a wavefront's
 // logits are neighbours in the row. What is left, rows with a NaN among it, takes the largest key `top` times from memory. Bound by vector issue and, for one
-// row, by one compute unit's: 1x50257 fp32 with 20 alternatives 10.1 us, 256x32000 bf16 with five 9.0, 1024x50257 bf16 with 20 49. One row spread over 13
+// row, by one compute unit's: 1x50257 fp32 with 20 alternatives 10.1 us, 256x32000 bf16 with five 8.5, 1024x32000 bf16 with 20 24. One row spread over 13
 // workgroups that a second launch joins: 6.3 + 8.7 us, and a launch and a workspace more on the host.
 constexpr int kListed = 1024;
 template <typename T, int E>
@@ -580,7 +596,7 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
           for (int j = 0; j < 8; ++j) y[j] = to_f32(row[min(i + j * blockDim.x, vocab - 1)]);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {   // the last logit may come more than once
-            const uint64_t k = rank_key(y[j] != y[j] ? 0xfffffffeu : order_of(y[j]), min(i + j * blockDim.x, vocab - 1));
+            const uint64_t k = rank_key(full_order(y[j]), min(i + j * blockDim.x, vocab - 1));
             if (k < below && k > best) best = k;
           }
         }
@@ -598,6 +614,142 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
       }
     }
     if (beyond(a.m, c)) a = extreme_block(row, vocab, a.m, c, sums);
+    if (wave == 0) write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
+    if (r + gridDim.x < rows) __syncthreads();
+  }
+}
+
+// The same for many long rows: as k_logprobs, and every wavefront lists the logits that may be among its `top` largest by their index: those that reach what
+// `top` lanes' maxima of its pieces so far do (found again after 1, 2, 4, 8, ... pieces), later on without what only equals it, for `top` others come before
+// that. A full list keeps what `top` of its lanes reach; a
+// piece with more of them than the list has room for, with masked logits to take or with a NaN goes through exact_top. Bound by vector issue and by the search's chain of dependent steps: 1024x50257 bf16 with
+// 20 alternatives 34 us (20.6 without any), of lowest values but for seven 38, 1024x131000 70; the bound found again with every piece that has hits 36.5, values
+// read again as they are listed 37.6.
+constexpr int kKept = 128;
+template <int E>
+__host__ __device__ constexpr int many_scratch(int top) { return (E + 2) * top > 2 * kKept ? (E + 2) * top : 2 * kKept; }   // keys a wavefront
+template <typename T, int E>
+__global__ __launch_bounds__(512) void k_logprobs_many(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
+                                                       int64_t ignore, int top, Outputs o) {
+  typedef Piece<T, E> P;
+  __shared__ Soft sums[8];
+  __shared__ uint32_t bounds[8], lists[8][kKept];
+  __shared__ int listed;
+  extern __shared__ uint64_t keys[];   // a wavefront's for exact_top, then the row's list and room to order it
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, step = waves * P::kSize;
+  uint64_t* const scratch = keys + wave * many_scratch<E>(top);
+  uint32_t* const kept = lists[wave];
+  const float c = fminf(scale * kLog2e, FLT_MAX);
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* row = x + r * ld;
+    const int off = pack_offset(row, vocab), end = (int)vocab + off;
+    P p;
+    p.load(row, wave * P::kSize, off, vocab);
+    Target g{};
+    if (wave == 0) g = load_target(row, targets, r, vocab);
+    if (threadIdx.x == 0) listed = 0;
+    Soft a{-INFINITY, 0.f, 0.f};
+    int count = 0;
+    uint32_t low = 0;   // order of the least logit that is wanted
+    float high = -INFINITY;
+    // The list's keys, two a lane, and what `top` lanes' reach.
+    uint64_t k0, k1;
+    auto kept_keys = [&] {
+      auto key = [&](int i) {
+        const uint32_t k = i < count ? kept[i] : 0u;
+        const float v = to_f32(row[k]);
+        return i < count ? rank_key(full_order(v), k) : 0;
+      };
+      k0 = key(lane), k1 = key(lane + kWave);
+      return reached_by((uint32_t)(max(k0, k1) >> 32), top, kBoundBits);
+    };
+    // Puts those that reach a bound to list + the number of all before them, which the caller's `add` gives.
+    auto put = [&](uint32_t bound, uint64_t* list, auto&& add) {
+      const bool b0 = k0 && (uint32_t)(k0 >> 32) >= bound, b1 = k1 && (uint32_t)(k1 >> 32) >= bound;
+      int all, at = count_before(b0 + b1, &all);
+      at += add(all);
+      if (b0) list[at++] = k0;
+      if (b1) list[at] = k1;
+      return all;
+    };
+    auto filter = [&] {
+      const uint32_t bound = kept_keys();
+      count = put(bound, scratch, [](int) { return 0; });
+      low = max(low, bound + 1);
+      wave_sync();
+      uint64_t key = lane < count ? scratch[lane] : 0;
+      if (count > kWave) {
+        key = in_order(scratch, count, top, scratch);
+        count = top;
+      }
+      if (lane < count) kept[lane] = key_index(key);
+      wave_sync();
+    };
+    for (int first = wave * P::kSize, turn = 0; first < end; first += step, ++turn) {
+      float v[E];
+      P next;
+      if (first + step < end) next.load(row, first + step, off, vocab);
+      p.unpack(v);
+      const float most = most_of(v);
+      add_piece(a, v, most, c);
+      high = fmaxf(high, most);
+      const bool special = __ballot(a.s != a.s) != 0;
+      if (special || low == 0 || __ballot(most >= key_value((uint64_t)low << 32))) {
+        uint32_t bound = low;
+        if ((turn & (turn - 1)) == 0) bound = max(low, reached_by(order_of(high), top, kBoundBits));
+        bool whole = special || bound <= order_of(-INFINITY);
+        if (!whole) {
+          const float least = key_value((uint64_t)bound << 32);
+          uint32_t below = 0;   // a bit each: the sign of the distance, shifted in
+#pragma unroll
+          for (int i = 0; i < E; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[i] - least), 31);
+          uint32_t hits = ~below << (32 - E);   // logit i is bit 31 - i
+          int more, at = count_before(__popc(hits), &more);
+          if (count + more > kKept && count) filter();
+          whole = count + more > kKept;
+          if (!whole) {
+            if (bound > low) low = bound + 1;
+            at += count;
+            count += more;
+            while (hits) {
+              const int i = __clz(hits);
+              hits &= ~(0x80000000u >> i);
+              kept[at++] = (uint32_t)p.index(i);
+            }
+            wave_sync();
+          }
+        }
+        if (whole) {
+          const uint64_t key = exact_top(row, p, top, scratch);
+          if (count > kKept - LOPT_TOP_MAX) filter();
+          if (key) kept[count + lane] = key_index(key);   // the first lanes'
+          wave_sync();
+          count += __popcll(__ballot(key != 0));
+          const uint64_t last = readlane(key, top - 1);
+          if (last) low = max(low, (uint32_t)(last >> 32) + 1);
+        }
+      }
+      p = next;
+    }
+    a = wave_join(a, c);
+    const uint32_t own = kept_keys();
+    if (lane == 0) {
+      sums[wave] = a;
+      bounds[wave] = own;
+    }
+    __syncthreads();
+    put(wave_max(lane < waves ? bounds[lane] : 0u), keys, [&](int all) {
+      int begin = 0;
+      if (lane == 0) begin = atomicAdd(&listed, all);
+      return __builtin_amdgcn_readfirstlane(begin);
+    });
+    a = lane < waves ? sums[lane] : Soft{-INFINITY, 0.f, 0.f};
+    const float most = wave_max(a.m);
+    __syncthreads();
+    uint64_t key = 0;
+    if (wave == 0) key = top_of_list(keys, listed, top, keys + waves * kKept);
+    if (beyond(most, c)) a = extreme_block(row, vocab, most, c, sums);
+    else if (wave == 0) a = wave_join(a, c);
     if (wave == 0) write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
     if (r + gridDim.x < rows) __syncthreads();
   }
@@ -628,7 +780,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_split(const T* __restrict__
         p.unpack(v);
         const float most = most_of(v);
         add_piece(a, v, most, c);
-        if (TOP) key = piece_top(p, v, most, top, __ballot(a.s != a.s) != 0, lists + wave * 34 * top);
+        if (TOP) key = piece_top(row, p, v, most, top, __ballot(a.s != a.s) != 0, lists + wave * 34 * top);
         p = next;
       }
       a = wave_join(a, c);
@@ -684,7 +836,7 @@ inline void with_lane(int lane, F&& f) {
 }
 
 // How rows are shared out. `lane`: logits a lane.
-enum RowForm { kRowWave, kRowBlock, kRowSplit };
+enum RowForm { kRowWave, kRowBlock, kRowMany, kRowSplit };
 struct RowPlan {
   RowForm form;
   int lane, waves;
@@ -698,6 +850,11 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
     // 4.3 / 4.4 / 5.0, 256x8000 6.9 / 7.3 / 7.8, 1024x8000 13.1 / 10.4 / 10.0, 1x16000 8.0 / 6.5 / 6.5, 256x16000 9.1 / 7.3 / 8.5, 1024x16000 25 / 16.3 / 14.1
     // (fp32 26 / 20.6 / 17.3), 1x32000 - / 8.6 / 7.7, 256x32000 - / 9.2 / 8.3 (fp32 - / 10.7 / 10.6), 1024x32000 - / 29 / 24 (fp32 - / 37 / 30).
     const int lane = n <= 8 * 1024 || (n <= 16 * 1024 && rows <= 256) ? 32 : 64;
+    // Many long rows, eight wavefronts a row down to one, as many as make 4096 in all. us of it and of the other two: 256x32000 bf16 11 / 8.6, 300x33000 16.7 /
+    // 16.0, 512x50257 22 / 26, 1024x50257 34 / 48 (fp32 40 / 56), 8192x50257 184 / 323, 1024x32000 26 / 24, 2048x32000 40 / 44, 2048x16000 25 / 23; 64x131000
+    // 23 / 14, 128x70000 fp32 20 / 25, 128x131000 28 / 31, 1024x131000 70 / 153. 1024x50257 with 8 / 4 / 2: 39 / 34 / 40.
+    if (n > 32 * 1024 ? rows > (n > 64 * 1024 ? 127 : 256) : n > 16 * 1024 && rows >= 2048)
+      return RowPlan{kRowMany, 16, (int)std::clamp<int64_t>(4096 / rows, 1, 8), 0, 0};
     if (n <= 64 * 1024) return RowPlan{kRowBlock, lane, (int)((n + lane * kWave - 1) / (lane * kWave)), 0, 0};
     return RowPlan{kRowSplit, 32, 4, 1, (n + 2047) / 2048};
   }
@@ -837,6 +994,12 @@ lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* t
           if (plan.form == kRowWave) {
             auto kernel = top ? k_logprobs_short<T, true, E> : k_logprobs_short<T, false, E>;
             hipLaunchKernelGGL(kernel, dim3(blocks), block, plan.waves * (E + 2) * top * sizeof(uint64_t), stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
+            return;
+          }
+        if constexpr (E == 16)
+          if (plan.form == kRowMany) {
+            const size_t lds = plan.waves * many_scratch<E>((int)top) * sizeof(uint64_t);
+            hipLaunchKernelGGL((k_logprobs_many<T, E>), dim3(blocks), block, lds, stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
             return;
           }
         if constexpr (E >= 32)

@@ -522,6 +522,25 @@ def test_token_logprobs_ties_and_orders(vocab):
                 check_logp(np.stack([row, row[::-1]]), kind, np.array([777, 3]), scale, 32, what=f"{name} {kind}")
 
 
+@pytest.mark.parametrize("rows,vocab,kind,top", [(300, 33001, "bf16", 20), (130, 66003, "fp32", 32), (513, 32777, "fp16", 1), (2049, 16403, "bf16", 5), (130, 65537, "bf16", 32)])
+def test_token_logprobs_many_long_rows(rows, vocab, kind, top):
+    """Rows whose alternatives come early, late, everywhere or nowhere, between ordinary ones."""
+    x, t = logits_case(rows, vocab, rows + vocab)
+    at = np.arange(vocab)
+    low = -3.3895314e38 if kind != "fp16" else -65504.0
+    special = [np.zeros(vocab), at / 512.0, -at / 512.0, at % 3.0, np.maximum(at - vocab + 30.0, 0), np.where(at % 512 == 8, at / 1024.0, -np.inf), np.where(at % 7 == 3, -low, 0.0),
+               np.where(at % 2, 0.0, -0.0), np.where(at >= vocab - 40, 1.0, 0.0), np.full(vocab, low), np.where(at == 777, 0.5, -np.inf), np.full(vocab, -np.inf),
+               np.where(at % 5 == 1, at % 11, low), np.where(at < vocab - 7, low, 1.0), np.where(at < 7, 1.0, low), np.where(at < vocab - 3, -np.inf, 1.0), np.full(vocab, np.nan),
+               np.where(at == vocab - 1, np.nan, x[0]), np.where(at == 5000, np.inf, x[1]), np.where(at < 12000, -np.inf, x[2]), np.where(at % 4096 < 2000, x[3], -np.inf),
+               np.repeat(at[:(vocab + 99) // 100], 100)[:vocab] / 16.0]
+    for i, row in enumerate(special):
+        x[5 * i] = row
+    t[7], t[8] = -100, vocab
+    check_logp(x, kind, t, 1.0, top)
+    x, t = logits_case(rows, vocab, rows * vocab, masked=0.6)
+    check_logp(x, kind, t, 0.5, top)
+
+
 @pytest.mark.parametrize("rows,vocab", [(4, 100), (3, 3000), (300, 5000), (2, 140000)])
 def test_token_logprobs_of_large_logits(rows, vocab):
     """A common offset costs nothing beyond the logits' own rounding; the largest and smallest that the types hold stay right."""
