@@ -621,10 +621,9 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
 
 // The same for many long rows: as k_logprobs, and every wavefront lists the logits that may be among its `top` largest by their index: those that reach what
 // `top` lanes' maxima of its pieces so far do (found again after 1, 2, 4, 8, ... pieces), later on without what only equals it, for `top` others come before
-// that. A full list keeps what `top` of its lanes reach; a
-// piece with more of them than the list has room for, with masked logits to take or with a NaN goes through exact_top. Bound by vector issue and by the search's chain of dependent steps: 1024x50257 bf16 with
-// 20 alternatives 34 us (20.6 without any), of lowest values but for seven 38, 1024x131000 70; the bound found again with every piece that has hits 36.5, values
-// read again as they are listed 37.6.
+// that. A full list keeps what `top` of its lanes reach; a piece with more of them than the list has room for, with masked logits to take or with a NaN goes
+// through exact_top. Bound by vector issue and by the search's dependent steps: 1024x50257 bf16 with 20 alternatives 34 us (20.6 without any), all but
+// seven logits of the lowest value 38, 1024x131000 70. The bound found again with every piece that has hits: 36.5; and values read again as they are listed: 37.6.
 constexpr int kKept = 128;
 template <int E>
 __host__ __device__ constexpr int many_scratch(int top) { return (E + 2) * top > 2 * kKept ? (E + 2) * top : 2 * kKept; }   // keys a wavefront
@@ -876,7 +875,10 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
 // us, 16384x1000 bf16 22 -> 15), take kBackPacks packs of 16 bytes a lane of a row, counted as in the forward pass from the pack in which the
 // gradient's row begins, so that stores are aligned (4096x50257 bf16, odd rows at odd elements: 184 -> 174 us); a logit's row at
 // another offset is read unaligned. Packs that reach out of the row go element by element. Accesses are nontemporal: nothing is read again here, and
-// what both arrays would push out of the caches is (256x50257 bf16 15 -> 12 us, 4096x32000 104 -> 96). us of 4096x50257 bf16 with 1, 2, 4, 8 packs: 176, 162, 160, 168.
+// what both arrays would push out of the caches is (4096x50257 bf16 181 -> 172 us). Spans of a row are neighbours in the grid, so that what is in flight lies together:
+// 4096x50257 bf16 172 -> 146 us, fp32 334 -> 284, 4096x32000 100 -> 87. Which span comes first turns every 64 rows, for a short last one would meet
+// the same XCDs and units in every row (8000x10007 69 us with the rows as neighbours, 79 with the spans, 62 turned; 74 turned every eight rows). us of
+// 4096x50257 bf16 with 2, 4, 8 packs: 159, 148, 158.
 constexpr int kBackPacks = 4;
 template <typename T, bool ENTROPY, int G>
 __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld, const int64_t* __restrict__ targets, const float* __restrict__ stats,
@@ -885,7 +887,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
   typedef typename Pack<T>::type pack;
   constexpr int V = Pack<T>::n, kSpan = kBackPacks * G * V, kRows = kBlock / G;
   const int lane = threadIdx.x % G;
-  for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < rows; r += (int64_t)gridDim.x * kRows) {
+  for (int64_t r = (int64_t)blockIdx.y * kRows + threadIdx.x / G; r < rows; r += (int64_t)gridDim.y * kRows) {
     const T* row = x + r * ld;
     T* out = dx + r * ld_d;
     const float m = stats[2 * r], log_s = stats[2 * r + 1];
@@ -904,7 +906,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_back(const T* x, int64_t ld
       return empty ? 0.f * A : d;
     };
     const int off = (int)((uintptr_t)out / sizeof(T) % V);
-    for (int64_t first = (int64_t)blockIdx.y * kSpan; first < (int64_t)vocab + off; first += (int64_t)gridDim.y * kSpan) {
+    for (int64_t first = (int64_t)((blockIdx.x + blockIdx.y / 64) % gridDim.x) * kSpan; first < (int64_t)vocab + off; first += (int64_t)gridDim.x * kSpan) {
       const int begin = (int)first + lane * V - off;
       pack in[kBackPacks];
 #pragma unroll
@@ -1057,7 +1059,7 @@ lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const i
       constexpr int G = decltype(g)::value;
       // a rest of less than an eighth of a span goes to workgroups that have one (16384x8191 bf16 108 -> 96 us; rests of a quarter 18 -> 21)
       const int64_t spans = (packs + kBackPacks * G - kBackPacks * G / 8) / (kBackPacks * G);
-      const dim3 grid((unsigned)std::min<int64_t>((rows + kBlock / G - 1) / (kBlock / G), 1 << 20), (unsigned)std::clamp<int64_t>(spans, 1, 1024));
+      const dim3 grid((unsigned)std::clamp<int64_t>(spans, 1, 1024), (unsigned)std::min<int64_t>((rows + kBlock / G - 1) / (kBlock / G), 65535));
       auto kernel = dentropy ? k_logprobs_back<T, true, G> : k_logprobs_back<T, false, G>;
       hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)logits, ld, targets, stats, entropy, dlogp, dentropy, (T*)dlogits, ld_d,
                          rows, (int)vocab, scale, ignore_index);
