@@ -391,9 +391,9 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_short(const T* __restrict__
   }
 }
 
-// A workgroup a row, its wavefronts a piece each in turn; the first wavefront joins what they have. Bound by memory and, nearly as much, by vector issue (9.3
-// instructions for 64 logits, the power of two among them): 4096x50257 bf16 76.6 us, 5.4 TB/s with the vector units busy three quarters of the time;
-// 4096x32000 bf16 45 us, 5.9; 2048x50257 fp32 74 us, 5.5. One pass with separate segments and a second launch to join them took 94 us.
+// A workgroup a row, its wavefronts a piece each in turn; the first wavefront joins what they have. Bound by memory and, nearly as much, by vector issue (9.9
+// instructions for 64 logits, the power of two among them): 4096x50257 bf16 75 us, 5.5 TB/s with the vector units busy four fifths of the time;
+// 12000x32000 bf16 135 us, 5.7; 3000x50257 fp32 101 us, 5.9. One pass with separate segments and a second launch to join them took 94 us.
 template <typename T, int E>
 __global__ __launch_bounds__(1024) void k_logprobs(const T* __restrict__ x, int64_t ld, const int64_t* __restrict__ targets, int64_t rows, uint32_t vocab, float scale,
                                                    int64_t ignore, Outputs o) {
@@ -858,12 +858,12 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab, uint32_t top) {
     return RowPlan{kRowSplit, 32, 4, 1, (n + 2047) / 2048};
   }
   if (n <= 64 * 2048 || rows >= 256) {
-    // Wavefronts: one for about eight pieces up to four, and with fewer than 1024 rows as many as make 4096 in all, 16 a compute unit. us, pieces of 8 / 16
-    // / 32 logits a lane: 40000x2500 bf16 one wavefront 42 / 51 / 79; 16384x8191 one 49 / 50 / 59, two 48 / 52 / 66, four 53 / 57 / 78; 5200x32000 one 69 / 66 / 73, four
-    // 61 / 60 / 62; 4096x50257 one 100 / 86 / 84, four 82 / 77 / 79; 2048x50257 fp32 one 87 / 71 / 72, four 79 / 74 / 72.
-    const int lane = n <= 8 * 1024 + 7 ? 8 : 16;
-    const int64_t pieces = (vocab + lane * kWave - 1) / (lane * kWave), long_rows = std::clamp<int64_t>((pieces + 4) / 8, 1, 4);
-    return RowPlan{kRowBlock, lane, (int)std::max(long_rows, std::min<int64_t>({16, pieces, 4096 / rows})), 0, 0};
+    // Wavefronts: one for about five pieces up to four, eight for many rows of 32 pieces and more, whose wavefronts' accesses then lie closer together, and with
+    // fewer than 1024 rows as many as make 4096 in all, 16 a compute unit. us with 1 / 2 / 4 / 8: 20000x5000 bf16 43 / 44 / 54, 16384x8191 56 / 55 / 62 / 89,
+    // 8192x10007 37 / 36 / 37, 8192x16000 - / 54 / 52 / 58, 12000x32000 - / - / 135 / 135, 4096x50257 - / 88 / 77 / 75 (fp32 3000 rows 104 / 101), 2048x131000 - / - / 102 /
+    // 96, 1024x50257 - / 29 / 23 / 25. With pieces of 8 logits a lane: 20000x5000 46, 16384x8191 58, 4096x50257 84, 256x8000 3.9 (3.5); of 32: 16384x8191 66.
+    const int64_t pieces = (vocab + 1023) / 1024, long_rows = pieces >= 32 && rows >= 2048 ? 8 : std::clamp<int64_t>((pieces + 4) / 5, 1, 4);
+    return RowPlan{kRowBlock, 16, (int)std::max(long_rows, std::min<int64_t>({16, pieces, 4096 / rows})), 0, 0};
   }
   const int64_t pieces = (n + 2047) / 2048, per = std::clamp<int64_t>(rows * pieces / 16384, 1, 8);
   return RowPlan{kRowSplit, 32, 4, per, (pieces + per - 1) / per};
@@ -1009,7 +1009,7 @@ lopt_status lopt_token_logprobs(const void* logits, int64_t ld, const int64_t* t
             hipLaunchKernelGGL((k_logprobs_top<T, E>), dim3(blocks), block, 0, stream, x, ld, tg, rows, n, scale, ignore_index, (int)top, o);
             return;
           }
-        if constexpr (E <= 16) hipLaunchKernelGGL((k_logprobs<T, E>), dim3(blocks), block, 0, stream, x, ld, tg, rows, n, scale, ignore_index, o);
+        if constexpr (E == 16) hipLaunchKernelGGL((k_logprobs<T, E>), dim3(blocks), block, 0, stream, x, ld, tg, rows, n, scale, ignore_index, o);
       });
       return;
     }
