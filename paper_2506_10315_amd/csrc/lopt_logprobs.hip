@@ -23,20 +23,23 @@ __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t u = (uint32_t)(key >> 32);
   return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
+// What to subtract from a logit so that the sign says whether it lies below a bound: an infinite bound's difference from itself has none.
+__device__ __forceinline__ float least_of(float bound) { return fminf(bound, FLT_MAX); }
 
 // Running softmax sums of some logits x. With c = scale / ln 2, the hardware's 2^x, m = the largest of them and b = m c rounded:
 //   s = sum 2^t,   h = sum 2^t t,   t = x c - b in one fused operation
-// b's own rounding, m c - b = delta, is the same for every logit of the row and is taken out of ln S at the end, so that large logits lose nothing:
+// b's own rounding, m c - b = delta, is the same for every logit of the row and is taken out of ln S at the end:
 //   ln S = ln s - delta ln 2,   entropy = ln s - ln 2 h / s
-// which is one vector instruction a logit less than x - m, then times c. b stays within 1e30; a row whose largest logit lies beyond (masks of the type's
-// lowest value on the whole row) is summed again by extreme_sums.
+// which is one vector instruction a logit less than x - m, then times c. It adds delta to every exponent, so b is held within 2^24, where delta is half a unit
+// at most (at 1.44e10 it would be 440, and 2^t infinite). A lane or piece of logits below that (masks of -1e9 and less) adds 0; a row whose
+// largest logit lies outside is summed again by extreme_sums.
 // A masked logit has t = -infinity and 2^t = 0; for the product t is held to a finite value.
 struct Soft { float m, s, h; };
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-constexpr float kMostBase = 1e30f;
+constexpr float kMostBase = 16777216.f;
 
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
-__device__ __forceinline__ float base_of(float m, float c) { return fmaxf(m * c, -kMostBase); }
+__device__ __forceinline__ float base_of(float m, float c) { return __builtin_amdgcn_fmed3f(m * c, -kMostBase, kMostBase); }
 
 // a's sums seen from a larger m.
 __device__ __forceinline__ Soft rebase(Soft a, float m, float c) {
@@ -48,8 +51,8 @@ __device__ __forceinline__ Soft wave_join(Soft a, float c) {
   return Soft{a.m, wave_sum(a.s), wave_sum(a.h)};
 }
 
-// Rows whose largest logit m is finite, but beyond kMostBase times 1 / c: summed again by differences from m, which may be as large as the type allows. `at`:
-// the first logit of this lane, `step` from one to the next.
+// Rows whose largest logit m is beyond kMostBase times 1 / c: summed again by differences from m, which may be as large as the type allows (+infinity: its
+// difference from itself makes the sums NaN). `at`: the first logit of this lane, `step` from one to the next.
 __device__ __forceinline__ bool beyond(float m, float c) { return fabsf(m * c) >= kMostBase && m != -INFINITY; }
 template <typename T>
 __device__ Soft extreme_sums(const T* row, uint32_t n, float m, float c, uint32_t at, uint32_t step) {
@@ -489,13 +492,14 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
     const bool special = a.s != a.s;
     // Which logits reach the bound, a bit each: the sign of their distance, shifted in. There are few, and their values are read again.
     constexpr int kWords = E / 32;
+    const float least = least_of(bound);
     uint32_t hits[kWords];
     int pass = 0, all, at;
 #pragma unroll
     for (int w = 0; w < kWords; ++w) {
       uint32_t below = 0;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[w * 32 + i] - bound), 31);
+      for (int i = 0; i < 32; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[w * 32 + i] - least), 31);
       hits[w] = ~below;   // logit i of the word is bit 31 - i
       pass += __popc(hits[w]);
     }
@@ -698,7 +702,7 @@ __global__ __launch_bounds__(512) void k_logprobs_many(const T* __restrict__ x, 
         if ((turn & (turn - 1)) == 0) bound = max(low, reached_by(order_of(high), top, kBoundBits));
         bool whole = special || bound <= order_of(-INFINITY);
         if (!whole) {
-          const float least = key_value((uint64_t)bound << 32);
+          const float least = least_of(key_value((uint64_t)bound << 32));
           uint32_t below = 0;   // a bit each: the sign of the distance, shifted in
 #pragma unroll
           for (int i = 0; i < E; ++i) below = __builtin_amdgcn_alignbit(below, __builtin_bit_cast(uint32_t, v[i] - least), 31);

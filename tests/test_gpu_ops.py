@@ -555,6 +555,43 @@ def test_token_logprobs_of_large_logits(rows, vocab):
         check_logp(y, "fp32", t, 1.0, 4, what=f"{value}")
 
 
+def _finite_mask_rows(vocab, value, x):
+    """Rows of `x` (ordinary logits) with `value` < 0 in the place of a mask over single logits, lanes, pieces and all but one, rows of such values alone, and
+    rows whose largest logit is of that size."""
+    at = np.arange(vocab)
+    masks = [np.random.default_rng(vocab).random(vocab) < 0.5, at // 4 % 64 < 40, at // 8 % 64 < 40, at % 4096 < 2100, at != vocab // 3, at >= vocab // 2]
+    rows = [np.where(m, value, x[i]) for i, m in enumerate(masks)]
+    rows += [np.full(vocab, value), value * (1.0 + at % 5 / 64.0), np.where(at == vocab // 2, -value, x[6]), np.where(at % 3 == 1, -value, value)]
+    return rows
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab,top", [(70, 100, 5), (70, 900, 0), (70, 2000, 20), (70, 3000, 0), (70, 20000, 5), (300, 33001, 5), (70, 50257, 0), (70, 50257, 20),
+                                            (70, 70001, 5), (70, 140000, 0)])
+def test_token_logprobs_under_finite_masks(rows, vocab, top, kind):
+    """-1e9 to -1e29 as masks, and maxima of that size: every form of the pass, whole lanes and pieces of them."""
+    for scale in (1.0, 0.5, 10.0) if vocab < 30000 else (1.0, 10.0) if kind == "bf16" else (1.0,):
+        x, t = logits_case(rows, vocab, rows + vocab)
+        for i, value in enumerate((-1e9, -1e10, -1e12, -1e18, -1e20, -1e29)):
+            for j, row in enumerate(_finite_mask_rows(vocab, value, x)):
+                x[i + 6 * j] = row
+        check_logp(x, kind, t, scale, top, what=f"scale {scale}")
+
+
+@pytest.mark.parametrize("rows,vocab,top", [(8, 100, 5), (8, 3000, 0), (8, 20000, 5), (300, 5000, 0), (300, 33001, 5), (3, 70001, 5), (3, 140000, 0)])
+def test_token_logprobs_of_large_products(rows, vocab, top):
+    """Scales close to greedy, and products of scale and logit on both sides of where the sums' base may lie."""
+    x, t = logits_case(rows, vocab, vocab)
+    for kind in TYPES:
+        for scale in (1e4, 1e6, 1e9):
+            check_logp(x, kind, t, scale, top, what=f"{kind} scale {scale}")
+    steps = np.round(4 * x)
+    for offset in (11629080.0, -11629080.0, 5814540.0, 46516320.0, -46516320.0):   # products of 2^23, 2^24 and 2^26 with 1 / ln 2
+        check_logp(steps + np.float32(offset), "fp32", t, 1.0, top, what=f"offset {offset}")
+    for scale in (1e-6, 1e-5, 1e-4):
+        check_logp((1e13 + 1e6 * steps).astype(np.float32), "fp32", t, scale, top, what=f"offset 1e13 scale {scale}")
+
+
 def test_token_logprobs_special_rows_and_targets():
     import torch
     x, t = logits_case(12, 5000, 5)
