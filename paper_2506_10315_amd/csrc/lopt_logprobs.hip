@@ -579,16 +579,17 @@ __global__ __launch_bounds__(1024) void k_logprobs_top(const T* __restrict__ x, 
       __syncthreads();
       count += min(wanted, have);
     }
-    uint64_t key = 0;
+    uint64_t key = 0, masked = 0;
+    if (found && count < top) {   // at most 31 are not masked: the first 64 have to hold enough that are
+      masked = __ballot(lane < vocab && to_f32(row[min(lane, (int)vocab - 1)]) == -INFINITY);
+      found = __popcll(masked) >= top - count;
+    }
     if (found) {
       if (wave == 0) {
         key = count >= top ? top_of_list(list, count, top, buffer) : in_order(list, count, top, buffer);
-        if (count < top) {   // at most 31 are not masked: the first 64 hold enough that are
-          uint64_t masked = __ballot(lane < vocab && to_f32(row[min(lane, (int)vocab - 1)]) == -INFINITY);
-          if (lane >= count && lane < top) {
-            for (int k = count; k < lane; ++k) masked &= masked - 1;
-            key = rank_key(order_of(-INFINITY), __builtin_ctzll(masked));
-          }
+        if (lane >= count && lane < top) {
+          for (int k = count; k < lane; ++k) masked &= masked - 1;
+          key = rank_key(order_of(-INFINITY), __builtin_ctzll(masked));
         }
       }
     } else {

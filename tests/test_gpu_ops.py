@@ -592,6 +592,15 @@ def test_token_logprobs_of_large_products(rows, vocab, top):
         check_logp((1e13 + 1e6 * steps).astype(np.float32), "fp32", t, scale, top, what=f"offset 1e13 scale {scale}")
 
 
+@pytest.mark.parametrize("vocab", [3000, 20000, 50257])
+def test_token_logprobs_alternatives_are_in_the_vocabulary(vocab):
+    """Fewer than `top` positive logits, none of them masked, the others zeros of either sign."""
+    at = np.arange(vocab)
+    x = np.stack([np.where(at % 2, -0.0, -0.0), np.where(at == 17, 1.0, -0.0), np.where(at >= vocab - 3, at, -0.0), np.where(at < 3, 0.5, 0.0)])
+    for kind in TYPES:
+        check_logp(x, kind, np.zeros(4, dtype=np.int64), 1.0, 5, what=kind)
+
+
 def test_token_logprobs_special_rows_and_targets():
     import torch
     x, t = logits_case(12, 5000, 5)
