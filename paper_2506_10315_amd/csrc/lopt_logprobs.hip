@@ -23,8 +23,9 @@ __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t u = (uint32_t)(key >> 32);
   return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
-// What to subtract from a logit so that the sign says whether it lies below a bound: an infinite bound's difference from itself has none.
-__device__ __forceinline__ float least_of(float bound) { return fminf(bound, FLT_MAX); }
+// What to subtract from a logit so that the sign says whether it lies below a bound. Both zeros less -0 are +0, -0 less +0 would be -0; an infinite bound's
+// difference from itself has no sign.
+__device__ __forceinline__ float least_of(float bound) { return bound == 0.f ? -0.f : fminf(bound, FLT_MAX); }
 
 // Running softmax sums of some logits x. With c = scale / ln 2, the hardware's 2^x, m = the largest of them and b = m c rounded:
 //   s = sum 2^t,   h = sum 2^t t,   t = x c - b in one fused operation

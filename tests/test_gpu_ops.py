@@ -601,6 +601,41 @@ def test_token_logprobs_alternatives_are_in_the_vocabulary(vocab):
         check_logp(x, kind, np.zeros(4, dtype=np.int64), 1.0, 5, what=kind)
 
 
+def _zero_rows(vocab, seed):
+    """Rows whose best alternatives are zeros of either sign, few enough for a list of candidates."""
+    r = np.random.default_rng(seed)
+    below = lambda: -np.abs(r.standard_normal(vocab)) - 0.5
+    rows = [np.full(vocab, -0.0)]
+    for n in (1, 3, 20, 62, 100, 700):
+        for sign in (0, 1, 2):
+            row, at = below(), r.choice(vocab, min(n, vocab // 2), replace=False)
+            row[at] = -0.0 if sign == 0 else 0.0 if sign == 1 else np.where(np.arange(len(at)) % 2, 0.0, -0.0)
+            rows.append(row)
+    at = r.choice(vocab, 60, replace=False)
+    for positive, mask in ((1, -2.0), (4, -2.0), (19, -2.0), (31, -2.0), (4, -np.inf), (4, -60000.0), (0, -np.inf), (0, -60000.0)):
+        row = np.full(vocab, mask)
+        row[at[:positive]] = 1.0 + np.arange(positive)
+        row[at[positive:]] = -0.0              # the rest of the `top` best
+        rows.append(row)
+    few = np.full(vocab, -0.0)
+    few[at[:3]] = 0.0                          # ties with all of the others
+    some = np.full(vocab, -0.0)
+    some[at[:4]] = [3.0, 2.0, 1.0, 0.5]
+    tiny = np.full(vocab, -1e-39)
+    tiny[at[:9]] = -0.0
+    return rows + [few, some, tiny]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(32, 900), (32, 3000), (32, 20000), (300, 33001), (32, 50257), (32, 140000), (130, 66003)])
+def test_token_logprobs_alternatives_among_zeros_of_both_signs(rows, vocab, kind):
+    x, t = logits_case(rows, vocab, vocab)
+    for i, row in enumerate(_zero_rows(vocab, vocab)):
+        x[i] = row
+    for top in (5, 32) if vocab < 30000 else (20,):
+        check_logp(x, kind, t, 1.0, top, what=f"top {top}")
+
+
 def test_token_logprobs_special_rows_and_targets():
     import torch
     x, t = logits_case(12, 5000, 5)
