@@ -158,6 +158,8 @@ def _clip(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], 
     nbytes = L.lopt_clip_workspace(n, at[0])
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     _run(L.lopt_clip_grads, device.index, n, *at, max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
+    if out is not None:   # autograd has to see that they were written
+        torch.autograd.graph.increment_version(out)
     return norm
 
 

@@ -148,6 +148,23 @@ def test_clip_in_place(kind):
     assert params[-1].grad is None
 
 
+def test_clip_is_seen_by_autograd():
+    import torch
+    for clip in (lambda g: ops().clip_grads([g], 0.5, out=[g]), lambda g: ops().clip_grads([g.clone()], 0.5, out=[g]), lambda g: ops().clip_grad_norm_([_param(g)], 0.5)):
+        w, g = torch.ones(5, device="cuda:0", requires_grad=True), torch.full((5,), 2.0, device="cuda:0")
+        y = (w * g).sum()              # keeps g for its backward pass
+        before = g._version
+        clip(g)
+        assert g._version > before
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    g = torch.ones(3, device="cuda:0")
+    before = g._version
+    ops().grad_norm([g])
+    ops().clip_grads([g], 0.5)
+    assert g._version == before
+
+
 def test_clip_special_values():
     import torch
     f = lambda *v: torch.tensor(v, device="cuda:0")
