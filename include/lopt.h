@@ -253,7 +253,7 @@ const char* lopt_pass_name(int pass);
 
 /* ---- The rest of the training loop around lopt_step: from the last hidden state to the gradients and the loss value that
  * the step takes. These calls take no context and keep nothing between calls: every argument that is not marked _host is
- * DEVICE memory owned by the caller, every call may run on any host thread and any stream, allocates nothing and can be
+ * DEVICE memory owned by the caller, every call may run on any host thread and any stream, allocates nothing on the device and can be
  * captured into a HIP graph (with host arrays read while it is captured). They launch on the current device, to which
  * `hip_stream` has to belong. Arrays need the alignment of their elements only; `ld_*` are distances between rows in elements. A
  * workspace holds nothing that survives a call and needs no initial contents; 16-byte alignment. Inputs and outputs may not
@@ -267,10 +267,11 @@ typedef enum { LOPT_F32 = 0, LOPT_BF16 = 1, LOPT_F16 = 2 } lopt_type;
  * (the sum in 64 bits: no square overflows or vanishes). counts_host[n]: elements of each tensor, >= 0, in any number below 2^40;
  * grads_host[n], out_host[n]: device pointers (null where the count is 0); types_host[n], out_types_host[n]: lopt_type of each.
  * out_host null: the norm alone, nothing is scaled. out_host[i] may be grads_host[i] if its type is the same: gradients are
- * clipped in place, and nothing is written where c is 1. norm: one float, not null.
+ * clipped in place, and nothing is written where c is 1. No other memory may be shared between outputs, or between an output and a
+ * gradient: a tensor listed twice is not clipped in place. norm: one float, not null.
  * A norm that is NaN makes c and every output NaN; an infinite norm makes finite gradients 0 and infinite ones NaN.
  * max_norm >= 0; +infinity: c = 1 for any finite norm.
- * Errors: LOPT_EINVAL (null, type, alignment, max_norm, workspace too small), LOPT_ESHAPE (count), LOPT_EHIP. */
+ * Errors: LOPT_EINVAL (null, type, alignment, overlap, max_norm, workspace too small), LOPT_ESHAPE (count), LOPT_ENOMEM, LOPT_EHIP. */
 #define LOPT_CLIP_EPS 1e-6f
 size_t lopt_clip_workspace(size_t n, const int64_t* counts_host);
 lopt_status lopt_clip_grads(size_t n, const int64_t* counts_host, const void* const* grads_host,

@@ -3,6 +3,8 @@
 // nothing.
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "lopt_ops.h"
 
@@ -164,6 +166,32 @@ int grid_of(int64_t here, int64_t all) { return (int)std::min<int64_t>(here, std
 // with more than 0.75 * 2^30 chunks.
 size_t most_parts(size_t n, int64_t chunks) { return (size_t)std::min<int64_t>(chunks, kGrid + kLeast * ((int64_t)((n + kBatch - 1) / kBatch) + (chunks >> 29))); }
 
+// Workgroups read and write the tensors in no order: an output that shares memory with another one, or with a gradient that is not its own, would come
+// out differently from call to call. Lists whose outputs lie in ascending order, as in one flat buffer, are not sorted.
+lopt_status check_overlap(size_t n, const int64_t* counts, const void* const* grads, const uint32_t* types, void* const* out, const uint32_t* out_types) {
+  struct Span { uintptr_t begin, end; };
+  const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[n]);
+  if (!spans) return fail_call(LOPT_ENOMEM, "out of host memory");
+  size_t m = 0;
+  bool sorted = true;
+  for (size_t i = 0; i < n; ++i) {
+    if (counts[i] == 0) continue;
+    const uintptr_t begin = (uintptr_t)out[i];
+    sorted = sorted && (m == 0 || spans[m - 1].begin < begin);
+    spans[m++] = Span{begin, begin + (uintptr_t)counts[i] * type_bytes(out_types[i])};
+  }
+  if (!sorted) std::sort(spans.get(), spans.get() + m, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  for (size_t k = 1; k < m; ++k)
+    if (spans[k].begin < spans[k - 1].end) return fail_call(LOPT_EINVAL, "two outputs overlap");
+  for (size_t i = 0; i < n; ++i) {
+    if (counts[i] == 0 || out[i] == grads[i]) continue;
+    const uintptr_t begin = (uintptr_t)grads[i], end = begin + (uintptr_t)counts[i] * type_bytes(types[i]);
+    const Span* next = std::lower_bound(spans.get(), spans.get() + m, end, [](const Span& a, uintptr_t e) { return a.begin < e; });
+    if (next != spans.get() && next[-1].end > begin) return fail_call(LOPT_EINVAL, "tensor %zu: an output overlaps this gradient", i);
+  }
+  return LOPT_OK;
+}
+
 }  // namespace
 }  // namespace lopt
 
@@ -196,6 +224,7 @@ lopt_status lopt_clip_grads(size_t n, const int64_t* counts, const void* const* 
     if (out && out[i] == grads[i] && types[i] != out_types[i]) return fail_call(LOPT_EINVAL, "tensor %zu: in place, but of another type", i);
     chunks += chunks_of(counts[i]);
   }
+  if (n > 0 && out) LOPT_CHECK(check_overlap(n, counts, grads, types, out, out_types));
   LOPT_CHECK(check_workspace(workspace, workspace_bytes, std::max<size_t>(16, most_parts(n, chunks) * sizeof(double))));
   hipStream_t stream = (hipStream_t)hip_stream;
   double* part = (double*)workspace;

@@ -180,7 +180,7 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
 
 def clip_grad_norm_(parameters: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float) -> torch.Tensor:
     """Clips the `.grad` of the parameters in place and returns the norm before. Parameters without a gradient are
-    skipped."""
+    skipped; a gradient that is listed twice is refused."""
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
     grads = [p.grad for p in parameters if p.grad is not None]

@@ -165,6 +165,19 @@ def test_clip_is_seen_by_autograd():
     assert g._version == before
 
 
+def test_clip_refuses_a_gradient_listed_twice_in_place():
+    import torch
+    from paper_2506_10315_amd import LoptError
+    g, other = torch.full((5000,), 2.0, device="cuda:0"), torch.ones(3, device="cuda:0")
+    for call in (lambda: ops().clip_grad_norm_([_param(g), _param(other), _param(g)], 0.5), lambda: ops().clip_grads([g, g], 0.5, out=[g, g]),
+                 lambda: ops().clip_grads([g[:3000], g[2000:]], 0.5, out=[g[:3000], g[2000:]])):
+        with pytest.raises(LoptError, match="overlap"):
+            call()
+    assert bool((g == 2).all()) and bool((other == 1).all())
+    (a, b), n = ops().clip_grads([g, g], 0.5)      # into tensors of their own
+    assert float(n) == pytest.approx(200.0) and torch.equal(a, b) and float(a[7]) == pytest.approx(2 * 0.5 / 200.0)
+
+
 def test_clip_special_values():
     import torch
     f = lambda *v: torch.tensor(v, device="cuda:0")

@@ -50,6 +50,26 @@ def test_clip_refusals(L):
     assert L.lopt_clip_workspace(2, counts) >= 16 and L.lopt_clip_workspace(0, None) >= 16
 
 
+def test_clip_refuses_outputs_that_share_memory(L):
+    """Two workgroups would read and write the same elements, in no order."""
+    def clip(grads, out, counts=None, types=None, out_types=None, ws=None):
+        n = len(grads)
+        return _clip(L, counts=counts or (10,) * n, grads=grads, types=types or (0,) * n, out=out, out_types=out_types or (0,) * n, ws=ws)
+    for grads, out in (((P, P), (P, P)), ((P, P, 2 * P), (P, P, 2 * P)), ((2 * P, P, 2 * P), (2 * P, P, 2 * P)), ((P, 2 * P), (3 * P, 3 * P)),
+                       ((P, 2 * P), (3 * P, 3 * P + 36)), ((P, 2 * P), (3 * P + 36, 3 * P)), ((P, P + 36), (P, P + 36))):
+        _refused(L, clip(grads, out), EINVAL, "overlap")
+    for grads, out in (((P, 2 * P), (3 * P, P)), ((P, 2 * P), (2 * P, 3 * P)), ((P, 2 * P), (2 * P, P)), ((P, P), (P, 2 * P)), ((P,), (P + 8,)), ((P,), (P - 36,)),
+                       ((P, 2 * P), (P, 2 * P + 4))):
+        _refused(L, clip(grads, out), EINVAL, "overlap")
+    _refused(L, clip((P, P + 20), (2 * P, 2 * P + 20), types=(1, 1)), EINVAL, "overlap")     # outputs twice as wide as the gradients
+    # neighbours, gradients listed twice that go elsewhere, empty tensors, in place: on to the next check
+    for grads, out in (((P, P + 40), (P, P + 40)), ((P + 40, P), (P + 40, P)), ((P, P), (2 * P, 2 * P + 40)), ((P,), (P + 40,)), ((P,), (P - 40,)),
+                       ((P, 2 * P, 3 * P), (3 * P + 40, 2 * P, P + 40))):
+        _refused(L, clip(grads, out), EINVAL, "workspace")
+    _refused(L, clip((P, P, None), (P, P, None), counts=(10, 0, 0)), EINVAL, "workspace")
+    _refused(L, _clip(L, counts=(10, 10), grads=(P, P), types=(0, 0), ws=None, null=("out", "out_types")), EINVAL, "workspace")     # the norm alone only reads
+
+
 def _norm(L, x=P, ld_x=8, w=P, b=P, y=2 * P, ld_y=8, mean=P, rstd=P, rows=4, cols=8, eps=1e-5, kind=0, wkind=0):
     return L.lopt_layer_norm(x, ld_x, w, b, y, ld_y, mean, rstd, rows, cols, eps, kind, wkind, None)
 
