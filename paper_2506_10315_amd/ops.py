@@ -180,10 +180,11 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
 
 def clip_grad_norm_(parameters: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float) -> torch.Tensor:
     """Clips the `.grad` of the parameters in place and returns the norm before. Parameters without a gradient are
-    skipped; a gradient that is listed twice is refused."""
-    if isinstance(parameters, torch.Tensor):
-        parameters = [parameters]
+    skipped, and if none has one the norm is 0; a gradient that is listed twice is refused."""
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
     grads = [p.grad for p in parameters if p.grad is not None]
+    if parameters and not grads:
+        return torch.zeros((), dtype=torch.float32, device=parameters[0].device)
     return _clip(grads, grads, max_norm)
 
 

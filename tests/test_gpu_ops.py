@@ -178,6 +178,16 @@ def test_clip_refuses_a_gradient_listed_twice_in_place():
     assert float(n) == pytest.approx(200.0) and torch.equal(a, b) and float(a[7]) == pytest.approx(2 * 0.5 / 200.0)
 
 
+def test_clip_without_a_gradient():
+    import torch
+    ps = [torch.nn.Parameter(torch.ones(3, device="cuda:0")) for _ in range(2)]
+    for params in (ps, iter(ps), ps[0]):
+        n = ops().clip_grad_norm_(params, 1.0)
+        assert float(n) == 0.0 and n.shape == () and n.dtype == torch.float32 and n.is_cuda
+    with pytest.raises(ValueError):
+        ops().clip_grad_norm_([], 1.0)
+
+
 def test_clip_special_values():
     import torch
     f = lambda *v: torch.tensor(v, device="cuda:0")
