@@ -299,32 +299,37 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, i
   }
 }
 
-// The partial sums of `parts` workgroups, added up in double: a workgroup takes 32 columns of one of the two sums, 32 lanes a row of partial sums.
+// The partial sums of `parts` workgroups, added up in double: a workgroup takes 32 columns of one of the two sums, 32 lanes a row of partial sums. A launch
+// has no more than 2^32 threads in a row: the workgroups of more than kMostColumnBlocks go round.
+constexpr int64_t kMostColumnBlocks = 1 << 20;
 template <typename W>
 __global__ __launch_bounds__(1024) void k_norm_columns_sum(const float* __restrict__ part, int64_t parts, uint32_t cols, W* __restrict__ dw, W* __restrict__ db) {
   __shared__ double sums[32][33];
   const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
   W* out = blockIdx.y ? db : dw;
   if (!out) return;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + col;
-  double s = 0.0;
-  if (c < cols) {
-    const float* p = part + (uint64_t)blockIdx.y * cols + c;
-    int64_t k = row;
-    for (; k + 32 * 7 < parts; k += 32 * 8) {
-      float v[8];
+  for (uint64_t first = (uint64_t)blockIdx.x * 32; first < cols; first += (uint64_t)gridDim.x * 32) {
+    const uint64_t c = first + col;
+    double s = 0.0;
+    if (c < cols) {
+      const float* p = part + (uint64_t)blockIdx.y * cols + c;
+      int64_t k = row;
+      for (; k + 32 * 7 < parts; k += 32 * 8) {
+        float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = p[2 * (k + 32 * i) * cols];
+        for (int i = 0; i < 8; ++i) v[i] = p[2 * (k + 32 * i) * cols];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += (double)v[i];
+        for (int i = 0; i < 8; ++i) s += (double)v[i];
+      }
+      for (; k < parts; k += 32) s += (double)p[2 * k * cols];
     }
-    for (; k < parts; k += 32) s += (double)p[2 * k * cols];
-  }
-  sums[row][col] = s;
-  __syncthreads();
-  if (row == 0 && c < cols) {
-    for (int i = 1; i < 32; ++i) s += sums[i][col];
-    out[c] = from_f32<W>((float)s);
+    sums[row][col] = s;
+    __syncthreads();
+    if (row == 0 && c < cols) {
+      for (int i = 1; i < 32; ++i) s += sums[i][col];
+      out[c] = from_f32<W>((float)s);
+    }
+    if (first + (uint64_t)gridDim.x * 32 < cols) __syncthreads();
   }
 }
 
@@ -616,7 +621,7 @@ lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
     if (columns)
       with_type(weight_type, [&](auto u) {
         using W = decltype(u);
-        hipLaunchKernelGGL(k_norm_columns_sum<W>, dim3((n_cols + 31) / 32, 2), dim3(1024), 0, stream, (const float*)part, parts, n_cols, (W*)dweight, (W*)dbias);
+        hipLaunchKernelGGL(k_norm_columns_sum<W>, dim3((unsigned)std::min(((int64_t)cols + 31) / 32, kMostColumnBlocks), 2), dim3(1024), 0, stream, (const float*)part, parts, n_cols, (W*)dweight, (W*)dbias);
       });
   });
   return launch_status("lopt_layer_norm_backward");

@@ -429,6 +429,18 @@ def test_layer_norm_backward_strides_and_margins():
     close(db, want[2], tol[2], "broadcast db")
 
 
+def test_layer_norm_backward_of_more_columns_than_a_launch_has_threads():
+    import torch
+    cols = (1 << 27) + 45           # 32 threads a column
+    gen = torch.Generator(device="cuda:0").manual_seed(1)
+    x, dy = (torch.randn(1, cols, device="cuda:0", generator=gen).bfloat16() for _ in range(2))
+    mean, rstd = torch.tensor([0.25], device="cuda:0"), torch.tensor([1.5], device="cuda:0")
+    _, dw, db = ops().layer_norm_backward(dy, x, None, mean, rstd, need=(False, True, True))
+    want = dy.double() * ((x.double() - 0.25) * 1.5)
+    assert bool(((dw.double() - want[0]).abs() <= 4 * U * want[0].abs()).all())     # a difference and two products
+    assert torch.equal(db, dy[0].float())
+
+
 def test_layer_norm_autograd_against_differences():
     import torch
     r = np.random.default_rng(21)
