@@ -151,7 +151,6 @@ __global__ __launch_bounds__(kBlock) void k_clip_scale(const ClipBatch b, const 
     if (f == 1.f && t.in == t.out) continue;
     const int count = Walk::count(b, w.k, c);
     const int64_t at = (int64_t)(c - t.first) * kChunk;
-    float v[16];
     if (t.type == LOPT_F32 || t.out_type == LOPT_F32) scale_chunk<4>(t, at, count, f);
     else scale_chunk<8>(t, at, count, f);
   }
