@@ -31,13 +31,13 @@ __device__ __forceinline__ float least_of(float bound) { return bound == 0.f ? -
 //   s = sum 2^t,   h = sum 2^t t,   t = x c - b in one fused operation
 // b's own rounding, m c - b = delta, is the same for every logit of the row and is taken out of ln S at the end:
 //   ln S = ln s - delta ln 2,   entropy = ln s - ln 2 h / s
-// which is one vector instruction a logit less than x - m, then times c. It adds delta to every exponent, so b is held within 2^24, where delta is half a unit
-// at most (at 1.44e10 it would be 440, and 2^t infinite). A lane or piece of logits below that (masks of -1e9 and less) adds 0; a row whose
-// largest logit lies outside is summed again by extreme_sums.
+// which is one vector instruction a logit less than x - m, then times c. It adds delta to every exponent, so b is held within 2^28, where delta is 8
+// at most (at 1.44e10 it would be 440, and 2^t infinite): logits of 1.8e8, or of 180 at a scale of 1e6. A lane or piece of logits below that (masks of -1e9 and
+// less) adds 0; a row whose largest logit lies outside is summed again by extreme_sums.
 // A masked logit has t = -infinity and 2^t = 0; for the product t is held to a finite value.
 struct Soft { float m, s, h; };
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-constexpr float kMostBase = 16777216.f;
+constexpr float kMostBase = 268435456.f;
 
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float base_of(float m, float c) { return __builtin_amdgcn_fmed3f(m * c, -kMostBase, kMostBase); }
@@ -52,36 +52,7 @@ __device__ __forceinline__ Soft wave_join(Soft a, float c) {
   return Soft{a.m, wave_sum(a.s), wave_sum(a.h)};
 }
 
-// Rows whose largest logit m is beyond kMostBase times 1 / c: summed again by differences from m, which may be as large as the type allows (+infinity: its
-// difference from itself makes the sums NaN). `at`: the first logit of this lane, `step` from one to the next.
-__device__ __forceinline__ bool beyond(float m, float c) { return fabsf(m * c) >= kMostBase && m != -INFINITY; }
-template <typename T>
-__device__ Soft extreme_sums(const T* row, uint32_t n, float m, float c, uint32_t at, uint32_t step) {
-  Soft a{m, 0.f, 0.f};
-  for (uint32_t i = at; i < n; i += 8 * step) {
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = i + k * step < n ? to_f32(row[i + k * step]) : -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float t = i + k * step < n ? (v[k] - m) * c : -INFINITY, e = exp2_hw(t);
-      a.s += e;
-      a.h += e * fmaxf(t, -FLT_MAX);
-    }
-  }
-  return Soft{m, wave_sum(a.s), wave_sum(a.h)};
-}
-// By the whole workgroup; `sums`: what the wavefronts have, free for this on entry.
-template <typename T>
-__device__ Soft extreme_block(const T* row, uint32_t n, float m, float c, Soft* sums) {
-  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  const Soft own = extreme_sums(row, n, m, c, threadIdx.x, blockDim.x);
-  __syncthreads();
-  if (lane == 0) sums[threadIdx.x >> 6] = own;
-  __syncthreads();
-  const Soft a = lane < waves ? sums[lane] : Soft{m, 0.f, 0.f};
-  return Soft{m, wave_sum(a.s), wave_sum(a.h)};
-}
+__device__ __forceinline__ bool beyond(float m, float c) { return fabsf(m * c) >= kMostBase && m != -INFINITY; }   // see extreme_sums
 
 struct Outputs {
   float* logp;
@@ -209,6 +180,39 @@ __device__ __forceinline__ void add_piece(Soft& a, const float (&x)[E], float mo
     a.s += e;
     a.h += e * fmaxf(t, -kMostBase);
   }
+}
+
+// Rows whose largest logit m is beyond kMostBase times 1 / c: summed again by differences from m, which may be as large as the type allows (+infinity: its
+// difference from itself makes the sums NaN). By one wavefront of `waves`, in pieces as in the first pass: 4096x50257 bf16 at a scale of 1e8 119 us, 75 at 1.
+template <typename T>
+__device__ Soft extreme_sums(const T* row, uint32_t n, float m, float c, int wave, int waves) {
+  typedef Piece<T, 16> P;
+  const int off = pack_offset(row, n), end = (int)n + off;
+  Soft a{m, 0.f, 0.f};
+  for (int first = wave * P::kSize; first < end; first += waves * P::kSize) {
+    P p;
+    p.load(row, first, off, n);
+    float v[16];
+    p.unpack(v);
+#pragma unroll
+    for (float x : v) {
+      const float t = (x - m) * c, e = exp2_hw(t);
+      a.s += e;
+      a.h += e * fmaxf(t, -FLT_MAX);
+    }
+  }
+  return Soft{m, wave_sum(a.s), wave_sum(a.h)};
+}
+// By the whole workgroup; `sums`: what the wavefronts have, free for this on entry.
+template <typename T>
+__device__ Soft extreme_block(const T* row, uint32_t n, float m, float c, Soft* sums) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const Soft own = extreme_sums(row, n, m, c, wave, waves);
+  __syncthreads();
+  if (lane == 0) sums[wave] = own;
+  __syncthreads();
+  const Soft a = lane < waves ? sums[lane] : Soft{m, 0.f, 0.f};
+  return Soft{m, wave_sum(a.s), wave_sum(a.h)};
 }
 
 // The largest number that at least `need` of the lanes' numbers reach, bit by bit from the top; 0 if fewer than that are not 0. With fewer than 32 `bits`
@@ -390,7 +394,7 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_short(const T* __restrict__
     a = wave_join(a, c);
     uint64_t key = 0;
     if (TOP) key = piece_top(row, p, v, most, top, a.s != a.s, lists + wave * (E + 2) * top);
-    if (beyond(a.m, c)) a = extreme_sums(row, vocab, a.m, c, lane, kWave);
+    if (beyond(a.m, c)) a = extreme_sums(row, vocab, a.m, c, 0, 1);
     write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
   }
 }
@@ -822,7 +826,7 @@ __global__ __launch_bounds__(kWave) void k_logprobs_join(const T* __restrict__ x
     }
     a = wave_join(a, c);
     if (last) {
-      if (beyond(a.m, c)) a = extreme_sums(x + r * ld, vocab, a.m, c, lane, kWave);
+      if (beyond(a.m, c)) a = extreme_sums(x + r * ld, vocab, a.m, c, 0, 1);
       write_row(o, r, lane, a, c, g, vocab, scale, ignore, top, key);
     } else {
       if (lane < 3) part_out[3 * unit + lane] = lane == 0 ? a.m : lane == 1 ? a.s : a.h;

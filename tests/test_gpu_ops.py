@@ -688,6 +688,23 @@ def test_token_logprobs_alternatives_among_zeros_of_both_signs(rows, vocab, kind
         check_logp(x, kind, t, 1.0, top, what=f"top {top}")
 
 
+@pytest.mark.parametrize("rows,vocab,top", [(8, 5, 3), (8, 100, 5), (8, 3001, 0), (8, 20000, 5), (300, 5000, 0), (300, 33001, 5), (3, 70001, 5), (3, 140000, 0)])
+def test_token_logprobs_where_the_second_pass_begins(rows, vocab, top):
+    """Products of scale and logit on both sides of 2^28 / ln 2 and some powers of two away, at any offset of the rows."""
+    import torch
+    x, t = logits_case(rows, vocab, vocab)
+    steps = np.round(4 * x)
+    for k in (27, 28, 29, 30):
+        for sign in (1, -1):
+            check_logp(16 * steps + np.float32(sign * 2.0 ** k * math.log(2)), "fp32", t, 1.0, top, what=f"offset {sign} 2^{k}")
+            check_logp(steps + np.float32(sign * 2.0 ** (k - 6) * math.log(2)), "fp32", t, 64.0, top, what=f"offset {sign} 2^{k}, scale 64")
+    for kind in TYPES:
+        full = torch.zeros(rows, vocab + 9, dtype=tt(kind), device="cuda:0")
+        for off, scale in ((1, 1e7), (3, 5e7), (7, 1e8), (2, 1e9)):
+            full[:, off:off + vocab] = dev(x, kind)[0]
+            check_logp(full[:, off:off + vocab], kind, t, scale, top, what=f"{kind} scale {scale}")
+
+
 def test_token_logprobs_special_rows_and_targets():
     import torch
     x, t = logits_case(12, 5000, 5)
