@@ -1,7 +1,8 @@
 // Layer norm and its gradient. Forward, per row: mean = sum x / n, rstd = 1 / sqrt(sum (x - mean)^2 / n + eps), y = (x - mean) rstd w + b, in two
 // sums over a row that is held, never sum x^2 - mean^2. Backward, with h = (x - mean) rstd and a = dy w: dx = rstd (a - sum(a) / n - h sum(a h) / n),
 // dw = sum over the rows of dy h, db of dy. Both are bound by memory where there is enough of it (two and three arrays once each), by
-// the launches below some 10 MB.
+// the launches below some 10 MB. Times below are of calls one behind the other in a graph, on the same inputs; those of a single kernel are from a kernel trace, where
+// launches do not overlap, so that two of them add up to more than the call.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -171,7 +172,7 @@ template <int G> constexpr bool kAhead = G < 1024;
 struct Vectors { const void* w; const void* b; uint32_t type; };
 
 // Every group takes rows a grid apart and asks for the next before it works on the one it has. us (TB/s of one read and one write): 12608x768 bf16 9.5
-// (4.1), 16384x2048 bf16 22 (6.2), 8192x4096 bf16 23 (5.8), 1024x16384 fp32 30 (4.5), 1x1024 2.2.
+// (4.1), 16384x2048 bf16 22.4 (6.0), 8192x4096 bf16 22.5 (6.0), 1024x16384 fp32 28 (4.8), 1x1024 2.8.
 template <typename T, int G, int N>
 __global__ __launch_bounds__(Group<G>::kThreads) void k_norm(const T* x, int64_t ld_x, Vectors wb, T* y, int64_t ld_y, float* __restrict__ mean_out,
                                                              float* __restrict__ rstd_out, int64_t rows, uint32_t cols, float eps) {
@@ -226,8 +227,8 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_norm(const T* x, int64_t
 
 // The gradient of the same rows. The columns' sums stay in each lane's registers over all of its rows; at the end the workgroup's groups add theirs
 // up through LDS, half to half (one after the other: 100000x100 bf16 23 us, so 19), and the workgroup writes one row of partial sums:
-// part[block][2][cols], 16 bytes a lane (single floats: 1024x16384 bf16 45 us, so 31). The two launches, us (TB/s of two reads and one write): 8192x1024 bf16
-// 13 + 4 (3.0), 16384x2048 bf16 38 (5.3), 8192x4096 bf16 38 (5.4), 5001x1531 fp16 14.5 + 4; dx alone 16384x2048 33.
+// part[block][2][cols], 16 bytes a lane (single floats: 1024x16384 bf16 45 us, so 31). Both launches, us (TB/s of two reads and one write): 8192x1024 bf16
+// 15.9 (3.2; the kernels 13.2 and 3.9), 16384x2048 bf16 38 (5.3), 8192x4096 bf16 38 (5.3), 5001x1531 fp16 18.3 (2.5; 15.8 and 3.9); dx alone 16384x2048 33.
 template <typename T, int G, int N>
 __global__ __launch_bounds__(Group<G>::kThreads) void k_norm_back(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const void* __restrict__ weight,
                                                                   uint32_t weight_type, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(1024) void k_norm_columns_sum(const float* __restri
 }
 
 // ---- rows too long for registers (above 32768 columns, backward 16384; fp32 the same): one workgroup a row, which reads it again (from L2) for every
-// use. us: 200x65536 bf16 17, backward 56 (dx 21); 2000x20000 bf16 backward 88.
+// use. us: 200x65536 bf16 16, backward 53 (dx alone 22); 2000x20000 bf16 40, backward 87 (dx alone 52).
 // Calls f(first element, pack or element count) over a row: packs of 16 bytes, four in flight a thread, then what is left element by element.
 template <int V, typename F>
 __device__ __forceinline__ void along_row(uint32_t cols, F&& f) {
@@ -413,7 +414,8 @@ __global__ __launch_bounds__(1024) void k_norm_long(const T* x, int64_t ld_x, Ve
   }
 }
 
-constexpr int kSlab = 32;   // rows whose column sums one lane adds up
+// Rows whose column sums one lane adds up. With few rows that leaves few wavefronts: 200x65536 bf16 7 x 129 of them, 35 us of the backward pass's 53.
+constexpr int kSlab = 32;
 
 // Partial sums of dy xh and dy over a slab of rows, a pack of columns a lane; the pack that would pass the row's end ends with it, and gives the columns that
 // it shares the same sums. Runs before dx, which may overwrite dy or x.
@@ -511,15 +513,17 @@ bool with_group(int64_t cols, F&& f) {
   return false;
 }
 // Elements a lane holds at most: forward the row and two vectors, backward two rows, one vector and two sums. 32 and 16 leave
-// every wavefront of a workgroup of 1024 the 128 registers that it can have.
+// every wavefront of a workgroup of 1024 the 128 registers that it can have; smaller groups, whose wavefronts could have more, keep to the same.
 constexpr int kMostForward = 32, kMostBackward = 16;
 
 int64_t slabs_of(int64_t rows) { return (rows + kSlab - 1) / kSlab; }
 
 // Workgroups of the backward pass over rows in registers, at most this many: each writes one row of partial sums. us with 128 / 256 / 512, before partial sums
 // left in 16-byte accesses: groups of 64 and 256 lanes 16384x2048 bf16 110 / 62 / 44, 8192x4096 bf16 70 / 44 / 45; of 1024 lanes, where a row of partial sums is
-// long beside the rows summed up, 4096x8192 bf16 67 / 49 / 59, 1024x16384 bf16 43 / 45 / 70, 2048x5504 fp32 38 / 32 / 36. 768 or 1024 workgroups for groups of 64, or
-// twice the lanes in each: no gain.
+// long beside the rows summed up, 4096x8192 bf16 67 / 49 / 59, 1024x16384 bf16 43 / 45 / 70, 2048x5504 fp32 38 / 32 / 36. The kernel alone on inputs
+// that change, with 512 / 768 / 1024 workgroups, and of twice the lanes with 512 / 256: 8192x768 bf16 12.3 / 11.8 / 14.1, 15.6 / 12.4; 8192x1024 14.5 / 14.6 / 16.2, 18.2 /
+// 14.6; 12608x768 15.2 / 14.8 / 17.4, 18.6 / 15.7; 100000x100 18.8 / 17.6 / 18.1, 18.9 / 20.0; 16384x2048 36.2 / 36.4 / 36.5; 8192x4096 36.5 / 36.6 / 40.1. The sums of the
+// partial rows take 3.9 to 4.3 with 256 to 1024 of them at up to 1024 columns.
 template <int G>
 int64_t back_blocks(int64_t rows) { return std::min<int64_t>((rows + Group<G>::kRows - 1) / Group<G>::kRows, G == 1024 ? 256 : 512); }
 template <int V>
