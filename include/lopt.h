@@ -298,6 +298,42 @@ lopt_status lopt_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
                                      void* dbias, int64_t rows, int64_t cols, uint32_t type, uint32_t weight_type,
                                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Dropout of `rows` rows of `cols` >= 1 elements of `type`, by a counter-based generator, so that no mask is stored:
+ *   y = x / (1 - p) where the element stays, else 0 (whatever x is there, NaN included)
+ * Row r's elements 4k to 4k + 3 have the four words of Philox4x32 with ten rounds, key = the seed, counter = (k, r, the offset's lower
+ * and upper 32 bits), the key's and the offset's lower 32 bits first; an element stays if its word >= p 2^32 (rounded to a whole number). The mask is
+ * a function of (seed, offset, row, column) alone, the same for every type, distance of rows and call below. The gradient is the same call on the gradient.
+ * seed_device: null, or one uint64_t on the device that is the seed in place of `seed`, read when the kernel runs: a captured graph
+ * drops other elements in every replay if the program changes it. 0 <= p <= 1. y may be x (with the same ld).
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, cols or ld out of range), LOPT_EHIP. */
+lopt_status lopt_dropout(const void* x, int64_t ld_x, void* y, int64_t ld_y, int64_t rows, int64_t cols, uint32_t type,
+                         float p, uint64_t seed, const uint64_t* seed_device, uint64_t offset, void* hip_stream);
+
+/* Dropout, residual addition and layer norm:
+ *   h = residual + dropout(x),   y = layer_norm(h)
+ * h has `residual_type`, which is `type` or LOPT_F32, and the norm is of h as it is stored, so that lopt_layer_norm of h gives the same; x and y have `type`,
+ * weight and bias (each may be null) `weight_type`. mean, rstd: as in lopt_layer_norm, of h. y or h may be x or residual where the element sizes and
+ * ld are the same; they may not be each other. p = 0: no generator runs. Errors: as lopt_layer_norm and lopt_dropout. */
+lopt_status lopt_dropout_add_layer_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_res, const void* weight,
+                                        const void* bias, void* y, int64_t ld_y, void* h, int64_t ld_h, float* mean,
+                                        float* rstd, int64_t rows, int64_t cols, float eps, uint32_t type,
+                                        uint32_t residual_type, uint32_t weight_type, float p, uint64_t seed,
+                                        const uint64_t* seed_device, uint64_t offset, void* hip_stream);
+
+/* Its gradient, from dy (of y, `type`) and dh (of h, `residual_type`; null: 0):
+ *   dresidual = dh + the gradient that lopt_layer_norm_backward gives for (dy, h),   dx = dropout(dresidual before it is rounded),   dweight, dbias as there
+ * dx, dresidual, dweight and dbias may be null (not wanted). dx or dresidual may be dy, dh or h where the element sizes and ld are
+ * the same; they may not be each other. workspace: lopt_dropout_add_layer_norm_workspace bytes, may be null where that is 0 or neither dweight nor dbias is
+ * wanted. With zero rows dweight and dbias are 0. */
+size_t lopt_dropout_add_layer_norm_workspace(int64_t rows, int64_t cols);
+lopt_status lopt_dropout_add_layer_norm_backward(const void* dy, int64_t ld_dy, const void* dh, int64_t ld_dh, const void* h,
+                                                 int64_t ld_h, const void* weight, const float* mean, const float* rstd,
+                                                 void* dx, int64_t ld_dx, void* dresidual, int64_t ld_dres, void* dweight,
+                                                 void* dbias, int64_t rows, int64_t cols, uint32_t type,
+                                                 uint32_t residual_type, uint32_t weight_type, float p, uint64_t seed,
+                                                 const uint64_t* seed_device, uint64_t offset, void* workspace,
+                                                 size_t workspace_bytes, void* hip_stream);
+
 /* Log probabilities under softmax(scale x) of each row x of `vocab` >= 1 logits: with m = max x, z = scale (x - m), S = sum e^z
  *   logp = z[target] - ln S,   entropy = ln S - sum(e^z z) / S,   stats = (m, ln S) for the backward pass
  *   top_logp, top_index [rows x top]: the `top` largest logits in order, the lowest index first among equals

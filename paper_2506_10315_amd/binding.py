@@ -105,6 +105,16 @@ def lib() -> C.CDLL:
     L.lopt_token_logprobs.restype = C.c_int
     L.lopt_token_logprobs_backward.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, u32, f32, i64, vp]
     L.lopt_token_logprobs_backward.restype = C.c_int
+    u64 = C.c_uint64
+    drop = [f32, u64, vp, u64]   # p, seed, seed_device, offset
+    L.lopt_dropout.argtypes = [vp, i64, vp, i64, i64, i64, u32, *drop, vp]
+    L.lopt_dropout.restype = C.c_int
+    L.lopt_dropout_add_layer_norm.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, i64, f32, u32, u32, u32, *drop, vp]
+    L.lopt_dropout_add_layer_norm.restype = C.c_int
+    L.lopt_dropout_add_layer_norm_workspace.argtypes = [i64, i64]
+    L.lopt_dropout_add_layer_norm_workspace.restype = sz
+    L.lopt_dropout_add_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, i64, u32, u32, u32, *drop, vp, sz, vp]
+    L.lopt_dropout_add_layer_norm_backward.restype = C.c_int
     L.lopt_last_error.argtypes = [vp]
     L.lopt_last_error.restype = C.c_char_p
     _lib = L

@@ -25,6 +25,8 @@ UNITS = [
     ("lopt_clip.hip", "clip", []),
     ("lopt_layer_norm.hip", "layer_norm", []),
     ("lopt_logprobs.hip", "logprobs", []),
+    ("lopt_dropout.hip", "dropout", []),
+    ("lopt_add_norm.hip", "add_norm", []),
 ]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -16,6 +16,7 @@ import torch
 from .binding import _check, lib
 
 __all__ = ["clip_grads", "clip_grad_norm_", "grad_norm", "layer_norm", "layer_norm_forward", "layer_norm_backward",
+           "dropout", "dropout_forward", "dropout_add_layer_norm", "dropout_add_layer_norm_forward", "dropout_add_layer_norm_backward",
            "TokenLogprobs", "token_logprobs", "token_logprobs_forward", "token_logprobs_backward", "TOP_MAX"]
 
 TOP_MAX = 32          # LOPT_TOP_MAX
@@ -261,6 +262,158 @@ class _LayerNorm(torch.autograd.Function):
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
     """Layer norm over the last dimension, with gradients for x, weight and bias."""
     return _LayerNorm.apply(x, weight, bias, eps)
+
+
+# ---------------------------------------------------------------------------------------------- dropout
+
+Seed = Union[int, torch.Tensor]
+
+
+def _seed(seed: Seed, offset: int, like: torch.Tensor) -> Tuple[int, Optional[torch.Tensor], int]:
+    """(seed, tensor that holds it or None, offset) as the boundary takes them."""
+    if not 0 <= offset < 1 << 64:
+        raise ValueError(f"offset={offset} outside [0, 2^64)")
+    if isinstance(seed, torch.Tensor):
+        if seed.dtype is not torch.int64 or seed.numel() != 1 or seed.get_device() != like.get_device():
+            raise ValueError(f"seed is {tuple(seed.shape)} of {seed.dtype} on {seed.device}; one int64 on {like.device} is needed")
+        return 0, seed, offset
+    if not 0 <= seed < 1 << 64:
+        raise ValueError(f"seed={seed} outside [0, 2^64)")
+    return seed, None, offset
+
+
+def dropout_forward(x: torch.Tensor, p: float, seed: Seed, offset: int = 0) -> torch.Tensor:
+    """x / (1 - p) where an element stays, else 0, in x's type. Which elements stay is a function of seed, offset and the element's row and column
+    (rows of the last dimension) alone; nothing is stored, and the backward pass is the same call on the gradient. A seed that is one int64 on
+    the device is read when the kernel runs."""
+    kind = _type("x", x)
+    x2, rows, cols, ld = _matrix("x", x)
+    number, tensor, offset = _seed(seed, offset, x)
+    y = _new(x)
+    _run(lib().lopt_dropout, x.get_device(), x2.data_ptr(), ld, y.data_ptr(), cols, rows, cols, kind, p, number, _ptr(tensor), offset)
+    return y
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, offset):
+        ctx.args = p, None if isinstance(seed, torch.Tensor) else seed, offset
+        if isinstance(seed, torch.Tensor):
+            ctx.save_for_backward(seed)
+        return dropout_forward(x, p, seed, offset)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        p, seed, offset = ctx.args
+        return dropout_forward(dy, p, ctx.saved_tensors[0] if seed is None else seed, offset), None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, seed: Seed, offset: int = 0) -> torch.Tensor:
+    """dropout_forward with the gradient for x. A program gives every step another seed and every call within a step another
+    offset."""
+    return _Dropout.apply(x, p, seed, offset)
+
+
+def dropout_add_layer_norm_forward(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                                   p: float = 0.0, seed: Seed = 0, offset: int = 0,
+                                   eps: float = 1e-5) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(y, h, mean, rstd) with h = residual + dropout(x) and y = layer_norm(h): y has x's type, h the residual's, which is x's or
+    float32. The norm is of h as it is stored."""
+    kind = _type("x", x)
+    x2, rows, cols, ld = _matrix("x", x)
+    if residual.shape != x.shape or residual.get_device() != x.get_device():
+        raise ValueError(f"residual is {tuple(residual.shape)} on {residual.device}; x is {tuple(x.shape)} on {x.device}")
+    rkind = _type("residual", residual)
+    r2, _, _, ld_res = _matrix("residual", residual)
+    wtype = 0
+    if weight is not None:
+        wtype = _type("weight", weight)
+        weight = _expect("weight", weight, x, weight.dtype, (cols,))
+    if bias is not None:
+        if weight is None:
+            wtype = _type("bias", bias)
+        bias = _expect("bias", bias, x, bias.dtype if weight is None else weight.dtype, (cols,))
+    number, tensor, offset = _seed(seed, offset, x)
+    y, h = _new(x), _new(residual)
+    mean = _floats(rows, x.shape[:-1], x.device)
+    rstd = torch.empty_like(mean)
+    _run(lib().lopt_dropout_add_layer_norm, x.get_device(), x2.data_ptr(), ld, r2.data_ptr(), ld_res, _ptr(weight), _ptr(bias), y.data_ptr(), cols,
+         h.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), rows, cols, eps, kind, rkind, wtype, p, number, _ptr(tensor), offset)
+    return y, h, mean, rstd
+
+
+def dropout_add_layer_norm_backward(dy: torch.Tensor, dh: Optional[torch.Tensor], h: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                                    rstd: torch.Tensor, p: float = 0.0, seed: Seed = 0, offset: int = 0,
+                                    need: Tuple[bool, bool, bool, bool] = (True, True, True, True), bias_type: Optional[torch.dtype] = None):
+    """(dx, dresidual, dweight, dbias) of dropout_add_layer_norm_forward from the gradients of y and of h (None: 0); `need` says which are wanted,
+    the others are None. dx has dy's type, dresidual h's. Without dropout dx and dresidual of one type are the same tensor."""
+    kind, rkind = _type("dy", dy), _type("h", h)
+    dy2, rows, cols, ld_dy = _matrix("dy", dy)
+    for name, t in (("h", h), ("dh", dh)):
+        if t is not None and (t.shape != dy.shape or t.dtype is not h.dtype or t.get_device() != dy.get_device()):
+            raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype} on {t.device}; {tuple(dy.shape)} of {h.dtype} on {dy.device} is needed")
+    h2, _, _, ld_h = _matrix("h", h)
+    dh2, ld_dh = None, 0
+    if dh is not None:
+        dh2, _, _, ld_dh = _matrix("dh", dh)
+    wtype = weight.dtype if weight is not None else bias_type or torch.float32
+    if wtype not in _TYPES:
+        raise ValueError(f"weights of {wtype}; float32, bfloat16 or float16 is needed")
+    if weight is not None:
+        weight = _expect("weight", weight, dy, wtype, (cols,))
+    shape = dy.shape[:-1]
+    mean = _expect("mean", mean, dy, torch.float32, shape)
+    rstd = _expect("rstd", rstd, dy, torch.float32, shape)
+    number, tensor, offset = _seed(seed, offset, dy)
+    same = p == 0.0 and kind == rkind
+    dres = _new(h) if need[1] or (need[0] and same) else None
+    dx = _new(dy) if need[0] and not same else None
+    dw = db = None
+    if need[2]:
+        dw = torch.empty_like(weight) if weight is not None else torch.empty(cols, dtype=wtype, device=dy.device)
+    if need[3]:
+        db = torch.empty_like(dw) if dw is not None else torch.empty(cols, dtype=wtype, device=dy.device)
+    L = lib()
+    nbytes = L.lopt_dropout_add_layer_norm_workspace(rows, cols) if need[2] or need[3] else 0
+    ws = _workspace(nbytes, dy.device)
+    _run(L.lopt_dropout_add_layer_norm_backward, dy.get_device(), dy2.data_ptr(), ld_dy, _ptr(dh2), ld_dh, h2.data_ptr(), ld_h, _ptr(weight), mean.data_ptr(),
+         rstd.data_ptr(), _ptr(dx), cols, _ptr(dres), cols, _ptr(dw), _ptr(db), rows, cols, kind, rkind, _TYPES[wtype], p, number, _ptr(tensor), offset, _ptr(ws),
+         nbytes)
+    return (dres if same and need[0] else dx), (dres if need[1] else None), dw, db
+
+
+class _DropoutAddLayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, p, seed, offset, eps):
+        y, h, mean, rstd = dropout_add_layer_norm_forward(x, residual, weight, bias, p, seed, offset, eps)
+        on_device = isinstance(seed, torch.Tensor)
+        ctx.save_for_backward(h, weight, mean, rstd, seed if on_device else None)
+        ctx.args = p, None if on_device else seed, offset
+        ctx.like = x.dtype
+        ctx.bias_type = None if bias is None else bias.dtype
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh):
+        if dy is None and dh is None:
+            return (None,) * 8
+        h, weight, mean, rstd, tensor = ctx.saved_tensors
+        p, seed, offset = ctx.args
+        if dy is None:   # the norm's output was not used
+            dy = torch.zeros(h.shape, dtype=ctx.like, device=h.device)
+        grads = dropout_add_layer_norm_backward(dy, dh, h, weight, mean, rstd, p, tensor if seed is None else seed, offset, ctx.needs_input_grad[:4],
+                                                ctx.bias_type)
+        return (*grads, None, None, None, None)
+
+
+def dropout_add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                           p: float = 0.0, seed: Seed = 0, offset: int = 0, eps: float = 1e-5) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(y, h): the block's output x is dropped, joins the residual stream, h, and the stream is normalised for the next block, y. With gradients
+    for x, residual, weight and bias."""
+    return _DropoutAddLayerNorm.apply(x, residual, weight, bias, p, seed, offset, eps)
 
 
 # ---------------------------------------------------------------------------------------------- token log probabilities
