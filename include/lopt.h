@@ -360,6 +360,28 @@ lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const i
                                          int64_t ld_d, int64_t rows, int64_t vocab, uint32_t type, float scale,
                                          int64_t ignore_index, void* hip_stream);
 
+/* KL divergence of each row's p = softmax(scale x) from q = softmax(scale r), x and r rows of `vocab` >= 1 logits of one type:
+ *   kl = sum p (ln p - ln q) >= 0,   stats [rows x 5] = (max x, ln sum e^(scale (x - max x)), max r, the same of r,
+ *                                                       sum p d with d = scale ((x - r) - (max x - max r)))   for the backward pass
+ * mask[rows]: 0 where a row does not count, whose kl and stats are 0 and whose logits are not read; null: every row counts.
+ * A token of which both logits are -infinity counts nothing, nor does one that x alone masks; one that r alone masks makes kl +infinity, however unlikely it is.
+ * A row that x masks whole has kl 0. A row with a NaN or +infinity in either has kl NaN. Finite masks, to the type's lowest value, are numbers; a kl beyond
+ * 1e38 may come out as +infinity. scale > 0, finite. workspace: lopt_token_kl_workspace bytes, may be null where that is 0.
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, vocab or ld out of range; vocab <= LOPT_VOCAB_MAX), LOPT_EHIP. */
+size_t lopt_token_kl_workspace(int64_t rows, int64_t vocab);
+lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, const uint8_t* mask, int64_t rows,
+                          int64_t vocab, uint32_t type, float scale, float* kl, float* stats, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients, with g = dkl[row] and d as above:
+ *   dlogits = g scale p (d - sum p d),   dref = g scale (q - p)
+ * Either may be null (not wanted). Rows that do not count, rows that x masks whole and rows of dkl 0 have the gradient 0 whatever their logits; that of another
+ * row whose kl is infinite or NaN is NaN. dlogits or dref may be logits or ref (with the same ld); they may not be each other. */
+lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, const uint8_t* mask,
+                                   const float* stats, const float* dkl, void* dlogits, int64_t ld_d, void* dref,
+                                   int64_t ld_dref, int64_t rows, int64_t vocab, uint32_t type, float scale,
+                                   void* hip_stream);
+
 /* Message for the last non-OK status returned through this context ("" if none). With a
  * null ctx: the message of the last failed call without a context on this thread. */
 const char* lopt_last_error(const lopt_ctx* ctx);

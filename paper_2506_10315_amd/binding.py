@@ -115,6 +115,12 @@ def lib() -> C.CDLL:
     L.lopt_dropout_add_layer_norm_workspace.restype = sz
     L.lopt_dropout_add_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, i64, u32, u32, u32, *drop, vp, sz, vp]
     L.lopt_dropout_add_layer_norm_backward.restype = C.c_int
+    L.lopt_token_kl_workspace.argtypes = [i64, i64]
+    L.lopt_token_kl_workspace.restype = sz
+    L.lopt_token_kl.argtypes = [vp, i64, vp, i64, vp, i64, i64, u32, f32, vp, vp, vp, sz, vp]
+    L.lopt_token_kl.restype = C.c_int
+    L.lopt_token_kl_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, i64, i64, u32, f32, vp]
+    L.lopt_token_kl_backward.restype = C.c_int
     L.lopt_last_error.argtypes = [vp]
     L.lopt_last_error.restype = C.c_char_p
     _lib = L

@@ -27,6 +27,7 @@ UNITS = [
     ("lopt_logprobs.hip", "logprobs", []),
     ("lopt_dropout.hip", "dropout", []),
     ("lopt_add_norm.hip", "add_norm", []),
+    ("lopt_kl.hip", "kl", []),
 ]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,377 @@
+// KL divergence of each row's softmax(scale x) from softmax(scale r), and its gradient for both: running maxima and sums, one pass over both rows of logits.
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "lopt_softmax.h"
+
+namespace lopt {
+namespace {
+
+// Running sums of some pairs of logits, mx and mr the largest of either (the type's lowest where all are masked), e = 2^(c (x - mx)) and f = 2^(c (r - mr)) with
+// c = scale / ln 2:
+//   sx = sum e,   sr = sum f,   w = sum (f - e),   h = sum e d   with d = scale ((x - r) - (mx - mr))
+//   KL = h / sx + ln(sr / sx)
+// Differences from the maxima and between the two lose nothing where they are near, however large the logits are. Of two sharp distributions both terms
+// are far smaller than the sums, which begin with the same 1: there ln(sr / sx) = ln(1 + w / sx), whose rounding goes with w (1x10 fp32 of KL 1e-4: off by 4e-5 with the
+// sums alone; by 2e-4 with the maxima's products rounded as in the token log probabilities, for e and f are not 1 at them). `most`: the largest d; it is infinite where r
+// masks a token that x does not (or where finite logits are 3.4e38 apart). For the product d is held to a finite value, which masked tokens, e = 0, need.
+struct Apart { float mx, mr, sx, sr, w, h, most; };
+__device__ __forceinline__ Apart nothing() { return Apart{-FLT_MAX, -FLT_MAX, 0.f, 0.f, 0.f, 0.f, -INFINITY}; }
+__device__ __forceinline__ float shift_of(float mx, float mr, float scale) { return fminf(scale * (mx - mr), FLT_MAX); }
+
+// a's sums seen from larger maxima.
+__device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, float c, float scale) {
+  const float fx = exp2_hw((a.mx - mx) * c), fr = exp2_hw((a.mr - mr) * c), fs = fx * a.sx;
+  const float moved = shift_of(a.mx, a.mr, scale) - shift_of(mx, mr, scale);
+  return Apart{mx, mr, fs, fr * a.sr, fr * a.w + (fr - fx) * a.sx, fx * a.h + (fs == 0.f ? 0.f : fs * moved), a.most};
+}
+__device__ __forceinline__ Apart wave_join(Apart a, float c, float scale) {
+  a = rebase(a, wave_max(a.mx), wave_max(a.mr), c, scale);
+  return Apart{a.mx, a.mr, wave_sum(a.sx), wave_sum(a.sr), wave_sum(a.w), wave_sum(a.h), wave_max(a.most)};
+}
+
+template <int E>
+__device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], float c, float scale) {
+  a = rebase(a, fmaxf(a.mx, most_of(x)), fmaxf(a.mr, most_of(r)), c, scale);
+  const float shift = shift_of(a.mx, a.mr, scale);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float e = exp2_hw((x[i] - a.mx) * c), f = exp2_hw((r[i] - a.mr) * c), d = __builtin_fmaf(x[i] - r[i], scale, -shift);
+    a.most = fmaxf(a.most, d);
+    a.sx += e;
+    a.sr += f;
+    a.w += f - e;
+    a.h += e * __builtin_amdgcn_fmed3f(d, -FLT_MAX, FLT_MAX);
+  }
+}
+
+template <typename T>
+struct Rows {
+  const T* x;
+  const T* r;
+  int64_t ld_x, ld_r, rows;
+  uint32_t n;
+  float scale;
+  const uint8_t* keep;   // null: every row counts
+};
+struct Outputs {
+  float* kl;
+  float* stats;
+};
+
+// A row's outputs from its sums, by one lane. Sums that are 0 belong to a row that is masked whole; a NaN or +infinity is in the sum.
+__device__ __forceinline__ void write_row(const Outputs& o, int64_t row, Apart a) {
+  const float ratio = a.w / a.sx;
+  float mean = a.h / a.sx, kl = mean + (fabsf(ratio) < 0.5f ? log1pf(ratio) : logf(a.sr / a.sx));
+  kl = kl < 0.f ? 0.f : kl;
+  if (a.sr == 0.f || a.most == INFINITY) kl = mean = INFINITY;
+  if (a.sx == 0.f) kl = mean = 0.f;
+  if (!(a.sx < INFINITY && a.sr < INFINITY)) kl = mean = NAN;
+  o.kl[row] = kl;
+  float* s = o.stats + 5 * row;
+  s[0] = a.sx == 0.f ? -INFINITY : a.mx;
+  s[1] = logf(a.sx);
+  s[2] = a.sr == 0.f ? -INFINITY : a.mr;
+  s[3] = logf(a.sr);
+  s[4] = mean;
+}
+__device__ __forceinline__ void write_nothing(const Outputs& o, int64_t row) {
+  o.kl[row] = 0.f;
+#pragma unroll
+  for (int i = 0; i < 5; ++i) o.stats[5 * row + i] = 0.f;
+}
+
+// Rows of one piece: a wavefront each.
+template <typename T, int E>
+__global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, Outputs o) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float c = fminf(a.scale * kLog2e, FLT_MAX);
+  for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < a.rows; row += (int64_t)gridDim.x * 4) {
+    if (a.keep && !a.keep[row]) {
+      if (lane == 0) write_nothing(o, row);
+      continue;
+    }
+    const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
+    const int off = pack_offset(x, a.n);
+    Piece<T, E> p, q;
+    p.load(x, 0, off, a.n);
+    q.load(r, 0, off, a.n);
+    float u[E], v[E];
+    p.unpack(u);
+    q.unpack(v);
+    Apart s = nothing();
+    add_piece(s, u, v, c, a.scale);
+    s = wave_join(s, c, a.scale);
+    if (lane == 0) write_row(o, row, s);
+  }
+}
+
+// A wavefront's sums over every `step`-th element's piece of a row, from `first` to `end`, counted from the pack in which the row of x begins.
+template <typename T, int E>
+__device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* r, int off, int64_t first, int64_t end, int64_t step, float c) {
+  typedef Piece<T, E> P;
+  Apart s = nothing();
+  P p, q;
+  if (first < end) {
+    p.load(x, (int)first, off, a.n);
+    q.load(r, (int)first, off, a.n);
+  }
+  for (; first < end; first += step) {
+    float u[E], v[E];
+    P next_p, next_q;
+    if (first + step < end) {
+      next_p.load(x, (int)(first + step), off, a.n);
+      next_q.load(r, (int)(first + step), off, a.n);
+    }
+    p.unpack(u);
+    q.unpack(v);
+    add_piece(s, u, v, c, a.scale);
+    p = next_p;
+    q = next_q;
+  }
+  return s;
+}
+
+// Joins what the wavefronts of a workgroup have; every thread gets it. `sums`: free before.
+__device__ __forceinline__ Apart block_join(Apart s, float c, float scale, Apart* sums) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  s = wave_join(s, c, scale);
+  if (lane == 0) sums[wave] = s;
+  __syncthreads();
+  s = lane < waves ? sums[lane] : nothing();
+  return wave_join(s, c, scale);
+}
+
+// A workgroup a row, its wavefronts a piece each in turn.
+template <typename T, int E>
+__global__ __launch_bounds__(1024) void k_kl(Rows<T> a, Outputs o) {
+  typedef Piece<T, E> P;
+  __shared__ Apart sums[16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const float c = fminf(a.scale * kLog2e, FLT_MAX);
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    if (a.keep && !a.keep[row]) {
+      if (threadIdx.x == 0) write_nothing(o, row);
+      continue;
+    }
+    const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
+    const int off = pack_offset(x, a.n);
+    Apart s = sums_of<T, E>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize, c);
+    s = block_join(s, c, a.scale, sums);
+    if (threadIdx.x == 0) write_row(o, row, s);
+    if (row + gridDim.x < a.rows) __syncthreads();
+  }
+}
+
+// Few rows too long for one workgroup: segments of `pieces` pieces, a workgroup of four wavefronts each, and a workgroup a row that joins them.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments, uint32_t pieces, Apart* __restrict__ part) {
+  typedef Piece<T, 16> P;
+  __shared__ Apart sums[4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float c = fminf(a.scale * kLog2e, FLT_MAX);
+  for (int64_t unit = blockIdx.x; unit < a.rows * segments; unit += gridDim.x) {
+    const int64_t row = unit / segments, from = (unit - row * segments) * pieces * P::kSize;
+    if (a.keep && !a.keep[row]) continue;
+    const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
+    const int off = pack_offset(x, a.n);
+    const int64_t end = min(from + (int64_t)pieces * P::kSize, (int64_t)a.n + off);
+    Apart s = sums_of<T, 16>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize, c);
+    s = block_join(s, c, a.scale, sums);
+    if (threadIdx.x == 0) part[unit] = s;
+    __syncthreads();
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t segments, const Apart* __restrict__ part) {
+  __shared__ Apart sums[16];
+  const float c = fminf(a.scale * kLog2e, FLT_MAX);
+  const int64_t row = blockIdx.x;   // a workgroup for every row
+  if (a.keep && !a.keep[row]) {
+    if (threadIdx.x == 0) write_nothing(o, row);
+    return;
+  }
+  Apart s = nothing();
+  for (int64_t i = threadIdx.x; i < segments; i += 1024) {
+    const Apart b = part[row * segments + i];
+    const float mx = fmaxf(s.mx, b.mx), mr = fmaxf(s.mr, b.mr);
+    const Apart p = rebase(s, mx, mr, c, a.scale), q = rebase(b, mx, mr, c, a.scale);
+    s = Apart{mx, mr, p.sx + q.sx, p.sr + q.sr, p.w + q.w, p.h + q.h, fmaxf(p.most, q.most)};
+  }
+  s = block_join(s, c, a.scale, sums);
+  if (threadIdx.x == 0) write_row(o, row, s);
+}
+
+// How rows are shared out.
+enum RowForm { kRowWave, kRowBlock, kRowSplit };
+struct RowPlan {
+  RowForm form;
+  int lane, waves;              // logits a lane, wavefronts
+  int64_t pieces, segments;     // kRowSplit
+};
+inline RowPlan plan_rows(int64_t rows, int64_t vocab) {
+  const int64_t n = vocab + 7;   // a row counted from its pack
+  if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, 0, 0};
+  const int64_t pieces = (n + 1023) / 1024;
+  if (n <= 64 * 2048 || rows >= 256) {
+    const int64_t long_rows = pieces >= 32 && rows >= 2048 ? 8 : std::clamp<int64_t>((pieces + 4) / 5, 1, 4);
+    return RowPlan{kRowBlock, 16, (int)std::max(long_rows, std::min<int64_t>({16, pieces, 4096 / rows})), 0, 0};
+  }
+  const int64_t per = std::clamp<int64_t>(rows * pieces / 2048, 4, 32);
+  return RowPlan{kRowSplit, 16, 4, per, (pieces + per - 1) / per};
+}
+
+// The gradients, element by element, with d = scale ((x - r) - (mx - mr)) and g = dkl:
+//   dx = g scale p (d - mean d under p),   dr = g scale (q - p)
+// Bound by memory: two reads and one or two writes of the logits. Laid out as the gradient of the token log probabilities.
+template <typename T, bool DX, bool DR, int G>
+__global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, const float* __restrict__ stats, const float* __restrict__ dkl, T* dx, int64_t ld_dx, T* dr,
+                                                    int64_t ld_dr) {
+  typedef typename Pack<T>::type pack;
+  constexpr int V = Pack<T>::n, kPacks = 2, kSpan = kPacks * G * V, kRows = kBlock / G;
+  const int lane = threadIdx.x % G, vocab = (int)a.n;
+  for (int64_t row = (int64_t)blockIdx.y * kRows + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.y * kRows) {
+    const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
+    T *out_x = DX ? dx + row * ld_dx : nullptr, *out_r = DR ? dr + row * ld_dr : nullptr;
+    const float* s = stats + 5 * row;
+    const float mx = s[0], ln_sx = s[1], mr = s[2], ln_sr = s[3], mean = s[4], g = a.keep && !a.keep[row] ? 0.f : dkl[row];
+    const bool zero = g == 0.f || (mx == -INFINITY && ln_sx == -INFINITY);
+    const bool r_empty = mr == -INFINITY;
+    const float A = zero ? 0.f : mean == INFINITY ? NAN : g * a.scale, dm = mx - mr;
+    auto gradient = [&](float u, float v, float& gx, float& gr) {
+      const float p = exp2_hw((a.scale * (u - mx) - ln_sx) * kLog2e);
+      if (DX) gx = A * (p * (__builtin_amdgcn_fmed3f(((u - v) - dm) * a.scale, -FLT_MAX, FLT_MAX) - mean));
+      if (DR) gr = A * ((r_empty ? 0.f : exp2_hw((a.scale * (v - mr) - ln_sr) * kLog2e)) - p);
+    };
+    const T* grid_row = DX ? out_x : out_r;
+    const int off = (int)((uintptr_t)grid_row / sizeof(T) % V);
+    for (int64_t first = (int64_t)((blockIdx.x + blockIdx.y / 64) % gridDim.x) * kSpan; first < (int64_t)vocab + off; first += (int64_t)gridDim.x * kSpan) {
+      const int begin = (int)first + lane * V - off;
+      pack in_x[kPacks], in_r[kPacks];
+#pragma unroll
+      for (int j = 0; j < kPacks; ++j) {
+        const int k = begin + j * G * V;
+        if (!zero && k >= 0 && k <= vocab - V) {
+          in_x[j] = __builtin_nontemporal_load((const pack*)(x + k));
+          in_r[j] = __builtin_nontemporal_load((const pack*)(r + k));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kPacks; ++j) {
+        const int k = begin + j * G * V;
+        if (k >= 0 && k <= vocab - V) {
+          pack o_x = {}, o_r = {};
+          if (!zero) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              float gx = 0.f, gr = 0.f;
+              gradient(to_f32(in_x[j][e]), to_f32(in_r[j][e]), gx, gr);
+              o_x[e] = from_f32<T>(gx);
+              o_r[e] = from_f32<T>(gr);
+            }
+          }
+          if (DX) __builtin_nontemporal_store(o_x, (pack*)(out_x + k));
+          if (DR) __builtin_nontemporal_store(o_r, (pack*)(out_r + k));
+        } else if (k > -V && k < vocab) {
+          for (int i = max(k, 0); i < min(k + V, vocab); ++i) {
+            float gx = 0.f, gr = 0.f;
+            if (!zero) gradient(to_f32(x[i]), to_f32(r[i]), gx, gr);
+            if (DX) out_x[i] = from_f32<T>(gx);
+            if (DR) out_r[i] = from_f32<T>(gr);
+          }
+        }
+      }
+    }
+  }
+}
+
+lopt_status check_logits(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, int64_t rows, int64_t vocab, uint32_t type, float scale) {
+  LOPT_CHECK(check_type("type", type));
+  LOPT_CHECK(check_matrix(rows, vocab, "vocab"));
+  if (vocab > LOPT_VOCAB_MAX) return fail_call(LOPT_ESHAPE, "vocab=%lld is above %d", (long long)vocab, LOPT_VOCAB_MAX);
+  LOPT_CHECK(check_ld("ld", rows, vocab, ld, false));
+  LOPT_CHECK(check_ld("ld_ref", rows, vocab, ld_ref, false));
+  if (!(scale > 0.f) || std::isinf(scale)) return fail_call(LOPT_EINVAL, "scale must be finite and > 0");
+  LOPT_CHECK(check_array("logits", logits, type_bytes(type), rows > 0));
+  return check_array("ref", ref, type_bytes(type), rows > 0);
+}
+
+}  // namespace
+}  // namespace lopt
+
+using namespace lopt;
+
+extern "C" {
+
+size_t lopt_token_kl_workspace(int64_t rows, int64_t vocab) {
+  if (rows <= 0 || vocab <= 0 || rows > 0x7fffffffLL || vocab > 0x7fffffffLL) return 0;
+  const RowPlan plan = plan_rows(rows, vocab);
+  return plan.form == kRowSplit ? (size_t)rows * (size_t)plan.segments * sizeof(Apart) : 0;
+}
+
+lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, const uint8_t* mask, int64_t rows, int64_t vocab, uint32_t type,
+                          float scale, float* kl, float* stats, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  LOPT_CHECK(check_logits(logits, ld, ref, ld_ref, rows, vocab, type, scale));
+  LOPT_CHECK(check_array("kl", kl, 4, rows > 0));
+  LOPT_CHECK(check_array("stats", stats, 4, rows > 0));
+  LOPT_CHECK(check_workspace(workspace, workspace_bytes, lopt_token_kl_workspace(rows, vocab)));
+  if (rows == 0) return LOPT_OK;
+  const Outputs o{kl, stats};
+  const RowPlan plan = plan_rows(rows, vocab);
+  hipStream_t stream = (hipStream_t)hip_stream;
+  with_type(type, [&](auto t) {
+    using T = decltype(t);
+    const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, mask};
+    const dim3 block(plan.waves * kWave);
+    if (plan.form == kRowWave) {
+      const dim3 grid((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 20));
+      auto kernel = plan.lane == 8 ? k_kl_short<T, 8> : plan.lane == 16 ? k_kl_short<T, 16> : k_kl_short<T, 32>;
+      hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, o);
+    } else if (plan.form == kRowBlock) {
+      hipLaunchKernelGGL((k_kl<T, 16>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), block, 0, stream, a, o);
+    } else {
+      Apart* part = (Apart*)workspace;
+      hipLaunchKernelGGL(k_kl_split<T>, dim3((unsigned)std::min<int64_t>(rows * plan.segments, 1 << 22)), block, 0, stream, a, plan.segments, (uint32_t)plan.pieces, part);
+      hipLaunchKernelGGL(k_kl_join<T>, dim3((unsigned)rows), dim3(1024), 0, stream, a, o, plan.segments, (const Apart*)part);
+    }
+  });
+  return launch_status("lopt_token_kl");
+}
+
+lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, const uint8_t* mask, const float* stats, const float* dkl,
+                                   void* dlogits, int64_t ld_d, void* dref, int64_t ld_dref, int64_t rows, int64_t vocab, uint32_t type, float scale,
+                                   void* hip_stream) {
+  LOPT_CHECK(check_logits(logits, ld, ref, ld_ref, rows, vocab, type, scale));
+  LOPT_CHECK(check_array("stats", stats, 4, rows > 0));
+  LOPT_CHECK(check_array("dkl", dkl, 4, rows > 0));
+  LOPT_CHECK(check_array("dlogits", dlogits, type_bytes(type), false));
+  LOPT_CHECK(check_array("dref", dref, type_bytes(type), false));
+  if (dlogits) LOPT_CHECK(check_ld("ld_d", rows, vocab, ld_d, true));
+  if (dref) LOPT_CHECK(check_ld("ld_dref", rows, vocab, ld_dref, true));
+  if (dlogits && dlogits == dref && rows > 0) return fail_call(LOPT_EINVAL, "dlogits and dref are the same memory");
+  const struct { const char* name; const void* out; int64_t ld; } outs[2] = {{"dlogits", dlogits, ld_d}, {"dref", dref, ld_dref}};
+  for (const auto& q : outs)
+    if (q.out && rows > 1 && ((q.out == logits && q.ld != ld) || (q.out == ref && q.ld != ld_ref)))
+      return fail_call(LOPT_EINVAL, "%s is an input, but its ld is not that input's", q.name);
+  if (rows == 0 || (!dlogits && !dref)) return LOPT_OK;
+  with_type(type, [&](auto t) {
+    using T = decltype(t);
+    const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, mask};
+    const int64_t packs = (vocab + 2 * Pack<T>::n - 2) / Pack<T>::n;   // that a row may touch
+    auto launch = [&](auto g) {
+      constexpr int G = decltype(g)::value, kSpan = 2 * G;
+      const int64_t spans = (packs + kSpan - kSpan / 8) / kSpan;
+      const dim3 grid((unsigned)std::clamp<int64_t>(spans, 1, 1024), (unsigned)std::min<int64_t>((rows + kBlock / G - 1) / (kBlock / G), 65535));
+      auto kernel = !dref ? k_kl_back<T, true, false, G> : !dlogits ? k_kl_back<T, false, true, G> : k_kl_back<T, true, true, G>;
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)hip_stream, a, stats, dkl, (T*)dlogits, ld_d, (T*)dref, ld_dref);
+    };
+    if (packs <= 2 * 16) launch(std::integral_constant<int, 16>{});
+    else if (packs <= 2 * 64) launch(std::integral_constant<int, 64>{});
+    else launch(std::integral_constant<int, kBlock>{});
+  });
+  return launch_status("lopt_token_kl_backward");
+}
+
+}  // extern "C"

@@ -5,7 +5,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "lopt_ops.h"
+#include "lopt_softmax.h"
 
 namespace lopt {
 namespace {
@@ -36,12 +36,6 @@ __device__ __forceinline__ float least_of(float bound) { return bound == 0.f ? -
 // less) adds 0; a row whose largest logit lies outside is summed again by extreme_sums.
 // A masked logit has t = -infinity and 2^t = 0; for the product t is held to a finite value.
 struct Soft { float m, s, h; };
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-constexpr float kMostBase = 268435456.f;
-
-__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
-__device__ __forceinline__ float base_of(float m, float c) { return __builtin_amdgcn_fmed3f(m * c, -kMostBase, kMostBase); }
-
 // a's sums seen from a larger m.
 __device__ __forceinline__ Soft rebase(Soft a, float m, float c) {
   const float diff = base_of(a.m, c) - base_of(m, c), f = exp2_hw(diff), fs = f * a.s;
@@ -51,8 +45,6 @@ __device__ __forceinline__ Soft wave_join(Soft a, float c) {
   a = rebase(a, wave_max(a.m), c);
   return Soft{a.m, wave_sum(a.s), wave_sum(a.h)};
 }
-
-__device__ __forceinline__ bool beyond(float m, float c) { return fabsf(m * c) >= kMostBase && m != -INFINITY; }   // see extreme_sums
 
 struct Outputs {
   float* logp;
@@ -95,80 +87,6 @@ __device__ __forceinline__ void write_row(const Outputs& o, int64_t r, int lane,
   }
 }
 
-// A wavefront takes a piece of a row at a time, E = 8 to 64 logits a lane in accesses of 16 bytes. Accesses are aligned: `off` elements ahead of the row
-// begin a pack of 16 bytes, and pieces and packs are counted from there (rows at odd elements of 16 bits: 4096x50257 98 us, 83 at 50258; counted from
-// their own start). The pack that would begin ahead of the row begins with it, the one that would pass the row's end ends
-// with it, and the elements that they share with the pack beside them are masked.
-template <typename T>
-__device__ __forceinline__ int pack_offset(const T* row, uint32_t n) {
-  return n >= (uint32_t)Pack<T>::n ? (int)((uintptr_t)row / sizeof(T) % Pack<T>::n) : 0;
-}
-template <typename T, int E>
-struct Piece {
-  static constexpr int V = Pack<T>::n, N = E / V, kSize = E * kWave;
-  typedef typename Pack<T>::type pack;
-  pack raw[N];
-  int first, off, n;
-  // Where the lane's pack j would begin, in elements of the row, and where it does.
-  __device__ __forceinline__ int place(int j) const { return first + (j * kWave + (int)(threadIdx.x & 63)) * V - off; }
-  __device__ __forceinline__ int begin(int j) const { return max(min(place(j), n - V), 0); }
-  __device__ __forceinline__ int index(int i) const { return begin(i / V) + i % V; }
-  // Whether an element is one, and this lane's.
-  __device__ __forceinline__ bool mine(int i) const {
-    const int p = place(i / V), k = index(i);
-    return k >= p && k < min(p + V, n);
-  }
-  // Element of lane 0 that the wavefront's j-th packs begin with: below 0, they begin ahead of the row; n or above, they lie behind it.
-  __device__ __forceinline__ int from(int j) const { return first + j * kWave * V - off; }
-  __device__ __forceinline__ void load(const T* row, int first_, int off_, int n_) {
-    first = first_, off = off_, n = n_;
-    if (n >= V) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) raw[j] = *(const pack*)(row + begin(j));
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i) raw[i / V][i % V] = mine(i) ? row[index(i)] : (T)-INFINITY;
-    }
-  }
-  // Elements that are not the lane's become masked ones, where they lie. Of a row's packs one wavefront's first and one's last are mixed.
-  __device__ __forceinline__ void mask() {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if (from(j) >= 0 && from(j) + kWave * V <= n) continue;
-      if (from(j) >= n) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) raw[j][e] = (T)-INFINITY;
-      } else {
-        raw[j] = masked(raw[j], j);
-      }
-    }
-  }
-  __device__ __forceinline__ pack masked(pack v, int j) const {
-    const int low = place(j) - begin(j), high = min(low + V, n - begin(j));   // of the pack's elements, the lane's
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = e >= low && e < high ? v[e] : (T)-INFINITY;
-    return v;
-  }
-  __device__ __forceinline__ void unpack(float (&x)[E]) {
-    mask();
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = to_f32(raw[i / V][i % V]);
-  }
-  // Pack j alone, read again (rows of a pack at least).
-  __device__ __forceinline__ void values(const T* row, int j, float (&x)[V]) const {
-    const pack v = masked(*(const pack*)(row + begin(j)), j);
-#pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = to_f32(v[e]);
-  }
-};
-
-template <int E>
-__device__ __forceinline__ float most_of(const float (&x)[E]) {
-  float m = x[0];
-#pragma unroll
-  for (int i = 1; i < E; ++i) m = fmaxf(m, x[i]);
-  return m;
-}
 template <int E>
 __device__ __forceinline__ void add_piece(Soft& a, const float (&x)[E], float most, float c) {
   const float m = fmaxf(a.m, most);

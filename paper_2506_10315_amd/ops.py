@@ -17,7 +17,8 @@ from .binding import _check, lib
 
 __all__ = ["clip_grads", "clip_grad_norm_", "grad_norm", "layer_norm", "layer_norm_forward", "layer_norm_backward",
            "dropout", "dropout_forward", "dropout_add_layer_norm", "dropout_add_layer_norm_forward", "dropout_add_layer_norm_backward",
-           "TokenLogprobs", "token_logprobs", "token_logprobs_forward", "token_logprobs_backward", "TOP_MAX"]
+           "TokenLogprobs", "token_logprobs", "token_logprobs_forward", "token_logprobs_backward", "TOP_MAX",
+           "token_kl", "token_kl_forward", "token_kl_backward"]
 
 TOP_MAX = 32          # LOPT_TOP_MAX
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # lopt_type
@@ -505,3 +506,69 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], scale:
     """token_logprobs_forward with gradients for the logits from logp and entropy. The mean of -logp over the tokens that are
     not ignored is the loss that LearnedOptTorch.step takes."""
     return TokenLogprobs(*_TokenLogprobs.apply(logits, targets, scale, top, ignore_index))
+
+
+# ---------------------------------------------------------------------------------------------- KL divergence to reference logits
+
+def _mask(mask: Optional[torch.Tensor], like: torch.Tensor, shape) -> Optional[torch.Tensor]:
+    return None if mask is None else _expect("mask", mask, like, torch.bool, shape)
+
+
+def _two_logits(logits: torch.Tensor, ref: torch.Tensor):
+    kind = _type("logits", logits)
+    if ref.shape != logits.shape or ref.dtype is not logits.dtype or ref.get_device() != logits.get_device():
+        raise ValueError(f"ref is {tuple(ref.shape)} of {ref.dtype} on {ref.device}; logits are {tuple(logits.shape)} of {logits.dtype} on {logits.device}")
+    x, rows, vocab, ld = _matrix("logits", logits)
+    r, _, _, ld_ref = _matrix("ref", ref)
+    return kind, x, ld, r, ld_ref, rows, vocab
+
+
+def token_kl_forward(logits: torch.Tensor, ref: torch.Tensor, scale: float = 1.0, mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(kl, stats): the KL divergence of softmax(scale * logits) from softmax(scale * ref) of every row, float32 of logits.shape[:-1], and what the
+    backward pass needs of the rows. `mask` (bool, logits.shape[:-1]): rows that count, the others have 0."""
+    kind, x, ld, r, ld_ref, rows, vocab = _two_logits(logits, ref)
+    shape, dev = logits.shape[:-1], logits.device
+    mask = _mask(mask, logits, shape)
+    kl = _floats(rows, shape, dev)
+    stats = _rows_of(rows, shape, 5, torch.float32, dev)
+    L = lib()
+    nbytes = L.lopt_token_kl_workspace(rows, vocab)
+    ws = _workspace(nbytes, dev)
+    _run(L.lopt_token_kl, dev.index, x.data_ptr(), ld, r.data_ptr(), ld_ref, _ptr(mask), rows, vocab, kind, scale, kl.data_ptr(), stats.data_ptr(), _ptr(ws), nbytes)
+    return kl, stats
+
+
+def token_kl_backward(logits: torch.Tensor, ref: torch.Tensor, stats: torch.Tensor, dkl: torch.Tensor, scale: float = 1.0, mask: Optional[torch.Tensor] = None,
+                      need: Tuple[bool, bool] = (True, False)) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dlogits, dref) from the gradient of kl; `need` says which are wanted, the others are None. `stats` is the forward pass's."""
+    kind, x, ld, r, ld_ref, rows, vocab = _two_logits(logits, ref)
+    shape = logits.shape[:-1]
+    mask = _mask(mask, logits, shape)
+    stats = _expect("stats", stats, logits, torch.float32, shape + (5,))
+    dkl = _expect("dkl", dkl, logits, torch.float32, shape)
+    dx, dr = (_new(t) if wanted else None for t, wanted in zip((logits, ref), need))
+    _run(lib().lopt_token_kl_backward, logits.get_device(), x.data_ptr(), ld, r.data_ptr(), ld_ref, _ptr(mask), stats.data_ptr(), dkl.data_ptr(), _ptr(dx), vocab,
+         _ptr(dr), vocab, rows, vocab, kind, scale)
+    return dx, dr
+
+
+class _TokenKl(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ref, scale, mask):
+        kl, stats = token_kl_forward(logits, ref, scale, mask)
+        ctx.save_for_backward(logits, ref, stats, mask)
+        ctx.scale = scale
+        return kl
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dkl):
+        logits, ref, stats, mask = ctx.saved_tensors
+        dx, dr = token_kl_backward(logits, ref, stats, dkl, ctx.scale, mask, ctx.needs_input_grad[:2])
+        return dx, dr, None, None
+
+
+def token_kl(logits: torch.Tensor, ref: torch.Tensor, scale: float = 1.0, mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """token_kl_forward's kl with gradients for logits and ref: as a policy's distance from its reference, which has no gradient, or, with a teacher's logits
+    first and the student's second, as the loss of a distillation."""
+    return _TokenKl.apply(logits, ref, scale, mask)
