@@ -382,6 +382,70 @@ lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* r
                                    int64_t ld_dref, int64_t rows, int64_t vocab, uint32_t type, float scale,
                                    void* hip_stream);
 
+/* Clipped policy loss over `seqs` sequences of up to `tokens` >= 1 tokens. Of each token, with ratio = e^(logp - old_logp), A its advantage:
+ *   surrogate = -min(ratio A, max(1 - clip_low, min(ratio, 1 + clip_high)) A)   (0 where A is 0),   clipped = whether the bound is what the min takes
+ *   kl = e^u - 1 - u with u = ref_logp - logp, or what `kl` holds, or 0;   drift = ratio - 1 - ln ratio
+ *   loss = mean(surrogate) + kl_coef mean(kl) - entropy_coef mean(entropy)
+ *   stats[8] = means of surrogate, kl, entropy, clipped, ratio, drift; tokens that count; sequences that have one
+ * Tokens whose mask byte is 0 do not count, whatever is in their places. per_sequence 0: the means are over all tokens that count; else over the
+ * sequences that have one, of the mean over each. Where nothing counts all of these are 0.
+ * logp, kl and entropy are float32, old_logp, advantages and ref_logp of the types that go with them; `ld_*`: distances of rows.
+ * advantage_per_sequence: advantages holds one value for each sequence, ld_advantages apart. ref_logp, kl, entropy and mask may be null; ref_logp and kl are not both
+ * given. 0 <= clip_low <= 1, clip_high >= 0 (infinite: no bound). counts[seqs]: tokens of each sequence that count, for the backward pass; it may be
+ * null where per_sequence is 0. workspace: lopt_policy_loss_workspace bytes, may be null where that is 0.
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE, LOPT_EHIP. */
+typedef struct {
+  const float* logp;       int64_t ld_logp;
+  const void* old_logp;    int64_t ld_old;
+  const void* advantages;  int64_t ld_advantages;
+  const void* ref_logp;    int64_t ld_ref;
+  const float* kl;         int64_t ld_kl;
+  const float* entropy;    int64_t ld_entropy;
+  const uint8_t* mask;     int64_t ld_mask;
+  int64_t seqs, tokens;
+  double clip_low, clip_high, kl_coef, entropy_coef;
+  uint32_t old_type, advantage_type, ref_type;   /* lopt_type */
+  uint32_t advantage_per_sequence, per_sequence, reserved;
+} lopt_policy;
+size_t lopt_policy_loss_workspace(int64_t seqs, int64_t tokens);
+lopt_status lopt_policy_loss(const lopt_policy* terms_host, float* loss, float* stats, float* counts, void* workspace,
+                             size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients from that of the loss, dloss[1], and the forward pass's stats and counts (null where per_sequence is 0), each seqs x tokens
+ * without gaps, 0 where a token does not count:
+ *   dlogp = dloss w (the slope of -min(...) + kl_coef (1 - e^u) where ref_logp is given),   dkl = dloss w kl_coef,   dentropy = -dloss w entropy_coef
+ * with w the token's share of the means. At a bound itself the slope is that of the ratio. Each may be null (not wanted); dkl needs kl, dentropy entropy. */
+lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float* stats, const float* counts, const float* dloss,
+                                      float* dlogp, float* dkl, float* dentropy, void* hip_stream);
+
+/* Loss of pairs of answers, of which the first is preferred: logp has 2 x pairs rows of up to `tokens` >= 1 tokens, the chosen answers in the first
+ * `pairs` rows, the rejected ones in the same order behind them. With s_j = sum of logp - ref over the tokens of row j that count (per token with `average`;
+ * 0 for a row that has none), m = s_chosen - s_rejected and z = beta m - margin:
+ *   LOPT_PREFERENCE_SIGMOID  -(1 - label_smoothing) ln sigma(z) - label_smoothing ln sigma(-z)
+ *   LOPT_PREFERENCE_HINGE    max(0, 1 - z)
+ *   LOPT_PREFERENCE_SQUARED  (m - 1 / (2 beta))^2     (margin and label_smoothing 0)
+ *   loss = mean over the pairs,   rewards[2 x pairs] = beta s,   stats[4] = means of m > 0, beta m, the chosen answers' rewards, the rejected ones'
+ *   coef[2 x pairs] = d loss / d logp of each row's tokens, for the backward pass
+ * ref: null (0), or of ref_type: 2 x pairs rows of tokens, or with ref_sums one value a row, its sum, ld_ref apart. mask: 2 x pairs rows of bytes, null: every token
+ * counts. Sums are in 64 bits. With zero pairs loss and stats are 0. beta > 0. workspace: lopt_preference_loss_workspace bytes, may be null where that is 0.
+ * Errors: LOPT_EINVAL, LOPT_ESHAPE, LOPT_EHIP. */
+typedef enum { LOPT_PREFERENCE_SIGMOID = 0, LOPT_PREFERENCE_HINGE = 1, LOPT_PREFERENCE_SQUARED = 2 } lopt_preference_kind;
+typedef struct {
+  const float* logp;    int64_t ld_logp;
+  const void* ref;      int64_t ld_ref;
+  const uint8_t* mask;  int64_t ld_mask;
+  int64_t pairs, tokens;
+  double beta, label_smoothing, margin;
+  uint32_t ref_type, ref_sums, kind, average;
+} lopt_preference;
+size_t lopt_preference_loss_workspace(int64_t pairs, int64_t tokens);
+lopt_status lopt_preference_loss(const lopt_preference* terms_host, float* loss, float* stats, float* rewards, float* coef,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradient, 2 x pairs rows of `tokens` without gaps: dlogp = dloss[0] coef[row] where a token counts, else 0. */
+lopt_status lopt_preference_loss_backward(const float* coef, const uint8_t* mask, int64_t ld_mask, const float* dloss, float* dlogp,
+                                          int64_t pairs, int64_t tokens, void* hip_stream);
+
 /* Message for the last non-OK status returned through this context ("" if none). With a
  * null ctx: the message of the last failed call without a context on this thread. */
 const char* lopt_last_error(const lopt_ctx* ctx);

@@ -121,6 +121,19 @@ def lib() -> C.CDLL:
     L.lopt_token_kl.restype = C.c_int
     L.lopt_token_kl_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, i64, i64, u32, f32, vp]
     L.lopt_token_kl_backward.restype = C.c_int
+    # the structs of the losses' terms are handed over as packed bytes
+    L.lopt_policy_loss_workspace.argtypes = [i64, i64]
+    L.lopt_policy_loss_workspace.restype = sz
+    L.lopt_policy_loss.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+    L.lopt_policy_loss.restype = C.c_int
+    L.lopt_policy_loss_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    L.lopt_policy_loss_backward.restype = C.c_int
+    L.lopt_preference_loss_workspace.argtypes = [i64, i64]
+    L.lopt_preference_loss_workspace.restype = sz
+    L.lopt_preference_loss.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
+    L.lopt_preference_loss.restype = C.c_int
+    L.lopt_preference_loss_backward.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp]
+    L.lopt_preference_loss_backward.restype = C.c_int
     L.lopt_last_error.argtypes = [vp]
     L.lopt_last_error.restype = C.c_char_p
     _lib = L

@@ -28,6 +28,7 @@ UNITS = [
     ("lopt_dropout.hip", "dropout", []),
     ("lopt_add_norm.hip", "add_norm", []),
     ("lopt_kl.hip", "kl", []),
+    ("lopt_losses.hip", "losses", []),
 ]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,596 @@
+// Losses made of tokens' log probabilities, and their gradients: the clipped policy loss with KL and entropy terms, and the loss of pairs of
+// answers. A few operations a token, then sums over tokens, sequences and the batch in a fixed order, in 64 bits. Bound by memory where there are
+// millions of tokens, else by the launches: one workgroup does a small batch in one launch, more leave partial sums to a second launch of one.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "lopt_flat.h"
+
+namespace lopt {
+namespace {
+
+constexpr int kJoin = 1024;          // threads of the workgroup that joins, and of the one that does everything
+constexpr int kQuad = 4;             // neighbouring tokens of a lane
+constexpr int64_t kAlone = 16384;    // tokens up to which one workgroup does everything
+
+// Sum over groups of G lanes, a power of two up to 64; every lane gets it.
+template <typename V>
+__device__ __forceinline__ V lanes_sum(V v, int G) {
+  for (int d = 1; d < G; d *= 2) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Four neighbouring elements from element i on, `count` of them there.
+template <typename T>
+__device__ __forceinline__ void load_quad_as(const T* p, int count, float (&v)[kQuad]) {
+  typedef T quad __attribute__((ext_vector_type(kQuad), aligned(sizeof(T))));
+  if (count >= kQuad) {
+    const quad q = *(const quad*)p;
+#pragma unroll
+    for (int e = 0; e < kQuad; ++e) v[e] = to_f32(q[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kQuad; ++e) v[e] = e < count ? to_f32(p[e]) : 0.f;
+  }
+}
+__device__ __forceinline__ void load_quad_of(const void* p, uint32_t type, int64_t i, int count, float (&v)[kQuad]) {
+  if (type == LOPT_F32) load_quad_as((const float*)p + i, count, v);
+  else if (type == LOPT_BF16) load_quad_as((const bf16_t*)p + i, count, v);
+  else load_quad_as((const f16_t*)p + i, count, v);
+}
+__device__ __forceinline__ float load_one_of(const void* p, uint32_t type, int64_t i) {
+  return type == LOPT_F32 ? ((const float*)p)[i] : type == LOPT_BF16 ? to_f32(((const bf16_t*)p)[i]) : to_f32(((const f16_t*)p)[i]);
+}
+// Bit e: whether token e of the four is there and counts.
+__device__ __forceinline__ uint32_t load_mask(const uint8_t* mask, int64_t i, int count) {
+  typedef uint8_t quad __attribute__((ext_vector_type(kQuad), aligned(1)));
+  uint32_t bits = count >= kQuad ? 15u : (1u << count) - 1u;
+  if (!mask) return bits;
+  if (count >= kQuad) {
+    const quad q = *(const quad*)(mask + i);
+    return (q[0] ? 1u : 0u) | (q[1] ? 2u : 0u) | (q[2] ? 4u : 0u) | (q[3] ? 8u : 0u);
+  }
+  for (int e = 0; e < count; ++e)
+    if (!mask[i + e]) bits &= ~(1u << e);
+  return bits;
+}
+
+// How sequences are shared out: a group of `lanes` lanes takes a sequence, or one of its `pieces` of `length` tokens, four neighbouring tokens a lane in turn.
+// Few sequences are cut so that there are about 1024 pieces; a power of two of them, with which kJoin lanes of the join share out a sequence.
+struct Plan {
+  int lanes, threads;
+  int64_t pieces, length, units, blocks;
+  bool alone;
+};
+inline Plan plan_of(int64_t seqs, int64_t tokens) {
+  Plan p{};
+  p.lanes = tokens <= 64 ? 16 : tokens <= 256 ? 64 : kBlock;
+  p.alone = seqs * tokens <= kAlone && seqs * ((tokens + kQuad * p.lanes - 1) / (kQuad * p.lanes)) * p.lanes <= kAlone / kQuad;   // seqs * tokens < 2^62
+  p.pieces = 1;
+  if (!p.alone && p.lanes == kBlock)
+    while (p.pieces < 1024 && p.pieces * seqs < 1024 && p.pieces * kQuad * kBlock < tokens) p.pieces *= 2;
+  p.length = ((tokens + p.pieces - 1) / p.pieces + kQuad - 1) / kQuad * kQuad;
+  p.units = seqs * p.pieces;
+  p.threads = p.alone ? kJoin : kBlock;
+  const int64_t groups = p.threads / p.lanes;
+  // units of whole sequences go round and leave one partial sum a workgroup, pieces one each
+  p.blocks = p.alone ? 1 : p.pieces > 1 ? p.units : std::clamp<int64_t>((p.units + groups - 1) / groups, 1, 2048);
+  return p;
+}
+template <typename F>
+void with_lanes(int lanes, F&& f) {
+  if (lanes == 16) f(std::integral_constant<int, 16>{});
+  else if (lanes == 64) f(std::integral_constant<int, 64>{});
+  else f(std::integral_constant<int, kBlock>{});
+}
+
+// Sum over a group of G lanes of a workgroup that is a multiple of it; `red` has a value for each wavefront. Every wavefront of the workgroup calls it.
+template <int G, typename V>
+__device__ __forceinline__ V group_total(V v, V* red) {
+  if (G < kWave) return lanes_sum(v, G);
+  v = wave_sum(v);
+  if (G > kWave) {
+    constexpr int W = G / kWave;
+    const int wave = threadIdx.x >> 6, first = wave / W * W;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[wave] = v;
+    __syncthreads();
+    v = red[first];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v += red[first + i];
+  }
+  return v;
+}
+// Over the workgroup.
+template <typename V>
+__device__ __forceinline__ V block_total(V v, V* red) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  V s = red[0];
+  for (unsigned i = 1; i < blockDim.x / kWave; ++i) s += red[i];
+  return s;
+}
+
+// ---------------------------------------------------------------------------------------------- policy loss
+
+// e^v - 1 - v, for small v by its series, of which the first term left out is 1e-10 of the sum at 0.5.
+__device__ __forceinline__ float exp_rest(float v) {
+  if (!(fabsf(v) < 0.5f)) return expm1f(v) - v;
+  float s = 1.f / 3628800.f;
+  s = s * v + 1.f / 362880.f;
+  s = s * v + 1.f / 40320.f;
+  s = s * v + 1.f / 5040.f;
+  s = s * v + 1.f / 720.f;
+  s = s * v + 1.f / 120.f;
+  s = s * v + 1.f / 24.f;
+  s = s * v + 1.f / 6.f;
+  s = s * v + 0.5f;
+  return s * (v * v);
+}
+
+// A token's terms. Which side of a bound the ratio lies on, which decides over the whole gradient, is found in 64 bits, where the difference of the logarithms has
+// no rounding that matters; its values are in 32.
+struct Bounds { double low, high; float at_low, at_high; };   // ln(1 - clip_low), ln(1 + clip_high) and what they are the logarithms of
+struct Terms { float surrogate, kl, ratio, drift, slope; bool clipped; };
+__device__ __forceinline__ Terms token_terms(float logp, float old, float adv, const Bounds& b, bool has_ref, float ref, float kl_coef) {
+  Terms t{};
+  const double d = (double)logp - (double)old;
+  t.drift = exp_rest((float)d);
+  t.ratio = expf((float)d);
+  t.clipped = adv > 0.f ? d > b.high : adv < 0.f && d < b.low;
+  const float bound = adv > 0.f ? b.at_high : b.at_low;
+  t.surrogate = adv == 0.f ? 0.f : -adv * (t.clipped ? bound : t.ratio);
+  t.slope = t.clipped ? 0.f : t.surrogate;
+  if (has_ref) {
+    const float u = ref - logp;
+    t.kl = exp_rest(u);
+    t.slope -= kl_coef * (t.kl + u);   // d kl / d logp = 1 - e^u
+  }
+  return t;
+}
+
+// Sums in the order of the stats: surrogate, kl, entropy, clipped, ratio, drift, tokens, sequences.
+constexpr int kSums = 8;
+
+__device__ __forceinline__ void write_policy(const double (&sum)[kSums], const lopt_policy& a, float* loss, float* stats) {
+  const double n = a.per_sequence ? sum[7] : sum[6], w = n > 0.0 ? 1.0 / n : 0.0;
+  double mean[6];
+#pragma unroll
+  for (int i = 0; i < 6; ++i) mean[i] = n > 0.0 ? sum[i] * w : 0.0;
+  double v = mean[0];
+  if (a.ref_logp || a.kl) v += a.kl_coef * mean[1];
+  if (a.entropy) v -= a.entropy_coef * mean[2];
+  *loss = (float)v;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) stats[i] = (float)mean[i];
+  stats[6] = (float)sum[6];
+  stats[7] = (float)sum[7];
+}
+
+// The sums of units of whole sequences (`pieces` is 1), one row of them a workgroup, or of pieces, one row each; with `alone` the loss.
+template <int G, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_policy(lopt_policy a, Bounds b, int64_t pieces, int64_t length, int64_t units, double* __restrict__ part, bool alone,
+                                                     float* __restrict__ loss, float* __restrict__ stats, float* __restrict__ counts) {
+  __shared__ double red[kThreads / kWave];
+  const int lane = threadIdx.x % G;
+  constexpr int kGroups = kThreads / G;
+  double sum[kSums] = {};
+  const float kl_coef = (float)a.kl_coef;
+  // every wavefront goes through the loop as often, for the barriers of the group's sums
+  for (int64_t base = (int64_t)blockIdx.x * kGroups; base < units; base += (int64_t)gridDim.x * kGroups) {
+    const int64_t unit = base + threadIdx.x / G;
+    const bool have = unit < units;
+    const int64_t seq = have ? unit / pieces : 0, from = have ? (unit - seq * pieces) * length : 0, to = have ? min(from + length, a.tokens) : 0;
+    double own[7] = {};
+    const float adv_seq = have && a.advantage_per_sequence ? load_one_of(a.advantages, a.advantage_type, seq * a.ld_advantages) : 0.f;
+    for (int64_t t = from + lane * kQuad; t < to; t += G * kQuad) {
+      const int count = (int)min(to - t, (int64_t)kQuad);
+      float logp[kQuad], old[kQuad], adv[kQuad] = {adv_seq, adv_seq, adv_seq, adv_seq}, ref[kQuad] = {}, kl[kQuad] = {}, ent[kQuad] = {};
+      const uint32_t bits = load_mask(a.mask, seq * a.ld_mask + t, count);
+      load_quad_as(a.logp + seq * a.ld_logp + t, count, logp);
+      load_quad_of(a.old_logp, a.old_type, seq * a.ld_old + t, count, old);
+      if (!a.advantage_per_sequence) load_quad_of(a.advantages, a.advantage_type, seq * a.ld_advantages + t, count, adv);
+      if (a.ref_logp) load_quad_of(a.ref_logp, a.ref_type, seq * a.ld_ref + t, count, ref);
+      if (a.kl) load_quad_as(a.kl + seq * a.ld_kl + t, count, kl);
+      if (a.entropy) load_quad_as(a.entropy + seq * a.ld_entropy + t, count, ent);
+#pragma unroll
+      for (int e = 0; e < kQuad; ++e) {
+        const Terms q = token_terms(logp[e], old[e], adv[e], b, a.ref_logp != nullptr, ref[e], kl_coef);
+        const bool counts_in = bits >> e & 1;
+        own[0] += counts_in ? (double)q.surrogate : 0.0;
+        own[1] += counts_in ? (double)(a.kl ? kl[e] : q.kl) : 0.0;
+        own[2] += counts_in ? (double)ent[e] : 0.0;
+        own[3] += counts_in && q.clipped ? 1.0 : 0.0;
+        own[4] += counts_in ? (double)q.ratio : 0.0;
+        own[5] += counts_in ? (double)q.drift : 0.0;
+        own[6] += counts_in ? 1.0 : 0.0;
+      }
+    }
+    if (pieces == 1) {   // the sequence is whole
+      const double n = group_total<G>(own[6], red);
+      const double w = a.per_sequence && n > 0.0 ? 1.0 / n : 1.0;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) sum[i] += w * own[i];
+      sum[6] += own[6];
+      if (lane == 0 && have) {
+        sum[7] += n > 0.0 ? 1.0 : 0.0;
+        if (counts) counts[seq] = (float)n;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 7; ++i) sum[i] += own[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) sum[i] = block_total(sum[i], red);
+  if (threadIdx.x != 0) return;
+  if (alone) {
+    write_policy(sum, a, loss, stats);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) part[(int64_t)blockIdx.x * kSums + i] = sum[i];
+  }
+}
+
+// Joins `rows` rows of sums. Of pieces, `lanes` lanes take a sequence.
+__global__ __launch_bounds__(kJoin) void k_policy_join(lopt_policy a, int64_t rows, int64_t pieces, const double* __restrict__ part, float* __restrict__ loss,
+                                                       float* __restrict__ stats, float* __restrict__ counts) {
+  __shared__ double red[kJoin / kWave];
+  double sum[kSums] = {};
+  if (pieces == 1) {
+    for (int64_t k = threadIdx.x; k < rows; k += kJoin) {
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) sum[i] += part[k * kSums + i];
+    }
+  } else {
+    const int lanes = (int)min(pieces, (int64_t)kWave), lane = threadIdx.x % lanes;
+    for (int64_t base = 0; base < a.seqs; base += kJoin / lanes) {
+      const int64_t seq = base + threadIdx.x / lanes;
+      double own[7] = {};
+      if (seq < a.seqs) {
+        for (int64_t k = lane; k < pieces; k += lanes) {
+#pragma unroll
+          for (int i = 0; i < 7; ++i) own[i] += part[(seq * pieces + k) * kSums + i];
+        }
+      }
+      const double n = lanes_sum(own[6], lanes), w = a.per_sequence && n > 0.0 ? 1.0 / n : 1.0;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) sum[i] += w * own[i];
+      sum[6] += own[6];
+      if (lane == 0 && seq < a.seqs) {
+        sum[7] += n > 0.0 ? 1.0 : 0.0;
+        if (counts) counts[seq] = (float)n;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) sum[i] = block_total(sum[i], red);
+  if (threadIdx.x == 0) write_policy(sum, a, loss, stats);
+}
+
+__device__ __forceinline__ void store_quad_of(float* p, int count, const float (&v)[kQuad]) {
+  typedef float quad __attribute__((ext_vector_type(kQuad), aligned(4)));
+  if (count >= kQuad) {
+    *(quad*)p = quad{v[0], v[1], v[2], v[3]};
+  } else {
+    for (int e = 0; e < count; ++e) p[e] = v[e];
+  }
+}
+
+// The gradients, four tokens a thread, all terms formed again.
+__global__ __launch_bounds__(kBlock) void k_policy_back(lopt_policy a, Bounds b, Flat f, const float* __restrict__ stats, const float* __restrict__ counts,
+                                                        const float* __restrict__ dloss, float* __restrict__ dlogp, float* __restrict__ dkl, float* __restrict__ dentropy) {
+  const float up = *dloss, whole = stats[a.per_sequence ? 7 : 6];
+  const float kl_coef = (float)a.kl_coef, entropy_coef = (float)a.entropy_coef;
+  for (int64_t first = (int64_t)blockIdx.x * kBlock; first < f.total; first += (int64_t)gridDim.x * kBlock) {
+    const Chunk chunk(f, first);
+    int64_t seq;
+    uint32_t t;
+    if (!chunk.at(f, kQuad, threadIdx.x, seq, t)) continue;
+    const int count = (int)min(f.cols - t, (uint32_t)kQuad);
+    const uint32_t bits = load_mask(a.mask, seq * a.ld_mask + t, count);
+    // of a token that counts there are a sequence that has one and a batch that has one
+    const float w = up / (a.per_sequence ? whole * counts[seq] : whole);
+    if (dlogp) {
+      const float adv_seq = a.advantage_per_sequence ? load_one_of(a.advantages, a.advantage_type, seq * a.ld_advantages) : 0.f;
+      float logp[kQuad], old[kQuad], adv[kQuad] = {adv_seq, adv_seq, adv_seq, adv_seq}, ref[kQuad] = {}, o[kQuad];
+      load_quad_as(a.logp + seq * a.ld_logp + t, count, logp);
+      load_quad_of(a.old_logp, a.old_type, seq * a.ld_old + t, count, old);
+      if (!a.advantage_per_sequence) load_quad_of(a.advantages, a.advantage_type, seq * a.ld_advantages + t, count, adv);
+      if (a.ref_logp) load_quad_of(a.ref_logp, a.ref_type, seq * a.ld_ref + t, count, ref);
+#pragma unroll
+      for (int e = 0; e < kQuad; ++e)
+        o[e] = bits >> e & 1 ? w * token_terms(logp[e], old[e], adv[e], b, a.ref_logp != nullptr, ref[e], kl_coef).slope : 0.f;
+      store_quad_of(dlogp + seq * a.tokens + t, count, o);
+    }
+    auto same = [&](float* out, float v) {
+      float o[kQuad];
+#pragma unroll
+      for (int e = 0; e < kQuad; ++e) o[e] = bits >> e & 1 ? v : 0.f;
+      store_quad_of(out + seq * a.tokens + t, count, o);
+    };
+    if (dkl) same(dkl, w * kl_coef);
+    if (dentropy) same(dentropy, -w * entropy_coef);
+  }
+}
+
+lopt_status check_policy(const lopt_policy* a) {
+  if (!a) return fail_call(LOPT_EINVAL, "terms_host is null");
+  LOPT_CHECK(check_matrix(a->seqs, a->tokens, "tokens"));
+  LOPT_CHECK(check_type("old_type", a->old_type));
+  LOPT_CHECK(check_type("advantage_type", a->advantage_type));
+  LOPT_CHECK(check_type("ref_type", a->ref_type));
+  const bool any = a->seqs > 0;
+  LOPT_CHECK(check_array("logp", a->logp, 4, any));
+  LOPT_CHECK(check_array("old_logp", a->old_logp, type_bytes(a->old_type), any));
+  LOPT_CHECK(check_array("advantages", a->advantages, type_bytes(a->advantage_type), any));
+  LOPT_CHECK(check_array("ref_logp", a->ref_logp, type_bytes(a->ref_type), false));
+  LOPT_CHECK(check_array("kl", a->kl, 4, false));
+  LOPT_CHECK(check_array("entropy", a->entropy, 4, false));
+  LOPT_CHECK(check_ld("ld_logp", a->seqs, a->tokens, a->ld_logp, false));
+  LOPT_CHECK(check_ld("ld_old", a->seqs, a->tokens, a->ld_old, false));
+  LOPT_CHECK(check_ld("ld_advantages", a->seqs, a->tokens, a->ld_advantages, false));
+  if (a->ref_logp) LOPT_CHECK(check_ld("ld_ref", a->seqs, a->tokens, a->ld_ref, false));
+  if (a->kl) LOPT_CHECK(check_ld("ld_kl", a->seqs, a->tokens, a->ld_kl, false));
+  if (a->entropy) LOPT_CHECK(check_ld("ld_entropy", a->seqs, a->tokens, a->ld_entropy, false));
+  if (a->mask) LOPT_CHECK(check_ld("ld_mask", a->seqs, a->tokens, a->ld_mask, false));
+  if (a->ref_logp && a->kl) return fail_call(LOPT_EINVAL, "ref_logp and kl are both given");
+  if (!(a->clip_low >= 0.0 && a->clip_low <= 1.0)) return fail_call(LOPT_EINVAL, "clip_low must be in [0, 1]");
+  if (!(a->clip_high >= 0.0)) return fail_call(LOPT_EINVAL, "clip_high must be >= 0");
+  if (!std::isfinite(a->kl_coef) || !std::isfinite(a->entropy_coef)) return fail_call(LOPT_EINVAL, "kl_coef and entropy_coef must be finite");
+  return LOPT_OK;
+}
+Bounds bounds_of(const lopt_policy& a) { return Bounds{std::log1p(-a.clip_low), std::log1p(a.clip_high), (float)(1.0 - a.clip_low), (float)(1.0 + a.clip_high)}; }
+
+// ---------------------------------------------------------------------------------------------- preference loss
+
+struct Answer { double sum, count; };   // of log ratios, and of the tokens that count
+
+// What the join of a pair gives: loss and statistics added up over the pairs, what the backward pass needs written.
+struct PairOutputs {
+  float* loss;
+  float* stats;
+  float* rewards;
+  float* coef;
+};
+constexpr int kPairSums = 5;   // loss, right ones, margins, rewards of the chosen, of the rejected
+
+__device__ __forceinline__ void write_pair(const lopt_preference& a, int64_t pair, Answer chosen, Answer rejected, const PairOutputs& o, double (&sum)[kPairSums]) {
+  if (a.ref && a.ref_sums) {
+    chosen.sum -= load_one_of(a.ref, a.ref_type, pair * a.ld_ref);
+    rejected.sum -= load_one_of(a.ref, a.ref_type, (a.pairs + pair) * a.ld_ref);
+  }
+  double per[2] = {1.0, 1.0};
+  if (a.average) {
+    per[0] = fmax(chosen.count, 1.0);
+    per[1] = fmax(rejected.count, 1.0);
+    chosen.sum /= per[0];
+    rejected.sum /= per[1];
+  }
+  const double m = chosen.sum - rejected.sum, z = a.beta * m - a.margin;
+  double loss, slope;   // slope: d loss / d m
+  if (a.kind == LOPT_PREFERENCE_SIGMOID) {
+    const double soft = log1p(exp(-fabs(z))), s = a.label_smoothing;
+    loss = (1.0 - s) * (fmax(-z, 0.0) + soft) + s * (fmax(z, 0.0) + soft);
+    slope = a.beta * (1.0 / (1.0 + exp(-z)) - (1.0 - s));
+  } else if (a.kind == LOPT_PREFERENCE_HINGE) {
+    loss = fmax(1.0 - z, 0.0);
+    slope = z < 1.0 ? -a.beta : 0.0;
+  } else {
+    const double off = m - 0.5 / a.beta;
+    loss = off * off;
+    slope = 2.0 * off;
+  }
+  if (z != z) loss = slope = z;   // a NaN is not less than a bound
+  slope /= (double)a.pairs;
+  const double rc = a.beta * chosen.sum, rr = a.beta * rejected.sum;
+  o.rewards[pair] = (float)rc;
+  o.rewards[a.pairs + pair] = (float)rr;
+  o.coef[pair] = (float)(slope / per[0]);
+  o.coef[a.pairs + pair] = (float)(-slope / per[1]);
+  sum[0] += loss;
+  sum[1] += m > 0.0 ? 1.0 : 0.0;
+  sum[2] += a.beta * m;
+  sum[3] += rc;
+  sum[4] += rr;
+}
+
+// All pairs, by one workgroup of kJoin threads; `lanes` lanes take a pair.
+__device__ __forceinline__ void join_pairs(const lopt_preference& a, int64_t pieces, const Answer* part, const PairOutputs& o, double* red) {
+  double sum[kPairSums] = {};
+  const int lanes = (int)min(pieces, (int64_t)kWave), lane = threadIdx.x % lanes;
+  for (int64_t base = 0; base < a.pairs; base += kJoin / lanes) {
+    const int64_t pair = base + threadIdx.x / lanes;
+    Answer own[2] = {};
+    if (pair < a.pairs) {
+      for (int64_t k = lane; k < pieces; k += lanes) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const Answer q = part[(i * a.pairs + pair) * pieces + k];
+          own[i].sum += q.sum;
+          own[i].count += q.count;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      own[i].sum = lanes_sum(own[i].sum, lanes);
+      own[i].count = lanes_sum(own[i].count, lanes);
+    }
+    if (lane == 0 && pair < a.pairs) write_pair(a, pair, own[0], own[1], o, sum);
+  }
+#pragma unroll
+  for (int i = 0; i < kPairSums; ++i) sum[i] = block_total(sum[i], red);
+  if (threadIdx.x == 0) {
+    const double w = a.pairs > 0 ? 1.0 / (double)a.pairs : 0.0;
+    *o.loss = (float)(sum[0] * w);
+#pragma unroll
+    for (int i = 1; i < kPairSums; ++i) o.stats[i - 1] = (float)(sum[i] * w);
+  }
+}
+
+template <int G, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_preference(lopt_preference a, int64_t pieces, int64_t length, int64_t units, Answer* part, bool alone, PairOutputs o) {
+  __shared__ double red[kThreads / kWave];
+  const int lane = threadIdx.x % G;
+  constexpr int kGroups = kThreads / G;
+  const bool has_ref = a.ref && !a.ref_sums;
+  for (int64_t base = (int64_t)blockIdx.x * kGroups; base < units; base += (int64_t)gridDim.x * kGroups) {
+    const int64_t unit = base + threadIdx.x / G;
+    const bool have = unit < units;
+    const int64_t seq = have ? unit / pieces : 0, from = have ? (unit - seq * pieces) * length : 0, to = have ? min(from + length, a.tokens) : 0;
+    double sum = 0.0, n = 0.0;
+    for (int64_t t = from + lane * kQuad; t < to; t += G * kQuad) {
+      const int count = (int)min(to - t, (int64_t)kQuad);
+      float logp[kQuad], ref[kQuad] = {};
+      const uint32_t bits = load_mask(a.mask, seq * a.ld_mask + t, count);
+      load_quad_as(a.logp + seq * a.ld_logp + t, count, logp);
+      if (has_ref) load_quad_of(a.ref, a.ref_type, seq * a.ld_ref + t, count, ref);
+#pragma unroll
+      for (int e = 0; e < kQuad; ++e) sum += bits >> e & 1 ? (double)logp[e] - (double)ref[e] : 0.0;
+      n += (double)__popc(bits);
+    }
+    sum = group_total<G>(sum, red);
+    n = group_total<G>(n, red);
+    if (lane == 0 && have) part[unit] = Answer{sum, n};
+  }
+  if (alone) {
+    __syncthreads();   // the workgroup's own partial sums
+    join_pairs(a, pieces, part, o, red);
+  }
+}
+__global__ __launch_bounds__(kJoin) void k_preference_join(lopt_preference a, int64_t pieces, const Answer* __restrict__ part, PairOutputs o) {
+  __shared__ double red[kJoin / kWave];
+  join_pairs(a, pieces, part, o, red);
+}
+
+__global__ __launch_bounds__(kBlock) void k_preference_back(const float* __restrict__ coef, const uint8_t* __restrict__ mask, int64_t ld_mask, const float* __restrict__ dloss,
+                                                            float* __restrict__ dlogp, Flat f) {
+  const float up = *dloss;
+  for (int64_t first = (int64_t)blockIdx.x * kBlock; first < f.total; first += (int64_t)gridDim.x * kBlock) {
+    const Chunk chunk(f, first);
+    int64_t seq;
+    uint32_t t;
+    if (!chunk.at(f, kQuad, threadIdx.x, seq, t)) continue;
+    const int count = (int)min(f.cols - t, (uint32_t)kQuad);
+    const uint32_t bits = load_mask(mask, seq * ld_mask + t, count);
+    const float v = up * coef[seq];
+    float o[kQuad];
+#pragma unroll
+    for (int e = 0; e < kQuad; ++e) o[e] = bits >> e & 1 ? v : 0.f;
+    store_quad_of(dlogp + seq * (int64_t)f.cols + t, count, o);
+  }
+}
+
+unsigned flat_blocks(const Flat& f) { return (unsigned)std::min<int64_t>((f.total + kBlock - 1) / kBlock, 1 << 22); }
+
+}  // namespace
+}  // namespace lopt
+
+using namespace lopt;
+
+extern "C" {
+
+size_t lopt_policy_loss_workspace(int64_t seqs, int64_t tokens) {
+  if (seqs < 0 || tokens <= 0 || seqs > 0x7fffffffLL || tokens > 0x7fffffffLL) return 0;
+  const Plan p = plan_of(seqs, tokens);
+  return p.alone ? 0 : (size_t)p.blocks * kSums * sizeof(double);
+}
+
+lopt_status lopt_policy_loss(const lopt_policy* terms_host, float* loss, float* stats, float* counts, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  LOPT_CHECK(check_policy(terms_host));
+  const lopt_policy a = *terms_host;
+  LOPT_CHECK(check_array("loss", loss, 4, true));
+  LOPT_CHECK(check_array("stats", stats, 4, true));
+  LOPT_CHECK(check_array("counts", counts, 4, a.per_sequence && a.seqs > 0));
+  LOPT_CHECK(check_workspace(workspace, workspace_bytes, lopt_policy_loss_workspace(a.seqs, a.tokens)));
+  const Plan p = plan_of(a.seqs, a.tokens);
+  hipStream_t stream = (hipStream_t)hip_stream;
+  double* part = (double*)workspace;
+  with_lanes(p.lanes, [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    auto kernel = p.alone ? k_policy<G, kJoin> : k_policy<G, kBlock>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, bounds_of(a), p.pieces, p.length, p.units, part, p.alone, loss, stats, counts);
+  });
+  if (!p.alone) hipLaunchKernelGGL(k_policy_join, dim3(1), dim3(kJoin), 0, stream, a, p.blocks, p.pieces, (const double*)part, loss, stats, counts);
+  return launch_status("lopt_policy_loss");
+}
+
+lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float* stats, const float* counts, const float* dloss, float* dlogp, float* dkl,
+                                      float* dentropy, void* hip_stream) {
+  LOPT_CHECK(check_policy(terms_host));
+  const lopt_policy a = *terms_host;
+  LOPT_CHECK(check_array("stats", stats, 4, true));
+  LOPT_CHECK(check_array("counts", counts, 4, a.per_sequence && a.seqs > 0));
+  LOPT_CHECK(check_array("dloss", dloss, 4, true));
+  LOPT_CHECK(check_array("dlogp", dlogp, 4, false));
+  LOPT_CHECK(check_array("dkl", dkl, 4, false));
+  LOPT_CHECK(check_array("dentropy", dentropy, 4, false));
+  if (dkl && !a.kl) return fail_call(LOPT_EINVAL, "dkl without kl");
+  if (dentropy && !a.entropy) return fail_call(LOPT_EINVAL, "dentropy without entropy");
+  if (a.seqs == 0 || !(dlogp || dkl || dentropy)) return LOPT_OK;
+  const Flat f = flat_of(a.seqs, a.tokens, kQuad);
+  hipLaunchKernelGGL(k_policy_back, dim3(flat_blocks(f)), dim3(kBlock), 0, (hipStream_t)hip_stream, a, bounds_of(a), f, stats, counts, dloss, dlogp, dkl, dentropy);
+  return launch_status("lopt_policy_loss_backward");
+}
+
+size_t lopt_preference_loss_workspace(int64_t pairs, int64_t tokens) {
+  if (pairs <= 0 || tokens <= 0 || pairs > 0x3fffffffLL || tokens > 0x7fffffffLL) return 0;
+  return (size_t)plan_of(2 * pairs, tokens).units * sizeof(Answer);
+}
+
+lopt_status lopt_preference_loss(const lopt_preference* terms_host, float* loss, float* stats, float* rewards, float* coef, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+  if (!terms_host) return fail_call(LOPT_EINVAL, "terms_host is null");
+  const lopt_preference a = *terms_host;
+  if (a.pairs < 0 || a.pairs > 0x3fffffffLL) return fail_call(LOPT_ESHAPE, "pairs=%lld outside [0, 2^30-1]", (long long)a.pairs);
+  LOPT_CHECK(check_matrix(2 * a.pairs, a.tokens, "tokens"));
+  LOPT_CHECK(check_type("ref_type", a.ref_type));
+  const bool any = a.pairs > 0;
+  LOPT_CHECK(check_array("logp", a.logp, 4, any));
+  LOPT_CHECK(check_array("ref", a.ref, type_bytes(a.ref_type), false));
+  LOPT_CHECK(check_ld("ld_logp", 2 * a.pairs, a.tokens, a.ld_logp, false));
+  if (a.ref) LOPT_CHECK(check_ld("ld_ref", 2 * a.pairs, a.tokens, a.ld_ref, false));
+  if (a.mask) LOPT_CHECK(check_ld("ld_mask", 2 * a.pairs, a.tokens, a.ld_mask, false));
+  if (a.kind > LOPT_PREFERENCE_SQUARED) return fail_call(LOPT_EINVAL, "kind %u is not a lopt_preference_kind", a.kind);
+  if (!(a.beta > 0.0) || std::isinf(a.beta)) return fail_call(LOPT_EINVAL, "beta must be finite and > 0");
+  if (!(a.label_smoothing >= 0.0 && a.label_smoothing <= 1.0)) return fail_call(LOPT_EINVAL, "label_smoothing must be in [0, 1]");
+  if (a.label_smoothing != 0.0 && a.kind != LOPT_PREFERENCE_SIGMOID) return fail_call(LOPT_EINVAL, "label_smoothing goes with the sigmoid only");
+  if (!std::isfinite(a.margin)) return fail_call(LOPT_EINVAL, "margin must be finite");
+  if (a.margin != 0.0 && a.kind == LOPT_PREFERENCE_SQUARED) return fail_call(LOPT_EINVAL, "margin does not go with the squared loss");
+  LOPT_CHECK(check_array("loss", loss, 4, true));
+  LOPT_CHECK(check_array("stats", stats, 4, true));
+  LOPT_CHECK(check_array("rewards", rewards, 4, any));
+  LOPT_CHECK(check_array("coef", coef, 4, any));
+  LOPT_CHECK(check_workspace(workspace, workspace_bytes, lopt_preference_loss_workspace(a.pairs, a.tokens)));
+  const Plan p = plan_of(2 * a.pairs, a.tokens);
+  hipStream_t stream = (hipStream_t)hip_stream;
+  Answer* part = (Answer*)workspace;
+  const PairOutputs o{loss, stats, rewards, coef};
+  with_lanes(p.lanes, [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    auto kernel = p.alone ? k_preference<G, kJoin> : k_preference<G, kBlock>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, p.pieces, p.length, p.units, part, p.alone, o);
+  });
+  if (!p.alone) hipLaunchKernelGGL(k_preference_join, dim3(1), dim3(kJoin), 0, stream, a, p.pieces, (const Answer*)part, o);
+  return launch_status("lopt_preference_loss");
+}
+
+lopt_status lopt_preference_loss_backward(const float* coef, const uint8_t* mask, int64_t ld_mask, const float* dloss, float* dlogp, int64_t pairs, int64_t tokens,
+                                          void* hip_stream) {
+  if (pairs < 0 || pairs > 0x3fffffffLL) return fail_call(LOPT_ESHAPE, "pairs=%lld outside [0, 2^30-1]", (long long)pairs);
+  LOPT_CHECK(check_matrix(2 * pairs, tokens, "tokens"));
+  if (mask) LOPT_CHECK(check_ld("ld_mask", 2 * pairs, tokens, ld_mask, false));
+  LOPT_CHECK(check_array("coef", coef, 4, pairs > 0));
+  LOPT_CHECK(check_array("dloss", dloss, 4, true));
+  LOPT_CHECK(check_array("dlogp", dlogp, 4, pairs > 0));
+  if (pairs == 0) return LOPT_OK;
+  const Flat f = flat_of(2 * pairs, tokens, kQuad);
+  hipLaunchKernelGGL(k_preference_back, dim3(flat_blocks(f)), dim3(kBlock), 0, (hipStream_t)hip_stream, coef, mask, ld_mask, dloss, dlogp, f);
+  return launch_status("lopt_preference_loss_backward");
+}
+
+}  // extern "C"

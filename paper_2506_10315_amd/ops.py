@@ -8,6 +8,7 @@ Tensors are CUDA tensors of float32, bfloat16 or float16; `layer_norm` and `toke
 from __future__ import annotations
 
 import operator
+import struct
 from array import array
 from typing import Iterable, List, NamedTuple, Optional, Sequence, Tuple, Union
 
@@ -18,7 +19,9 @@ from .binding import _check, lib
 __all__ = ["clip_grads", "clip_grad_norm_", "grad_norm", "layer_norm", "layer_norm_forward", "layer_norm_backward",
            "dropout", "dropout_forward", "dropout_add_layer_norm", "dropout_add_layer_norm_forward", "dropout_add_layer_norm_backward",
            "TokenLogprobs", "token_logprobs", "token_logprobs_forward", "token_logprobs_backward", "TOP_MAX",
-           "token_kl", "token_kl_forward", "token_kl_backward"]
+           "token_kl", "token_kl_forward", "token_kl_backward",
+           "PolicyLoss", "policy_loss", "policy_loss_forward", "policy_loss_backward",
+           "PreferenceLoss", "preference_loss", "preference_loss_forward", "preference_loss_backward"]
 
 TOP_MAX = 32          # LOPT_TOP_MAX
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # lopt_type
@@ -572,3 +575,207 @@ def token_kl(logits: torch.Tensor, ref: torch.Tensor, scale: float = 1.0, mask: 
     """token_kl_forward's kl with gradients for logits and ref: as a policy's distance from its reference, which has no gradient, or, with a teacher's logits
     first and the student's second, as the loss of a distillation."""
     return _TokenKl.apply(logits, ref, scale, mask)
+
+
+# ---------------------------------------------------------------------------------------------- losses of log probabilities
+
+_POLICY = struct.Struct("=" + "Qq" * 7 + "2q4d6I")          # lopt_policy
+_PREFERENCE = struct.Struct("=" + "Qq" * 3 + "2q3d4I")      # lopt_preference
+_KINDS = {"sigmoid": 0, "hinge": 1, "squared": 2}           # lopt_preference_kind
+_REDUCTIONS = {"tokens": 0, "sequences": 1}
+
+
+def _rows_like(name: str, t: torch.Tensor, like: torch.Tensor, shape, dtype: Optional[torch.dtype]) -> Tuple[torch.Tensor, int]:
+    """(tensor, elements from row to row) of `t`, which has to be of this shape and type (None: one of the module's) on `like`'s device."""
+    if t.shape != shape or t.get_device() != like.get_device() or (t.dtype is not dtype if dtype is not None else t.dtype not in _TYPES):
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype} on {t.device}; {tuple(shape)} of {dtype or 'float32, bfloat16 or float16'} "
+                         f"on {like.device} is needed")
+    t, _, _, ld = _matrix(name, t)
+    return t, ld
+
+
+def _optional_rows(name: str, t: Optional[torch.Tensor], like: torch.Tensor, dtype: Optional[torch.dtype]) -> Tuple[Optional[torch.Tensor], int, int]:
+    """(tensor, its address or 0, elements from row to row)."""
+    if t is None:
+        return None, 0, 0
+    t, ld = _rows_like(name, t, like, like.shape, dtype)
+    return t, t.data_ptr(), ld
+
+
+class PolicyLoss(NamedTuple):
+    loss: torch.Tensor                  # one float32
+    stats: torch.Tensor                 # [8]: means of surrogate, kl, entropy, clipped, ratio, drift; tokens and sequences that count
+    counts: Optional[torch.Tensor]      # tokens of each sequence that count, with reduction="sequences"
+
+
+def _policy_terms(logp, old_logp, advantages, mask, clip, ref_logp, kl, kl_coef, entropy, entropy_coef, reduction):
+    """(lopt_policy as bytes, the tensors that it points to, sequences, tokens)"""
+    if _type("logp", logp) != 0:
+        raise ValueError(f"logp is of {logp.dtype}; float32 is needed")
+    x, seqs, tokens, ld = _matrix("logp", logp)
+    old, ld_old = _rows_like("old_logp", old_logp, logp, logp.shape, None)
+    each = advantages.shape == logp.shape
+    if each:
+        adv, ld_adv = _rows_like("advantages", advantages, logp, logp.shape, None)
+    else:   # one a sequence
+        if advantages.dtype not in _TYPES:
+            raise ValueError(f"advantages are of {advantages.dtype}; float32, bfloat16 or float16 is needed")
+        adv, ld_adv = _expect("advantages", advantages, logp, advantages.dtype, logp.shape[:-1]), 1
+    if ref_logp is not None and kl is not None:
+        raise ValueError("ref_logp and kl are both given")
+    if kl_coef and ref_logp is None and kl is None:
+        raise ValueError("kl_coef without ref_logp or kl")
+    if entropy_coef and entropy is None:
+        raise ValueError("entropy_coef without entropy")
+    if reduction not in _REDUCTIONS:
+        raise ValueError(f"reduction={reduction!r}; 'tokens' or 'sequences' is needed")
+    ref, ref_at, ld_ref = _optional_rows("ref_logp", ref_logp, logp, None)
+    k, k_at, ld_k = _optional_rows("kl", kl, logp, torch.float32)
+    ent, ent_at, ld_ent = _optional_rows("entropy", entropy, logp, torch.float32)
+    m, m_at, ld_m = _optional_rows("mask", mask, logp, torch.bool)
+    low, high = clip
+    terms = _POLICY.pack(x.data_ptr(), ld, old.data_ptr(), ld_old, adv.data_ptr(), ld_adv, ref_at, ld_ref, k_at, ld_k, ent_at, ld_ent, m_at, ld_m, seqs, tokens,
+                         low, high, kl_coef, entropy_coef, _TYPES[old.dtype], _TYPES[adv.dtype], 0 if ref is None else _TYPES[ref.dtype], not each,
+                         _REDUCTIONS[reduction], 0)
+    return terms, (x, old, adv, ref, k, ent, m), seqs, tokens
+
+
+def policy_loss_forward(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                        clip: Tuple[float, float] = (0.2, 0.2), ref_logp: Optional[torch.Tensor] = None, kl: Optional[torch.Tensor] = None,
+                        kl_coef: float = 0.0, entropy: Optional[torch.Tensor] = None, entropy_coef: float = 0.0, reduction: str = "tokens") -> PolicyLoss:
+    """Clipped policy loss of tokens' log probabilities `logp` (float32 [..., tokens]) against those they were drawn with, with a KL term, of which `ref_logp`
+    gives an estimate and `kl` (of token_kl) the value, and an entropy bonus. `advantages`: one a token, or one a sequence (logp.shape[:-1]). `mask`
+    (bool): tokens that count. `reduction`: mean over the tokens, or over the sequences of the mean over each. Formulas: lopt_policy_loss."""
+    terms, alive, seqs, tokens = _policy_terms(logp, old_logp, advantages, mask, clip, ref_logp, kl, kl_coef, entropy, entropy_coef, reduction)
+    dev = logp.device
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    stats = torch.empty(8, dtype=torch.float32, device=dev)
+    counts = torch.empty(seqs, dtype=torch.float32, device=dev) if reduction == "sequences" else None
+    L = lib()
+    nbytes = L.lopt_policy_loss_workspace(seqs, tokens)
+    ws = _workspace(nbytes, dev)
+    _run(L.lopt_policy_loss, dev.index, terms, loss.data_ptr(), stats.data_ptr(), _ptr(counts), _ptr(ws), nbytes)
+    return PolicyLoss(loss, stats, counts)
+
+
+def policy_loss_backward(dloss: torch.Tensor, forward: PolicyLoss, logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
+                         mask: Optional[torch.Tensor] = None, clip: Tuple[float, float] = (0.2, 0.2), ref_logp: Optional[torch.Tensor] = None,
+                         kl: Optional[torch.Tensor] = None, kl_coef: float = 0.0, entropy: Optional[torch.Tensor] = None, entropy_coef: float = 0.0,
+                         reduction: str = "tokens", need: Tuple[bool, bool, bool] = (True, True, True)):
+    """(dlogp, dkl, dentropy) from the gradient of the loss and what policy_loss_forward of the same arguments gave; `need` says which are wanted, the
+    others are None, as are those of tensors that are not given."""
+    terms, alive, seqs, tokens = _policy_terms(logp, old_logp, advantages, mask, clip, ref_logp, kl, kl_coef, entropy, entropy_coef, reduction)
+    dloss = _expect("dloss", dloss, logp, torch.float32, ())
+    stats = _expect("stats", forward.stats, logp, torch.float32, (8,))
+    counts = _expect("counts", forward.counts, logp, torch.float32, (seqs,)) if reduction == "sequences" else None
+    dlogp = _new(logp) if need[0] else None
+    dkl = _new(kl) if need[1] and kl is not None else None
+    dentropy = _new(entropy) if need[2] and entropy is not None else None
+    _run(lib().lopt_policy_loss_backward, logp.get_device(), terms, stats.data_ptr(), _ptr(counts), dloss.data_ptr(), _ptr(dlogp), _ptr(dkl), _ptr(dentropy))
+    return dlogp, dkl, dentropy
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logp, kl, entropy, old_logp, advantages, mask, ref_logp, args):
+        r = policy_loss_forward(logp, old_logp, advantages, mask, ref_logp=ref_logp, kl=kl, entropy=entropy, **args)
+        ctx.save_for_backward(logp, kl, entropy, old_logp, advantages, mask, ref_logp, r.stats, r.counts)
+        ctx.args = args
+        ctx.mark_non_differentiable(*[t for t in (r.stats, r.counts) if t is not None])
+        return r.loss, r.stats, r.counts
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, *_):
+        logp, kl, entropy, old_logp, advantages, mask, ref_logp, stats, counts = ctx.saved_tensors
+        grads = policy_loss_backward(dloss, PolicyLoss(None, stats, counts), logp, old_logp, advantages, mask, ref_logp=ref_logp, kl=kl, entropy=entropy,
+                                     need=ctx.needs_input_grad[:3], **ctx.args)
+        return (*grads, None, None, None, None, None)
+
+
+def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                clip: Tuple[float, float] = (0.2, 0.2), ref_logp: Optional[torch.Tensor] = None, kl: Optional[torch.Tensor] = None, kl_coef: float = 0.0,
+                entropy: Optional[torch.Tensor] = None, entropy_coef: float = 0.0, reduction: str = "tokens") -> PolicyLoss:
+    """policy_loss_forward with gradients of the loss for logp, kl and entropy. The others are constants: one that asks for a gradient is refused."""
+    for name, t in (("old_logp", old_logp), ("advantages", advantages), ("ref_logp", ref_logp)):
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} asks for a gradient, which this loss does not give; detach it")
+    args = {"clip": clip, "kl_coef": kl_coef, "entropy_coef": entropy_coef, "reduction": reduction}
+    return PolicyLoss(*_PolicyLoss.apply(logp, kl, entropy, old_logp, advantages, mask, ref_logp, args))
+
+
+class PreferenceLoss(NamedTuple):
+    loss: torch.Tensor       # one float32
+    rewards: torch.Tensor    # [2 * pairs]: beta times each answer's sum of log ratios
+    stats: torch.Tensor      # [4]: share of right ones, mean margin of the rewards, mean reward of the chosen and of the rejected
+    coef: torch.Tensor       # [2 * pairs]: the slope of each answer's tokens, for the backward pass
+
+
+def preference_loss_forward(logp: torch.Tensor, ref_logp: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, beta: float = 0.1,
+                            kind: str = "sigmoid", label_smoothing: float = 0.0, margin: float = 0.0, average: bool = False) -> PreferenceLoss:
+    """Loss of pairs of answers from their tokens' log probabilities `logp`, float32 [2 * pairs, tokens]: the chosen answers' rows first, then the rejected ones' in
+    the same order. `ref_logp`: the reference's, of the same shape or summed up ([2 * pairs]); None: 0. `mask` (bool): tokens that count. `kind`: "sigmoid",
+    "hinge" or "squared". `average`: log ratios a token instead of an answer. Formulas: lopt_preference_loss."""
+    if _type("logp", logp) != 0 or logp.dim() != 2 or logp.shape[0] % 2:
+        raise ValueError(f"logp is {tuple(logp.shape)} of {logp.dtype}; float32 of an even number of rows is needed")
+    if kind not in _KINDS:
+        raise ValueError(f"kind={kind!r}; one of {', '.join(map(repr, _KINDS))} is needed")
+    x, rows, tokens, ld = _matrix("logp", logp)
+    m, m_at, ld_m = _optional_rows("mask", mask, logp, torch.bool)
+    sums = ref_logp is not None and ref_logp.dim() == 1
+    if sums:
+        if ref_logp.dtype not in _TYPES:
+            raise ValueError(f"ref_logp is of {ref_logp.dtype}; float32, bfloat16 or float16 is needed")
+        ref = _expect("ref_logp", ref_logp, logp, ref_logp.dtype, (rows,))
+        ref_at, ld_ref = ref.data_ptr(), 1
+    else:
+        ref, ref_at, ld_ref = _optional_rows("ref_logp", ref_logp, logp, None)
+    dev = logp.device
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    rewards = torch.empty(rows, dtype=torch.float32, device=dev)
+    coef = torch.empty_like(rewards)
+    stats = torch.empty(4, dtype=torch.float32, device=dev)
+    L = lib()
+    nbytes = L.lopt_preference_loss_workspace(rows // 2, tokens)
+    ws = _workspace(nbytes, dev)
+    terms = _PREFERENCE.pack(x.data_ptr(), ld, ref_at, ld_ref, m_at, ld_m, rows // 2, tokens, beta, label_smoothing, margin,
+                             0 if ref is None else _TYPES[ref.dtype], sums, _KINDS[kind], bool(average))
+    _run(L.lopt_preference_loss, dev.index, terms, loss.data_ptr(), stats.data_ptr(), rewards.data_ptr(), coef.data_ptr(), _ptr(ws), nbytes)
+    return PreferenceLoss(loss, rewards, stats, coef)
+
+
+def preference_loss_backward(dloss: torch.Tensor, forward: PreferenceLoss, logp: torch.Tensor, mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dlogp from the gradient of the loss and what preference_loss_forward gave."""
+    if _type("logp", logp) != 0 or logp.dim() != 2 or logp.shape[0] % 2:
+        raise ValueError(f"logp is {tuple(logp.shape)} of {logp.dtype}; float32 of an even number of rows is needed")
+    rows, tokens = logp.shape
+    m, m_at, ld_m = _optional_rows("mask", mask, logp, torch.bool)
+    dloss = _expect("dloss", dloss, logp, torch.float32, ())
+    coef = _expect("coef", forward.coef, logp, torch.float32, (rows,))
+    dlogp = _new(logp)
+    _run(lib().lopt_preference_loss_backward, logp.get_device(), coef.data_ptr(), m_at, ld_m, dloss.data_ptr(), dlogp.data_ptr(), rows // 2, tokens)
+    return dlogp
+
+
+class _PreferenceLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logp, ref_logp, mask, args):
+        r = preference_loss_forward(logp, ref_logp, mask, **args)
+        ctx.save_for_backward(logp, mask, r.coef)
+        ctx.mark_non_differentiable(r.rewards, r.stats, r.coef)
+        return r.loss, r.rewards, r.stats, r.coef
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, *_):
+        logp, mask, coef = ctx.saved_tensors
+        return preference_loss_backward(dloss, PreferenceLoss(None, None, None, coef), logp, mask), None, None, None
+
+
+def preference_loss(logp: torch.Tensor, ref_logp: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, beta: float = 0.1,
+                    kind: str = "sigmoid", label_smoothing: float = 0.0, margin: float = 0.0, average: bool = False) -> PreferenceLoss:
+    """preference_loss_forward with the gradient of the loss for logp. The reference is a constant: one that asks for a gradient is refused."""
+    if ref_logp is not None and ref_logp.requires_grad and torch.is_grad_enabled():
+        raise ValueError("ref_logp asks for a gradient, which this loss does not give; detach it")
+    args = {"beta": beta, "kind": kind, "label_smoothing": label_smoothing, "margin": margin, "average": average}
+    return PreferenceLoss(*_PreferenceLoss.apply(logp, ref_logp, mask, args))
