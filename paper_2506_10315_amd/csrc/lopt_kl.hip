@@ -11,39 +11,107 @@ namespace {
 
 // Running sums of some pairs of logits, mx and mr the largest of either (the type's lowest where all are masked), e = 2^(c (x - mx)) and f = 2^(c (r - mr)) with
 // c = scale / ln 2:
-//   sx = sum e,   sr = sum f,   w = sum (f - e),   h = sum e d   with d = scale ((x - r) - (mx - mr))
-//   KL = h / sx + ln(sr / sx)
+//   sx = sum e,   sr = sum f,   w = sum (f - e),   h = sum e d   with d = c ((x - r) - (mx - mr))
+//   KL = ln 2 h / sx + ln(sr / sx)
 // Differences from the maxima and between the two lose nothing where they are near, however large the logits are. Of two sharp distributions both terms
 // are far smaller than the sums, which begin with the same 1: there ln(sr / sx) = ln(1 + w / sx), whose rounding goes with w (1x10 fp32 of KL 1e-4: off by 4e-5 with the
-// sums alone; by 2e-4 with the maxima's products rounded as in the token log probabilities, for e and f are not 1 at them). `most`: the largest d; it is infinite where r
-// masks a token that x does not (or where finite logits are 3.4e38 apart). For the product d is held to a finite value, which masked tokens, e = 0, need.
+// sums alone; by 2e-4 with the maxima's products rounded as in the token log probabilities, for e and f are not 1 at them). `most`: the largest d that was
+// not near; it is infinite where r masks a token that x does not (or where finite logits are 3.4e38 apart). A NaN makes the maximum and by it the sums NaN.
 struct Apart { float mx, mr, sx, sr, w, h, most; };
 __device__ __forceinline__ Apart nothing() { return Apart{-FLT_MAX, -FLT_MAX, 0.f, 0.f, 0.f, 0.f, -INFINITY}; }
-__device__ __forceinline__ float shift_of(float mx, float mr, float scale) { return fminf(scale * (mx - mr), FLT_MAX); }
+__device__ __forceinline__ float shift_of(float mx, float mr, float c) { return fminf(c * (mx - mr), FLT_MAX); }
+// The same of a wavefront or more. Lanes add up some hundred terms each in 32 bits, whose roundings are many and independent; the sums over the lanes and what is made of them
+// are in 64, for KL is the small difference of its two terms (32 bits throughout: 1.6e-6 of the KL of 64 rows, so 2e-7).
+struct Total { double sx, sr, w, h; float mx, mr, most; };
 
+// 2^-d - 1 for |d| <= 4: that of a quarter of d, to 4e-8 of it, squared twice, by (1 + s)^2 - 1 = s (s + 2).
+__device__ __forceinline__ float less_one(float d) {
+  float s = -9.43454013e-10f;
+  s = __builtin_fmaf(s, d, 3.81747935e-08f);
+  s = __builtin_fmaf(s, d, -1.30198002e-06f);
+  s = __builtin_fmaf(s, d, 3.75662583e-05f);
+  s = __builtin_fmaf(s, d, -8.67252099e-04f);
+  s = __builtin_fmaf(s, d, 1.50141658e-02f);
+  s = __builtin_fmaf(s, d, -1.73286795e-01f) * d;
+  s = __builtin_fmaf(s, s, s + s);
+  return __builtin_fmaf(s, s, s + s);
+}
+
+// What a change to larger maxima makes of sums: factors of e and f, the second less the first, what d moves by. Near maxima's second factor goes by
+// the move, as f went by d.
+template <typename V> struct Move { V fx, fr, apart, moved; };
+constexpr float kNear = 64.f;
+template <typename V>
+__device__ __forceinline__ Move<V> move_of(float mx0, float mr0, float mx, float mr, float c) {
+  const float moved = shift_of(mx0, mr0, c) - shift_of(mx, mr, c), fx = exp2_hw((mx0 - mx) * c), less = fabsf(moved) <= 4.f ? less_one(moved) : exp2_hw(-moved) - 1.f;
+  if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, moved};
+  const float fr = exp2_hw((mr0 - mr) * c);
+  return Move<V>{fx, fr, fr - fx, moved};
+}
 // a's sums seen from larger maxima.
-__device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, float c, float scale) {
-  const float fx = exp2_hw((a.mx - mx) * c), fr = exp2_hw((a.mr - mr) * c), fs = fx * a.sx;
-  const float moved = shift_of(a.mx, a.mr, scale) - shift_of(mx, mr, scale);
-  return Apart{mx, mr, fs, fr * a.sr, fr * a.w + (fr - fx) * a.sx, fx * a.h + (fs == 0.f ? 0.f : fs * moved), a.most};
+__device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, float c) {
+  const Move<float> m = move_of<float>(a.mx, a.mr, mx, mr, c);
+  const float fs = m.fx * a.sx;
+  return Apart{mx, mr, fs, m.fr * a.sr, m.fr * a.w + m.apart * a.sx, m.fx * a.h + (fs == 0.f ? 0.f : fs * m.moved), a.most};
 }
-__device__ __forceinline__ Apart wave_join(Apart a, float c, float scale) {
-  a = rebase(a, wave_max(a.mx), wave_max(a.mr), c, scale);
-  return Apart{a.mx, a.mr, wave_sum(a.sx), wave_sum(a.sr), wave_sum(a.w), wave_sum(a.h), wave_max(a.most)};
+// Over a wavefront, seen from maxima that none of its lanes exceeds.
+__device__ __forceinline__ Total wave_total(Apart a, float mx, float mr, float c) {
+  a = rebase(a, mx, mr, c);
+  return Total{wave_sum((double)a.sx), wave_sum((double)a.sr), wave_sum((double)a.w), wave_sum((double)a.h), mx, mr, wave_max(a.most)};
 }
 
+// The largest, NaN where there is one.
 template <int E>
-__device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], float c, float scale) {
-  a = rebase(a, fmaxf(a.mx, most_of(x)), fmaxf(a.mr, most_of(r)), c, scale);
-  const float shift = shift_of(a.mx, a.mr, scale);
+__device__ __forceinline__ float strict_most_of(const float (&x)[E], float m) {
+#pragma unroll
+  for (int i = 0; i < E; ++i) m = __builtin_elementwise_maximum(m, x[i]);
+  return m;
+}
+
+// Where all d of a wavefront's piece are within kNear (or none, both logits being masked), f = e 2^-d, so that what e was rounded by is in f too and cancels in KL: with
+// an f by itself 1501 fp16 logits at a scale of 0.5 are off by 5e-7 of KL, so 2e-7. An e below 2^-126 has an f below 2^-62, which adds nothing.
+// FINE: q - 1 goes by less_one where all d allow it, and not by q, whose rounding next to 1 is what remains of a KL that few unlikely tokens
+// make up: of rows of some ten logits by 5e-6. It takes half as many instructions again as q; in long rows such roundings are many.
+template <int E, bool FINE>
+__device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], float c) {
+  a = rebase(a, strict_most_of(x, a.mx), strict_most_of(r, a.mr), c);
+  const float shift = shift_of(a.mx, a.mr, c);
+  float d[E], far = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float e = exp2_hw((x[i] - a.mx) * c), f = exp2_hw((r[i] - a.mr) * c), d = __builtin_fmaf(x[i] - r[i], scale, -shift);
-    a.most = fmaxf(a.most, d);
+    d[i] = __builtin_fmaf(x[i] - r[i], c, -shift);
+    far = fmaxf(far, fabsf(d[i]));
+  }
+  if (FINE && __ballot(far > 4.f) == 0) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float e = exp2_hw((x[i] - a.mx) * c), near = __builtin_amdgcn_fmed3f(d[i], -4.f, 4.f), g = e * less_one(near);
+      a.sx += e;
+      a.sr += e + g;
+      a.w += g;
+      a.h = __builtin_fmaf(e, near, a.h);
+    }
+    return;
+  }
+  if (__ballot(far > kNear) == 0) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float e = exp2_hw((x[i] - a.mx) * c), near = __builtin_amdgcn_fmed3f(d[i], -kNear, kNear), q = exp2_hw(-near);
+      a.sx += e;
+      a.sr = __builtin_fmaf(e, q, a.sr);
+      a.w = __builtin_fmaf(e, q - 1.f, a.w);
+      a.h = __builtin_fmaf(e, near, a.h);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float e = exp2_hw((x[i] - a.mx) * c), f = exp2_hw((r[i] - a.mr) * c);
+    a.most = fmaxf(a.most, d[i]);
     a.sx += e;
     a.sr += f;
     a.w += f - e;
-    a.h += e * __builtin_amdgcn_fmed3f(d, -FLT_MAX, FLT_MAX);
+    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d[i], -FLT_MAX, FLT_MAX), a.h);   // a masked token's is finite, for e is 0
   }
 }
 
@@ -62,20 +130,21 @@ struct Outputs {
 };
 
 // A row's outputs from its sums, by one lane. Sums that are 0 belong to a row that is masked whole; a NaN or +infinity is in the sum.
-__device__ __forceinline__ void write_row(const Outputs& o, int64_t row, Apart a) {
-  const float ratio = a.w / a.sx;
-  float mean = a.h / a.sx, kl = mean + (fabsf(ratio) < 0.5f ? log1pf(ratio) : logf(a.sr / a.sx));
-  kl = kl < 0.f ? 0.f : kl;
-  if (a.sr == 0.f || a.most == INFINITY) kl = mean = INFINITY;
-  if (a.sx == 0.f) kl = mean = 0.f;
-  if (!(a.sx < INFINITY && a.sr < INFINITY)) kl = mean = NAN;
+__device__ __forceinline__ void write_row(const Outputs& o, int64_t row, const Total& a, float c) {
+  // what the shift of every d was rounded by is in sr as well, so that KL does not have it; the stats have it taken out
+  constexpr double ln2 = 0.693147180559945309417;
+  const double ratio = a.w / a.sx, rounded = ln2 * ((double)shift_of(a.mx, a.mr, c) - (double)c * ((double)a.mx - (double)a.mr)), mean = ln2 * a.h / a.sx;
+  float kl = fmaxf((float)(mean + (fabs(ratio) < 0.5 ? log1p(ratio) : log(a.sr / a.sx))), 0.f), shifted = (float)(mean + rounded);
+  if (a.sr == 0.0 || a.most == INFINITY) kl = shifted = INFINITY;
+  if (a.sx == 0.0) kl = shifted = 0.f;
+  if (!(a.sx < INFINITY && a.sr < INFINITY)) kl = shifted = NAN;
   o.kl[row] = kl;
   float* s = o.stats + 5 * row;
-  s[0] = a.sx == 0.f ? -INFINITY : a.mx;
-  s[1] = logf(a.sx);
-  s[2] = a.sr == 0.f ? -INFINITY : a.mr;
-  s[3] = logf(a.sr);
-  s[4] = mean;
+  s[0] = a.sx == 0.0 ? -INFINITY : a.mx;
+  s[1] = logf((float)a.sx);
+  s[2] = a.sr == 0.0 ? -INFINITY : a.mr;
+  s[3] = logf((float)a.sr) - (a.sr == 0.0 ? 0.f : (float)rounded);
+  s[4] = shifted;
 }
 __device__ __forceinline__ void write_nothing(const Outputs& o, int64_t row) {
   o.kl[row] = 0.f;
@@ -102,9 +171,9 @@ __global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, Outputs o) {
     p.unpack(u);
     q.unpack(v);
     Apart s = nothing();
-    add_piece(s, u, v, c, a.scale);
-    s = wave_join(s, c, a.scale);
-    if (lane == 0) write_row(o, row, s);
+    add_piece<E, true>(s, u, v, c);
+    const Total t = wave_total(s, wave_max(s.mx), wave_max(s.mr), c);
+    if (lane == 0) write_row(o, row, t, c);
   }
 }
 
@@ -127,28 +196,38 @@ __device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* 
     }
     p.unpack(u);
     q.unpack(v);
-    add_piece(s, u, v, c, a.scale);
+    add_piece<E, false>(s, u, v, c);
     p = next_p;
     q = next_q;
   }
   return s;
 }
 
-// Joins what the wavefronts of a workgroup have; every thread gets it. `sums`: free before.
-__device__ __forceinline__ Apart block_join(Apart s, float c, float scale, Apart* sums) {
+// Joins what the wavefronts of a workgroup have, from common maxima; thread 0 gets it. `room`: free before, and after another barrier.
+struct Room { float mx[16], mr[16]; Total total[16]; };
+__device__ __forceinline__ Total block_total(const Apart& s, float c, Room& room) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  s = wave_join(s, c, scale);
-  if (lane == 0) sums[wave] = s;
+  float mx = wave_max(s.mx), mr = wave_max(s.mr);
+  if (lane == 0) room.mx[wave] = mx, room.mr[wave] = mr;
   __syncthreads();
-  s = lane < waves ? sums[lane] : nothing();
-  return wave_join(s, c, scale);
+  mx = wave_max(lane < waves ? room.mx[lane] : -FLT_MAX);
+  mr = wave_max(lane < waves ? room.mr[lane] : -FLT_MAX);
+  Total t = wave_total(s, mx, mr, c);
+  if (lane == 0) room.total[wave] = t;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int i = 1; i < waves; ++i) {
+      const Total& o = room.total[i];
+      t = Total{t.sx + o.sx, t.sr + o.sr, t.w + o.w, t.h + o.h, mx, mr, fmaxf(t.most, o.most)};
+    }
+  return t;
 }
 
 // A workgroup a row, its wavefronts a piece each in turn.
 template <typename T, int E>
 __global__ __launch_bounds__(1024) void k_kl(Rows<T> a, Outputs o) {
   typedef Piece<T, E> P;
-  __shared__ Apart sums[16];
+  __shared__ Room room;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const float c = fminf(a.scale * kLog2e, FLT_MAX);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -158,18 +237,18 @@ __global__ __launch_bounds__(1024) void k_kl(Rows<T> a, Outputs o) {
     }
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
-    Apart s = sums_of<T, E>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize, c);
-    s = block_join(s, c, a.scale, sums);
-    if (threadIdx.x == 0) write_row(o, row, s);
+    const Apart s = sums_of<T, E>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize, c);
+    const Total t = block_total(s, c, room);
+    if (threadIdx.x == 0) write_row(o, row, t, c);
     if (row + gridDim.x < a.rows) __syncthreads();
   }
 }
 
 // Few rows too long for one workgroup: segments of `pieces` pieces, a workgroup of four wavefronts each, and a workgroup a row that joins them.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments, uint32_t pieces, Apart* __restrict__ part) {
+__global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments, uint32_t pieces, Total* __restrict__ part) {
   typedef Piece<T, 16> P;
-  __shared__ Apart sums[4];
+  __shared__ Room room;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = fminf(a.scale * kLog2e, FLT_MAX);
   for (int64_t unit = blockIdx.x; unit < a.rows * segments; unit += gridDim.x) {
@@ -178,30 +257,54 @@ __global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
     const int64_t end = min(from + (int64_t)pieces * P::kSize, (int64_t)a.n + off);
-    Apart s = sums_of<T, 16>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize, c);
-    s = block_join(s, c, a.scale, sums);
-    if (threadIdx.x == 0) part[unit] = s;
+    const Apart s = sums_of<T, 16>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize, c);
+    const Total t = block_total(s, c, room);
+    if (threadIdx.x == 0) part[unit] = t;
     __syncthreads();
   }
 }
 template <typename T>
-__global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t segments, const Apart* __restrict__ part) {
-  __shared__ Apart sums[16];
+__global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t segments, const Total* __restrict__ part) {
+  __shared__ Room room;
   const float c = fminf(a.scale * kLog2e, FLT_MAX);
   const int64_t row = blockIdx.x;   // a workgroup for every row
   if (a.keep && !a.keep[row]) {
     if (threadIdx.x == 0) write_nothing(o, row);
     return;
   }
-  Apart s = nothing();
+  // from common maxima, each segment's sums in 64 bits; the factors are rounded to 32, each for itself
+  float mx = -FLT_MAX, mr = -FLT_MAX;
   for (int64_t i = threadIdx.x; i < segments; i += 1024) {
-    const Apart b = part[row * segments + i];
-    const float mx = fmaxf(s.mx, b.mx), mr = fmaxf(s.mr, b.mr);
-    const Apart p = rebase(s, mx, mr, c, a.scale), q = rebase(b, mx, mr, c, a.scale);
-    s = Apart{mx, mr, p.sx + q.sx, p.sr + q.sr, p.w + q.w, p.h + q.h, fmaxf(p.most, q.most)};
+    mx = fmaxf(mx, part[row * segments + i].mx);
+    mr = fmaxf(mr, part[row * segments + i].mr);
   }
-  s = block_join(s, c, a.scale, sums);
-  if (threadIdx.x == 0) write_row(o, row, s);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  mx = wave_max(mx);
+  mr = wave_max(mr);
+  if (lane == 0) room.mx[wave] = mx, room.mr[wave] = mr;
+  __syncthreads();
+  mx = wave_max(room.mx[lane & 15]);
+  mr = wave_max(room.mr[lane & 15]);
+  Total t{0.0, 0.0, 0.0, 0.0, mx, mr, -INFINITY};
+  for (int64_t i = threadIdx.x; i < segments; i += 1024) {
+    const Total b = part[row * segments + i];
+    const Move<double> m = move_of<double>(b.mx, b.mr, mx, mr, c);
+    const double fs = m.fx * b.sx;
+    t.sx += fs;
+    t.sr += m.fr * b.sr;
+    t.w += m.fr * b.w + m.apart * b.sx;
+    t.h += m.fx * b.h + (fs == 0.0 ? 0.0 : fs * m.moved);
+    t.most = fmaxf(t.most, b.most);
+  }
+  t = Total{wave_sum(t.sx), wave_sum(t.sr), wave_sum(t.w), wave_sum(t.h), mx, mr, wave_max(t.most)};
+  if (lane == 0) room.total[wave] = t;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int i = 1; i < 16; ++i) {
+    const Total& b = room.total[i];
+    t = Total{t.sx + b.sx, t.sr + b.sr, t.w + b.w, t.h + b.h, mx, mr, fmaxf(t.most, b.most)};
+  }
+  write_row(o, row, t, c);
 }
 
 // How rows are shared out.
@@ -308,7 +411,7 @@ extern "C" {
 size_t lopt_token_kl_workspace(int64_t rows, int64_t vocab) {
   if (rows <= 0 || vocab <= 0 || rows > 0x7fffffffLL || vocab > 0x7fffffffLL) return 0;
   const RowPlan plan = plan_rows(rows, vocab);
-  return plan.form == kRowSplit ? (size_t)rows * (size_t)plan.segments * sizeof(Apart) : 0;
+  return plan.form == kRowSplit ? (size_t)rows * (size_t)plan.segments * sizeof(Total) : 0;
 }
 
 lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, const uint8_t* mask, int64_t rows, int64_t vocab, uint32_t type,
@@ -332,9 +435,9 @@ lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64
     } else if (plan.form == kRowBlock) {
       hipLaunchKernelGGL((k_kl<T, 16>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), block, 0, stream, a, o);
     } else {
-      Apart* part = (Apart*)workspace;
+      Total* part = (Total*)workspace;
       hipLaunchKernelGGL(k_kl_split<T>, dim3((unsigned)std::min<int64_t>(rows * plan.segments, 1 << 22)), block, 0, stream, a, plan.segments, (uint32_t)plan.pieces, part);
-      hipLaunchKernelGGL(k_kl_join<T>, dim3((unsigned)rows), dim3(1024), 0, stream, a, o, plan.segments, (const Apart*)part);
+      hipLaunchKernelGGL(k_kl_join<T>, dim3((unsigned)rows), dim3(1024), 0, stream, a, o, plan.segments, (const Total*)part);
     }
   });
   return launch_status("lopt_token_kl");
