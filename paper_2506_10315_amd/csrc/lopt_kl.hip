@@ -13,7 +13,8 @@ namespace {
 // c = scale / ln 2:
 //   sx = sum e,   sr = sum f,   w = sum (f - e),   h = sum e d   with d = c ((x - r) - (mx - mr))
 //   KL = ln 2 h / sx + ln(sr / sx)
-// Differences from the maxima and between the two lose nothing where they are near, however large the logits are. Of two sharp distributions both terms
+// Differences from the maxima and between the two lose nothing where they are near, however large the logits are; where a constant of more than kOffset lies between the two
+// rows, d goes by (x - mx) - (r - mr). Of two sharp distributions both terms
 // are far smaller than the sums, which begin with the same 1: there ln(sr / sx) = ln(1 + w / sx), whose rounding goes with w (1x10 fp32 of KL 1e-4: off by 4e-5 with the
 // sums alone; by 2e-4 with the maxima's products rounded as in the token log probabilities, for e and f are not 1 at them). `most`: the largest d that was
 // not near; it is infinite where r masks a token that x does not (or where finite logits are 3.4e38 apart). A NaN makes the maximum and by it the sums NaN.
@@ -40,10 +41,11 @@ __device__ __forceinline__ float less_one(float d) {
 // What a change to larger maxima makes of sums: factors of e and f, the second less the first, what d moves by. Near maxima's second factor goes by
 // the move, as f went by d.
 template <typename V> struct Move { V fx, fr, apart, moved; };
-constexpr float kNear = 64.f;
+constexpr float kNear = 64.f, kOffset = 32.f;
 template <typename V>
 __device__ __forceinline__ Move<V> move_of(float mx0, float mr0, float mx, float mr, float c) {
-  const float moved = shift_of(mx0, mr0, c) - shift_of(mx, mr, c), fx = exp2_hw((mx0 - mx) * c), less = fabsf(moved) <= 4.f ? less_one(moved) : exp2_hw(-moved) - 1.f;
+  const bool close_by = fabsf(mx0 - mr0) <= kOffset && fabsf(mx - mr) <= kOffset;
+  const float moved = close_by ? shift_of(mx0, mr0, c) - shift_of(mx, mr, c) : c * ((mx0 - mx) - (mr0 - mr)), fx = exp2_hw((mx0 - mx) * c), less = fabsf(moved) <= 4.f ? less_one(moved) : exp2_hw(-moved) - 1.f;
   if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, moved};
   const float fr = exp2_hw((mr0 - mr) * c);
   return Move<V>{fx, fr, fr - fx, moved};
@@ -76,7 +78,7 @@ template <int E, bool FINE>
 __device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], float c) {
   a = rebase(a, strict_most_of(x, a.mx), strict_most_of(r, a.mr), c);
   const float shift = shift_of(a.mx, a.mr, c);
-  float d[E], far = 0.f;
+  float d[E], far = fabsf(a.mx - a.mr) <= kOffset ? 0.f : INFINITY;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     d[i] = __builtin_fmaf(x[i] - r[i], c, -shift);
@@ -106,12 +108,13 @@ __device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const f
   }
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float e = exp2_hw((x[i] - a.mx) * c), f = exp2_hw((r[i] - a.mr) * c);
-    a.most = fmaxf(a.most, d[i]);
+    const float dx = x[i] - a.mx, dr = r[i] - a.mr, e = exp2_hw(dx * c), f = exp2_hw(dr * c), d = dx - dr;
+    a.most = fmaxf(a.most, d);
     a.sx += e;
     a.sr += f;
     a.w += f - e;
-    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d[i], -FLT_MAX, FLT_MAX), a.h);   // a masked token's is finite, for e is 0
+    // 16 e and a sixteenth of d, which may be the type's largest; that of a masked token is finite, for e is 0
+    a.h = __builtin_fmaf(16.f * e, __builtin_amdgcn_fmed3f(d * (c / 16.f), -FLT_MAX, FLT_MAX), a.h);
   }
 }
 
@@ -133,7 +136,8 @@ struct Outputs {
 __device__ __forceinline__ void write_row(const Outputs& o, int64_t row, const Total& a, float c) {
   // what the shift of every d was rounded by is in sr as well, so that KL does not have it; the stats have it taken out
   constexpr double ln2 = 0.693147180559945309417;
-  const double ratio = a.w / a.sx, rounded = ln2 * ((double)shift_of(a.mx, a.mr, c) - (double)c * ((double)a.mx - (double)a.mr)), mean = ln2 * a.h / a.sx;
+  const double ratio = a.w / a.sx, mean = ln2 * a.h / a.sx;
+  const double rounded = fabsf(a.mx - a.mr) <= kOffset ? ln2 * ((double)shift_of(a.mx, a.mr, c) - (double)c * ((double)a.mx - (double)a.mr)) : 0.0;
   float kl = fmaxf((float)(mean + (fabs(ratio) < 0.5 ? log1p(ratio) : log(a.sr / a.sx))), 0.f), shifted = (float)(mean + rounded);
   if (a.sr == 0.0 || a.most == INFINITY) kl = shifted = INFINITY;
   if (a.sx == 0.0) kl = shifted = 0.f;
@@ -342,10 +346,13 @@ __global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, const float* __re
     const float mx = s[0], ln_sx = s[1], mr = s[2], ln_sr = s[3], mean = s[4], g = a.keep && !a.keep[row] ? 0.f : dkl[row];
     const bool zero = g == 0.f || (mx == -INFINITY && ln_sx == -INFINITY);
     const bool r_empty = mr == -INFINITY;
-    const float A = zero ? 0.f : mean == INFINITY ? NAN : g * a.scale, dm = mx - mr;
+    const float A = zero ? 0.f : mean == INFINITY ? NAN : g * a.scale;
+    // d by way of x - r, or of the maxima where a constant lies between the rows
+    const bool close_by = fabsf(mx - mr) <= kOffset;
+    const float ux = close_by ? 0.f : mx, ur = close_by ? 0.f : mr, dm = close_by ? mx - mr : 0.f;
     auto gradient = [&](float u, float v, float& gx, float& gr) {
       const float p = exp2_hw((a.scale * (u - mx) - ln_sx) * kLog2e);
-      if (DX) gx = A * (p * (__builtin_amdgcn_fmed3f(((u - v) - dm) * a.scale, -FLT_MAX, FLT_MAX) - mean));
+      if (DX) gx = A * (p * (__builtin_amdgcn_fmed3f((((u - ux) - (v - ur)) - dm) * a.scale, -FLT_MAX, FLT_MAX) - mean));
       if (DR) gr = A * ((r_empty ? 0.f : exp2_hw((a.scale * (v - mr) - ln_sr) * kLog2e)) - p);
     };
     const T* grid_row = DX ? out_x : out_r;
