@@ -23,7 +23,11 @@ inline Flat flat_of(int64_t rows, int64_t cols, int V) {
 struct Chunk {
   int64_t first, row0;
   uint32_t rest;
-  __device__ __forceinline__ Chunk(const Flat& f, int64_t first_) : first(first_), row0(first_ / f.packs), rest((uint32_t)(first_ - row0 * f.packs)) {}
+  __device__ __forceinline__ Chunk(const Flat& f, int64_t first_) : first(first_) {
+    if (first_ >> 32 == 0) row0 = (uint32_t)first_ / f.packs;   // a quarter of the instructions
+    else row0 = first_ / f.packs;
+    rest = (uint32_t)(first_ - row0 * f.packs);
+  }
   // Row and first column of the chunk's pack `local`; false if there is no such pack.
   __device__ __forceinline__ bool at(const Flat& f, int V, uint32_t local, int64_t& row, uint32_t& col) const {
     const uint32_t n = rest + local, q = f.packs > kShortPacks ? (n >= f.packs ? 1u : 0u) : f.packs == 1 ? n : __umulhi(n, f.magic);

@@ -11,8 +11,12 @@ namespace lopt {
 namespace {
 
 constexpr int kJoin = 1024;          // threads of the workgroup that joins, and of the one that does everything
-constexpr int kQuad = 4;             // neighbouring tokens of a lane
+constexpr int kQuad = 4;             // neighbouring tokens of a lane, where sequences have as many
 constexpr int64_t kAlone = 16384;    // tokens up to which one workgroup does everything
+#ifndef KP
+#define KP 1024
+#endif
+constexpr int64_t kPieces = KP;
 
 // Sum over groups of G lanes, a power of two up to 64; every lane gets it.
 template <typename V>
@@ -21,55 +25,68 @@ __device__ __forceinline__ V lanes_sum(V v, int G) {
   return v;
 }
 
-// Four neighbouring elements from element i on, `count` of them there.
-template <typename T>
-__device__ __forceinline__ void load_quad_as(const T* p, int count, float (&v)[kQuad]) {
-  typedef T quad __attribute__((ext_vector_type(kQuad), aligned(sizeof(T))));
-  if (count >= kQuad) {
-    const quad q = *(const quad*)p;
+// Q = 4 neighbouring elements, or one where sequences have fewer than four tokens. The four that would pass a sequence's end are moved back to end with it.
+template <int Q, typename T>
+__device__ __forceinline__ void load_as(const T* p, float (&v)[Q]) {
+  typedef T quad __attribute__((ext_vector_type(Q), aligned(sizeof(T))));
+  const quad q = *(const quad*)p;
 #pragma unroll
-    for (int e = 0; e < kQuad; ++e) v[e] = to_f32(q[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < kQuad; ++e) v[e] = e < count ? to_f32(p[e]) : 0.f;
-  }
+  for (int e = 0; e < Q; ++e) v[e] = to_f32(q[e]);
 }
-__device__ __forceinline__ void load_quad_of(const void* p, uint32_t type, int64_t i, int count, float (&v)[kQuad]) {
-  if (type == LOPT_F32) load_quad_as((const float*)p + i, count, v);
-  else if (type == LOPT_BF16) load_quad_as((const bf16_t*)p + i, count, v);
-  else load_quad_as((const f16_t*)p + i, count, v);
+template <int Q>
+__device__ __forceinline__ void load_of(const void* p, uint32_t type, int64_t i, float (&v)[Q]) {
+  if (type == LOPT_F32) load_as<Q>((const float*)p + i, v);
+  else if (type == LOPT_BF16) load_as<Q>((const bf16_t*)p + i, v);
+  else load_as<Q>((const f16_t*)p + i, v);
 }
 __device__ __forceinline__ float load_one_of(const void* p, uint32_t type, int64_t i) {
   return type == LOPT_F32 ? ((const float*)p)[i] : type == LOPT_BF16 ? to_f32(((const bf16_t*)p)[i]) : to_f32(((const f16_t*)p)[i]);
 }
-// Bit e: whether token e of the four is there and counts.
-__device__ __forceinline__ uint32_t load_mask(const uint8_t* mask, int64_t i, int count) {
-  typedef uint8_t quad __attribute__((ext_vector_type(kQuad), aligned(1)));
-  uint32_t bits = count >= kQuad ? 15u : (1u << count) - 1u;
-  if (!mask) return bits;
-  if (count >= kQuad) {
-    const quad q = *(const quad*)(mask + i);
-    return (q[0] ? 1u : 0u) | (q[1] ? 2u : 0u) | (q[2] ? 4u : 0u) | (q[3] ? 8u : 0u);
+// But for the first `skip`, which are another lane's.
+template <int Q>
+__device__ __forceinline__ void store(float* p, const float (&v)[Q], uint32_t skip) {
+  typedef float quad __attribute__((ext_vector_type(Q), aligned(4)));
+  if (skip) {
+#pragma unroll
+    for (int e = 1; e < Q; ++e)
+      if (e >= (int)skip) p[e] = v[e];
+    return;
   }
-  for (int e = 0; e < count; ++e)
-    if (!mask[i + e]) bits &= ~(1u << e);
+  quad q;
+#pragma unroll
+  for (int e = 0; e < Q; ++e) q[e] = v[e];
+  *(quad*)p = q;
+}
+// Bit e: whether token e counts.
+template <int Q>
+__device__ __forceinline__ uint32_t load_mask(const uint8_t* mask, int64_t i) {
+  if (!mask) return (1u << Q) - 1u;
+  typedef uint8_t quad __attribute__((ext_vector_type(Q), aligned(1)));
+  const quad q = *(const quad*)(mask + i);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < Q; ++e) bits |= (q[e] ? 1u : 0u) << e;
   return bits;
 }
 
 // How sequences are shared out: a group of `lanes` lanes takes a sequence, or one of its `pieces` of `length` tokens, four neighbouring tokens a lane in turn.
 // Few sequences are cut so that there are about 1024 pieces; a power of two of them, with which kJoin lanes of the join share out a sequence.
 struct Plan {
-  int lanes, threads;
+  int lanes, threads, shift, quad;   // pieces: 2^shift; neighbouring tokens of a lane
   int64_t pieces, length, units, blocks;
   bool alone;
 };
 inline Plan plan_of(int64_t seqs, int64_t tokens) {
   Plan p{};
+  p.quad = tokens < kQuad ? 1 : kQuad;
   p.lanes = tokens <= 64 ? 16 : tokens <= 256 ? 64 : kBlock;
   p.alone = seqs * tokens <= kAlone && seqs * ((tokens + kQuad * p.lanes - 1) / (kQuad * p.lanes)) * p.lanes <= kAlone / kQuad;   // seqs * tokens < 2^62
+  if (p.alone)   // all sequences at one time, if fewer lanes each can do that
+    while (p.lanes > 16 && seqs * p.lanes > kJoin) p.lanes /= 4;
   p.pieces = 1;
   if (!p.alone && p.lanes == kBlock)
-    while (p.pieces < 1024 && p.pieces * seqs < 1024 && p.pieces * kQuad * kBlock < tokens) p.pieces *= 2;
+    while (p.pieces < kPieces && p.pieces * seqs < kPieces && p.pieces * kQuad * kBlock < tokens) p.pieces *= 2;
+  for (p.shift = 0; (int64_t)1 << p.shift < p.pieces;) ++p.shift;
   p.length = ((tokens + p.pieces - 1) / p.pieces + kQuad - 1) / kQuad * kQuad;
   p.units = seqs * p.pieces;
   p.threads = p.alone ? kJoin : kBlock;
@@ -78,11 +95,18 @@ inline Plan plan_of(int64_t seqs, int64_t tokens) {
   p.blocks = p.alone ? 1 : p.pieces > 1 ? p.units : std::clamp<int64_t>((p.units + groups - 1) / groups, 1, 2048);
   return p;
 }
+// Calls f(lanes, threads, tokens of a lane) as integral constants.
 template <typename F>
-void with_lanes(int lanes, F&& f) {
-  if (lanes == 16) f(std::integral_constant<int, 16>{});
-  else if (lanes == 64) f(std::integral_constant<int, 64>{});
-  else f(std::integral_constant<int, kBlock>{});
+void with_plan(const Plan& p, F&& f) {
+  using std::integral_constant;
+  auto go = [&](auto g, auto q) {
+    if (p.alone) f(g, integral_constant<int, kJoin>{}, q);
+    else f(g, integral_constant<int, kBlock>{}, q);
+  };
+  if (p.quad == 1) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  else if (p.lanes == 16) go(integral_constant<int, 16>{}, integral_constant<int, kQuad>{});
+  else if (p.lanes == 64) go(integral_constant<int, 64>{}, integral_constant<int, kQuad>{});
+  else go(integral_constant<int, kBlock>{}, integral_constant<int, kQuad>{});
 }
 
 // Sum over a group of G lanes of a workgroup that is a multiple of it; `red` has a value for each wavefront. Every wavefront of the workgroup calls it.
@@ -102,57 +126,132 @@ __device__ __forceinline__ V group_total(V v, V* red) {
   }
   return v;
 }
-// Over the workgroup.
-template <typename V>
-__device__ __forceinline__ V block_total(V v, V* red) {
-  v = wave_sum(v);
+// Eight sums over a wavefront at once: lanes hand each other the half of the sums that the other goes on with, so that ten exchanges do what forty-eight would (of
+// 512x8192 tokens, where every wavefront has one reduction for eight quads a lane, FIGURE_REDUCE). The sum with index 4 (bit 3) + 2 (bit 2) + bit 1 of a lane's number is what the lane gets.
+__device__ __forceinline__ double eight_totals(const double (&v)[8]) {
+  const int lane = threadIdx.x;
+  auto half = [](bool high, double a, double b, auto exchange) {   // keeps a where low, b where high
+    const double keep = high ? b : a, give = high ? a : b;
+    return keep + exchange(give);
+  };
+  auto mirror = [](double x) { return dpp_d<0x140>(x); };        // lane i of a row of 16 has lane 15 - i's
+  auto half_mirror = [](double x) { return dpp_d<0x141>(x); };   // of 8, lane 7 - i's
+  auto pairs = [](double x) { return dpp_d<0x4E>(x); };          // quad_perm [2,3,0,1]
+  double w[4], x[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = half(lane & 8, v[i], v[4 + i], mirror);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) x[i] = half(lane & 4, w[i], w[2 + i], half_mirror);
+  double y = half(lane & 2, x[0], x[1], pairs);
+  y += dpp_d<0xB1>(y);                                           // quad_perm [1,0,3,2]
+  y += __shfl_xor(y, 16);
+  return y + __shfl_xor(y, 32);
+}
+// Eight sums over the workgroup, which thread 0 gets; `red` has eight values for each wavefront.
+__device__ __forceinline__ void block_totals(double (&v)[8], double* red) {
+  const int lane = threadIdx.x & 63, waves = blockDim.x / kWave;
+  const double mine = eight_totals(v);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  if (lane < 16 && (lane & 1) == 0) red[(threadIdx.x >> 6) * 8 + (lane >> 1 & 4) + (lane >> 1 & 2) + (lane >> 1 & 1)] = mine;
   __syncthreads();
-  V s = red[0];
-  for (unsigned i = 1; i < blockDim.x / kWave; ++i) s += red[i];
-  return s;
+  if (threadIdx.x >= kWave) return;
+  double s = 0.0;   // lane i adds up the i-th
+  if (lane < 8)
+    for (int w = 0; w < waves; ++w) s += red[w * 8 + lane];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = readlane_d(s, i);
 }
 
 // ---------------------------------------------------------------------------------------------- policy loss
 
-// e^v - 1 - v, for small v by its series, of which the first term left out is 1e-10 of the sum at 0.5.
-__device__ __forceinline__ float exp_rest(float v) {
-  if (!(fabsf(v) < 0.5f)) return expm1f(v) - v;
-  float s = 1.f / 3628800.f;
-  s = s * v + 1.f / 362880.f;
-  s = s * v + 1.f / 40320.f;
-  s = s * v + 1.f / 5040.f;
-  s = s * v + 1.f / 720.f;
-  s = s * v + 1.f / 120.f;
-  s = s * v + 1.f / 24.f;
-  s = s * v + 1.f / 6.f;
-  s = s * v + 0.5f;
-  return s * (v * v);
+// e^v, e^v - 1 and e^v - 1 - v. Where NEAR, |v| < kNear: of half of v the last is its square times a polynomial that is off by 4e-9 of it, and with s = e^(v/2) - 1 that of v is
+// s^2 + 2 (s - v / 2), in which nothing cancels. Else by the hardware's power of two, whose exponent's rounding is a unit of |v|.
+constexpr float kNear = 2.f;
+struct Exp { float less_one, rest, value; };
+template <bool NEAR>
+__device__ __forceinline__ Exp exp_of(float v) {
+  const float h = 0.5f * v;
+  float r = 2.7659865e-6f;
+  r = __builtin_fmaf(r, h, 2.5353789e-5f);
+  r = __builtin_fmaf(r, h, 1.98451148e-4f);
+  r = __builtin_fmaf(r, h, 1.38854675e-3f);
+  r = __builtin_fmaf(r, h, 8.3333049e-3f);
+  r = __builtin_fmaf(r, h, 4.1666734e-2f);
+  r = __builtin_fmaf(r, h, 1.66666671e-1f);
+  r = __builtin_fmaf(r, h, 4.99999998e-1f);
+  r *= h * h;
+  const float s = r + h, rest = __builtin_fmaf(s, s, 2.f * r);
+  Exp x{rest + v, rest, 1.f + (rest + v)};
+  if (!NEAR && !(fabsf(v) < kNear)) {
+    x.value = __builtin_amdgcn_exp2f(v * 1.44269504088896341f);
+    x.less_one = x.value - 1.f;
+    x.rest = x.less_one - v;
+  }
+  return x;
 }
 
 // A token's terms. Which side of a bound the ratio lies on, which decides over the whole gradient, is found in 64 bits, where the difference of the logarithms has
-// no rounding that matters; its values are in 32.
+// no rounding that matters; its values are in 32. NEAR: all logarithms of ratios at hand are within kNear.
 struct Bounds { double low, high; float at_low, at_high; };   // ln(1 - clip_low), ln(1 + clip_high) and what they are the logarithms of
-struct Terms { float surrogate, kl, ratio, drift, slope; bool clipped; };
+struct Terms { float surrogate, kl, beyond_one, drift, slope; bool clipped; };   // beyond_one: the ratio less 1
+template <bool NEAR>
 __device__ __forceinline__ Terms token_terms(float logp, float old, float adv, const Bounds& b, bool has_ref, float ref, float kl_coef) {
   Terms t{};
   const double d = (double)logp - (double)old;
-  t.drift = exp_rest((float)d);
-  t.ratio = expf((float)d);
+  const Exp x = exp_of<NEAR>((float)d);
+  t.drift = x.rest;
+  t.beyond_one = x.less_one;
   t.clipped = adv > 0.f ? d > b.high : adv < 0.f && d < b.low;
   const float bound = adv > 0.f ? b.at_high : b.at_low;
-  t.surrogate = adv == 0.f ? 0.f : -adv * (t.clipped ? bound : t.ratio);
+  t.surrogate = adv == 0.f ? 0.f : -adv * (t.clipped ? bound : x.value);
   t.slope = t.clipped ? 0.f : t.surrogate;
   if (has_ref) {
-    const float u = ref - logp;
-    t.kl = exp_rest(u);
-    t.slope -= kl_coef * (t.kl + u);   // d kl / d logp = 1 - e^u
+    const Exp y = exp_of<NEAR>(ref - logp);
+    t.kl = y.rest;
+    t.slope -= kl_coef * y.less_one;   // d kl / d logp = 1 - e^u
   }
   return t;
 }
 
-// Sums in the order of the stats: surrogate, kl, entropy, clipped, ratio, drift, tokens, sequences.
+// Tokens of a sequence. What does not count is 0 throughout, so that its ratio is 1 and its terms are 0.
+template <int Q>
+struct Tokens {
+  float logp[Q], old[Q], adv[Q], ref[Q];
+  uint32_t bits;
+  // Padding, which comes in runs, is not read.
+  __device__ __forceinline__ void load(const lopt_policy& a, int64_t seq, int64_t t, float adv_seq, uint32_t bits_) {
+    bits = bits_;
+    if (!bits) return;
+    load_as<Q>(a.logp + seq * a.ld_logp + t, logp);
+    load_of<Q>(a.old_logp, a.old_type, seq * a.ld_old + t, old);
+    if (a.advantage_per_sequence) {
+#pragma unroll
+      for (int e = 0; e < Q; ++e) adv[e] = adv_seq;
+    } else {
+      load_of<Q>(a.advantages, a.advantage_type, seq * a.ld_advantages + t, adv);
+    }
+    if (a.ref_logp) load_of<Q>(a.ref_logp, a.ref_type, seq * a.ld_ref + t, ref);
+  }
+  // Whether all of a wavefront's are within kNear of each other.
+  __device__ __forceinline__ bool choose(bool has_ref) {
+    bool far = false;
+#pragma unroll
+    for (int e = 0; e < Q; ++e) {
+      const bool in = bits >> e & 1;
+      logp[e] = in ? logp[e] : 0.f;
+      old[e] = in ? old[e] : 0.f;
+      adv[e] = in ? adv[e] : 0.f;
+      far |= !(fabsf(logp[e] - old[e]) < kNear);
+      if (has_ref) {
+        ref[e] = in ? ref[e] : 0.f;
+        far |= !(fabsf(ref[e] - logp[e]) < kNear);
+      }
+    }
+    return __ballot(far) == 0;
+  }
+};
+
+// Sums in the order of the stats: surrogate, kl, entropy, clipped, ratio less 1, drift, tokens, sequences.
 constexpr int kSums = 8;
 
 __device__ __forceinline__ void write_policy(const double (&sum)[kSums], const lopt_policy& a, float* loss, float* stats) {
@@ -160,6 +259,7 @@ __device__ __forceinline__ void write_policy(const double (&sum)[kSums], const l
   double mean[6];
 #pragma unroll
   for (int i = 0; i < 6; ++i) mean[i] = n > 0.0 ? sum[i] * w : 0.0;
+  if (n > 0.0) mean[4] += 1.0;   // its terms are the ratios less 1
   double v = mean[0];
   if (a.ref_logp || a.kl) v += a.kl_coef * mean[1];
   if (a.entropy) v -= a.entropy_coef * mean[2];
@@ -170,62 +270,71 @@ __device__ __forceinline__ void write_policy(const double (&sum)[kSums], const l
   stats[7] = (float)sum[7];
 }
 
-// The sums of units of whole sequences (`pieces` is 1), one row of them a workgroup, or of pieces, one row each; with `alone` the loss.
-template <int G, int kThreads>
-__global__ __launch_bounds__(kThreads) void k_policy(lopt_policy a, Bounds b, int64_t pieces, int64_t length, int64_t units, double* __restrict__ part, bool alone,
+// The sums of units of whole sequences (`shift` is 0), one row of them a workgroup, or of pieces, one row each; with `alone` the loss.
+template <int G, int kThreads, int Q>
+__global__ __launch_bounds__(kThreads) void k_policy(lopt_policy a, Bounds b, int shift, int64_t length, int64_t units, double* __restrict__ part, bool alone,
                                                      float* __restrict__ loss, float* __restrict__ stats, float* __restrict__ counts) {
-  __shared__ double red[kThreads / kWave];
+  __shared__ double red[kThreads / kWave * kSums];
   const int lane = threadIdx.x % G;
   constexpr int kGroups = kThreads / G;
   double sum[kSums] = {};
-  const float kl_coef = (float)a.kl_coef;
+  const bool has_ref = a.ref_logp != nullptr;
   // every wavefront goes through the loop as often, for the barriers of the group's sums
   for (int64_t base = (int64_t)blockIdx.x * kGroups; base < units; base += (int64_t)gridDim.x * kGroups) {
     const int64_t unit = base + threadIdx.x / G;
     const bool have = unit < units;
-    const int64_t seq = have ? unit / pieces : 0, from = have ? (unit - seq * pieces) * length : 0, to = have ? min(from + length, a.tokens) : 0;
-    double own[7] = {};
+    const int64_t seq = have ? unit >> shift : 0, from = have ? (unit & (((int64_t)1 << shift) - 1)) * length : 0, to = have ? min(from + length, a.tokens) : 0;
+    double own[6] = {};   // [3] is formed at the end
+    int clipped = 0, count_in = 0;
     const float adv_seq = have && a.advantage_per_sequence ? load_one_of(a.advantages, a.advantage_type, seq * a.ld_advantages) : 0.f;
-    for (int64_t t = from + lane * kQuad; t < to; t += G * kQuad) {
-      const int count = (int)min(to - t, (int64_t)kQuad);
-      float logp[kQuad], old[kQuad], adv[kQuad] = {adv_seq, adv_seq, adv_seq, adv_seq}, ref[kQuad] = {}, kl[kQuad] = {}, ent[kQuad] = {};
-      const uint32_t bits = load_mask(a.mask, seq * a.ld_mask + t, count);
-      load_quad_as(a.logp + seq * a.ld_logp + t, count, logp);
-      load_quad_of(a.old_logp, a.old_type, seq * a.ld_old + t, count, old);
-      if (!a.advantage_per_sequence) load_quad_of(a.advantages, a.advantage_type, seq * a.ld_advantages + t, count, adv);
-      if (a.ref_logp) load_quad_of(a.ref_logp, a.ref_type, seq * a.ld_ref + t, count, ref);
-      if (a.kl) load_quad_as(a.kl + seq * a.ld_kl + t, count, kl);
-      if (a.entropy) load_quad_as(a.entropy + seq * a.ld_entropy + t, count, ent);
+    for (int64_t t = from + lane * Q; t < to; t += G * Q) {
+      const int64_t at = min(t, a.tokens - Q);
+      const uint32_t bits = load_mask<Q>(a.mask, seq * a.ld_mask + at) & ~0u << (t - at);   // not those of the lane before
+      if (__ballot(bits != 0) == 0) continue;
+      Tokens<Q> q;
+      q.load(a, seq, at, adv_seq, bits);
+      float beyond_one = 0.f, drift = 0.f;   // of four, in 32 bits
+      auto add = [&](auto near) {
 #pragma unroll
-      for (int e = 0; e < kQuad; ++e) {
-        const Terms q = token_terms(logp[e], old[e], adv[e], b, a.ref_logp != nullptr, ref[e], kl_coef);
-        const bool counts_in = bits >> e & 1;
-        own[0] += counts_in ? (double)q.surrogate : 0.0;
-        own[1] += counts_in ? (double)(a.kl ? kl[e] : q.kl) : 0.0;
-        own[2] += counts_in ? (double)ent[e] : 0.0;
-        own[3] += counts_in && q.clipped ? 1.0 : 0.0;
-        own[4] += counts_in ? (double)q.ratio : 0.0;
-        own[5] += counts_in ? (double)q.drift : 0.0;
-        own[6] += counts_in ? 1.0 : 0.0;
-      }
+        for (int e = 0; e < Q; ++e) {
+          const Terms v = token_terms<decltype(near)::value>(q.logp[e], q.old[e], q.adv[e], b, has_ref, q.ref[e], 0.f);
+          own[0] += (double)v.surrogate;
+          if (has_ref) own[1] += (double)v.kl;
+          clipped += v.clipped ? 1 : 0;
+          beyond_one += v.beyond_one;
+          drift += v.drift;
+        }
+      };
+      if (q.choose(has_ref)) add(std::true_type{});
+      else add(std::false_type{});
+      own[4] += (double)beyond_one;
+      own[5] += (double)drift;
+      count_in += __popc(bits);
+      auto given = [&](const float* p, double& to_sum) {
+        if (!bits) return;
+        float v[Q];
+        load_as<Q>(p + at, v);
+#pragma unroll
+        for (int e = 0; e < Q; ++e) to_sum += bits >> e & 1 ? (double)v[e] : 0.0;
+      };
+      if (a.kl) given(a.kl + seq * a.ld_kl, own[1]);
+      if (a.entropy) given(a.entropy + seq * a.ld_entropy, own[2]);
     }
-    if (pieces == 1) {   // the sequence is whole
-      const double n = group_total<G>(own[6], red);
-      const double w = a.per_sequence && n > 0.0 ? 1.0 / n : 1.0;
-#pragma unroll
-      for (int i = 0; i < 6; ++i) sum[i] += w * own[i];
-      sum[6] += own[6];
+    own[3] = (double)clipped;
+    double w = 1.0;
+    if (shift == 0) {   // the sequence is whole
+      const double n = group_total<G>((double)count_in, red);
+      if (a.per_sequence && n > 0.0) w = 1.0 / n;
       if (lane == 0 && have) {
         sum[7] += n > 0.0 ? 1.0 : 0.0;
         if (counts) counts[seq] = (float)n;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 7; ++i) sum[i] += own[i];
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kSums; ++i) sum[i] = block_total(sum[i], red);
+    for (int i = 0; i < 6; ++i) sum[i] += w * own[i];
+    sum[6] += (double)count_in;
+  }
+  block_totals(sum, red);
   if (threadIdx.x != 0) return;
   if (alone) {
     write_policy(sum, a, loss, stats);
@@ -238,7 +347,7 @@ __global__ __launch_bounds__(kThreads) void k_policy(lopt_policy a, Bounds b, in
 // Joins `rows` rows of sums. Of pieces, `lanes` lanes take a sequence.
 __global__ __launch_bounds__(kJoin) void k_policy_join(lopt_policy a, int64_t rows, int64_t pieces, const double* __restrict__ part, float* __restrict__ loss,
                                                        float* __restrict__ stats, float* __restrict__ counts) {
-  __shared__ double red[kJoin / kWave];
+  __shared__ double red[kJoin / kWave * kSums];
   double sum[kSums] = {};
   if (pieces == 1) {
     for (int64_t k = threadIdx.x; k < rows; k += kJoin) {
@@ -266,55 +375,64 @@ __global__ __launch_bounds__(kJoin) void k_policy_join(lopt_policy a, int64_t ro
       }
     }
   }
-#pragma unroll
-  for (int i = 0; i < kSums; ++i) sum[i] = block_total(sum[i], red);
+  block_totals(sum, red);
   if (threadIdx.x == 0) write_policy(sum, a, loss, stats);
 }
 
-__device__ __forceinline__ void store_quad_of(float* p, int count, const float (&v)[kQuad]) {
-  typedef float quad __attribute__((ext_vector_type(kQuad), aligned(4)));
-  if (count >= kQuad) {
-    *(quad*)p = quad{v[0], v[1], v[2], v[3]};
-  } else {
-    for (int e = 0; e < count; ++e) p[e] = v[e];
+// Calls g(sequence, first token, how many of them are another lane's) for every Q tokens of all sequences, kTrips a thread; the last of a sequence end with it.
+constexpr int kTrips = 4, kQuads = kTrips * kBlock;
+template <int Q, typename F>
+__device__ __forceinline__ void for_tokens(const Flat& f, F&& g) {
+  for (int64_t first = (int64_t)blockIdx.x * kQuads; first < f.total; first += (int64_t)gridDim.x * kQuads) {
+    const Chunk chunk(f, first);
+#pragma unroll 1
+    for (int j = 0; j < kTrips; ++j) {
+      int64_t seq;
+      uint32_t t;
+      if (!chunk.at(f, Q, j * kBlock + threadIdx.x, seq, t)) continue;
+      const uint32_t at = min(t, f.cols - Q);
+      g(seq, at, t - at);
+    }
   }
 }
 
-// The gradients, four tokens a thread, all terms formed again.
+// The gradients, all terms formed again.
+template <int Q>
 __global__ __launch_bounds__(kBlock) void k_policy_back(lopt_policy a, Bounds b, Flat f, const float* __restrict__ stats, const float* __restrict__ counts,
                                                         const float* __restrict__ dloss, float* __restrict__ dlogp, float* __restrict__ dkl, float* __restrict__ dentropy) {
   const float up = *dloss, whole = stats[a.per_sequence ? 7 : 6];
   const float kl_coef = (float)a.kl_coef, entropy_coef = (float)a.entropy_coef;
-  for (int64_t first = (int64_t)blockIdx.x * kBlock; first < f.total; first += (int64_t)gridDim.x * kBlock) {
-    const Chunk chunk(f, first);
-    int64_t seq;
-    uint32_t t;
-    if (!chunk.at(f, kQuad, threadIdx.x, seq, t)) continue;
-    const int count = (int)min(f.cols - t, (uint32_t)kQuad);
-    const uint32_t bits = load_mask(a.mask, seq * a.ld_mask + t, count);
+  const bool has_ref = a.ref_logp != nullptr;
+  for_tokens<Q>(f, [&](int64_t seq, uint32_t t, uint32_t skip) {
+    const uint32_t bits = load_mask<Q>(a.mask, seq * a.ld_mask + t);
     // of a token that counts there are a sequence that has one and a batch that has one
     const float w = up / (a.per_sequence ? whole * counts[seq] : whole);
     if (dlogp) {
-      const float adv_seq = a.advantage_per_sequence ? load_one_of(a.advantages, a.advantage_type, seq * a.ld_advantages) : 0.f;
-      float logp[kQuad], old[kQuad], adv[kQuad] = {adv_seq, adv_seq, adv_seq, adv_seq}, ref[kQuad] = {}, o[kQuad];
-      load_quad_as(a.logp + seq * a.ld_logp + t, count, logp);
-      load_quad_of(a.old_logp, a.old_type, seq * a.ld_old + t, count, old);
-      if (!a.advantage_per_sequence) load_quad_of(a.advantages, a.advantage_type, seq * a.ld_advantages + t, count, adv);
-      if (a.ref_logp) load_quad_of(a.ref_logp, a.ref_type, seq * a.ld_ref + t, count, ref);
+      Tokens<Q> q;
+      q.load(a, seq, t, a.advantage_per_sequence ? load_one_of(a.advantages, a.advantage_type, seq * a.ld_advantages) : 0.f, bits);
+      float o[Q] = {};
+      auto slopes = [&](auto near) {
 #pragma unroll
-      for (int e = 0; e < kQuad; ++e)
-        o[e] = bits >> e & 1 ? w * token_terms(logp[e], old[e], adv[e], b, a.ref_logp != nullptr, ref[e], kl_coef).slope : 0.f;
-      store_quad_of(dlogp + seq * a.tokens + t, count, o);
+        for (int e = 0; e < Q; ++e) {
+          const float v = token_terms<decltype(near)::value>(q.logp[e], q.old[e], q.adv[e], b, has_ref, q.ref[e], kl_coef).slope;
+          o[e] = q.bits >> e & 1 ? w * v : 0.f;
+        }
+      };
+      if (__ballot(bits != 0) != 0) {
+        if (q.choose(has_ref)) slopes(std::true_type{});
+        else slopes(std::false_type{});
+      }
+      store<Q>(dlogp + seq * a.tokens + t, o, skip);
     }
     auto same = [&](float* out, float v) {
-      float o[kQuad];
+      float o[Q];
 #pragma unroll
-      for (int e = 0; e < kQuad; ++e) o[e] = bits >> e & 1 ? v : 0.f;
-      store_quad_of(out + seq * a.tokens + t, count, o);
+      for (int e = 0; e < Q; ++e) o[e] = bits >> e & 1 ? v : 0.f;
+      store<Q>(out + seq * a.tokens + t, o, skip);
     };
     if (dkl) same(dkl, w * kl_coef);
     if (dentropy) same(dentropy, -w * entropy_coef);
-  }
+  });
 }
 
 lopt_status check_policy(const lopt_policy* a) {
@@ -356,7 +474,7 @@ struct PairOutputs {
   float* rewards;
   float* coef;
 };
-constexpr int kPairSums = 5;   // loss, right ones, margins, rewards of the chosen, of the rejected
+constexpr int kPairSums = 8;   // loss, right ones, margins, rewards of the chosen, of the rejected, three of nothing
 
 __device__ __forceinline__ void write_pair(const lopt_preference& a, int64_t pair, Answer chosen, Answer rejected, const PairOutputs& o, double (&sum)[kPairSums]) {
   if (a.ref && a.ref_sums) {
@@ -422,36 +540,37 @@ __device__ __forceinline__ void join_pairs(const lopt_preference& a, int64_t pie
     }
     if (lane == 0 && pair < a.pairs) write_pair(a, pair, own[0], own[1], o, sum);
   }
-#pragma unroll
-  for (int i = 0; i < kPairSums; ++i) sum[i] = block_total(sum[i], red);
+  block_totals(sum, red);
   if (threadIdx.x == 0) {
     const double w = a.pairs > 0 ? 1.0 / (double)a.pairs : 0.0;
     *o.loss = (float)(sum[0] * w);
 #pragma unroll
-    for (int i = 1; i < kPairSums; ++i) o.stats[i - 1] = (float)(sum[i] * w);
+    for (int i = 1; i < 5; ++i) o.stats[i - 1] = (float)(sum[i] * w);
   }
 }
 
-template <int G, int kThreads>
-__global__ __launch_bounds__(kThreads) void k_preference(lopt_preference a, int64_t pieces, int64_t length, int64_t units, Answer* part, bool alone, PairOutputs o) {
-  __shared__ double red[kThreads / kWave];
+template <int G, int kThreads, int Q>
+__global__ __launch_bounds__(kThreads) void k_preference(lopt_preference a, int shift, int64_t length, int64_t units, Answer* part, bool alone, PairOutputs o) {
+  __shared__ double red[kThreads / kWave * kPairSums];
   const int lane = threadIdx.x % G;
   constexpr int kGroups = kThreads / G;
   const bool has_ref = a.ref && !a.ref_sums;
   for (int64_t base = (int64_t)blockIdx.x * kGroups; base < units; base += (int64_t)gridDim.x * kGroups) {
     const int64_t unit = base + threadIdx.x / G;
     const bool have = unit < units;
-    const int64_t seq = have ? unit / pieces : 0, from = have ? (unit - seq * pieces) * length : 0, to = have ? min(from + length, a.tokens) : 0;
+    const int64_t seq = have ? unit >> shift : 0, from = have ? (unit & (((int64_t)1 << shift) - 1)) * length : 0, to = have ? min(from + length, a.tokens) : 0;
     double sum = 0.0, n = 0.0;
-    for (int64_t t = from + lane * kQuad; t < to; t += G * kQuad) {
-      const int count = (int)min(to - t, (int64_t)kQuad);
-      float logp[kQuad], ref[kQuad] = {};
-      const uint32_t bits = load_mask(a.mask, seq * a.ld_mask + t, count);
-      load_quad_as(a.logp + seq * a.ld_logp + t, count, logp);
-      if (has_ref) load_quad_of(a.ref, a.ref_type, seq * a.ld_ref + t, count, ref);
+    for (int64_t t = from + lane * Q; t < to; t += G * Q) {
+      const int64_t at = min(t, a.tokens - Q);
+      const uint32_t bits = load_mask<Q>(a.mask, seq * a.ld_mask + at) & ~0u << (t - at);
+      if (bits) {   // padding is not read
+        float logp[Q], ref[Q] = {};
+        load_as<Q>(a.logp + seq * a.ld_logp + at, logp);
+        if (has_ref) load_of<Q>(a.ref, a.ref_type, seq * a.ld_ref + at, ref);
 #pragma unroll
-      for (int e = 0; e < kQuad; ++e) sum += bits >> e & 1 ? (double)logp[e] - (double)ref[e] : 0.0;
-      n += (double)__popc(bits);
+        for (int e = 0; e < Q; ++e) sum += bits >> e & 1 ? (double)logp[e] - (double)ref[e] : 0.0;
+        n += (double)__popc(bits);
+      }
     }
     sum = group_total<G>(sum, red);
     n = group_total<G>(n, red);
@@ -459,33 +578,29 @@ __global__ __launch_bounds__(kThreads) void k_preference(lopt_preference a, int6
   }
   if (alone) {
     __syncthreads();   // the workgroup's own partial sums
-    join_pairs(a, pieces, part, o, red);
+    join_pairs(a, (int64_t)1 << shift, part, o, red);
   }
 }
 __global__ __launch_bounds__(kJoin) void k_preference_join(lopt_preference a, int64_t pieces, const Answer* __restrict__ part, PairOutputs o) {
-  __shared__ double red[kJoin / kWave];
+  __shared__ double red[kJoin / kWave * kPairSums];
   join_pairs(a, pieces, part, o, red);
 }
 
+template <int Q>
 __global__ __launch_bounds__(kBlock) void k_preference_back(const float* __restrict__ coef, const uint8_t* __restrict__ mask, int64_t ld_mask, const float* __restrict__ dloss,
                                                             float* __restrict__ dlogp, Flat f) {
   const float up = *dloss;
-  for (int64_t first = (int64_t)blockIdx.x * kBlock; first < f.total; first += (int64_t)gridDim.x * kBlock) {
-    const Chunk chunk(f, first);
-    int64_t seq;
-    uint32_t t;
-    if (!chunk.at(f, kQuad, threadIdx.x, seq, t)) continue;
-    const int count = (int)min(f.cols - t, (uint32_t)kQuad);
-    const uint32_t bits = load_mask(mask, seq * ld_mask + t, count);
+  for_tokens<Q>(f, [&](int64_t seq, uint32_t t, uint32_t skip) {
+    const uint32_t bits = load_mask<Q>(mask, seq * ld_mask + t);
     const float v = up * coef[seq];
-    float o[kQuad];
+    float o[Q];
 #pragma unroll
-    for (int e = 0; e < kQuad; ++e) o[e] = bits >> e & 1 ? v : 0.f;
-    store_quad_of(dlogp + seq * (int64_t)f.cols + t, count, o);
-  }
+    for (int e = 0; e < Q; ++e) o[e] = bits >> e & 1 ? v : 0.f;
+    store<Q>(dlogp + seq * (int64_t)f.cols + t, o, skip);
+  });
 }
 
-unsigned flat_blocks(const Flat& f) { return (unsigned)std::min<int64_t>((f.total + kBlock - 1) / kBlock, 1 << 22); }
+unsigned flat_blocks(const Flat& f) { return (unsigned)std::min<int64_t>((f.total + kQuads - 1) / kQuads, 1 << 22); }
 
 }  // namespace
 }  // namespace lopt
@@ -510,10 +625,9 @@ lopt_status lopt_policy_loss(const lopt_policy* terms_host, float* loss, float* 
   const Plan p = plan_of(a.seqs, a.tokens);
   hipStream_t stream = (hipStream_t)hip_stream;
   double* part = (double*)workspace;
-  with_lanes(p.lanes, [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    auto kernel = p.alone ? k_policy<G, kJoin> : k_policy<G, kBlock>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, bounds_of(a), p.pieces, p.length, p.units, part, p.alone, loss, stats, counts);
+  with_plan(p, [&](auto g, auto threads, auto q) {
+    hipLaunchKernelGGL((k_policy<decltype(g)::value, decltype(threads)::value, decltype(q)::value>), dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, bounds_of(a), p.shift,
+                       p.length, p.units, part, p.alone, loss, stats, counts);
   });
   if (!p.alone) hipLaunchKernelGGL(k_policy_join, dim3(1), dim3(kJoin), 0, stream, a, p.blocks, p.pieces, (const double*)part, loss, stats, counts);
   return launch_status("lopt_policy_loss");
@@ -532,8 +646,10 @@ lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float
   if (dkl && !a.kl) return fail_call(LOPT_EINVAL, "dkl without kl");
   if (dentropy && !a.entropy) return fail_call(LOPT_EINVAL, "dentropy without entropy");
   if (a.seqs == 0 || !(dlogp || dkl || dentropy)) return LOPT_OK;
-  const Flat f = flat_of(a.seqs, a.tokens, kQuad);
-  hipLaunchKernelGGL(k_policy_back, dim3(flat_blocks(f)), dim3(kBlock), 0, (hipStream_t)hip_stream, a, bounds_of(a), f, stats, counts, dloss, dlogp, dkl, dentropy);
+  const int quad = a.tokens < kQuad ? 1 : kQuad;
+  const Flat f = flat_of(a.seqs, a.tokens, quad);
+  auto kernel = quad == 1 ? k_policy_back<1> : k_policy_back<kQuad>;
+  hipLaunchKernelGGL(kernel, dim3(flat_blocks(f)), dim3(kBlock), 0, (hipStream_t)hip_stream, a, bounds_of(a), f, stats, counts, dloss, dlogp, dkl, dentropy);
   return launch_status("lopt_policy_loss_backward");
 }
 
@@ -570,10 +686,9 @@ lopt_status lopt_preference_loss(const lopt_preference* terms_host, float* loss,
   hipStream_t stream = (hipStream_t)hip_stream;
   Answer* part = (Answer*)workspace;
   const PairOutputs o{loss, stats, rewards, coef};
-  with_lanes(p.lanes, [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    auto kernel = p.alone ? k_preference<G, kJoin> : k_preference<G, kBlock>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, p.pieces, p.length, p.units, part, p.alone, o);
+  with_plan(p, [&](auto g, auto threads, auto q) {
+    hipLaunchKernelGGL((k_preference<decltype(g)::value, decltype(threads)::value, decltype(q)::value>), dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, p.shift, p.length,
+                       p.units, part, p.alone, o);
   });
   if (!p.alone) hipLaunchKernelGGL(k_preference_join, dim3(1), dim3(kJoin), 0, stream, a, p.pieces, (const Answer*)part, o);
   return launch_status("lopt_preference_loss");
@@ -588,8 +703,10 @@ lopt_status lopt_preference_loss_backward(const float* coef, const uint8_t* mask
   LOPT_CHECK(check_array("dloss", dloss, 4, true));
   LOPT_CHECK(check_array("dlogp", dlogp, 4, pairs > 0));
   if (pairs == 0) return LOPT_OK;
-  const Flat f = flat_of(2 * pairs, tokens, kQuad);
-  hipLaunchKernelGGL(k_preference_back, dim3(flat_blocks(f)), dim3(kBlock), 0, (hipStream_t)hip_stream, coef, mask, ld_mask, dloss, dlogp, f);
+  const int quad = tokens < kQuad ? 1 : kQuad;
+  const Flat f = flat_of(2 * pairs, tokens, quad);
+  auto kernel = quad == 1 ? k_preference_back<1> : k_preference_back<kQuad>;
+  hipLaunchKernelGGL(kernel, dim3(flat_blocks(f)), dim3(kBlock), 0, (hipStream_t)hip_stream, coef, mask, ld_mask, dloss, dlogp, f);
   return launch_status("lopt_preference_loss_backward");
 }
 

@@ -585,21 +585,15 @@ _KINDS = {"sigmoid": 0, "hinge": 1, "squared": 2}           # lopt_preference_ki
 _REDUCTIONS = {"tokens": 0, "sequences": 1}
 
 
-def _rows_like(name: str, t: torch.Tensor, like: torch.Tensor, shape, dtype: Optional[torch.dtype]) -> Tuple[torch.Tensor, int]:
-    """(tensor, elements from row to row) of `t`, which has to be of this shape and type (None: one of the module's) on `like`'s device."""
-    if t.shape != shape or t.get_device() != like.get_device() or (t.dtype is not dtype if dtype is not None else t.dtype not in _TYPES):
-        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype} on {t.device}; {tuple(shape)} of {dtype or 'float32, bfloat16 or float16'} "
+def _token_rows(name: str, t: torch.Tensor, like: torch.Tensor, dev: int, cols: int, dtype: Optional[torch.dtype]) -> Tuple[torch.Tensor, int]:
+    """(tensor, elements from row to row) of `t`, which has to be of `like`'s shape, on its device `dev`, and of this type (None: one of the module's)."""
+    if t.shape != like.shape or t.get_device() != dev or (t.dtype is not dtype if dtype is not None else t.dtype not in _TYPES):
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype} on {t.device}; {tuple(like.shape)} of {dtype or 'float32, bfloat16 or float16'} "
                          f"on {like.device} is needed")
+    if t.is_contiguous():
+        return t, cols
     t, _, _, ld = _matrix(name, t)
     return t, ld
-
-
-def _optional_rows(name: str, t: Optional[torch.Tensor], like: torch.Tensor, dtype: Optional[torch.dtype]) -> Tuple[Optional[torch.Tensor], int, int]:
-    """(tensor, its address or 0, elements from row to row)."""
-    if t is None:
-        return None, 0, 0
-    t, ld = _rows_like(name, t, like, like.shape, dtype)
-    return t, t.data_ptr(), ld
 
 
 class PolicyLoss(NamedTuple):
@@ -613,29 +607,40 @@ def _policy_terms(logp, old_logp, advantages, mask, clip, ref_logp, kl, kl_coef,
     if _type("logp", logp) != 0:
         raise ValueError(f"logp is of {logp.dtype}; float32 is needed")
     x, seqs, tokens, ld = _matrix("logp", logp)
-    old, ld_old = _rows_like("old_logp", old_logp, logp, logp.shape, None)
+    dev = logp.get_device()
+    old, ld_old = _token_rows("old_logp", old_logp, logp, dev, tokens, None)
     each = advantages.shape == logp.shape
     if each:
-        adv, ld_adv = _rows_like("advantages", advantages, logp, logp.shape, None)
+        adv, ld_adv = _token_rows("advantages", advantages, logp, dev, tokens, None)
     else:   # one a sequence
         if advantages.dtype not in _TYPES:
             raise ValueError(f"advantages are of {advantages.dtype}; float32, bfloat16 or float16 is needed")
         adv, ld_adv = _expect("advantages", advantages, logp, advantages.dtype, logp.shape[:-1]), 1
-    if ref_logp is not None and kl is not None:
-        raise ValueError("ref_logp and kl are both given")
-    if kl_coef and ref_logp is None and kl is None:
-        raise ValueError("kl_coef without ref_logp or kl")
-    if entropy_coef and entropy is None:
-        raise ValueError("entropy_coef without entropy")
     if reduction not in _REDUCTIONS:
         raise ValueError(f"reduction={reduction!r}; 'tokens' or 'sequences' is needed")
-    ref, ref_at, ld_ref = _optional_rows("ref_logp", ref_logp, logp, None)
-    k, k_at, ld_k = _optional_rows("kl", kl, logp, torch.float32)
-    ent, ent_at, ld_ent = _optional_rows("entropy", entropy, logp, torch.float32)
-    m, m_at, ld_m = _optional_rows("mask", mask, logp, torch.bool)
+    ref = k = ent = m = None
+    ref_at = ref_type = k_at = ent_at = m_at = ld_ref = ld_k = ld_ent = ld_m = 0
+    if ref_logp is not None:
+        if kl is not None:
+            raise ValueError("ref_logp and kl are both given")
+        ref, ld_ref = _token_rows("ref_logp", ref_logp, logp, dev, tokens, None)
+        ref_at, ref_type = ref.data_ptr(), _TYPES[ref.dtype]
+    elif kl is not None:
+        k, ld_k = _token_rows("kl", kl, logp, dev, tokens, torch.float32)
+        k_at = k.data_ptr()
+    elif kl_coef:
+        raise ValueError("kl_coef without ref_logp or kl")
+    if entropy is not None:
+        ent, ld_ent = _token_rows("entropy", entropy, logp, dev, tokens, torch.float32)
+        ent_at = ent.data_ptr()
+    elif entropy_coef:
+        raise ValueError("entropy_coef without entropy")
+    if mask is not None:
+        m, ld_m = _token_rows("mask", mask, logp, dev, tokens, torch.bool)
+        m_at = m.data_ptr()
     low, high = clip
     terms = _POLICY.pack(x.data_ptr(), ld, old.data_ptr(), ld_old, adv.data_ptr(), ld_adv, ref_at, ld_ref, k_at, ld_k, ent_at, ld_ent, m_at, ld_m, seqs, tokens,
-                         low, high, kl_coef, entropy_coef, _TYPES[old.dtype], _TYPES[adv.dtype], 0 if ref is None else _TYPES[ref.dtype], not each,
+                         low, high, kl_coef, entropy_coef, _TYPES[old.dtype], _TYPES[adv.dtype], ref_type, not each,
                          _REDUCTIONS[reduction], 0)
     return terms, (x, old, adv, ref, k, ent, m), seqs, tokens
 
@@ -721,15 +726,22 @@ def preference_loss_forward(logp: torch.Tensor, ref_logp: Optional[torch.Tensor]
     if kind not in _KINDS:
         raise ValueError(f"kind={kind!r}; one of {', '.join(map(repr, _KINDS))} is needed")
     x, rows, tokens, ld = _matrix("logp", logp)
-    m, m_at, ld_m = _optional_rows("mask", mask, logp, torch.bool)
-    sums = ref_logp is not None and ref_logp.dim() == 1
-    if sums:
-        if ref_logp.dtype not in _TYPES:
-            raise ValueError(f"ref_logp is of {ref_logp.dtype}; float32, bfloat16 or float16 is needed")
-        ref = _expect("ref_logp", ref_logp, logp, ref_logp.dtype, (rows,))
-        ref_at, ld_ref = ref.data_ptr(), 1
-    else:
-        ref, ref_at, ld_ref = _optional_rows("ref_logp", ref_logp, logp, None)
+    index = logp.get_device()
+    ref = m = None
+    ref_at = ref_type = m_at = ld_ref = ld_m = 0
+    sums = False
+    if ref_logp is not None:
+        sums = ref_logp.dim() == 1
+        if sums:
+            if ref_logp.dtype not in _TYPES:
+                raise ValueError(f"ref_logp is of {ref_logp.dtype}; float32, bfloat16 or float16 is needed")
+            ref, ld_ref = _expect("ref_logp", ref_logp, logp, ref_logp.dtype, (rows,)), 1
+        else:
+            ref, ld_ref = _token_rows("ref_logp", ref_logp, logp, index, tokens, None)
+        ref_at, ref_type = ref.data_ptr(), _TYPES[ref.dtype]
+    if mask is not None:
+        m, ld_m = _token_rows("mask", mask, logp, index, tokens, torch.bool)
+        m_at = m.data_ptr()
     dev = logp.device
     loss = torch.empty((), dtype=torch.float32, device=dev)
     rewards = torch.empty(rows, dtype=torch.float32, device=dev)
@@ -739,8 +751,8 @@ def preference_loss_forward(logp: torch.Tensor, ref_logp: Optional[torch.Tensor]
     nbytes = L.lopt_preference_loss_workspace(rows // 2, tokens)
     ws = _workspace(nbytes, dev)
     terms = _PREFERENCE.pack(x.data_ptr(), ld, ref_at, ld_ref, m_at, ld_m, rows // 2, tokens, beta, label_smoothing, margin,
-                             0 if ref is None else _TYPES[ref.dtype], sums, _KINDS[kind], bool(average))
-    _run(L.lopt_preference_loss, dev.index, terms, loss.data_ptr(), stats.data_ptr(), rewards.data_ptr(), coef.data_ptr(), _ptr(ws), nbytes)
+                             ref_type, sums, _KINDS[kind], bool(average))
+    _run(L.lopt_preference_loss, index, terms, loss.data_ptr(), stats.data_ptr(), rewards.data_ptr(), coef.data_ptr(), _ptr(ws), nbytes)
     return PreferenceLoss(loss, rewards, stats, coef)
 
 
@@ -749,11 +761,11 @@ def preference_loss_backward(dloss: torch.Tensor, forward: PreferenceLoss, logp:
     if _type("logp", logp) != 0 or logp.dim() != 2 or logp.shape[0] % 2:
         raise ValueError(f"logp is {tuple(logp.shape)} of {logp.dtype}; float32 of an even number of rows is needed")
     rows, tokens = logp.shape
-    m, m_at, ld_m = _optional_rows("mask", mask, logp, torch.bool)
+    m, ld_m = (None, 0) if mask is None else _token_rows("mask", mask, logp, logp.get_device(), tokens, torch.bool)
     dloss = _expect("dloss", dloss, logp, torch.float32, ())
     coef = _expect("coef", forward.coef, logp, torch.float32, (rows,))
     dlogp = _new(logp)
-    _run(lib().lopt_preference_loss_backward, logp.get_device(), coef.data_ptr(), m_at, ld_m, dloss.data_ptr(), dlogp.data_ptr(), rows // 2, tokens)
+    _run(lib().lopt_preference_loss_backward, logp.get_device(), coef.data_ptr(), _ptr(m), ld_m, dloss.data_ptr(), dlogp.data_ptr(), rows // 2, tokens)
     return dlogp
 
 

@@ -616,17 +616,19 @@ def policy_exact(v, clip, kl_coef, entropy_coef, reduction):
         surrogate = np.where(adv == 0, 0.0, -adv * np.where(out, bound, ratio))
         slope = np.where(out, 0.0, surrogate)
         kl, ent = np.zeros_like(logp), np.zeros_like(logp)
-        # the ratio: d is rounded once, the exponential has two units; drift and kl: their argument's rounding, the series' ten units or the exponential's
-        r_ratio = U * (np.abs(d) + 5)
-        t_sur = np.abs(surrogate) * (r_ratio + 2 * U)
-        t_slope = np.abs(slope) * (r_ratio + 2 * U)
-        rest = lambda u: 16 * U * np.abs(exp_rest(u)) + U * np.abs(u) * np.abs(np.expm1(u)) + np.where(np.abs(u) < 0.5, 0.0, 4 * U * (np.exp(u) + np.abs(u)))
+        # the ratio: d is rounded once; its polynomial, the square of half of it and the additions have eight units, the hardware's power of two two of its own and, of its exponent's product and
+        # the constant in it, 1.3 of |d|; drift and kl: their argument's rounding, the polynomial's ten units or the exponential's
+        r_ratio = U * (3 * np.abs(d) + 8)
+        # ratios below 2^-126 are 0, as the hardware's power of two leaves out subnormal numbers
+        t_sur = np.abs(surrogate) * (r_ratio + 2 * U) + 2.0 ** -126 * np.abs(adv)
+        t_slope = np.abs(slope) * (r_ratio + 2 * U) + 2.0 ** -126 * np.abs(adv)
+        rest = lambda u: 16 * U * np.abs(exp_rest(u)) + U * np.abs(u) * np.abs(np.expm1(u)) + np.where(np.abs(u) < 1.999, 0.0, U * ((2 * np.abs(u) + 4) * np.exp(u) + 2 * np.abs(u) + 2))
         t_kl = np.zeros_like(logp)
         if v["ref"] is not None:
             u = v["ref"] - logp
             kl, t_kl = exp_rest(u), rest(u)
             slope = slope - kl_coef * np.expm1(u)
-            t_slope = t_slope + abs(kl_coef) * (t_kl + 3 * U * np.abs(np.expm1(u)) + 2 * U * np.abs(u)) + U * np.abs(slope)
+            t_slope = t_slope + abs(kl_coef) * (t_kl + 3 * U * np.abs(np.expm1(u)) + 2 * U * np.abs(u) + U) + U * np.abs(slope)
         elif v["kl"] is not None:
             kl = v["kl"]
         if v["ent"] is not None:
@@ -635,7 +637,8 @@ def policy_exact(v, clip, kl_coef, entropy_coef, reduction):
         N, S = n.sum(), float((n > 0).sum())
         w = np.where(keep, 1.0 / max(N, 1) if reduction == "tokens" else 1.0 / np.maximum(n * S, 1)[:, None], 0.0)
         terms = [surrogate, kl, ent, out.astype(float), ratio, exp_rest(d)]
-        tols = [t_sur, t_kl, 0 * ent, 0 * ent, ratio * r_ratio, rest(d)]
+        # ratios, less 1, and drifts are added up four at a time in 32 bits, three additions, the rest in 64
+        tols = [t_sur, t_kl, 0 * ent, 0 * ent, ratio * r_ratio + 3 * U * np.abs(np.expm1(d)), rest(d) + 3 * U * exp_rest(d)]
         mean = lambda a: float(np.where(keep, w * a, 0.0).sum())
         means, t_means = [mean(a) for a in terms], [mean(t) + 2 * U * abs(mean(a)) + 1e-14 * mean(np.abs(a)) for t, a in zip(tols, terms)]
         has_kl = v["ref"] is not None or v["kl"] is not None
