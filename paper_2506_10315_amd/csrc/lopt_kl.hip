@@ -182,21 +182,21 @@ __global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, Outputs o) {
 }
 
 // A wavefront's sums over every `step`-th element's piece of a row, from `first` to `end`, counted from the pack in which the row of x begins.
-template <typename T, int E>
+template <typename T, int E, bool NT>
 __device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* r, int off, int64_t first, int64_t end, int64_t step, float c) {
   typedef Piece<T, E> P;
   Apart s = nothing();
   P p, q;
   if (first < end) {
-    p.load(x, (int)first, off, a.n);
-    q.load(r, (int)first, off, a.n);
+    p.template load<NT>(x, (int)first, off, a.n);
+    q.template load<NT>(r, (int)first, off, a.n);
   }
   for (; first < end; first += step) {
     float u[E], v[E];
     P next_p, next_q;
     if (first + step < end) {
-      next_p.load(x, (int)(first + step), off, a.n);
-      next_q.load(r, (int)(first + step), off, a.n);
+      next_p.template load<NT>(x, (int)(first + step), off, a.n);
+      next_q.template load<NT>(r, (int)(first + step), off, a.n);
     }
     p.unpack(u);
     q.unpack(v);
@@ -208,7 +208,8 @@ __device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* 
 }
 
 // Joins what the wavefronts of a workgroup have, from common maxima; thread 0 gets it. `room`: free before, and after another barrier.
-struct Room { float mx[16], mr[16]; Total total[16]; };
+constexpr int kMostWaves = 8;
+struct Room { float mx[16], mr[16]; Total total[16]; };   // 16 for the join of segments
 __device__ __forceinline__ Total block_total(const Apart& s, float c, Room& room) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   float mx = wave_max(s.mx), mr = wave_max(s.mr);
@@ -227,9 +228,11 @@ __device__ __forceinline__ Total block_total(const Apart& s, float c, Room& room
   return t;
 }
 
-// A workgroup a row, its wavefronts a piece each in turn.
-template <typename T, int E>
-__global__ __launch_bounds__(1024) void k_kl(Rows<T> a, Outputs o) {
+// A workgroup a row, its wavefronts a piece each in turn. Bound by memory and by vector issue (21.6 instructions for a pair of logits, two powers of two among them, as 4 each): 4096x50257
+// bf16 of which an eighth does not count 145 us, 5.0 TB/s, where loads alone take 127; 3000x50257 fp32 220 us, 5.5 TB/s. Registers for four wavefronts a unit; fp32, whose packs take
+// twice as many, for three (spilled for four: 247 us), bf16 for three 159.
+template <typename T, int E, bool NT>
+__global__ __launch_bounds__(kMostWaves * kWave, sizeof(T) == 4 ? 3 : 4) void k_kl(Rows<T> a, Outputs o) {
   typedef Piece<T, E> P;
   __shared__ Room room;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -241,7 +244,7 @@ __global__ __launch_bounds__(1024) void k_kl(Rows<T> a, Outputs o) {
     }
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
-    const Apart s = sums_of<T, E>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize, c);
+    const Apart s = sums_of<T, E, NT>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize, c);
     const Total t = block_total(s, c, room);
     if (threadIdx.x == 0) write_row(o, row, t, c);
     if (row + gridDim.x < a.rows) __syncthreads();
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
     const int64_t end = min(from + (int64_t)pieces * P::kSize, (int64_t)a.n + off);
-    const Apart s = sums_of<T, 16>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize, c);
+    const Apart s = sums_of<T, 16, false>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize, c);
     const Total t = block_total(s, c, room);
     if (threadIdx.x == 0) part[unit] = t;
     __syncthreads();
@@ -311,6 +314,7 @@ __global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t 
   write_row(o, row, t, c);
 }
 
+constexpr int64_t kCacheBytes = 256 << 20;
 // How rows are shared out.
 enum RowForm { kRowWave, kRowBlock, kRowSplit };
 struct RowPlan {
@@ -322,12 +326,15 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab) {
   const int64_t n = vocab + 7;   // a row counted from its pack
   if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, 0, 0};
   const int64_t pieces = (n + 1023) / 1024;
-  if (n <= 64 * 2048 || rows >= 256) {
-    const int64_t long_rows = pieces >= 32 && rows >= 2048 ? 8 : std::clamp<int64_t>((pieces + 4) / 5, 1, 4);
-    return RowPlan{kRowBlock, 16, (int)std::max(long_rows, std::min<int64_t>({16, pieces, 4096 / rows})), 0, 0};
+  // Few long rows in segments, which costs a launch and a workspace more on the host, some 5 us. us in a graph, a workgroup a row / segments: 1x50257 fp32 14.2 / 9.1, 1x100000 bf16
+  // 21 / 8.8, 12x99760 fp32 23.5 / 10.3, 64x100000 bf16 24 / 16, 128x70000 18.4 / 19.5, 200x100000 25 / 29, 200x131000 fp32 40 / 42.
+  if (rows <= 64 ? n > 64 * 1024 : rows < 256 && n > 256 * 1024) {
+    const int64_t per = std::clamp<int64_t>(rows * pieces / 2048, 4, 32);
+    return RowPlan{kRowSplit, 16, 4, per, (pieces + per - 1) / per};
   }
-  const int64_t per = std::clamp<int64_t>(rows * pieces / 2048, 4, 32);
-  return RowPlan{kRowSplit, 16, 4, per, (pieces + per - 1) / per};
+  // Wavefronts: one for about five pieces up to four, with fewer than 1024 rows as many as make 4096 in all, up to eight. us with 1 / 2 / 4 / 8: 20000x5000 bf16 83 / 94 / 116,
+  // 8192x16000 104 / 110 / 113 / 130, 4096x50257 167 / 169 / 157 / 177, 2048x131000 239 / 217 / 211 / 218, 512x50257 62 / 42 / 27 / 26, 256x32000 38 / 22 / 14 / 12.
+  return RowPlan{kRowBlock, 16, (int)std::max(std::clamp<int64_t>((pieces + 4) / 5, 1, 4), std::min<int64_t>({kMostWaves, pieces, 4096 / rows})), 0, 0};
 }
 
 // The gradients, element by element, with d = scale ((x - r) - (mx - mr)) and g = dkl:
@@ -440,7 +447,10 @@ lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64
       auto kernel = plan.lane == 8 ? k_kl_short<T, 8> : plan.lane == 16 ? k_kl_short<T, 16> : k_kl_short<T, 32>;
       hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, o);
     } else if (plan.form == kRowBlock) {
-      hipLaunchKernelGGL((k_kl<T, 16>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), block, 0, stream, a, o);
+      // what the Infinity Cache cannot hold is not left there: 4096x50257 bf16 165 -> 157 us, 20000x5000 93 -> 83, but 1024x50257, which fits, 43 -> 46
+      const bool large = 2 * rows * vocab * (int64_t)sizeof(T) > kCacheBytes;
+      auto kernel = large ? k_kl<T, 16, true> : k_kl<T, 16, false>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), block, 0, stream, a, o);
     } else {
       Total* part = (Total*)workspace;
       hipLaunchKernelGGL(k_kl_split<T>, dim3((unsigned)std::min<int64_t>(rows * plan.segments, 1 << 22)), block, 0, stream, a, plan.segments, (uint32_t)plan.pieces, part);

@@ -42,11 +42,12 @@ struct Piece {
   }
   // Element of lane 0 that the wavefront's j-th packs begin with: below 0, they begin ahead of the row; n or above, they lie behind it.
   __device__ __forceinline__ int from(int j) const { return first + j * kWave * V - off; }
+  template <bool NT = false>
   __device__ __forceinline__ void load(const T* row, int first_, int off_, int n_) {
     first = first_, off = off_, n = n_;
     if (n >= V) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) raw[j] = *(const pack*)(row + begin(j));
+      for (int j = 0; j < N; ++j) raw[j] = NT ? __builtin_nontemporal_load((const pack*)(row + begin(j))) : *(const pack*)(row + begin(j));
     } else {
 #pragma unroll
       for (int i = 0; i < E; ++i) raw[i / V][i % V] = mine(i) ? row[index(i)] : (T)-INFINITY;
