@@ -11,7 +11,9 @@ namespace {
 // A workgroup takes kChunk neighbouring packs of 16 bytes, four a thread.
 constexpr int kPacks = 4, kChunk = kPacks * kBlock;
 
-template <typename T>
+// WHOLE: rows are whole packs, and a word is compared where it is needed. Else the pack that would pass a row's end ends with it, and its bits are moved with it (5001x1531 fp16 with the
+// elements of such packs loaded one by one 12.8 us, so FIGURE_ODD). 8192x4096 bf16 FIGURE_WHOLE us; with ten rounds of two exclusive ors each in place of one of three inputs 31.
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_dropout(const T* x, int64_t ld_x, T* y, int64_t ld_y, Flat f, Dropout d) {
   constexpr int V = Pack<T>::n;
   typedef typename Pack<T>::type pack;
@@ -27,23 +29,48 @@ __global__ __launch_bounds__(kBlock) void k_dropout(const T* x, int64_t ld_x, T*
     for (int j = 0; j < kPacks; ++j) {
       have[j] = chunk.at(f, V, j * kBlock + threadIdx.x, row[j], col[j]);
       in[j] = pack{};
-      if (have[j] && col[j] + V <= cols) in[j] = __builtin_nontemporal_load((const pack*)(x + row[j] * ld_x + col[j]));
+      if (have[j]) in[j] = __builtin_nontemporal_load((const pack*)(x + row[j] * ld_x + (WHOLE ? col[j] : min(col[j], cols - V))));
     }
 #pragma unroll
     for (int j = 0; j < kPacks; ++j) {
       if (!have[j]) continue;
-      const uint32_t bits = d.on ? words.stay<V>((uint32_t)row[j], col[j]) : ~0u;
-      T* out = y + row[j] * ld_y + col[j];
-      if (col[j] + V <= cols) {
-        pack o;
+      const uint32_t at = WHOLE ? col[j] : min(col[j], cols - V), skip = col[j] - at;
+      T* out = y + row[j] * ld_y + at;
+      pack o;
+      if (WHOLE && d.on && !d.none) {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+          uint32_t w[4];
+          words.four((uint32_t)row[j], col[j] / 4 + e / 4, w);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[e + i] = from_f32<T>(w[i] >= d.least ? to_f32(in[j][e + i]) * d.scale : 0.f);
+        }
+      } else {
+        const uint32_t bits = d.on ? words.stay<V>((uint32_t)row[j], col[j]) << skip : ~0u;
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] = from_f32<T>(where_bit(bits, e, to_f32(in[j][e]) * d.scale));
+      }
+      if (skip == 0) {
         __builtin_nontemporal_store(o, (pack*)out);
       } else {
-        const T* p = x + row[j] * ld_x + col[j];
-        for (uint32_t e = 0; e < cols - col[j]; ++e) out[e] = bits >> e & 1 ? from_f32<T>(to_f32(p[e]) * d.scale) : (T)0.f;
+#pragma unroll
+        for (int e = 1; e < V; ++e)
+          if (e >= (int)skip) out[e] = o[e];
       }
     }
+  }
+}
+
+// Rows shorter than a pack: an element a thread.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_dropout_narrow(const T* x, int64_t ld_x, T* y, int64_t ld_y, Flat f, Dropout d) {
+  const Words words(d);
+  for (int64_t first = (int64_t)blockIdx.x * kBlock; first < f.total; first += (int64_t)gridDim.x * kBlock) {
+    int64_t row;
+    uint32_t col;
+    if (!Chunk(f, first).at(f, 1, threadIdx.x, row, col)) continue;
+    const uint32_t bits = d.on ? words.stay<1>((uint32_t)row, col) : 1u;
+    y[row * ld_y + col] = from_f32<T>(where_bit(bits, 0, to_f32(x[row * ld_x + col]) * d.scale));
   }
 }
 
@@ -68,9 +95,12 @@ extern "C" lopt_status lopt_dropout(const void* x, int64_t ld_x, void* y, int64_
   if (rows == 0) return LOPT_OK;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    const Flat f = flat_of(rows, cols, Pack<T>::n);
-    const unsigned blocks = (unsigned)std::min<int64_t>((f.total + kChunk - 1) / kChunk, 1 << 22);
-    hipLaunchKernelGGL(k_dropout<T>, dim3(blocks), dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)x, ld_x, (T*)y, ld_y, f, d);
+    constexpr int V = Pack<T>::n;
+    const Flat f = flat_of(rows, cols, cols < V ? 1 : V);
+    const int chunk = cols < V ? kBlock : kChunk;
+    const unsigned blocks = (unsigned)std::min<int64_t>((f.total + chunk - 1) / chunk, 1 << 22);
+    auto kernel = cols < V ? k_dropout_narrow<T> : cols % V == 0 ? k_dropout<T, true> : k_dropout<T, false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), 0, (hipStream_t)hip_stream, (const T*)x, ld_x, (T*)y, ld_y, f, d);
   });
   return launch_status("lopt_dropout");
 }

@@ -32,6 +32,9 @@ inline lopt_status check_dropout(float p, const uint64_t* seed_device, Dropout* 
   return LOPT_OK;
 }
 
+// One instruction, which the compiler does not find by itself.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+
 // The generator of one launch, its key read.
 struct Words {
   uint32_t key0, key1, offset0, offset1, least;
@@ -43,30 +46,33 @@ struct Words {
     least = d.least;
     none = d.none;
   }
-  // Bit e: whether column 4 block + e of the row stays.
-  __device__ __forceinline__ uint32_t four(uint32_t row, uint32_t block) const {
+  // The words of columns 4 block to 4 block + 3 of the row.
+  __device__ __forceinline__ void four(uint32_t row, uint32_t block, uint32_t (&w)[4]) const {
     uint32_t c0 = block, c1 = row, c2 = offset0, c3 = offset1, k0 = key0, k1 = key1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
       const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-      c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-      c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+      c0 = xor3((uint32_t)(b >> 32), c1, k0);
+      c2 = xor3((uint32_t)(a >> 32), c3, k1);
       c1 = (uint32_t)b;
       c3 = (uint32_t)a;
       k0 += 0x9E3779B9u;
       k1 += 0xBB67AE85u;
     }
-    const uint32_t bits = (c0 >= least ? 1u : 0u) | (c1 >= least ? 2u : 0u) | (c2 >= least ? 4u : 0u) | (c3 >= least ? 8u : 0u);
-    return none ? 0u : bits;
+    w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
   }
-  // The same of V columns from `col` on, a multiple of 4 (of one column, any).
+  // Bit e: whether column `col` + e of the row stays, of V columns from a multiple of 4 on (of one column, any).
   template <int V>
   __device__ __forceinline__ uint32_t stay(uint32_t row, uint32_t col) const {
-    if (V == 1) return four(row, col / 4) >> (col & 3) & 1u;
-    uint32_t bits = 0;
+    uint32_t bits = 0, w[4];
 #pragma unroll
-    for (int e = 0; e < V; e += 4) bits |= four(row, (col + e) / 4) << e;
-    return bits;
+    for (int e = 0; e < V; e += 4) {
+      four(row, col / 4 + e / 4, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bits |= (w[i] >= least ? 1u : 0u) << (e + i);
+    }
+    if (none) bits = 0;
+    return V == 1 ? bits >> (col & 3) & 1u : bits;
   }
 };
 
