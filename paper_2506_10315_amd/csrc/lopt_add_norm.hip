@@ -83,15 +83,15 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_add_norm(const T* x, int
       for (int i = j * V; i < j * V + V; ++i) v[i] = v[i] * rstd * w[i] + b[i];
       RowOf<T, S>::store(y + r * ld_y, s, j, v + j * V);
     }
-    if (threadIdx.x % G == 0) {
+    if ((G > 64 ? threadIdx.x : threadIdx.x % G) == 0) {
       if (mean_out) mean_out[r] = mean;
       if (rstd_out) rstd_out[r] = rstd;
     }
   }
 }
 
-// The gradient of the same rows; the columns' sums as in the layer norm's.
-template <typename T, typename R, int G, int N>
+// The gradient of the same rows; the columns' sums as in the layer norm's, or not at all.
+template <typename T, typename R, int G, int N, bool COLUMNS>
 __global__ __launch_bounds__(Group<G>::kThreads) void k_add_norm_back(const T* dy, int64_t ld_dy, const R* dh, int64_t ld_dh, const R* h, int64_t ld_h,
                                                                       const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t ld_dx, R* dres,
                                                                       int64_t ld_dres, AddNorm a, Dropout d, float* __restrict__ part) {
@@ -132,8 +132,10 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_add_norm_back(const T* d
       const float g = rdy.get(i);
       xh[i] = (rh.get(i) - mu) * rs;
       v[i] = g * w[i];
-      sw[i] += g * xh[i];
-      sb[i] += g;
+      if (COLUMNS) {
+        sw[i] += g * xh[i];
+        sb[i] += g;
+      }
       const float am = s.mine(i) ? v[i] : 0.f;
       s1 += am;
       s2 += am * xh[i];
@@ -158,7 +160,8 @@ __global__ __launch_bounds__(Group<G>::kThreads) void k_add_norm_back(const T* d
       }
     }
   }
-  if (part) columns_of_block<S, G, kRows>(s, sw, sb, part, a.cols);
+  if constexpr (COLUMNS)
+    if (part) columns_of_block<S, G, kRows>(s, sw, sb, part, a.cols);
 }
 
 // ---- rows too long for registers: a workgroup a row, read again for every use.
@@ -266,12 +269,33 @@ __global__ __launch_bounds__(1024) void k_add_norm_long_rows(const T* dy, int64_
 // over fp32 in place of 27.5, 35 over bf16 in place of 23, 16384x2048 117 / 116, 5001x1531 fp16 28 / 28.
 constexpr int kMost = 16;
 
+// with_group's, and 192 lanes a row where they suffice: 5001x1531 fp16 forward 17.2 -> 16.0 us, backward 28.5 -> 26.4, 20000x1280 bf16 47 -> 42, 72 -> 65.
+template <int V, typename F>
+bool with_rows(int64_t cols, F&& f) {
+  constexpr int N = kMost / V / 2;
+  const int64_t packs = (cols + V - 1) / V;
+  if (packs > 128 * N && packs <= 192 * N) {
+    f(std::integral_constant<int, 192>{}, std::integral_constant<int, N>{});
+    return true;
+  }
+  return with_group<V, kMost>(cols, f);
+}
+
+// Rows of the widest group have no registers left for the columns' sums (1024x16384 bf16 over fp32 with spills 107 us, over bf16 76): theirs are
+// a pass of their own, as those of longer rows (78, 59).
+template <int V, int G, int N> constexpr bool kWide = G == 1024 && N * V == kMost;
+
+// Workgroups, each of which leaves a row of partial sums; for 192 lanes 512 / 768 / 1024 of them: 5001x1531 fp16 30.6 / 26.4 / 27.4 us, 1000x1531 14.5 / 16.5 / 19.7.
 template <int G>
-int64_t back_blocks(int64_t rows) { return std::min<int64_t>((rows + Group<G>::kRows - 1) / Group<G>::kRows, G == 1024 ? 256 : 512); }
+int64_t back_blocks(int64_t rows) {
+  return std::min<int64_t>((rows + Group<G>::kRows - 1) / Group<G>::kRows, G == 1024 ? 256 : G == 192 && rows >= 4096 ? 768 : 512);
+}
 template <int V>
 int64_t back_parts(int64_t rows, int64_t cols) {
   int64_t parts = slabs_of(rows);
-  with_group<V, kMost>(cols, [&](auto g, auto) { parts = back_blocks<decltype(g)::value>(rows); });
+  with_rows<V>(cols, [&](auto g, auto n) {
+    if (!kWide<V, decltype(g)::value, decltype(n)::value>) parts = back_blocks<decltype(g)::value>(rows);
+  });
   return parts;
 }
 
@@ -342,7 +366,7 @@ lopt_status lopt_dropout_add_layer_norm(const void* x, int64_t ld_x, const void*
   with_types(type, residual_type, [&](auto t, auto u) {
     using T = decltype(t);
     using R = decltype(u);
-    const bool held = with_group<Pack<T>::n, kMost>(cols, [&](auto g, auto n) {
+    const bool held = with_rows<Pack<T>::n>(cols, [&](auto g, auto n) {
       constexpr int G = decltype(g)::value, N = decltype(n)::value;
       const int64_t blocks = std::min<int64_t>((rows + Group<G>::kRows - 1) / Group<G>::kRows, G == 1024 ? 512 : 2048);
       hipLaunchKernelGGL((k_add_norm<T, R, G, N>), dim3((unsigned)blocks), dim3(Group<G>::kThreads), 0, stream, (const T*)x, ld_x, (const R*)residual, ld_res,
@@ -401,10 +425,13 @@ lopt_status lopt_dropout_add_layer_norm_backward(const void* dy, int64_t ld_dy, 
     int64_t parts = 0;
     if (rows > 0) {
       parts = back_parts<Pack<T>::n>(rows, cols);
-      const bool held = with_group<Pack<T>::n, kMost>(cols, [&](auto g, auto n) {
+      const bool held = with_rows<Pack<T>::n>(cols, [&](auto g, auto n) {
         constexpr int G = decltype(g)::value, N = decltype(n)::value;
-        hipLaunchKernelGGL((k_add_norm_back<T, R, G, N>), dim3((unsigned)parts), dim3(Group<G>::kThreads), 0, stream, (const T*)dy, ld_dy, (const R*)dh, ld_dh,
-                           (const R*)h, ld_h, mean, rstd, (T*)dx, ld_dx, (R*)dresidual, ld_dres, a, d, columns ? part : nullptr);
+        constexpr bool wide = kWide<Pack<T>::n, G, N>;
+        if (wide && columns) launch_long_columns<T, R>((const T*)dy, ld_dy, (const R*)h, ld_h, mean, rstd, rows, a.cols, parts, part, stream);
+        if (!wide || dx || dresidual)
+          hipLaunchKernelGGL((k_add_norm_back<T, R, G, N, !wide>), dim3((unsigned)(wide ? std::min<int64_t>(rows, 256) : parts)), dim3(Group<G>::kThreads), 0, stream, (const T*)dy,
+                             ld_dy, (const R*)dh, ld_dh, (const R*)h, ld_h, mean, rstd, (T*)dx, ld_dx, (R*)dresidual, ld_dres, a, d, columns && !wide ? part : nullptr);
       });
       if (!held) {
         if (columns) launch_long_columns<T, R>((const T*)dy, ld_dy, (const R*)h, ld_h, mean, rstd, rows, a.cols, parts, part, stream);

@@ -77,7 +77,7 @@ struct Share {
   int skip[P];
   bool have[P];
   __device__ __forceinline__ Share(uint32_t cols) {
-    const uint32_t lane = threadIdx.x & (G - 1);
+    const uint32_t lane = G > 64 ? threadIdx.x : threadIdx.x & (G - 1);   // groups of more than a wavefront are workgroups
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const uint32_t k = (j * G + lane) * V;
