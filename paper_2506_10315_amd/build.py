@@ -14,6 +14,7 @@ OBJ = os.path.join(PKG, "_build")
 
 # (source, object suffix, extra defines): the apply pass is compiled once per optimizer kind
 UNITS = [
+    ("lopt_add_norm.hip", "add_norm", []),   # the longest
     ("lopt_api.hip", "api", []),
     ("lopt_kernels.hip", "kernels", []),
     ("lopt_apply_valu.hip", "apply_small_fc", ["-DLOPT_APPLY_KIND=0"]),
@@ -26,7 +27,6 @@ UNITS = [
     ("lopt_layer_norm.hip", "layer_norm", []),
     ("lopt_logprobs.hip", "logprobs", []),
     ("lopt_dropout.hip", "dropout", []),
-    ("lopt_add_norm.hip", "add_norm", []),
     ("lopt_kl.hip", "kl", []),
     ("lopt_losses.hip", "losses", []),
 ]

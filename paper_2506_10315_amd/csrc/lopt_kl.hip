@@ -314,7 +314,6 @@ __global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t 
   write_row(o, row, t, c);
 }
 
-constexpr int64_t kCacheBytes = 256 << 20;
 // How rows are shared out.
 enum RowForm { kRowWave, kRowBlock, kRowSplit };
 struct RowPlan {

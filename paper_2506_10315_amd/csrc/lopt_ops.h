@@ -19,6 +19,8 @@ template <> struct Pack<float> { static constexpr int n = 4; typedef float type 
 template <> struct Pack<bf16_t> { static constexpr int n = 8; typedef bf16_t type __attribute__((ext_vector_type(8), aligned(2))); };
 template <> struct Pack<f16_t> { static constexpr int n = 8; typedef f16_t type __attribute__((ext_vector_type(8), aligned(2))); };
 
+constexpr int64_t kCacheBytes = 256 << 20;   // the Infinity Cache
+
 inline size_t type_bytes(uint32_t type) { return type == LOPT_F32 ? 4 : 2; }
 
 // Calls `f` with a value of the element type.

@@ -121,12 +121,13 @@ struct RowOf {
   static constexpr bool N = S::kPacks;
   typedef typename Run<T, N ? S::V : 1>::type pack;
   pack raw[S::P];
+  template <bool NT = false>
   __device__ __forceinline__ void load(const T* row, const S& s) {
 #pragma unroll
     for (int j = 0; j < S::P; ++j) {
       raw[j] = pack{};
       if (s.have[j]) {
-        if (N) raw[j] = *(const pack*)(row + s.at[j]);
+        if (N) raw[j] = NT ? __builtin_nontemporal_load((const pack*)(row + s.at[j])) : *(const pack*)(row + s.at[j]);
         else raw[j][0] = row[s.at[j]];
       }
     }

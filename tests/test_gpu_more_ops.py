@@ -248,6 +248,43 @@ def test_dropout_add_layer_norm_strides_and_margins(cols, kind, rkind):
     assert torch.equal(bh[:, :6], big[3][:, :6]) and torch.equal(bh[:, 6 + cols:], big[3][:, 6 + cols:])
 
 
+def test_dropout_add_layer_norm_beyond_the_cache():
+    """Arrays of more than 256 MB are read another way: the first rows with dropout, the last without, to the bit as by themselves."""
+    import torch
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    rows, cols, n = 25001, 1999, 65
+    x, dy = (torch.randn(rows, cols, device="cuda:0", generator=gen).bfloat16() for _ in range(2))
+    res, dh = (torch.randn(rows, cols, device="cuda:0", generator=gen) for _ in range(2))
+    w = torch.randn(cols, device="cuda:0", generator=gen)
+    for p, part in ((0.3, slice(0, n)), (0.0, slice(rows - n, rows))):
+        y, h, mean, rstd = ops().dropout_add_layer_norm_forward(x, res, w, w, p, 5, 6)
+        few = ops().dropout_add_layer_norm_forward(x[part], res[part], w, w, p, 5, 6)
+        # the second rows start off the grid in the one and the other alike: their distance is odd in both
+        for a, b in zip((y, h, mean, rstd), few):
+            assert torch.equal(a[part], b), p
+        got = ops().dropout_add_layer_norm_backward(dy, dh, h, w, mean, rstd, p, 5, 6)
+        few = ops().dropout_add_layer_norm_backward(dy[part], dh[part], h[part], w, mean[part], rstd[part], p, 5, 6)
+        assert torch.equal(got[0][part], few[0]) and torch.equal(got[1][part], few[1]), p
+        xh = (h - mean[:, None]) * rstd[:, None]
+        want = (dy.double() * xh).sum(0)
+        # xh has two roundings, a column 25001 terms: up to 144 a lane, then the tree
+        assert bool(((got[2].double() - want).abs() <= (144 + 30) * U * (dy.double() * xh).abs().sum(0)).all())
+
+
+def test_one_tensor_as_block_and_residual():
+    import torch
+    x = torch.randn(7, 64, device="cuda:0", requires_grad=True)
+    w = torch.randn(64, device="cuda:0")
+    for p in (0.0, 0.5):
+        x.grad = None
+        y, h = ops().dropout_add_layer_norm(x, x, w, None, p, 3)
+        (y.square().sum() + h.sum()).backward()
+        a, b = x.detach().clone().requires_grad_(), x.detach().clone().requires_grad_()
+        y, h = ops().dropout_add_layer_norm(a, b, w, None, p, 3)
+        (y.square().sum() + h.sum()).backward()
+        assert torch.equal(x.grad, a.grad + b.grad)
+
+
 def test_dropout_add_layer_norm_zero_rows():
     import torch
     x = torch.empty(0, 64, device="cuda:0", dtype=torch.bfloat16)
