@@ -68,8 +68,12 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t* mask, int64_t i) {
 }
 
 // How sequences are shared out: a group of `lanes` lanes takes a sequence, or one of its `pieces` of `length` tokens, four neighbouring tokens a lane in turn.
+// Of kMany sequences or more fewer lanes each go on more often, so that fewer are idle at the ends. us of the loss and its gradient with lanes for one time | for up to four:
+// 60000x30 35 | 26, 30000x100 50 | 36, 14000x200 33.6 | 31, 8000x400 50 | 36, 4000x700 35.3 | 28.4; of few 1000x100 12.5 | 14, 300x900 12.9 | 17. 200000x10 by 16 lanes each
+// 68, by 4 34.
 // Few sequences are cut so that there are about kPieces pieces, a power of two of each, with which lanes of the join share out a sequence. us of k_policy and its join for
 // 512x8192 tokens cut into 512, 1024, 2048, 4096: 23.8 + 4.0, 16.8 + 4.2, 19.0 + 5.1, 20.9 + 6.9.
+constexpr int64_t kMany = 2048;
 struct Plan {
   int lanes, threads, shift, quad;   // pieces: 2^shift; neighbouring tokens of a lane
   int64_t pieces, length, units, blocks;
@@ -78,7 +82,8 @@ struct Plan {
 inline Plan plan_of(int64_t seqs, int64_t tokens) {
   Plan p{};
   p.quad = tokens < kQuad ? 1 : kQuad;
-  p.lanes = tokens <= 64 ? 16 : tokens <= 256 ? 64 : kBlock;
+  const int most = seqs >= kMany ? 4 : 1;   // times that a lane goes on
+  p.lanes = tokens <= (most > 1 ? 2 : 1) * 4 * kQuad ? 4 : tokens <= 16 * kQuad * most ? 16 : tokens <= 64 * kQuad * most ? 64 : kBlock;
   if (seqs * tokens <= kAlone) {   // all sequences at one time, if fewer lanes each can do that
     int lanes = p.lanes;
     while (lanes > 16 && seqs * lanes > kJoin) lanes /= 4;
@@ -105,7 +110,8 @@ void with_plan(const Plan& p, F&& f) {
     if (p.alone) f(g, integral_constant<int, kJoin>{}, q);
     else f(g, integral_constant<int, kBlock>{}, q);
   };
-  if (p.quad == 1) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (p.quad == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+  else if (p.lanes == 4) go(integral_constant<int, 4>{}, integral_constant<int, kQuad>{});
   else if (p.lanes == 16) go(integral_constant<int, 16>{}, integral_constant<int, kQuad>{});
   else if (p.lanes == 64) go(integral_constant<int, 64>{}, integral_constant<int, kQuad>{});
   else go(integral_constant<int, kBlock>{}, integral_constant<int, kQuad>{});
@@ -514,8 +520,88 @@ __device__ __forceinline__ void write_pair(const lopt_preference& a, int64_t pai
   sum[4] += rr;
 }
 
-// All pairs, by one workgroup of kJoin threads; `lanes` lanes take a pair.
-__device__ __forceinline__ void join_pairs(const lopt_preference& a, int64_t pieces, const Answer* part, const PairOutputs& o, double* red) {
+// The loss and the statistics, by thread 0 of a workgroup whose threads have sums of pairs.
+__device__ __forceinline__ void write_preference(const lopt_preference& a, double (&sum)[kPairSums], const PairOutputs& o, double* red) {
+  block_totals(sum, red);
+  if (threadIdx.x != 0) return;
+  const double w = a.pairs > 0 ? 1.0 / (double)a.pairs : 0.0;
+  *o.loss = (float)(sum[0] * w);
+#pragma unroll
+  for (int i = 1; i < 5; ++i) o.stats[i - 1] = (float)(sum[i] * w);
+}
+
+// What Q tokens add to an answer.
+template <int Q>
+__device__ __forceinline__ void add_tokens(const lopt_preference& a, int64_t row, int64_t at, uint32_t bits, bool has_ref, Answer& own) {
+  if (!bits) return;   // padding is not read
+  float logp[Q], ref[Q] = {};
+  load_as<Q>(a.logp + row * a.ld_logp + at, logp);
+  if (has_ref) load_of<Q>(a.ref, a.ref_type, row * a.ld_ref + at, ref);
+#pragma unroll
+  for (int e = 0; e < Q; ++e) own.sum += bits >> e & 1 ? (double)logp[e] - (double)ref[e] : 0.0;
+  own.count += (double)__popc(bits);
+}
+
+// Whole answers: a group takes both of a pair and writes what it gives; workgroups leave one row of sums each, or with `alone` the loss. us of the loss and its gradient when
+// one workgroup joined all pairs | so: 30000x100 56 | 18.4, 100 000 pairs of few tokens 147 | 20.
+template <int G, int kThreads, int Q>
+__global__ __launch_bounds__(kThreads) void k_preference(lopt_preference a, double* __restrict__ part, bool alone, PairOutputs o) {
+  __shared__ double red[kThreads / kWave * kPairSums];
+  const int lane = threadIdx.x % G;
+  constexpr int kGroups = kThreads / G;
+  const bool has_ref = a.ref && !a.ref_sums;
+  double sum[kPairSums] = {};
+  for (int64_t base = (int64_t)blockIdx.x * kGroups; base < a.pairs; base += (int64_t)gridDim.x * kGroups) {
+    const int64_t pair = base + threadIdx.x / G;
+    const bool have = pair < a.pairs;
+    Answer own[2] = {};
+    for (int64_t t = lane * Q; have && t < a.tokens; t += G * Q) {
+      const int64_t at = min(t, a.tokens - Q);
+      uint32_t bits[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bits[i] = load_mask<Q>(a.mask, (i * a.pairs + pair) * a.ld_mask + at) & ~0u << (t - at);   // not those of the lane before
+#pragma unroll
+      for (int i = 0; i < 2; ++i) add_tokens<Q>(a, i * a.pairs + pair, at, bits[i], has_ref, own[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      own[i].sum = group_total<G>(own[i].sum, red);
+      own[i].count = group_total<G>(own[i].count, red);
+    }
+    if (lane == 0 && have) write_pair(a, pair, own[0], own[1], o, sum);
+  }
+  if (alone) return write_preference(a, sum, o, red);
+  block_totals(sum, red);
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int i = 0; i < kPairSums; ++i) part[(int64_t)blockIdx.x * kPairSums + i] = sum[i];
+}
+__global__ __launch_bounds__(kJoin) void k_preference_sums(lopt_preference a, int64_t rows, const double* __restrict__ part, PairOutputs o) {
+  __shared__ double red[kJoin / kWave * kPairSums];
+  double sum[kPairSums] = {};
+  for (int64_t k = threadIdx.x; k < rows; k += kJoin) {
+#pragma unroll
+    for (int i = 0; i < kPairSums; ++i) sum[i] += part[k * kPairSums + i];
+  }
+  write_preference(a, sum, o, red);
+}
+
+// Few long answers: a workgroup takes a piece, and one workgroup joins them, `lanes` lanes a pair.
+__global__ __launch_bounds__(kBlock) void k_preference_pieces(lopt_preference a, int shift, int64_t length, Answer* __restrict__ part) {
+  __shared__ double red[kBlock / kWave];
+  const bool has_ref = a.ref && !a.ref_sums;
+  const int64_t unit = blockIdx.x, row = unit >> shift, from = (unit & (((int64_t)1 << shift) - 1)) * length, to = min(from + length, a.tokens);   // a workgroup for every piece
+  Answer own{};
+  for (int64_t t = from + threadIdx.x * kQuad; t < to; t += kBlock * kQuad) {
+    const int64_t at = min(t, a.tokens - kQuad);
+    add_tokens<kQuad>(a, row, at, load_mask<kQuad>(a.mask, row * a.ld_mask + at) & ~0u << (t - at), has_ref, own);
+  }
+  own.sum = group_total<kBlock>(own.sum, red);
+  own.count = group_total<kBlock>(own.count, red);
+  if (threadIdx.x == 0) part[unit] = own;
+}
+__global__ __launch_bounds__(kJoin) void k_preference_join(lopt_preference a, int64_t pieces, const Answer* __restrict__ part, PairOutputs o) {
+  __shared__ double red[kJoin / kWave * kPairSums];
   double sum[kPairSums] = {};
   const int lanes = (int)min(pieces, (int64_t)kWave), lane = threadIdx.x % lanes;
   for (int64_t base = 0; base < a.pairs; base += kJoin / lanes) {
@@ -538,50 +624,7 @@ __device__ __forceinline__ void join_pairs(const lopt_preference& a, int64_t pie
     }
     if (lane == 0 && pair < a.pairs) write_pair(a, pair, own[0], own[1], o, sum);
   }
-  block_totals(sum, red);
-  if (threadIdx.x == 0) {
-    const double w = a.pairs > 0 ? 1.0 / (double)a.pairs : 0.0;
-    *o.loss = (float)(sum[0] * w);
-#pragma unroll
-    for (int i = 1; i < 5; ++i) o.stats[i - 1] = (float)(sum[i] * w);
-  }
-}
-
-template <int G, int kThreads, int Q>
-__global__ __launch_bounds__(kThreads) void k_preference(lopt_preference a, int shift, int64_t length, int64_t units, Answer* part, bool alone, PairOutputs o) {
-  __shared__ double red[kThreads / kWave * kPairSums];
-  const int lane = threadIdx.x % G;
-  constexpr int kGroups = kThreads / G;
-  const bool has_ref = a.ref && !a.ref_sums;
-  for (int64_t base = (int64_t)blockIdx.x * kGroups; base < units; base += (int64_t)gridDim.x * kGroups) {
-    const int64_t unit = base + threadIdx.x / G;
-    const bool have = unit < units;
-    const int64_t seq = have ? unit >> shift : 0, from = have ? (unit & (((int64_t)1 << shift) - 1)) * length : 0, to = have ? min(from + length, a.tokens) : 0;
-    double sum = 0.0, n = 0.0;
-    for (int64_t t = from + lane * Q; t < to; t += G * Q) {
-      const int64_t at = min(t, a.tokens - Q);
-      const uint32_t bits = load_mask<Q>(a.mask, seq * a.ld_mask + at) & ~0u << (t - at);
-      if (bits) {   // padding is not read
-        float logp[Q], ref[Q] = {};
-        load_as<Q>(a.logp + seq * a.ld_logp + at, logp);
-        if (has_ref) load_of<Q>(a.ref, a.ref_type, seq * a.ld_ref + at, ref);
-#pragma unroll
-        for (int e = 0; e < Q; ++e) sum += bits >> e & 1 ? (double)logp[e] - (double)ref[e] : 0.0;
-        n += (double)__popc(bits);
-      }
-    }
-    sum = group_total<G>(sum, red);
-    n = group_total<G>(n, red);
-    if (lane == 0 && have) part[unit] = Answer{sum, n};
-  }
-  if (alone) {
-    __syncthreads();   // the workgroup's own partial sums
-    join_pairs(a, (int64_t)1 << shift, part, o, red);
-  }
-}
-__global__ __launch_bounds__(kJoin) void k_preference_join(lopt_preference a, int64_t pieces, const Answer* __restrict__ part, PairOutputs o) {
-  __shared__ double red[kJoin / kWave * kPairSums];
-  join_pairs(a, pieces, part, o, red);
+  write_preference(a, sum, o, red);
 }
 
 template <int Q>
@@ -651,9 +694,18 @@ lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float
   return launch_status("lopt_policy_loss_backward");
 }
 
+static Plan preference_plan(int64_t pairs, int64_t tokens) {
+  Plan p = plan_of(2 * pairs, tokens);
+  if (p.pieces == 1 && !p.alone) {   // units are pairs
+    const int64_t groups = p.threads / p.lanes;
+    p.blocks = std::clamp<int64_t>((pairs + groups - 1) / groups, 1, 2048);
+  }
+  return p;
+}
 size_t lopt_preference_loss_workspace(int64_t pairs, int64_t tokens) {
   if (pairs <= 0 || tokens <= 0 || pairs > 0x3fffffffLL || tokens > 0x7fffffffLL) return 0;
-  return (size_t)plan_of(2 * pairs, tokens).units * sizeof(Answer);
+  const Plan p = preference_plan(pairs, tokens);
+  return p.alone ? 0 : p.pieces > 1 ? (size_t)p.units * sizeof(Answer) : (size_t)p.blocks * kPairSums * sizeof(double);
 }
 
 lopt_status lopt_preference_loss(const lopt_preference* terms_host, float* loss, float* stats, float* rewards, float* coef, void* workspace, size_t workspace_bytes,
@@ -680,15 +732,20 @@ lopt_status lopt_preference_loss(const lopt_preference* terms_host, float* loss,
   LOPT_CHECK(check_array("rewards", rewards, 4, any));
   LOPT_CHECK(check_array("coef", coef, 4, any));
   LOPT_CHECK(check_workspace(workspace, workspace_bytes, lopt_preference_loss_workspace(a.pairs, a.tokens)));
-  const Plan p = plan_of(2 * a.pairs, a.tokens);
+  const Plan p = preference_plan(a.pairs, a.tokens);
   hipStream_t stream = (hipStream_t)hip_stream;
-  Answer* part = (Answer*)workspace;
   const PairOutputs o{loss, stats, rewards, coef};
+  if (p.pieces > 1) {
+    Answer* part = (Answer*)workspace;
+    hipLaunchKernelGGL(k_preference_pieces, dim3((unsigned)p.units), dim3(kBlock), 0, stream, a, p.shift, p.length, part);
+    hipLaunchKernelGGL(k_preference_join, dim3(1), dim3(kJoin), 0, stream, a, p.pieces, (const Answer*)part, o);
+    return launch_status("lopt_preference_loss");
+  }
+  double* part = (double*)workspace;
   with_plan(p, [&](auto g, auto threads, auto q) {
-    hipLaunchKernelGGL((k_preference<decltype(g)::value, decltype(threads)::value, decltype(q)::value>), dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, p.shift, p.length,
-                       p.units, part, p.alone, o);
+    hipLaunchKernelGGL((k_preference<decltype(g)::value, decltype(threads)::value, decltype(q)::value>), dim3((unsigned)p.blocks), dim3(p.threads), 0, stream, a, part, p.alone, o);
   });
-  if (!p.alone) hipLaunchKernelGGL(k_preference_join, dim3(1), dim3(kJoin), 0, stream, a, p.pieces, (const Answer*)part, o);
+  if (!p.alone) hipLaunchKernelGGL(k_preference_sums, dim3(1), dim3(kJoin), 0, stream, a, p.blocks, (const double*)part, o);
   return launch_status("lopt_preference_loss");
 }
 

@@ -725,7 +725,7 @@ def check_policy(t, v, clip=(0.2, 0.28), kl_coef=0.05, entropy_coef=0.01, reduct
     return r, got
 
 
-POLICY_SHAPES = [(1, 1), (5, 1), (1, 3), (7, 5), (3, 64), (9, 65), (16, 257), (8, 128), (1, 16384), (1, 16385), (3, 5000), (4, 4097), (700, 3), (70000, 7), (300, 300), (1000, 60), (5, 20000), (1, 300001),
+POLICY_SHAPES = [(1, 1), (5, 1), (1, 3), (7, 5), (3, 64), (9, 65), (16, 257), (8, 128), (1, 16384), (1, 16385), (3, 5000), (4, 4097), (700, 3), (70000, 7), (20000, 10), (9000, 16), (40000, 3), (2048, 33), (2200, 130), (2100, 1001), (300, 300), (1000, 60), (5, 20000), (1, 300001),
                  (1023, 1100), (600, 2048), (2, 100003)]
 
 
@@ -907,7 +907,7 @@ def preference_inputs(pairs, tokens, seed, ref="tokens", rkind="fp32", spread=0.
     return logp, other, torch.from_numpy(keep).cuda()
 
 
-PREFERENCE_SHAPES = [(1, 1), (2, 3), (5, 64), (3, 65), (8, 512), (2, 257), (1, 4097), (1, 8193), (2, 16385), (3000, 5), (700, 130), (511, 1100), (512, 1025), (9, 33333), (1, 500001)]
+PREFERENCE_SHAPES = [(1, 1), (2, 3), (40000, 3), (9000, 20), (1100, 127), (1024, 1023), (5, 64), (3, 65), (8, 512), (2, 257), (1, 4097), (1, 8193), (2, 16385), (3000, 5), (700, 130), (511, 1100), (512, 1025), (9, 33333), (1, 500001)]
 
 
 @pytest.mark.parametrize("pairs,tokens", PREFERENCE_SHAPES)

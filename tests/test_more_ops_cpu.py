@@ -281,10 +281,11 @@ def test_preference_loss_refusals(L):
     for name in ("loss", "stats", "rewards", "coef"):
         _refused(L, _preference(L, **{name: None}), EINVAL, name)
         _refused(L, _preference(L, **{name: P + 2}), EINVAL, name)
-    need = L.lopt_preference_loss_workspace(4, 8)
-    assert need > 0 and L.lopt_preference_loss_workspace(0, 8) == 0
-    _refused(L, _preference(L, ws=None), EINVAL, "workspace")
-    _refused(L, _preference(L, ws_bytes=need - 1), EINVAL, "workspace")
+    need = L.lopt_preference_loss_workspace(64, 4096)
+    assert need > 0 and L.lopt_preference_loss_workspace(0, 8) == 0 and L.lopt_preference_loss_workspace(4, 8) == 0
+    large = dict(pairs=64, tokens=4096, ld_logp=4096, ld_ref=4096)
+    _refused(L, _preference(L, ws=None, **large), EINVAL, "workspace")
+    _refused(L, _preference(L, ws_bytes=need - 1, **large), EINVAL, "workspace")
 
 
 def test_preference_loss_backward_refusals(L):
