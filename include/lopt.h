@@ -385,7 +385,7 @@ lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* r
 /* Clipped policy loss over `seqs` sequences of up to `tokens` >= 1 tokens. Of each token, with ratio = e^(logp - old_logp), A its advantage:
  *   surrogate = -min(ratio A, max(1 - clip_low, min(ratio, 1 + clip_high)) A)   (0 where A is 0),   clipped = whether the bound is what the min takes
  *   kl = e^u - 1 - u with u = ref_logp - logp, or what `kl` holds, or 0;   drift = ratio - 1 - ln ratio
- *   loss = mean(surrogate) + kl_coef mean(kl) - entropy_coef mean(entropy)
+ *   loss = mean(surrogate) + kl_coef mean(kl) - entropy_coef mean(entropy)   (a term whose coefficient is 0 is only reported)
  *   stats[8] = means of surrogate, kl, entropy, clipped, ratio, drift; tokens that count; sequences that have one
  * Tokens whose mask byte is 0 do not count, whatever is in their places. per_sequence 0: the means are over all tokens that count; else over the
  * sequences that have one, of the mean over each. Where nothing counts all of these are 0.
@@ -420,8 +420,8 @@ lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float
 
 /* Loss of pairs of answers, of which the first is preferred: logp has 2 x pairs rows of up to `tokens` >= 1 tokens, the chosen answers in the first
  * `pairs` rows, the rejected ones in the same order behind them. With s_j = sum of logp - ref over the tokens of row j that count (per token with `average`;
- * 0 for a row that has none), m = s_chosen - s_rejected and z = beta m - margin:
- *   LOPT_PREFERENCE_SIGMOID  -(1 - label_smoothing) ln sigma(z) - label_smoothing ln sigma(-z)
+ * 0 for a row that has none, whatever its ref), m = s_chosen - s_rejected and z = beta m - margin:
+ *   LOPT_PREFERENCE_SIGMOID  -(1 - label_smoothing) ln sigma(z) - label_smoothing ln sigma(-z)   (a term whose weight is 0 is left out)
  *   LOPT_PREFERENCE_HINGE    max(0, 1 - z)
  *   LOPT_PREFERENCE_SQUARED  (m - 1 / (2 beta))^2     (margin and label_smoothing 0)
  *   loss = mean over the pairs,   rewards[2 x pairs] = beta s,   stats[4] = means of m > 0, beta m, the chosen answers' rewards, the rejected ones'

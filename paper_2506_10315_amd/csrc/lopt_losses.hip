@@ -269,8 +269,8 @@ __device__ __forceinline__ void write_policy(const double (&sum)[kSums], const l
   for (int i = 0; i < 6; ++i) mean[i] = n > 0.0 ? sum[i] * w : 0.0;
   if (n > 0.0) mean[4] += 1.0;   // its terms are the ratios less 1
   double v = mean[0];
-  if (a.ref_logp || a.kl) v += a.kl_coef * mean[1];
-  if (a.entropy) v -= a.entropy_coef * mean[2];
+  if ((a.ref_logp || a.kl) && a.kl_coef != 0.0) v += a.kl_coef * mean[1];   // infinite or NaN, it is only reported where its coefficient is 0
+  if (a.entropy && a.entropy_coef != 0.0) v -= a.entropy_coef * mean[2];
   *loss = (float)v;
 #pragma unroll
   for (int i = 0; i < 6; ++i) stats[i] = (float)mean[i];
@@ -482,8 +482,8 @@ constexpr int kPairSums = 8;   // loss, right ones, margins, rewards of the chos
 
 __device__ __forceinline__ void write_pair(const lopt_preference& a, int64_t pair, Answer chosen, Answer rejected, const PairOutputs& o, double (&sum)[kPairSums]) {
   if (a.ref && a.ref_sums) {
-    chosen.sum -= load_one_of(a.ref, a.ref_type, pair * a.ld_ref);
-    rejected.sum -= load_one_of(a.ref, a.ref_type, (a.pairs + pair) * a.ld_ref);
+    if (chosen.count > 0.0) chosen.sum -= load_one_of(a.ref, a.ref_type, pair * a.ld_ref);
+    if (rejected.count > 0.0) rejected.sum -= load_one_of(a.ref, a.ref_type, (a.pairs + pair) * a.ld_ref);
   }
   double per[2] = {1.0, 1.0};
   if (a.average) {
@@ -496,7 +496,9 @@ __device__ __forceinline__ void write_pair(const lopt_preference& a, int64_t pai
   double loss, slope;   // slope: d loss / d m
   if (a.kind == LOPT_PREFERENCE_SIGMOID) {
     const double soft = log1p(exp(-fabs(z))), s = a.label_smoothing;
-    loss = (1.0 - s) * (fmax(-z, 0.0) + soft) + s * (fmax(z, 0.0) + soft);
+    loss = 0.0;   // an infinite z adds nothing where its weight is 0
+    if (s != 1.0) loss += (1.0 - s) * (fmax(-z, 0.0) + soft);
+    if (s != 0.0) loss += s * (fmax(z, 0.0) + soft);
     slope = a.beta * (1.0 / (1.0 + exp(-z)) - (1.0 - s));
   } else if (a.kind == LOPT_PREFERENCE_HINGE) {
     loss = fmax(1.0 - z, 0.0);
@@ -677,7 +679,7 @@ lopt_status lopt_policy_loss(const lopt_policy* terms_host, float* loss, float* 
 lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float* stats, const float* counts, const float* dloss, float* dlogp, float* dkl,
                                       float* dentropy, void* hip_stream) {
   LOPT_CHECK(check_policy(terms_host));
-  const lopt_policy a = *terms_host;
+  lopt_policy a = *terms_host;
   LOPT_CHECK(check_array("stats", stats, 4, true));
   LOPT_CHECK(check_array("counts", counts, 4, a.per_sequence && a.seqs > 0));
   LOPT_CHECK(check_array("dloss", dloss, 4, true));
@@ -687,6 +689,7 @@ lopt_status lopt_policy_loss_backward(const lopt_policy* terms_host, const float
   if (dkl && !a.kl) return fail_call(LOPT_EINVAL, "dkl without kl");
   if (dentropy && !a.entropy) return fail_call(LOPT_EINVAL, "dentropy without entropy");
   if (a.seqs == 0 || !(dlogp || dkl || dentropy)) return LOPT_OK;
+  if (a.kl_coef == 0.0) a.ref_logp = nullptr;   // not in the loss
   const int quad = a.tokens < kQuad ? 1 : kQuad;
   const Flat f = flat_of(a.seqs, a.tokens, quad);
   auto kernel = quad == 1 ? k_policy_back<1> : k_policy_back<kQuad>;

@@ -826,6 +826,26 @@ def test_policy_loss_far_ratios():
         assert float(r.stats[6]) == 8
 
 
+def test_policy_terms_without_a_coefficient_are_only_reported():
+    import torch
+    for tokens in (5, 3000):
+        v = {k: torch.rand(40, tokens, device="cuda:0") for k in ("logp", "old", "adv", "ent")}
+        ref = torch.zeros_like(v["logp"])
+        logp = -v["logp"]
+        logp[3, 1] = -2000.0
+        old = logp - 0.1 * v["old"]
+        v["ent"][7, 2] = math.inf
+        dl = torch.ones((), device="cuda:0")
+        want = ops().policy_loss_forward(logp, old, v["adv"])
+        gw = ops().policy_loss_backward(dl, want, logp, old, v["adv"])[0]
+        for more in ({"ref_logp": ref}, {"kl": v["ent"]}):
+            r = ops().policy_loss_forward(logp, old, v["adv"], entropy=v["ent"], **more)
+            g = ops().policy_loss_backward(dl, r, logp, old, v["adv"], entropy=v["ent"], **more)
+            assert torch.equal(r.loss, want.loss) and torch.equal(g[0], gw) and bool(torch.isfinite(gw).all())
+            assert bool((g[2] == 0).all()) and (g[1] is None or bool((g[1] == 0).all()))
+            assert float(r.stats[1]) == math.inf and float(r.stats[2]) == math.inf
+
+
 def test_policy_loss_autograd_against_differences():
     import torch
     r = np.random.default_rng(12)
@@ -950,6 +970,24 @@ def test_preference_loss_special_values():
     for kind in ("sigmoid", "hinge", "squared"):
         r, g = check_preference(far, ref, mask, kind=kind)
         assert bool(torch.isfinite(r.loss)) and bool(torch.isfinite(g).all())
+    # a token of a rejected answer that cannot be: the pair is as far apart as can be
+    x = logp.clone()
+    was = bool(mask[9, 0])
+    x[9, 0], mask[9, 0] = -math.inf, True
+    for kind, smooth, want in (("sigmoid", 0.0, False), ("sigmoid", 0.1, True), ("hinge", 0.0, False), ("squared", 0.0, True)):
+        r = ops().preference_loss_forward(x, ref, mask, kind=kind, label_smoothing=smooth)
+        g = ops().preference_loss_backward(torch.ones((), device="cuda:0"), r, x, mask)
+        assert math.isinf(float(r.loss)) is want and not math.isnan(float(r.loss)), (kind, smooth)
+        assert float(r.rewards[9]) == -math.inf and bool(torch.isfinite(g[[0, 1, 4, 5]]).all())
+        if not want:
+            assert bool((g[[3, 9]] == 0).all())
+    mask[9, 0] = was
+    # sums of the reference where an answer has no tokens
+    sums = torch.where(mask, ref, 0.0).sum(1)
+    a = ops().preference_loss_forward(logp, sums, mask)
+    sums[~mask.any(1)] = math.nan
+    b = ops().preference_loss_forward(logp, sums, mask)
+    assert all(torch.equal(p, q) for p, q in zip(a, b)) and bool((b.rewards[~mask.any(1)] == 0).all())
     for kind in ("sigmoid", "hinge", "squared"):      # a NaN that counts
         x = logp.clone()
         x[5, 0] = math.nan
