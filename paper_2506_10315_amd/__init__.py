@@ -1,5 +1,5 @@
 """MI355X-native learned-optimizer step (small_fc_lopt, VeLO) and the operators of the training loop around it (`ops`:
-token log probabilities, layer norm, gradient clipping): thin binding over liblopt.so.
+token log probabilities, layer norm, dropout, KL divergence, policy and preference losses, gradient clipping): thin binding over liblopt.so.
 
 Every step of the optimizer and every operator runs in the HIP kernels behind the C boundary of include/lopt.h;
 this package only marshals arguments. There is no CPU fallback: if the library is not built,

@@ -1,10 +1,11 @@
 """The operators of a training loop around the optimizer step, on torch tensors: layer norm, token log probabilities with
-entropy and top alternatives, their gradients, and clipping by the global gradient norm.
+entropy and top alternatives, dropout (alone, and with residual and layer norm), the KL divergence to a reference's logits, the clipped policy loss and the
+preference loss, their gradients, and clipping by the global gradient norm.
 
 Nothing numerical happens here: every function checks its tensors, allocates outputs and workspace, and hands pointers to the
 call of the same name in include/lopt.h (formulas, masks and special values are described there) on the current stream.
-Tensors are CUDA tensors of float32, bfloat16 or float16; `layer_norm` and `token_logprobs` take part in autograd, the
-`*_forward` and `*_backward` functions are the passes by themselves."""
+Tensors are CUDA tensors of float32, bfloat16 or float16; `layer_norm`, `dropout`, `dropout_add_layer_norm`,
+`token_logprobs`, `token_kl`, `policy_loss` and `preference_loss` take part in autograd, the `*_forward` and `*_backward` functions are the passes by themselves."""
 from __future__ import annotations
 
 import operator

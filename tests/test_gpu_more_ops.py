@@ -73,6 +73,15 @@ def test_dropout(rows, cols, kind):
         assert not torch.equal(ops().dropout_forward(x, 0.5, 7, 0), ops().dropout_forward(x, 0.5, 7, 1))
 
 
+def test_dropout_beyond_32_bits_of_packs():
+    import torch
+    rows = (1 << 32) // 7 + 1000
+    x, xv = dev(np.array([1.0, 2.0, 3.0, 4.0, 5.0, 6.0, 7.0]), "fp16")
+    y = ops().dropout_forward(x[None].expand(rows, 7), 0.5, 11, 5)
+    for first in (0, (1 << 31) // 7 - 50, (1 << 32) // 7 - 50, rows - 100):
+        assert np.array_equal(host(y[first:first + 100]), dropped(np.broadcast_to(xv, (100, 7)), keep_of(100, 7, 0.5, 11, 5, first), 0.5))
+
+
 def test_dropout_rate_and_independence():
     """Shares of kept elements, of neighbours, of rows and of calls kept together: within five standard deviations of a binomial."""
     import torch
@@ -927,7 +936,7 @@ def preference_inputs(pairs, tokens, seed, ref="tokens", rkind="fp32", spread=0.
     return logp, other, torch.from_numpy(keep).cuda()
 
 
-PREFERENCE_SHAPES = [(1, 1), (2, 3), (40000, 3), (9000, 20), (1100, 127), (1024, 1023), (5, 64), (3, 65), (8, 512), (2, 257), (1, 4097), (1, 8193), (2, 16385), (3000, 5), (700, 130), (511, 1100), (512, 1025), (9, 33333), (1, 500001)]
+PREFERENCE_SHAPES = [(1, 1), (2, 3), (40000, 3), (9000, 20), (1100, 127), (1024, 1023), (2100, 1500), (1500, 1100), (5, 64), (3, 65), (8, 512), (2, 257), (1, 4097), (1, 8193), (2, 16385), (3000, 5), (700, 130), (511, 1100), (512, 1025), (9, 33333), (1, 500001)]
 
 
 @pytest.mark.parametrize("pairs,tokens", PREFERENCE_SHAPES)
