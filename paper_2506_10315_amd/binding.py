@@ -23,7 +23,10 @@ EXPORTS = ["lopt_default_config", "lopt_weights_count", "lopt_create", "lopt_des
            "lopt_profile_enable", "lopt_profile_read", "lopt_pass_name",
            "lopt_clip_workspace", "lopt_clip_grads", "lopt_layer_norm", "lopt_layer_norm_workspace",
            "lopt_layer_norm_backward", "lopt_token_logprobs_workspace", "lopt_token_logprobs",
-           "lopt_token_logprobs_backward"]
+           "lopt_token_logprobs_backward", "lopt_dropout", "lopt_dropout_add_layer_norm", "lopt_dropout_add_layer_norm_workspace",
+           "lopt_dropout_add_layer_norm_backward", "lopt_token_kl_workspace", "lopt_token_kl", "lopt_token_kl_backward",
+           "lopt_policy_loss_workspace", "lopt_policy_loss", "lopt_policy_loss_backward", "lopt_preference_loss_workspace",
+           "lopt_preference_loss", "lopt_preference_loss_backward"]
 
 
 class LoptError(RuntimeError):
