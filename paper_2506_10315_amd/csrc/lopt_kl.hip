@@ -56,10 +56,33 @@ __device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, float c) {
   const float fs = m.fx * a.sx;
   return Apart{mx, mr, fs, m.fr * a.sr, m.fr * a.w + m.apart * a.sx, m.fx * a.h + (fs == 0.f ? 0.f : fs * m.moved), a.most};
 }
-// Over a wavefront, seen from maxima that none of its lanes exceeds.
-__device__ __forceinline__ Total wave_total(Apart a, float mx, float mr, float c) {
+// Over a wavefront or each 16 of its lanes.
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+  if (G == kWave) return wave_max(v);
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  return fmaxf(v, dpp_f<0x140>(v));
+}
+template <int G>
+__device__ __forceinline__ double group_sum(double v) {
+  if (G == kWave) return wave_sum(v);
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  return v + dpp_d<0x140>(v);
+}
+template <int G>
+__device__ __forceinline__ bool none_of_group(bool v) {
+  const uint64_t bits = __ballot(v);
+  return G == kWave ? bits == 0 : (bits >> (threadIdx.x & 48) & 0xffff) == 0;
+}
+// Seen from maxima that none of the lanes exceeds.
+template <int G>
+__device__ __forceinline__ Total total_of(Apart a, float mx, float mr, float c) {
   a = rebase(a, mx, mr, c);
-  return Total{wave_sum((double)a.sx), wave_sum((double)a.sr), wave_sum((double)a.w), wave_sum((double)a.h), mx, mr, wave_max(a.most)};
+  return Total{group_sum<G>((double)a.sx), group_sum<G>((double)a.sr), group_sum<G>((double)a.w), group_sum<G>((double)a.h), mx, mr, group_max<G>(a.most)};
 }
 
 // The largest, NaN where there is one.
@@ -70,11 +93,11 @@ __device__ __forceinline__ float strict_most_of(const float (&x)[E], float m) {
   return m;
 }
 
-// Where all d of a wavefront's piece are within kNear (or none, both logits being masked), f = e 2^-d, so that what e was rounded by is in f too and cancels in KL: with
+// Where all d of a group's piece are within kNear (or none, both logits being masked), f = e 2^-d, so that what e was rounded by is in f too and cancels in KL: with
 // an f by itself 1501 fp16 logits at a scale of 0.5 are off by 5e-7 of KL, so 2e-7. An e below 2^-126 has an f below 2^-62, which adds nothing.
 // FINE: q - 1 goes by less_one where all d allow it, and not by q, whose rounding next to 1 is what remains of a KL that few unlikely tokens
 // make up: of rows of some ten logits by 5e-6. It takes half as many instructions again as q; in long rows such roundings are many.
-template <int E, bool FINE>
+template <int E, bool FINE, int G = kWave>
 __device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], float c) {
   a = rebase(a, strict_most_of(x, a.mx), strict_most_of(r, a.mr), c);
   const float shift = shift_of(a.mx, a.mr, c);
@@ -84,7 +107,7 @@ __device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const f
     d[i] = __builtin_fmaf(x[i] - r[i], c, -shift);
     far = fmaxf(far, fabsf(d[i]));
   }
-  if (FINE && __ballot(far > 4.f) == 0) {
+  if (FINE && none_of_group<G>(far > 4.f)) {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const float e = exp2_hw((x[i] - a.mx) * c), near = __builtin_amdgcn_fmed3f(d[i], -4.f, 4.f), g = e * less_one(near);
@@ -95,7 +118,7 @@ __device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const f
     }
     return;
   }
-  if (__ballot(far > kNear) == 0) {
+  if (none_of_group<G>(far > kNear)) {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const float e = exp2_hw((x[i] - a.mx) * c), near = __builtin_amdgcn_fmed3f(d[i], -kNear, kNear), q = exp2_hw(-near);
@@ -156,29 +179,36 @@ __device__ __forceinline__ void write_nothing(const Outputs& o, int64_t row) {
   for (int i = 0; i < 5; ++i) o.stats[5 * row + i] = 0.f;
 }
 
-// Rows of one piece: a wavefront each.
-template <typename T, int E>
-__global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, Outputs o) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Rows of one piece: G lanes each, `batch` <= G neighbouring ones in turn. Lane k of the group keeps the sums of the k-th, and all lanes make their rows' outputs at once.
+// Bound by vector issue, some 500 instructions a row of 64 lanes: batches, of which 8192 wavefronts have one each, spare most rows those of the outputs. us with a row a batch | so:
+// 20000x1000 bf16 35 | 32.6, 100000x100 fp32 with 64 lanes a row 111 | 94, with 16 26; with 4096 wavefronts 28.
+template <typename T, int E, int G>
+__global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, int batch, Outputs o) {
+  constexpr int kGroups = kBlock / G;
+  const int lane = threadIdx.x % G;
   const float c = fminf(a.scale * kLog2e, FLT_MAX);
-  for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < a.rows; row += (int64_t)gridDim.x * 4) {
-    if (a.keep && !a.keep[row]) {
-      if (lane == 0) write_nothing(o, row);
-      continue;
-    }
+  const int64_t group = (int64_t)blockIdx.x * kGroups + threadIdx.x / G, first = group * batch;   // a group for every batch
+  const int count = (int)max(min((int64_t)batch, a.rows - first), (int64_t)0);
+  Total own{};
+  for (int k = 0; k < count; ++k) {
+    const int64_t row = first + k;
+    if (a.keep && !a.keep[row]) continue;
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
-    Piece<T, E> p, q;
+    Piece<T, E, G> p, q;
     p.load(x, 0, off, a.n);
     q.load(r, 0, off, a.n);
     float u[E], v[E];
     p.unpack(u);
     q.unpack(v);
     Apart s = nothing();
-    add_piece<E, true>(s, u, v, c);
-    const Total t = wave_total(s, wave_max(s.mx), wave_max(s.mr), c);
-    if (lane == 0) write_row(o, row, t, c);
+    add_piece<E, true, G>(s, u, v, c);
+    const Total t = total_of<G>(s, group_max<G>(s.mx), group_max<G>(s.mr), c);
+    if (lane == k) own = t;
   }
+  if (lane >= count) return;
+  if (a.keep && !a.keep[first + lane]) write_nothing(o, first + lane);
+  else write_row(o, first + lane, own, c);
 }
 
 // A wavefront's sums over every `step`-th element's piece of a row, from `first` to `end`, counted from the pack in which the row of x begins.
@@ -217,7 +247,7 @@ __device__ __forceinline__ Total block_total(const Apart& s, float c, Room& room
   __syncthreads();
   mx = wave_max(lane < waves ? room.mx[lane] : -FLT_MAX);
   mr = wave_max(lane < waves ? room.mr[lane] : -FLT_MAX);
-  Total t = wave_total(s, mx, mr, c);
+  Total t = total_of<kWave>(s, mx, mr, c);
   if (lane == 0) room.total[wave] = t;
   __syncthreads();
   if (threadIdx.x == 0)
@@ -319,21 +349,24 @@ enum RowForm { kRowWave, kRowBlock, kRowSplit };
 struct RowPlan {
   RowForm form;
   int lane, waves;              // logits a lane, wavefronts
+  int lanes;                    // a row, kRowWave
   int64_t pieces, segments;     // kRowSplit
 };
 inline RowPlan plan_rows(int64_t rows, int64_t vocab) {
   const int64_t n = vocab + 7;   // a row counted from its pack
-  if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, 0, 0};
+  // us with 64 lanes a row / 16: 1024x100 fp32 5.5 / 5.2, 16384x100 19.5 / 7.9, 100000x300 bf16 97 / 61, 16384x500 fp16 20.6 / 14.8, 4096x500 bf16 8.7 / 7.2, but 1024x500 5.5 / 7.0
+  if (n <= 128 || (n <= 512 && rows >= 4096)) return RowPlan{kRowWave, n <= 128 ? 8 : n <= 256 ? 16 : 32, 4, 16, 0, 0};
+  if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, kWave, 0, 0};
   const int64_t pieces = (n + 1023) / 1024;
   // Few long rows in segments, which costs a launch and a workspace more on the host, some 5 us. us in a graph, a workgroup a row / segments: 1x50257 fp32 14.2 / 9.1, 1x100000 bf16
   // 21 / 8.8, 12x99760 fp32 23.5 / 10.3, 64x100000 bf16 24 / 16, 128x70000 18.4 / 19.5, 200x100000 25 / 29, 200x131000 fp32 40 / 42.
   if (rows <= 64 ? n > 64 * 1024 : rows < 256 && n > 256 * 1024) {
     const int64_t per = std::clamp<int64_t>(rows * pieces / 2048, 4, 32);
-    return RowPlan{kRowSplit, 16, 4, per, (pieces + per - 1) / per};
+    return RowPlan{kRowSplit, 16, 4, kWave, per, (pieces + per - 1) / per};
   }
   // Wavefronts: one for about five pieces up to four, with fewer than 1024 rows as many as make 4096 in all, up to eight. us with 1 / 2 / 4 / 8: 20000x5000 bf16 83 / 94 / 116,
   // 8192x16000 104 / 110 / 113 / 130, 4096x50257 167 / 169 / 157 / 177, 2048x131000 239 / 217 / 211 / 218, 512x50257 62 / 42 / 27 / 26, 256x32000 38 / 22 / 14 / 12.
-  return RowPlan{kRowBlock, 16, (int)std::max(std::clamp<int64_t>((pieces + 4) / 5, 1, 4), std::min<int64_t>({kMostWaves, pieces, 4096 / rows})), 0, 0};
+  return RowPlan{kRowBlock, 16, (int)std::max(std::clamp<int64_t>((pieces + 4) / 5, 1, 4), std::min<int64_t>({kMostWaves, pieces, 4096 / rows})), kWave, 0, 0};
 }
 
 // The gradients, element by element, with d = scale ((x - r) - (mx - mr)) and g = dkl:
@@ -442,9 +475,10 @@ lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64
     const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, mask};
     const dim3 block(plan.waves * kWave);
     if (plan.form == kRowWave) {
-      const dim3 grid((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 20));
-      auto kernel = plan.lane == 8 ? k_kl_short<T, 8> : plan.lane == 16 ? k_kl_short<T, 16> : k_kl_short<T, 32>;
-      hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, o);
+      const int lanes = plan.lanes, batch = (int)std::clamp<int64_t>(rows * lanes / kWave / 8192, 1, 16), per = kBlock / lanes * batch;
+      auto kernel = lanes == 16 ? plan.lane == 8 ? k_kl_short<T, 8, 16> : plan.lane == 16 ? k_kl_short<T, 16, 16> : k_kl_short<T, 32, 16>
+                                : plan.lane == 8 ? k_kl_short<T, 8, 64> : plan.lane == 16 ? k_kl_short<T, 16, 64> : k_kl_short<T, 32, 64>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + per - 1) / per)), block, 0, stream, a, batch, o);
     } else if (plan.form == kRowBlock) {
       // what the Infinity Cache cannot hold is not left there: 4096x50257 bf16 165 -> 157 us, 20000x5000 93 -> 83, but 1024x50257, which fits, 43 -> 46
       const bool large = 2 * rows * vocab * (int64_t)sizeof(T) > kCacheBytes;

@@ -17,7 +17,7 @@ __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float base_of(float m, float c) { return __builtin_amdgcn_fmed3f(m * c, -kMostBase, kMostBase); }
 __device__ __forceinline__ bool beyond(float m, float c) { return fabsf(m * c) >= kMostBase && m != -INFINITY; }
 
-// A wavefront takes a piece of a row at a time, E = 8 to 64 logits a lane in accesses of 16 bytes. Accesses are aligned: `off` elements ahead of the row
+// A wavefront, or a group of L of its lanes, takes a piece of a row at a time, E = 8 to 64 logits a lane in accesses of 16 bytes. Accesses are aligned: `off` elements ahead of the row
 // begin a pack of 16 bytes, and pieces and packs are counted from there (rows at odd elements of 16 bits: 4096x50257 98 us, 83 at 50258; counted from
 // their own start). The pack that would begin ahead of the row begins with it, the one that would pass the row's end ends
 // with it, and the elements that they share with the pack beside them are masked.
@@ -25,14 +25,14 @@ template <typename T>
 __device__ __forceinline__ int pack_offset(const T* row, uint32_t n) {
   return n >= (uint32_t)Pack<T>::n ? (int)((uintptr_t)row / sizeof(T) % Pack<T>::n) : 0;
 }
-template <typename T, int E>
+template <typename T, int E, int L = kWave>
 struct Piece {
-  static constexpr int V = Pack<T>::n, N = E / V, kSize = E * kWave;
+  static constexpr int V = Pack<T>::n, N = E / V, kSize = E * L;
   typedef typename Pack<T>::type pack;
   pack raw[N];
   int first, off, n;
   // Where the lane's pack j would begin, in elements of the row, and where it does.
-  __device__ __forceinline__ int place(int j) const { return first + (j * kWave + (int)(threadIdx.x & 63)) * V - off; }
+  __device__ __forceinline__ int place(int j) const { return first + (j * L + (int)(threadIdx.x % L)) * V - off; }
   __device__ __forceinline__ int begin(int j) const { return max(min(place(j), n - V), 0); }
   __device__ __forceinline__ int index(int i) const { return begin(i / V) + i % V; }
   // Whether an element is one, and this lane's.
@@ -40,8 +40,8 @@ struct Piece {
     const int p = place(i / V), k = index(i);
     return k >= p && k < min(p + V, n);
   }
-  // Element of lane 0 that the wavefront's j-th packs begin with: below 0, they begin ahead of the row; n or above, they lie behind it.
-  __device__ __forceinline__ int from(int j) const { return first + j * kWave * V - off; }
+  // Element of the first lane that the j-th packs begin with: below 0, they begin ahead of the row; n or above, they lie behind it.
+  __device__ __forceinline__ int from(int j) const { return first + j * L * V - off; }
   template <bool NT = false>
   __device__ __forceinline__ void load(const T* row, int first_, int off_, int n_) {
     first = first_, off = off_, n = n_;
@@ -57,7 +57,7 @@ struct Piece {
   __device__ __forceinline__ void mask() {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      if (from(j) >= 0 && from(j) + kWave * V <= n) continue;
+      if (from(j) >= 0 && from(j) + L * V <= n) continue;
       if (from(j) >= n) {
 #pragma unroll
         for (int e = 0; e < V; ++e) raw[j][e] = (T)-INFINITY;

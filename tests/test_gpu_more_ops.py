@@ -480,7 +480,7 @@ def logits_pair(rows, vocab, seed, masked=0.0, apart=0.3):
 
 
 KL_SHAPES = [(1, 1), (3, 1), (5, 2), (4, 7), (9, 8), (3, 9), (33, 63), (6, 64), (5, 65), (13, 505), (4, 513), (11, 1017), (3, 1025), (5, 2041), (7, 2048), (3, 2500), (2, 8191), (260, 3001),
-             (3, 50257), (2, 131065), (3, 131080), (1, 300007), (2100, 33000)]
+             (3, 50257), (2, 131065), (3, 131080), (1, 300007), (2100, 33000), (17, 121), (17, 122), (4100, 10), (4100, 130), (4099, 249), (4097, 505), (8193, 1)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -546,6 +546,35 @@ def test_token_kl_special_rows(vocab, kind):
     kl = host(check_kl(x, y, kind, what="special"))
     assert kl[0] == kl[1] == kl[10] == kl[11] == 0 and kl[2] == kl[3] == kl[19] == inf and np.isnan(kl[[5, 6, 7, 8, 20, 21]]).all() and np.isfinite(kl[[4, 9, 12, 13, 17]]).all()
     check_kl(x[:12], y[:12], kind, scale=2.0, what="special, scale 2")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", [9, 100, 200, 500])
+def test_token_kl_special_rows_among_many_short_ones(vocab, kind):
+    """Rows that share a wavefront, special ones beside ordinary ones, against the definition; none of them changes another."""
+    import torch
+    x, y = logits_pair(70, vocab, 40 + vocab)
+    a, b = (dev(v, kind)[0] for v in (x, y))
+    a[3], a[5, 1], a[6, 2], a[9, :4], b[9, :3] = -math.inf, math.nan, math.inf, -math.inf, -math.inf
+    b[11, 4], a[15], b[15], b[18] = -math.inf, a[15] + 512, b[15] - 512, -math.inf
+    a[21, 1:], b[22, 2], a[30, 3] = -math.inf, torch.finfo(tt(kind)).min, torch.finfo(tt(kind)).min
+    av, bv = host(a), host(b)
+    want = kl_exact(av, bv, 1.0)
+    tol, _ = kl_tolerance(av, bv, 1.0, want)
+    kl, stats = ops().token_kl_forward(a.repeat(60, 1), b.repeat(60, 1))
+    g = torch.ones_like(kl)
+    grads = ops().token_kl_backward(a.repeat(60, 1), b.repeat(60, 1), stats, g, need=(True, True))
+    for part in (kl[:70], kl[2100:2170], kl[-70:]):
+        close(part, want[0], tol, "kl")
+    few = ops().token_kl_forward(a, b)
+    for got, w in zip(grads, ops().token_kl_backward(a, b, few[1], g[:70], need=(True, True))):
+        assert torch.equal(got.reshape(60, 70, vocab)[-1].isnan(), w.isnan())
+    special = [3, 5, 6, 9, 11, 15, 18, 21, 22, 30]
+    plain = [i for i in range(70) if i not in special]
+    c, e = a.clone(), b.clone()
+    c[special], e[special] = a[0], b[0]
+    other = ops().token_kl_forward(c.repeat(60, 1), e.repeat(60, 1))[0]
+    assert torch.equal(kl.reshape(60, 70)[:, plain], other.reshape(60, 70)[:, plain])
 
 
 @pytest.mark.parametrize("vocab", [300, 5000, 140000])
