@@ -475,7 +475,8 @@ lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64
     const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, mask};
     const dim3 block(plan.waves * kWave);
     if (plan.form == kRowWave) {
-      const int lanes = plan.lanes, batch = (int)std::clamp<int64_t>(rows * lanes / kWave / 8192, 1, 16), per = kBlock / lanes * batch;
+      // so many rows that there would be 2^32 threads: as large batches as there can be
+      const int lanes = plan.lanes, batch = rows >> 26 ? lanes : (int)std::clamp<int64_t>(rows * lanes / kWave / 8192, 1, 16), per = kBlock / lanes * batch;
       auto kernel = lanes == 16 ? plan.lane == 8 ? k_kl_short<T, 8, 16> : plan.lane == 16 ? k_kl_short<T, 16, 16> : k_kl_short<T, 32, 16>
                                 : plan.lane == 8 ? k_kl_short<T, 8, 64> : plan.lane == 16 ? k_kl_short<T, 16, 64> : k_kl_short<T, 32, 64>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + per - 1) / per)), block, 0, stream, a, batch, o);

@@ -672,6 +672,15 @@ def test_token_kl_far_rows():
         assert torch.equal(p, q)
 
 
+def test_token_kl_of_very_many_rows():
+    import torch
+    x, y = (dev(v, "bf16")[0] for v in logits_pair(1, 520, 9))
+    rows = (1 << 26) + 77
+    kl, stats = ops().token_kl_forward(x.expand(rows, 520), y.expand(rows, 520))
+    one, its = ops().token_kl_forward(x, y)
+    assert bool((kl == one).all()) and bool((stats[-100:] == its).all()) and bool((stats[:100] == its).all())
+
+
 # ---------------------------------------------------------------------------------------------- policy loss
 
 def exp_rest(v):
