@@ -34,19 +34,19 @@ __device__ __forceinline__ bool none_of_group(bool v) {
 }
 // Seen from maxima that none of the lanes exceeds.
 template <int G>
-__device__ __forceinline__ Total total_of(Apart a, float mx, float mr, float c) {
-  a = rebase(a, mx, mr, c);
+__device__ __forceinline__ Total total_of(Apart a, float mx, float mr, Scale sc) {
+  a = rebase(a, mx, mr, sc);
   return Total{group_sum<G>((double)a.sx), group_sum<G>((double)a.sr), group_sum<G>((double)a.w), group_sum<G>((double)a.h), mx, mr, group_max<G>(a.most)};
 }
 
 // Adds a piece, by the way that all lanes of the group can take. FINE: rows of one piece.
 template <int E, bool FINE, int G = kWave>
-__device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], float c) {
+__device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], Scale sc) {
   float d[E];
-  const float far = differences_of(a, x, r, c, d);
-  if (FINE && none_of_group<G>(far > 4.f)) return add_fine(a, x, d, c);
-  if (none_of_group<G>(far > kNear)) return add_near(a, x, d, c);
-  add_far(a, x, r, c);
+  const float far = differences_of(a, x, r, sc, d);
+  if (FINE && none_of_group<G>(far > 4.f)) return add_fine(a, x, d, sc);
+  if (none_of_group<G>(far > kNear)) return add_near(a, x, d, sc);
+  add_far(a, x, r, sc);
 }
 
 template <typename T>
@@ -56,6 +56,7 @@ struct Rows {
   int64_t ld_x, ld_r, rows;
   uint32_t n;
   float scale;
+  Scale sc;
   const uint8_t* keep;   // null: every row counts
 };
 struct Outputs {
@@ -64,8 +65,8 @@ struct Outputs {
 };
 
 // A row's outputs, by one lane.
-__device__ __forceinline__ void write_row(const Outputs& o, int64_t row, const Total& a, float c) {
-  const RowResult r = result_of(a, c);
+__device__ __forceinline__ void write_row(const Outputs& o, int64_t row, const Total& a, Scale sc) {
+  const RowResult r = result_of(a, sc);
   o.kl[row] = r.kl;
 #pragma unroll
   for (int i = 0; i < 5; ++i) o.stats[5 * row + i] = r.stats[i];
@@ -83,7 +84,6 @@ template <typename T, int E, int G>
 __global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, int batch, Outputs o) {
   constexpr int kGroups = kBlock / G;
   const int lane = threadIdx.x % G;
-  const float c = fminf(a.scale * kLog2e, FLT_MAX);
   const int64_t group = (int64_t)blockIdx.x * kGroups + threadIdx.x / G, first = group * batch;   // a group for every batch
   const int count = (int)max(min((int64_t)batch, a.rows - first), (int64_t)0);
   Total own{};
@@ -99,18 +99,18 @@ __global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, int batch, Outpu
     p.unpack(u);
     q.unpack(v);
     Apart s = nothing();
-    add_piece<E, true, G>(s, u, v, c);
-    const Total t = total_of<G>(s, group_max<G>(s.mx), group_max<G>(s.mr), c);
+    add_piece<E, true, G>(s, u, v, a.sc);
+    const Total t = total_of<G>(s, group_max<G>(s.mx), group_max<G>(s.mr), a.sc);
     if (lane == k) own = t;
   }
   if (lane >= count) return;
   if (a.keep && !a.keep[first + lane]) write_nothing(o, first + lane);
-  else write_row(o, first + lane, own, c);
+  else write_row(o, first + lane, own, a.sc);
 }
 
 // A wavefront's sums over every `step`-th element's piece of a row, from `first` to `end`, counted from the pack in which the row of x begins.
 template <typename T, int E, bool NT>
-__device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* r, int off, int64_t first, int64_t end, int64_t step, float c) {
+__device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* r, int off, int64_t first, int64_t end, int64_t step) {
   typedef Piece<T, E> P;
   Apart s = nothing();
   P p, q;
@@ -127,7 +127,7 @@ __device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* 
     }
     p.unpack(u);
     q.unpack(v);
-    add_piece<E, false>(s, u, v, c);
+    add_piece<E, false>(s, u, v, a.sc);
     p = next_p;
     q = next_q;
   }
@@ -137,14 +137,14 @@ __device__ __forceinline__ Apart sums_of(const Rows<T>& a, const T* x, const T* 
 // Joins what the wavefronts of a workgroup have, from common maxima; thread 0 gets it. `room`: free before, and after another barrier.
 constexpr int kMostWaves = 8;
 struct Room { float mx[16], mr[16]; Total total[16]; };   // 16 for the join of segments
-__device__ __forceinline__ Total block_total(const Apart& s, float c, Room& room) {
+__device__ __forceinline__ Total block_total(const Apart& s, Scale sc, Room& room) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   float mx = wave_max(s.mx), mr = wave_max(s.mr);
   if (lane == 0) room.mx[wave] = mx, room.mr[wave] = mr;
   __syncthreads();
   mx = wave_max(lane < waves ? room.mx[lane] : -FLT_MAX);
   mr = wave_max(lane < waves ? room.mr[lane] : -FLT_MAX);
-  Total t = total_of<kWave>(s, mx, mr, c);
+  Total t = total_of<kWave>(s, mx, mr, sc);
   if (lane == 0) room.total[wave] = t;
   __syncthreads();
   if (threadIdx.x == 0)
@@ -163,7 +163,6 @@ __global__ __launch_bounds__(kMostWaves * kWave, sizeof(T) == 4 ? 3 : 4) void k_
   typedef Piece<T, E> P;
   __shared__ Room room;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const float c = fminf(a.scale * kLog2e, FLT_MAX);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     if (a.keep && !a.keep[row]) {
       if (threadIdx.x == 0) write_nothing(o, row);
@@ -171,9 +170,9 @@ __global__ __launch_bounds__(kMostWaves * kWave, sizeof(T) == 4 ? 3 : 4) void k_
     }
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
-    const Apart s = sums_of<T, E, NT>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize, c);
-    const Total t = block_total(s, c, room);
-    if (threadIdx.x == 0) write_row(o, row, t, c);
+    const Apart s = sums_of<T, E, NT>(a, x, r, off, wave * P::kSize, (int64_t)a.n + off, (int64_t)waves * P::kSize);
+    const Total t = block_total(s, a.sc, room);
+    if (threadIdx.x == 0) write_row(o, row, t, a.sc);
     if (row + gridDim.x < a.rows) __syncthreads();
   }
 }
@@ -184,15 +183,14 @@ __global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments
   typedef Piece<T, 16> P;
   __shared__ Room room;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const float c = fminf(a.scale * kLog2e, FLT_MAX);
   for (int64_t unit = blockIdx.x; unit < a.rows * segments; unit += gridDim.x) {
     const int64_t row = unit / segments, from = (unit - row * segments) * pieces * P::kSize;
     if (a.keep && !a.keep[row]) continue;
     const T *x = a.x + row * a.ld_x, *r = a.r + row * a.ld_r;
     const int off = pack_offset(x, a.n);
     const int64_t end = min(from + (int64_t)pieces * P::kSize, (int64_t)a.n + off);
-    const Apart s = sums_of<T, 16, false>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize, c);
-    const Total t = block_total(s, c, room);
+    const Apart s = sums_of<T, 16, false>(a, x, r, off, from + wave * P::kSize, end, 4 * P::kSize);
+    const Total t = block_total(s, a.sc, room);
     if (threadIdx.x == 0) part[unit] = t;
     __syncthreads();
   }
@@ -200,7 +198,6 @@ __global__ __launch_bounds__(kBlock) void k_kl_split(Rows<T> a, int64_t segments
 template <typename T>
 __global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t segments, const Total* __restrict__ part) {
   __shared__ Room room;
-  const float c = fminf(a.scale * kLog2e, FLT_MAX);
   const int64_t row = blockIdx.x;   // a workgroup for every row
   if (a.keep && !a.keep[row]) {
     if (threadIdx.x == 0) write_nothing(o, row);
@@ -219,7 +216,7 @@ __global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t 
   mx = wave_max(room.mx[lane & 15]);
   mr = wave_max(room.mr[lane & 15]);
   Total t{0.0, 0.0, 0.0, 0.0, mx, mr, -INFINITY};
-  for (int64_t i = threadIdx.x; i < segments; i += 1024) add_segment(t, part[row * segments + i], c);
+  for (int64_t i = threadIdx.x; i < segments; i += 1024) add_segment(t, part[row * segments + i], a.sc);
   t = Total{wave_sum(t.sx), wave_sum(t.sr), wave_sum(t.w), wave_sum(t.h), mx, mr, wave_max(t.most)};
   if (lane == 0) room.total[wave] = t;
   __syncthreads();
@@ -228,7 +225,7 @@ __global__ __launch_bounds__(1024) void k_kl_join(Rows<T> a, Outputs o, int64_t 
     const Total& b = room.total[i];
     t = Total{t.sx + b.sx, t.sr + b.sr, t.w + b.w, t.h + b.h, mx, mr, fmaxf(t.most, b.most)};
   }
-  write_row(o, row, t, c);
+  write_row(o, row, t, a.sc);
 }
 
 // How rows are shared out.
@@ -359,7 +356,7 @@ lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64
   hipStream_t stream = (hipStream_t)hip_stream;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, mask};
+    const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, scale_of(std::fmin(scale * kLog2e, FLT_MAX)), mask};
     const dim3 block(plan.waves * kWave);
     if (plan.form == kRowWave) {
       // so many rows that there would be 2^32 threads: as large batches as there can be
@@ -399,7 +396,7 @@ lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* r
   if (rows == 0 || (!dlogits && !dref)) return LOPT_OK;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, mask};
+    const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, scale_of(std::fmin(scale * kLog2e, FLT_MAX)), mask};
     const int64_t packs = (vocab + 2 * Pack<T>::n - 2) / Pack<T>::n;   // that a row may touch
     auto launch = [&](auto g) {
       constexpr int G = decltype(g)::value, kSpan = 2 * G;

@@ -2,6 +2,7 @@
 // them to 64 bits: a program that includes this there defines __device__, __forceinline__ and the three builtins.
 #pragma once
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 
@@ -10,14 +11,18 @@ namespace {
 
 // Running sums of some pairs of logits, mx and mr the largest of either (the type's lowest where all are masked), e = 2^(c (x - mx)) and f = 2^(c (r - mr)) with
 // c = scale / ln 2:
-//   sx = sum e,   sr = sum f,   w = sum (f - e),   h = sum e d   with d = c ((x - r) - (mx - mr))
-//   KL = ln 2 h / sx + ln(sr / sx)
+//   sx = sum e,   sr = sum f,   w = sum (f - e),   h = unit sum e d   with d = c ((x - r) - (mx - mr))
+//   KL = ln 2 h / (unit sx) + ln(sr / sx)
 // Differences from the maxima and between the two lose nothing where they are near, however large the logits are; where a constant of more than kOffset lies between the two
 // rows, d goes by (x - mx) - (r - mr). Of two sharp distributions both terms
 // are far smaller than the sums, which begin with the same 1: there ln(sr / sx) = ln(1 + w / sx), whose rounding goes with w (1x10 fp32 of KL 1e-4: off by 4e-5 with the
 // sums alone; by 2e-4 with the maxima's products rounded as in the token log probabilities, for e and f are not 1 at them). `most`: the largest d that was
 // not near; it is infinite where r masks a token that x does not (or where finite logits are 3.4e38 apart). A NaN makes the maximum and by it the sums NaN.
 struct Apart { float mx, mr, sx, sr, w, h, most; };
+// c, and a power of two by which it is 2^-26 to 2^-25. A lane whose tokens x masks all by a finite value has that value as its maximum and e = 1 for them, and r may have the type's lowest
+// there, c d being beyond the type: in this unit the sum of 2^25 of them is finite until the row's maxima take it away. (From c = 2^75 on the unit stays, and fewer are: rebase drops what is nothing beside the row's maxima even if it is infinite.)
+struct Scale { float c, unit; };
+inline Scale scale_of(float c) { return Scale{c, std::ldexp(1.f, -std::clamp(std::ilogb(c) + 26, -100, 100))}; }
 __device__ __forceinline__ Apart nothing() { return Apart{-FLT_MAX, -FLT_MAX, 0.f, 0.f, 0.f, 0.f, -INFINITY}; }
 __device__ __forceinline__ float shift_of(float mx, float mr, float c) { return fminf(c * (mx - mr), FLT_MAX); }
 // The same of a wavefront or more. Lanes add up some hundred terms each in 32 bits, whose roundings are many and independent; the sums over the lanes and what is made of them
@@ -37,23 +42,24 @@ __device__ __forceinline__ float less_one(float d) {
   return __builtin_fmaf(s, s, s + s);
 }
 
-// What a change to larger maxima makes of sums: factors of e and f, the second less the first, what d moves by. Near maxima's second factor goes by
+// What a change to larger maxima makes of sums: factors of e and f, the second less the first, what d moves by in the unit. Near maxima's second factor goes by
 // the move, as f went by d.
 template <typename V> struct Move { V fx, fr, apart, moved; };
 constexpr float kNear = 64.f, kOffset = 32.f;
 template <typename V>
-__device__ __forceinline__ Move<V> move_of(float mx0, float mr0, float mx, float mr, float c) {
+__device__ __forceinline__ Move<V> move_of(float mx0, float mr0, float mx, float mr, Scale s) {
+  const float c = s.c;
   const bool close_by = fabsf(mx0 - mr0) <= kOffset && fabsf(mx - mr) <= kOffset;
   const float moved = close_by ? shift_of(mx0, mr0, c) - shift_of(mx, mr, c) : c * ((mx0 - mx) - (mr0 - mr)), fx = __builtin_amdgcn_exp2f((mx0 - mx) * c), less = fabsf(moved) <= 4.f ? less_one(moved) : __builtin_amdgcn_exp2f(-moved) - 1.f;
-  if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, moved};
+  if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, moved * s.unit};
   const float fr = __builtin_amdgcn_exp2f((mr0 - mr) * c);
-  return Move<V>{fx, fr, fr - fx, moved};
+  return Move<V>{fx, fr, fr - fx, moved * s.unit};
 }
-// a's sums seen from larger maxima.
-__device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, float c) {
-  const Move<float> m = move_of<float>(a.mx, a.mr, mx, mr, c);
+// a's sums seen from larger maxima, beside which they may be nothing, whatever h is.
+__device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, Scale s) {
+  const Move<float> m = move_of<float>(a.mx, a.mr, mx, mr, s);
   const float fs = m.fx * a.sx;
-  return Apart{mx, mr, fs, m.fr * a.sr, m.fr * a.w + m.apart * a.sx, m.fx * a.h + (fs == 0.f ? 0.f : fs * m.moved), a.most};
+  return Apart{mx, mr, fs, m.fr * a.sr, m.fr * a.w + m.apart * a.sx, fs == 0.f ? 0.f : m.fx * a.h + fs * m.moved, a.most};
 }
 // The largest, NaN where there is one.
 template <int E>
@@ -65,13 +71,13 @@ __device__ __forceinline__ float strict_most_of(const float (&x)[E], float m) {
 
 // A lane's piece of logits beside the sums so far, which are seen from the new maxima: each d, and how far the largest lies from 0 (infinite where d has to go by the maxima).
 template <int E>
-__device__ __forceinline__ float differences_of(Apart& a, const float (&x)[E], const float (&r)[E], float c, float (&d)[E]) {
-  a = rebase(a, strict_most_of(x, a.mx), strict_most_of(r, a.mr), c);
-  const float shift = shift_of(a.mx, a.mr, c);
+__device__ __forceinline__ float differences_of(Apart& a, const float (&x)[E], const float (&r)[E], Scale s, float (&d)[E]) {
+  a = rebase(a, strict_most_of(x, a.mx), strict_most_of(r, a.mr), s);
+  const float shift = shift_of(a.mx, a.mr, s.c);
   float far = fabsf(a.mx - a.mr) <= kOffset ? 0.f : INFINITY;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    d[i] = __builtin_fmaf(x[i] - r[i], c, -shift);
+    d[i] = __builtin_fmaf(x[i] - r[i], s.c, -shift);
     far = fmaxf(far, fabsf(d[i]));
   }
   return far;
@@ -80,62 +86,67 @@ __device__ __forceinline__ float differences_of(Apart& a, const float (&x)[E], c
 // an f below 2^-62, which adds nothing. Of both logits masked there is no d. Here |d| <= 4: q - 1 goes by less_one, and not by q, whose rounding next to 1 is what remains of a KL that few
 // unlikely tokens make up: of rows of some ten logits by 5e-6. It takes half as many instructions again as q; in long rows such roundings are many.
 template <int E>
-__device__ __forceinline__ void add_fine(Apart& a, const float (&x)[E], const float (&d)[E], float c) {
+__device__ __forceinline__ void add_fine(Apart& a, const float (&x)[E], const float (&d)[E], Scale s) {
+  float h = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float e = __builtin_amdgcn_exp2f((x[i] - a.mx) * c), near = __builtin_amdgcn_fmed3f(d[i], -4.f, 4.f), g = e * less_one(near);
+    const float e = __builtin_amdgcn_exp2f((x[i] - a.mx) * s.c), near = __builtin_amdgcn_fmed3f(d[i], -4.f, 4.f), g = e * less_one(near);
     a.sx += e;
     a.sr += e + g;
     a.w += g;
-    a.h = __builtin_fmaf(e, near, a.h);
+    h = __builtin_fmaf(e, near, h);
   }
+  a.h = __builtin_fmaf(h, s.unit, a.h);
 }
 // |d| <= kNear.
 template <int E>
-__device__ __forceinline__ void add_near(Apart& a, const float (&x)[E], const float (&d)[E], float c) {
+__device__ __forceinline__ void add_near(Apart& a, const float (&x)[E], const float (&d)[E], Scale s) {
+  float h = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float e = __builtin_amdgcn_exp2f((x[i] - a.mx) * c), near = __builtin_amdgcn_fmed3f(d[i], -kNear, kNear), q = __builtin_amdgcn_exp2f(-near);
+    const float e = __builtin_amdgcn_exp2f((x[i] - a.mx) * s.c), near = __builtin_amdgcn_fmed3f(d[i], -kNear, kNear), q = __builtin_amdgcn_exp2f(-near);
     a.sx += e;
     a.sr = __builtin_fmaf(e, q, a.sr);
     a.w = __builtin_fmaf(e, q - 1.f, a.w);
-    a.h = __builtin_fmaf(e, near, a.h);
+    h = __builtin_fmaf(e, near, h);
   }
+  a.h = __builtin_fmaf(h, s.unit, a.h);
 }
 // Any d.
 template <int E>
-__device__ __forceinline__ void add_far(Apart& a, const float (&x)[E], const float (&r)[E], float c) {
+__device__ __forceinline__ void add_far(Apart& a, const float (&x)[E], const float (&r)[E], Scale s) {
+  const float c = s.c * s.unit;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float dx = x[i] - a.mx, dr = r[i] - a.mr, e = __builtin_amdgcn_exp2f(dx * c), f = __builtin_amdgcn_exp2f(dr * c), d = dx - dr;
+    const float dx = x[i] - a.mx, dr = r[i] - a.mr, e = __builtin_amdgcn_exp2f(dx * s.c), f = __builtin_amdgcn_exp2f(dr * s.c), d = dx - dr;
     a.most = fmaxf(a.most, d);
     a.sx += e;
     a.sr += f;
     a.w += f - e;
-    // 16 e and a sixteenth of d, which may be the type's largest; that of a masked token is finite, for e is 0
-    a.h = __builtin_fmaf(16.f * e, __builtin_amdgcn_fmed3f(d * (c / 16.f), -FLT_MAX, FLT_MAX), a.h);
+    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d, -FLT_MAX, FLT_MAX) * c, a.h);   // that of a masked token is finite, for e is 0
   }
 }
 
 // Sums of a segment seen from larger maxima, in 64 bits; the factors are rounded to 32, each for itself.
-__device__ __forceinline__ void add_segment(Total& t, const Total& b, float c) {
-  const Move<double> m = move_of<double>(b.mx, b.mr, t.mx, t.mr, c);
+__device__ __forceinline__ void add_segment(Total& t, const Total& b, Scale s) {
+  const Move<double> m = move_of<double>(b.mx, b.mr, t.mx, t.mr, s);
   const double fs = m.fx * b.sx;
   t.sx += fs;
   t.sr += m.fr * b.sr;
   t.w += m.fr * b.w + m.apart * b.sx;
-  t.h += m.fx * b.h + (fs == 0.0 ? 0.0 : fs * m.moved);
+  t.h += fs == 0.0 ? 0.0 : m.fx * b.h + fs * m.moved;
   t.most = fmaxf(t.most, b.most);
 }
 
 // A row's KL and stats from its sums. Sums that are 0 belong to a row that is masked whole; a NaN or +infinity is in the sum.
 struct RowResult { float kl, stats[5]; };
-__device__ __forceinline__ RowResult result_of(const Total& a, float c) {
+__device__ __forceinline__ RowResult result_of(const Total& a, Scale s) {
   // what the shift of every d was rounded by is in sr as well, so that KL does not have it; the stats have it taken out
   constexpr double ln2 = 0.693147180559945309417;
-  const double ratio = a.w / a.sx, mean = ln2 * a.h / a.sx;
-  const double rounded = fabsf(a.mx - a.mr) <= kOffset ? ln2 * ((double)shift_of(a.mx, a.mr, c) - (double)c * ((double)a.mx - (double)a.mr)) : 0.0;
-  float kl = fmaxf((float)(mean + (fabs(ratio) < 0.5 ? log1p(ratio) : log(a.sr / a.sx))), 0.f), shifted = (float)(mean + rounded);
+  const double ratio = a.w / a.sx, mean = ln2 * a.h / ((double)s.unit * a.sx);
+  const double rounded = fabsf(a.mx - a.mr) <= kOffset ? ln2 * ((double)shift_of(a.mx, a.mr, s.c) - (double)s.c * ((double)a.mx - (double)a.mr)) : 0.0;
+  float kl = (float)(mean + (fabs(ratio) < 0.5 ? log1p(ratio) : log(a.sr / a.sx))), shifted = (float)(mean + rounded);
+  if (kl < 0.f) kl = 0.f;   // a NaN stays one
   if (a.sr == 0.0 || a.most == INFINITY) kl = shifted = INFINITY;
   if (a.sx == 0.0) kl = shifted = 0.f;
   if (!(a.sx < INFINITY && a.sr < INFINITY)) kl = shifted = NAN;

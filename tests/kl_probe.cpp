@@ -19,7 +19,7 @@ static inline float most_strictly(float a, float b) { return std::isnan(a) || st
 #include "lopt_kl_sums.h"
 using namespace lopt;
 
-struct Shape { int lanes, pack, waves, pieces; float c; };
+struct Shape { int lanes, pack, waves, pieces; Scale sc; };
 
 // The sums of every wavefront's lanes over a segment from the logit `from` on, joined as a workgroup does. `fine`: rows of one piece.
 template <int E>
@@ -37,21 +37,21 @@ static Total segment(const Shape& s, const float* x, const float* r, int n, int6
           a[i] = k < n ? x[k] : -INFINITY;
           b[i] = k < n ? r[k] : -INFINITY;
         }
-        far = std::max(far, differences_of(all[w * s.lanes + lane], a, b, s.c, *(float (*)[E])&d[lane * E]));
+        far = std::max(far, differences_of(all[w * s.lanes + lane], a, b, s.sc, *(float (*)[E])&d[lane * E]));
       }
       for (int lane = 0; lane < s.lanes; ++lane) {
         Apart& a = all[w * s.lanes + lane];
         float (&p)[E] = *(float (*)[E])&u[lane * E], (&q)[E] = *(float (*)[E])&v[lane * E], (&t)[E] = *(float (*)[E])&d[lane * E];
-        if (fine && !(far > 4.f)) add_fine(a, p, t, s.c);
-        else if (!(far > kNear)) add_near(a, p, t, s.c);
-        else add_far(a, p, q, s.c);
+        if (fine && !(far > 4.f)) add_fine(a, p, t, s.sc);
+        else if (!(far > kNear)) add_near(a, p, t, s.sc);
+        else add_far(a, p, q, s.sc);
       }
     }
   float mx = -FLT_MAX, mr = -FLT_MAX;
   for (const Apart& a : all) mx = fmaxf(mx, a.mx), mr = fmaxf(mr, a.mr);
   Total t{0.0, 0.0, 0.0, 0.0, mx, mr, -INFINITY};
   for (Apart a : all) {
-    a = rebase(a, mx, mr, s.c);
+    a = rebase(a, mx, mr, s.sc);
     t.sx += a.sx, t.sr += a.sr, t.w += a.w, t.h += a.h;
     t.most = fmaxf(t.most, a.most);
   }
@@ -60,20 +60,20 @@ static Total segment(const Shape& s, const float* x, const float* r, int n, int6
 
 template <int E>
 static RowResult row_of(const Shape& s, const float* x, const float* r, int n) {
-  if (!s.pieces) return result_of(segment<E>(s, x, r, n, 0, n, s.waves == 1 && n <= s.lanes * E), s.c);
+  if (!s.pieces) return result_of(segment<E>(s, x, r, n, 0, n, s.waves == 1 && n <= s.lanes * E), s.sc);
   std::vector<Total> parts;
   for (int64_t from = 0; from < n; from += (int64_t)s.pieces * s.lanes * E)
     parts.push_back(segment<E>(s, x, r, n, from, std::min<int64_t>(from + (int64_t)s.pieces * s.lanes * E, n), false));
   Total t{0.0, 0.0, 0.0, 0.0, -FLT_MAX, -FLT_MAX, -INFINITY};
   for (const Total& p : parts) t.mx = fmaxf(t.mx, p.mx), t.mr = fmaxf(t.mr, p.mr);
-  for (const Total& p : parts) add_segment(t, p, s.c);
-  return result_of(t, s.c);
+  for (const Total& p : parts) add_segment(t, p, s.sc);
+  return result_of(t, s.sc);
 }
 
 int main(int argc, char** argv) {
   if (argc != 7) return 2;
   const int E = atoi(argv[2]);
-  const Shape s{atoi(argv[1]), atoi(argv[3]), atoi(argv[4]), atoi(argv[5]), fminf((float)atof(argv[6]) * 1.44269504088896341f, FLT_MAX)};
+  const Shape s{atoi(argv[1]), atoi(argv[3]), atoi(argv[4]), atoi(argv[5]), scale_of(fminf((float)atof(argv[6]) * 1.44269504088896341f, FLT_MAX))};
   int32_t size[2];
   if (fread(size, 4, 2, stdin) != 2) return 2;
   const size_t count = (size_t)size[0] * size[1];

@@ -1,0 +1,53 @@
+"""KL divergence where the logits and the reference's are masked by different finite values, down to the types' lowest, in every layout of the kernels, against the definition in float64.
+Rows and tolerances: those of the arithmetic's CPU test and of the kernels' own."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_more_ops import check_kl, kl_exact, kl_tolerance
+from tests.test_gpu_ops import TYPES, close, dev, host, ops, tt
+from tests.test_kl_sums_cpu import rows_that_x_masks
+
+pytestmark = pytest.mark.gpu
+
+VOCABS = [9, 100, 200, 500, 1500, 3000, 20000, 140000]
+
+
+def lowest(kind):
+    import torch
+    return torch.finfo(tt(kind)).min
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_tokens_that_x_masks_by_a_finite_value_and_r_by_the_lowest(vocab, kind):
+    x, y = rows_that_x_masks(vocab, lowest(kind))
+    for scale in (1.0,) if vocab > 3000 else (1.0, 0.5, 2.0):
+        kl = host(check_kl(x, y, kind, scale, what=f"scale {scale}"))
+        assert np.isfinite(kl).all()
+
+
+def repeated(x, y, kind, rows):
+    """kl and stats of `rows` rows, x's and y's over and over; each like the definition's."""
+    import torch
+    (a, av), (b, bv) = dev(x, kind), dev(y, kind)
+    want = kl_exact(av, bv, 1.0)
+    tol, _ = kl_tolerance(av, bv, 1.0, want)
+    n = x.shape[0]
+    at = torch.arange(rows, device="cuda:0") % n
+    kl, stats = ops().token_kl_forward(a[at], b[at])
+    k = np.arange(rows) % n
+    close(kl, want[0][k], tol[k], "kl")
+    close(stats[:, 4], want[1][k, 4], tol[k], "mean")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", [9, 200, 500])
+def test_many_short_rows_of_such_masks(vocab, kind):
+    repeated(*rows_that_x_masks(vocab, lowest(kind)), kind, 8200)
+
+
+@pytest.mark.parametrize("kind,vocab,rows", [("bf16", 262300, 70), ("fp32", 262300, 66), ("fp16", 20000, 3500), ("fp32", 20000, 1700), ("bf16", 20000, 3500)])
+def test_rows_in_segments_and_beyond_the_cache_of_such_masks(kind, vocab, rows):
+    """Some 70 rows of more than 2^18 logits are taken in segments; more than 256 MB of logits are read past the cache."""
+    x, y = rows_that_x_masks(vocab, lowest(kind))
+    repeated(x[::3], y[::3], kind, rows)

@@ -53,3 +53,35 @@ def test_sums(probe, form, vocab):
         y[5, 2] = np.inf
         got = check(probe, form, x, y, scale, (scale, masked, apart))
         assert got[1, 0] == 0 and got[2, 0] == np.inf and np.isnan(got[4:6, 0]).all()
+
+
+def runs_of(vocab):
+    """Runs of tokens at a row's beginning, in its middle and at its end, some of which whole lanes, pieces and wavefronts lie in."""
+    for length in sorted({1, min(16, vocab // 2), min(64, vocab // 3), vocab // 3}):
+        for first in sorted({0, (vocab - length) // 2, vocab - length}):
+            yield slice(first, first + length)
+
+
+def rows_that_x_masks(vocab, low, seed=3):
+    """x masks tokens by a finite value, down to the lowest, and r some of the same by the lowest: masked tokens that are their lane's largest in x while the row has far larger ones."""
+    x, y = logits_pair(1, vocab, seed)
+    at, rows = np.arange(vocab), []
+    kept = np.isin(at, [1, vocab // 2, vocab - 2, vocab - 1])
+    for mask in (low, -1e4):
+        for off in (at == 0, at % 2 == 0, at < vocab // 2, at >= vocab // 2):
+            rows.append((np.where(kept, x[0], mask), np.where(off & ~kept, low, y[0])))
+        for run in runs_of(vocab):
+            for step in (1, 2):
+                a, b = x[0].copy(), y[0].copy()
+                a[run] = mask
+                b[run][::step] = low
+                rows.append((a, b))
+    return tuple(np.stack(v) for v in zip(*rows))
+
+
+@pytest.mark.parametrize("low", [-3.4028234663852886e38, -3.3895313892515355e38])
+@pytest.mark.parametrize("form,vocab", FORMS)
+def test_tokens_that_x_masks_by_a_finite_value_and_r_by_the_lowest(probe, form, vocab, low):
+    x, y = rows_that_x_masks(vocab, low)
+    for scale in (1.0, 0.5, 2.0, 70.0, 1e-3):
+        check(probe, form, x, y, scale, scale)
