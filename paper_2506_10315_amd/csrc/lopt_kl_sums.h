@@ -21,8 +21,11 @@ namespace {
 struct Apart { float mx, mr, sx, sr, w, h, most; };
 // c, and a power of two by which it is 2^-26 to 2^-25. A lane whose tokens x masks all by a finite value has that value as its maximum and e = 1 for them, and r may have the type's lowest
 // there, c d being beyond the type: in this unit the sum of 2^25 of them is finite until the row's maxima take it away. (From c = 2^75 on the unit stays, and fewer are: rebase drops what is nothing beside the row's maxima even if it is infinite.)
-struct Scale { float c, unit; };
-inline Scale scale_of(float c) { return Scale{c, std::ldexp(1.f, -std::clamp(std::ilogb(c) + 26, -100, 100))}; }
+struct Scale { float c, unit, step; };   // step = c unit, which differences near the type's largest are multiplied by at once
+inline Scale scale_of(float c) {
+  const float unit = std::ldexp(1.f, -std::clamp(std::ilogb(c) + 26, -100, 100));
+  return Scale{c, unit, c * unit};
+}
 __device__ __forceinline__ Apart nothing() { return Apart{-FLT_MAX, -FLT_MAX, 0.f, 0.f, 0.f, 0.f, -INFINITY}; }
 __device__ __forceinline__ float shift_of(float mx, float mr, float c) { return fminf(c * (mx - mr), FLT_MAX); }
 // The same of a wavefront or more. Lanes add up some hundred terms each in 32 bits, whose roundings are many and independent; the sums over the lanes and what is made of them
@@ -48,12 +51,13 @@ template <typename V> struct Move { V fx, fr, apart, moved; };
 constexpr float kNear = 64.f, kOffset = 32.f;
 template <typename V>
 __device__ __forceinline__ Move<V> move_of(float mx0, float mr0, float mx, float mr, Scale s) {
-  const float c = s.c;
   const bool close_by = fabsf(mx0 - mr0) <= kOffset && fabsf(mx - mr) <= kOffset;
-  const float moved = close_by ? shift_of(mx0, mr0, c) - shift_of(mx, mr, c) : c * ((mx0 - mx) - (mr0 - mr)), fx = __builtin_amdgcn_exp2f((mx0 - mx) * c), less = fabsf(moved) <= 4.f ? less_one(moved) : __builtin_amdgcn_exp2f(-moved) - 1.f;
-  if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, moved * s.unit};
-  const float fr = __builtin_amdgcn_exp2f((mr0 - mr) * c);
-  return Move<V>{fx, fr, fr - fx, moved * s.unit};
+  const float apart = __builtin_amdgcn_fmed3f((mx0 - mx) - (mr0 - mr), -FLT_MAX, FLT_MAX);
+  const float moved = close_by ? shift_of(mx0, mr0, s.c) - shift_of(mx, mr, s.c) : s.c * apart, held = close_by ? moved * s.unit : apart * s.step;
+  const float fx = __builtin_amdgcn_exp2f((mx0 - mx) * s.c), less = fabsf(moved) <= 4.f ? less_one(moved) : __builtin_amdgcn_exp2f(-moved) - 1.f;
+  if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, held};
+  const float fr = __builtin_amdgcn_exp2f((mr0 - mr) * s.c);
+  return Move<V>{fx, fr, fr - fx, held};
 }
 // a's sums seen from larger maxima, beside which they may be nothing, whatever h is.
 __device__ __forceinline__ Apart rebase(Apart a, float mx, float mr, Scale s) {
@@ -115,7 +119,6 @@ __device__ __forceinline__ void add_near(Apart& a, const float (&x)[E], const fl
 // Any d.
 template <int E>
 __device__ __forceinline__ void add_far(Apart& a, const float (&x)[E], const float (&r)[E], Scale s) {
-  const float c = s.c * s.unit;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const float dx = x[i] - a.mx, dr = r[i] - a.mr, e = __builtin_amdgcn_exp2f(dx * s.c), f = __builtin_amdgcn_exp2f(dr * s.c), d = dx - dr;
@@ -123,7 +126,7 @@ __device__ __forceinline__ void add_far(Apart& a, const float (&x)[E], const flo
     a.sx += e;
     a.sr += f;
     a.w += f - e;
-    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d, -FLT_MAX, FLT_MAX) * c, a.h);   // that of a masked token is finite, for e is 0
+    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d, -FLT_MAX, FLT_MAX) * s.step, a.h);   // that of a masked token is finite, for e is 0
   }
 }
 

@@ -5,7 +5,7 @@ import pytest
 
 from tests.test_gpu_more_ops import check_kl, kl_exact, kl_tolerance
 from tests.test_gpu_ops import TYPES, close, dev, host, ops, tt
-from tests.test_kl_sums_cpu import rows_that_x_masks
+from tests.test_kl_sums_cpu import rows_that_x_masks, rows_with_unlikely_tokens_that_r_masks
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,20 @@ def test_rows_in_segments_and_beyond_the_cache_of_such_masks(kind, vocab, rows):
     """Some 70 rows of more than 2^18 logits are taken in segments; more than 256 MB of logits are read past the cache."""
     x, y = rows_that_x_masks(vocab, lowest(kind))
     repeated(x[::3], y[::3], kind, rows)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_unlikely_tokens_that_r_masks_by_the_lowest(vocab, kind):
+    x, y = rows_with_unlikely_tokens_that_r_masks(vocab, lowest(kind))
+    for scale in (1.0,) if vocab > 3000 else (1.0, 0.5):
+        kl = host(check_kl(x, y, kind, scale, what=f"scale {scale}"))
+        assert np.isfinite(kl).all()
+
+
+@pytest.mark.parametrize("kind,vocab,rows", [("bf16", 9, 8200), ("fp32", 200, 8200), ("fp16", 500, 8200), ("bf16", 500, 8200), ("bf16", 262300, 70), ("fp32", 262300, 66),
+                                             ("fp16", 20000, 3500), ("fp32", 20000, 1700), ("bf16", 20000, 3500)])
+def test_many_rows_segments_and_rows_beyond_the_cache_of_such_tokens(kind, vocab, rows):
+    for masked in (False, True):
+        x, y = rows_with_unlikely_tokens_that_r_masks(vocab, lowest(kind), masked)
+        repeated(x, y, kind, rows)

@@ -85,3 +85,32 @@ def test_tokens_that_x_masks_by_a_finite_value_and_r_by_the_lowest(probe, form, 
     x, y = rows_that_x_masks(vocab, low)
     for scale in (1.0, 0.5, 2.0, 70.0, 1e-3):
         check(probe, form, x, y, scale, scale)
+
+
+def rows_with_unlikely_tokens_that_r_masks(vocab, low, masked=False):
+    """Runs of tokens that x has at p = 1e-37, 1e-30 or 1e-4 each and r at the lowest value: KL is p times that value, 1e1 to 1e36. `masked`: x masks some others by the lowest."""
+    x, y = logits_pair(1, vocab, 4)
+    rows = []
+    for run in runs_of(vocab):
+        for under in (85.0, 69.0, 9.2):
+            if under < 10 and run.stop - run.start > 64:   # KL beyond 1e38
+                continue
+            a, b = x[0].copy(), y[0].copy()
+            a[run] = -np.inf
+            a[run] = a.max() - under
+            b[run] = low
+            if masked:
+                off = (np.arange(vocab) % 3 == 1) & (a < a.max() - 10)
+                off[run] = False
+                a[off] = low
+            rows.append((a, b))
+    return tuple(np.stack(v) for v in zip(*rows))
+
+
+@pytest.mark.parametrize("low", [-3.4028234663852886e38, -3.3895313892515355e38])
+@pytest.mark.parametrize("form,vocab", FORMS)
+def test_unlikely_tokens_that_r_masks_by_the_lowest(probe, form, vocab, low):
+    for masked in (False, True):
+        x, y = rows_with_unlikely_tokens_that_r_masks(vocab, low, masked)
+        for scale in (1.0, 0.5, 2.0):
+            assert np.isfinite(check(probe, form, x, y, scale, (scale, masked))[:, 0]).all()
