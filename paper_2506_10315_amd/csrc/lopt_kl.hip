@@ -269,13 +269,13 @@ __global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, const float* __re
     const float mx = s[0], ln_sx = s[1], mr = s[2], ln_sr = s[3], mean = s[4], g = a.keep && !a.keep[row] ? 0.f : dkl[row];
     const bool zero = g == 0.f || (mx == -INFINITY && ln_sx == -INFINITY);
     const bool r_empty = mr == -INFINITY;
-    const float A = zero ? 0.f : mean == INFINITY ? NAN : g * a.scale;
+    const float A = zero ? 0.f : mean < INFINITY ? g * a.scale : NAN;   // an infinite mean or none makes the whole row NaN
     // d by way of x - r, or of the maxima where a constant lies between the rows
     const bool close_by = fabsf(mx - mr) <= kOffset;
     const float ux = close_by ? 0.f : mx, ur = close_by ? 0.f : mr, dm = close_by ? mx - mr : 0.f;
     auto gradient = [&](float u, float v, float& gx, float& gr) {
       const float p = exp2_hw((a.scale * (u - mx) - ln_sx) * kLog2e);
-      if (DX) gx = A * (p * (__builtin_amdgcn_fmed3f((((u - ux) - (v - ur)) - dm) * a.scale, -FLT_MAX, FLT_MAX) - mean));
+      if (DX) gx = A * (p * __builtin_amdgcn_fmed3f(__builtin_fmaf(((u - ux) - (v - ur)) - dm, a.scale, -mean), -FLT_MAX, FLT_MAX));   // finite, for p may be 0
       if (DR) gr = A * ((r_empty ? 0.f : exp2_hw((a.scale * (v - mr) - ln_sr) * kLog2e)) - p);
     };
     const T* grid_row = DX ? out_x : out_r;

@@ -68,3 +68,16 @@ def test_many_rows_segments_and_rows_beyond_the_cache_of_such_tokens(kind, vocab
     for masked in (False, True):
         x, y = rows_with_unlikely_tokens_that_r_masks(vocab, lowest(kind), masked)
         repeated(x, y, kind, rows)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_gradient_of_tokens_of_no_probability_beside_such(vocab, kind):
+    """x masks others by the lowest value: their gradient is 0, however large the mean difference is."""
+    x, y = rows_with_unlikely_tokens_that_r_masks(vocab, lowest(kind), True)
+    x, y = (v[::4] for v in (x, y)) if vocab > 3000 else (x, y)
+    check_kl(x, y, kind)
+    (xt, xv), (yt, _) = dev(x, kind), dev(y, kind)
+    kl, stats = ops().token_kl_forward(xt, yt)
+    dx = host(ops().token_kl_backward(xt, yt, stats, kl.new_ones(kl.shape))[0])
+    assert np.isfinite(dx).all() and not dx[xv < xv.max(1, keepdims=True) - 200].any()
