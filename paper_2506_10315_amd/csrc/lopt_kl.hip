@@ -257,8 +257,8 @@ inline RowPlan plan_rows(int64_t rows, int64_t vocab) {
 //   dx = g scale p (d - mean d under p),   dr = g scale (q - p)
 // Bound by memory: two reads and one or two writes of the logits. Laid out as the gradient of the token log probabilities.
 template <typename T, bool DX, bool DR, int G>
-__global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, const float* __restrict__ stats, const float* __restrict__ dkl, T* dx, int64_t ld_dx, T* dr,
-                                                    int64_t ld_dr) {
+__global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, float lift, float drop, const float* __restrict__ stats, const float* __restrict__ dkl, T* dx, int64_t ld_dx,
+                                                    T* dr, int64_t ld_dr) {
   typedef typename Pack<T>::type pack;
   constexpr int V = Pack<T>::n, kPacks = 2, kSpan = kPacks * G * V, kRows = kBlock / G;
   const int lane = threadIdx.x % G, vocab = (int)a.n;
@@ -270,12 +270,15 @@ __global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, const float* __re
     const bool zero = g == 0.f || (mx == -INFINITY && ln_sx == -INFINITY);
     const bool r_empty = mr == -INFINITY;
     const float A = zero ? 0.f : mean < INFINITY ? g * a.scale : NAN;   // an infinite mean or none makes the whole row NaN
+    // d - mean under an unlikely token may be beyond the type where the token's gradient is not: for dx a power of two goes from the scale over to g
+    const bool lifted = fabsf(A * lift) < INFINITY;
+    const float Ax = lifted ? A * lift : A, scale_d = lifted ? a.scale * drop : a.scale, mean_d = lifted ? mean * drop : mean;
     // d by way of x - r, or of the maxima where a constant lies between the rows
     const bool close_by = fabsf(mx - mr) <= kOffset;
     const float ux = close_by ? 0.f : mx, ur = close_by ? 0.f : mr, dm = close_by ? mx - mr : 0.f;
     auto gradient = [&](float u, float v, float& gx, float& gr) {
       const float p = exp2_hw((a.scale * (u - mx) - ln_sx) * kLog2e);
-      if (DX) gx = A * (p * __builtin_amdgcn_fmed3f(__builtin_fmaf(((u - ux) - (v - ur)) - dm, a.scale, -mean), -FLT_MAX, FLT_MAX));   // finite, for p may be 0
+      if (DX) gx = Ax * (p * __builtin_amdgcn_fmed3f(__builtin_fmaf(((u - ux) - (v - ur)) - dm, scale_d, -mean_d), -FLT_MAX, FLT_MAX));   // finite, for p may be 0
       if (DR) gr = A * ((r_empty ? 0.f : exp2_hw((a.scale * (v - mr) - ln_sr) * kLog2e)) - p);
     };
     const T* grid_row = DX ? out_x : out_r;
@@ -398,12 +401,13 @@ lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* r
     using T = decltype(t);
     const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, scale_of(std::fmin(scale * kLog2e, FLT_MAX)), mask};
     const int64_t packs = (vocab + 2 * Pack<T>::n - 2) / Pack<T>::n;   // that a row may touch
+    const float lift = std::ldexp(1.f, std::clamp(std::ilogb(scale) + 1, 0, 16));
     auto launch = [&](auto g) {
       constexpr int G = decltype(g)::value, kSpan = 2 * G;
       const int64_t spans = (packs + kSpan - kSpan / 8) / kSpan;
       const dim3 grid((unsigned)std::clamp<int64_t>(spans, 1, 1024), (unsigned)std::min<int64_t>((rows + kBlock / G - 1) / (kBlock / G), 65535));
       auto kernel = !dref ? k_kl_back<T, true, false, G> : !dlogits ? k_kl_back<T, false, true, G> : k_kl_back<T, true, true, G>;
-      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)hip_stream, a, stats, dkl, (T*)dlogits, ld_d, (T*)dref, ld_dref);
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, (hipStream_t)hip_stream, a, lift, 1.f / lift, stats, dkl, (T*)dlogits, ld_d, (T*)dref, ld_dref);
     };
     if (packs <= 2 * 16) launch(std::integral_constant<int, 16>{});
     else if (packs <= 2 * 64) launch(std::integral_constant<int, 64>{});

@@ -81,3 +81,17 @@ def test_gradient_of_tokens_of_no_probability_beside_such(vocab, kind):
     kl, stats = ops().token_kl_forward(xt, yt)
     dx = host(ops().token_kl_backward(xt, yt, stats, kl.new_ones(kl.shape))[0])
     assert np.isfinite(dx).all() and not dx[xv < xv.max(1, keepdims=True) - 200].any()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", [9, 500, 3000, 140000])
+def test_gradient_where_the_scale_takes_differences_beyond_the_type(vocab, kind):
+    """scale (x - r) beyond 3.4e38 under tokens of p = 1e-6, whose gradient is a number."""
+    x, y = rows_with_unlikely_tokens_that_r_masks(vocab, lowest(kind))
+    x, y = x[2::3][:6], y[2::3][:6]
+    r = np.random.default_rng(vocab)
+    for scale in (1.0, 1.5, 2.0, 70.0, 1000.0):
+        a, b = r.uniform(-1.0, 0.0, x.shape) * 9 / scale, r.uniform(-1.0, 0.0, x.shape) * 9 / scale
+        run = y == np.float64(lowest(kind))
+        a = np.where(run, a.max() - 14.0 / scale - np.log(vocab) / scale, a)
+        check_kl(a, np.where(run, lowest(kind), b), kind, scale, what=f"scale {scale}")
