@@ -274,8 +274,12 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 Seed = Union[int, torch.Tensor]
 
 
-def _seed(seed: Seed, offset: int, like: torch.Tensor) -> Tuple[int, Optional[torch.Tensor], int]:
-    """(seed, tensor that holds it or None, offset) as the boundary takes them."""
+def _seed(seed: Optional[Seed], offset: int, like: torch.Tensor, p: float) -> Tuple[int, Optional[torch.Tensor], int]:
+    """(seed, tensor that holds it or None, offset) as the boundary takes them. Where p decides by itself there need be no seed."""
+    if seed is None:
+        if 0.0 < p < 1.0:
+            raise ValueError(f"p={p} without a seed, which would drop the same elements in every step")
+        seed = 0
     if not 0 <= offset < 1 << 64:
         raise ValueError(f"offset={offset} outside [0, 2^64)")
     if isinstance(seed, torch.Tensor):
@@ -293,7 +297,7 @@ def dropout_forward(x: torch.Tensor, p: float, seed: Seed, offset: int = 0) -> t
     the device is read when the kernel runs."""
     kind = _type("x", x)
     x2, rows, cols, ld = _matrix("x", x)
-    number, tensor, offset = _seed(seed, offset, x)
+    number, tensor, offset = _seed(seed, offset, x, p)
     y = _new(x)
     _run(lib().lopt_dropout, x.get_device(), x2.data_ptr(), ld, y.data_ptr(), cols, rows, cols, kind, p, number, _ptr(tensor), offset)
     return y
@@ -321,10 +325,10 @@ def dropout(x: torch.Tensor, p: float, seed: Seed, offset: int = 0) -> torch.Ten
 
 
 def dropout_add_layer_norm_forward(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
-                                   p: float = 0.0, seed: Seed = 0, offset: int = 0,
+                                   p: float = 0.0, seed: Optional[Seed] = None, offset: int = 0,
                                    eps: float = 1e-5) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
     """(y, h, mean, rstd) with h = residual + dropout(x) and y = layer_norm(h): y has x's type, h the residual's, which is x's or
-    float32. The norm is of h as it is stored."""
+    float32. The norm is of h as it is stored. `seed`: as in dropout_forward, needed where 0 < p < 1."""
     kind = _type("x", x)
     x2, rows, cols, ld = _matrix("x", x)
     if residual.shape != x.shape or residual.get_device() != x.get_device():
@@ -339,7 +343,7 @@ def dropout_add_layer_norm_forward(x: torch.Tensor, residual: torch.Tensor, weig
         if weight is None:
             wtype = _type("bias", bias)
         bias = _expect("bias", bias, x, bias.dtype if weight is None else weight.dtype, (cols,))
-    number, tensor, offset = _seed(seed, offset, x)
+    number, tensor, offset = _seed(seed, offset, x, p)
     y, h = _new(x), _new(residual)
     mean = _floats(rows, x.shape[:-1], x.device)
     rstd = torch.empty_like(mean)
@@ -349,7 +353,7 @@ def dropout_add_layer_norm_forward(x: torch.Tensor, residual: torch.Tensor, weig
 
 
 def dropout_add_layer_norm_backward(dy: torch.Tensor, dh: Optional[torch.Tensor], h: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
-                                    rstd: torch.Tensor, p: float = 0.0, seed: Seed = 0, offset: int = 0,
+                                    rstd: torch.Tensor, p: float = 0.0, seed: Optional[Seed] = None, offset: int = 0,
                                     need: Tuple[bool, bool, bool, bool] = (True, True, True, True), bias_type: Optional[torch.dtype] = None):
     """(dx, dresidual, dweight, dbias) of dropout_add_layer_norm_forward from the gradients of y and of h (None: 0); `need` says which are wanted,
     the others are None. dx has dy's type, dresidual h's. Without dropout dx and dresidual of one type are the same tensor."""
@@ -370,7 +374,7 @@ def dropout_add_layer_norm_backward(dy: torch.Tensor, dh: Optional[torch.Tensor]
     shape = dy.shape[:-1]
     mean = _expect("mean", mean, dy, torch.float32, shape)
     rstd = _expect("rstd", rstd, dy, torch.float32, shape)
-    number, tensor, offset = _seed(seed, offset, dy)
+    number, tensor, offset = _seed(seed, offset, dy, p)
     same = p == 0.0 and kind == rkind
     dres = _new(h) if need[1] or (need[0] and same) else None
     dx = _new(dy) if need[0] and not same else None
@@ -415,7 +419,7 @@ class _DropoutAddLayerNorm(torch.autograd.Function):
 
 
 def dropout_add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
-                           p: float = 0.0, seed: Seed = 0, offset: int = 0, eps: float = 1e-5) -> Tuple[torch.Tensor, torch.Tensor]:
+                           p: float = 0.0, seed: Optional[Seed] = None, offset: int = 0, eps: float = 1e-5) -> Tuple[torch.Tensor, torch.Tensor]:
     """(y, h): the block's output x is dropped, joins the residual stream, h, and the stream is normalised for the next block, y. With gradients
     for x, residual, weight and bias."""
     return _DropoutAddLayerNorm.apply(x, residual, weight, bias, p, seed, offset, eps)
