@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import os
 import sys
+from typing import Optional
 
 import torch
 
@@ -42,8 +43,8 @@ class TokenModel(torch.nn.Module):
         self.norm_w, self.norm_b = torch.nn.Parameter(torch.ones(width)), torch.nn.Parameter(torch.zeros(width))
         self.head = weight(vocab, width)
 
-    def forward(self, tokens: torch.Tensor, seed: int = 0) -> torch.Tensor:
-        """Logits. `seed`: that of this step's dropout, in training."""
+    def forward(self, tokens: torch.Tensor, seed: Optional[int] = None) -> torch.Tensor:
+        """Logits. `seed`: that of this step's dropout, which has to be given in training with it."""
         x = self.embed[tokens]
         if self.dropout and self.training:
             return self._dropped(x, seed)
@@ -52,7 +53,7 @@ class TokenModel(torch.nn.Module):
             x = x + torch.nn.functional.gelu(h @ b.up.t()) @ b.down.t()
         return ops.layer_norm(x, self.norm_w, self.norm_b) @ self.head.t()
 
-    def _dropped(self, x: torch.Tensor, seed: int) -> torch.Tensor:
+    def _dropped(self, x: torch.Tensor, seed: Optional[int]) -> torch.Tensor:
         """The same with dropout of the embedding and of what every block adds: each with its number as offset, with the addition and the norm behind it."""
         x = ops.dropout(x, self.dropout, seed, 0)
         norms = [(b.norm_w, b.norm_b) for b in self.blocks] + [(self.norm_w, self.norm_b)]
@@ -99,9 +100,9 @@ def step_on(loss, model, optimizer, max_norm: float = 1.0):
     return float(loss.detach()), float(norm)
 
 
-def train_step(model, optimizer, tokens, targets, max_norm: float = 1.0, entropy_weight: float = 0.01):
-    """One step of training; (loss, gradient norm before clipping)."""
-    loss = loss_of(model(tokens), targets, entropy_weight)
+def train_step(model, optimizer, tokens, targets, max_norm: float = 1.0, entropy_weight: float = 0.01, seed: Optional[int] = None):
+    """One step of training, its dropout drawn from `seed`, another one in every step; (loss, gradient norm before clipping)."""
+    loss = loss_of(model(tokens, seed), targets, entropy_weight)
     optimizer.zero_grad()
     loss.backward()
     norm = ops.clip_grad_norm_(model.parameters(), max_norm)
@@ -147,7 +148,7 @@ def main(steps: int = 5):
         with torch.no_grad():
             ref_logits = reference(tokens)
             ref_logp = ops.token_logprobs_forward(ref_logits, targets, ignore_index=IGNORE).logp
-        loss, norm = step_on(loss_of(model(tokens, seed=step), targets, 0.01), model, optimizer)
+        loss, norm = train_step(model, optimizer, tokens, targets, seed=step)
         print(f"with dropout, step {step}: loss {loss:.4f}, gradient norm {norm:.4f}", flush=True)
         p = policy_loss_of(model(tokens, seed=1000 + step), ref_logits, targets, ref_logp, torch.linspace(-1.0, 1.0, 16, device=device))
         print(f"policy loss, gradient norm: {step_on(p.loss, model, optimizer)}, kl {float(p.stats[1]):.5f}", flush=True)

@@ -25,3 +25,21 @@ def test_fused_dropout_without_a_seed():
         y, h = o.dropout_add_layer_norm(b, x, p=p, seed=0)
         (y.sum() + h.sum()).backward()
         assert torch.equal(a.grad, b.grad)
+
+
+def test_the_example_draws_by_its_steps_seed():
+    import torch
+    from tests.test_gpu_example import _example
+    import workloads as W
+    from paper_2506_10315_amd import LearnedOptTorch
+    ex = _example()
+
+    def step(**seed):
+        model = ex.TokenModel(vocab=200, width=64, depth=2, dropout=0.3).cuda()
+        opt = LearnedOptTorch(model.parameters(), W.velo_weights(0), kind="velo", lr=1e-3)
+        return ex.train_step(model, opt, *ex.batch(200, 4, 16, 0, "cuda:0"), **seed)
+
+    with pytest.raises(ValueError, match="without a seed"):
+        step()
+    first, again, other = step(seed=1), step(seed=1), step(seed=2)
+    assert first == again and first != other
