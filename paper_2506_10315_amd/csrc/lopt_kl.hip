@@ -43,7 +43,7 @@ __device__ __forceinline__ Total total_of(Apart a, float mx, float mr, Scale sc)
 template <int E, bool FINE, int G = kWave>
 __device__ __forceinline__ void add_piece(Apart& a, const float (&x)[E], const float (&r)[E], Scale sc) {
   float d[E];
-  const float far = differences_of(a, x, r, sc, d);
+  const float far = differences_of<E, FINE>(a, x, r, sc, d);
   if (FINE && none_of_group<G>(far > 4.f)) return add_fine(a, x, d, sc);
   if (none_of_group<G>(far > kNear)) return add_near(a, x, d, sc);
   add_far(a, x, r, sc);

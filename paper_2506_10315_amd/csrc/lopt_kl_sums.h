@@ -74,9 +74,12 @@ __device__ __forceinline__ float strict_most_of(const float (&x)[E], float m) {
 }
 
 // A lane's piece of logits beside the sums so far, which are seen from the new maxima: each d, and how far the largest lies from 0 (infinite where d has to go by the maxima).
-template <int E>
+// FIRST: there are no sums so far.
+template <int E, bool FIRST>
 __device__ __forceinline__ float differences_of(Apart& a, const float (&x)[E], const float (&r)[E], Scale s, float (&d)[E]) {
-  a = rebase(a, strict_most_of(x, a.mx), strict_most_of(r, a.mr), s);
+  const float mx = strict_most_of(x, a.mx), mr = strict_most_of(r, a.mr);
+  if (FIRST) a.mx = mx, a.mr = mr;
+  else a = rebase(a, mx, mr, s);
   const float shift = shift_of(a.mx, a.mr, s.c);
   float far = fabsf(a.mx - a.mr) <= kOffset ? 0.f : INFINITY;
 #pragma unroll

@@ -37,7 +37,9 @@ static Total segment(const Shape& s, const float* x, const float* r, int n, int6
           a[i] = k < n ? x[k] : -INFINITY;
           b[i] = k < n ? r[k] : -INFINITY;
         }
-        far = std::max(far, differences_of(all[w * s.lanes + lane], a, b, s.sc, *(float (*)[E])&d[lane * E]));
+        Apart& sums = all[w * s.lanes + lane];
+        float (&t)[E] = *(float (*)[E])&d[lane * E];
+        far = std::max(far, fine ? differences_of<E, true>(sums, a, b, s.sc, t) : differences_of<E, false>(sums, a, b, s.sc, t));
       }
       for (int lane = 0; lane < s.lanes; ++lane) {
         Apart& a = all[w * s.lanes + lane];
