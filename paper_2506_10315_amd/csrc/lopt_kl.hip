@@ -79,7 +79,7 @@ __device__ __forceinline__ void write_nothing(const Outputs& o, int64_t row) {
 
 // Rows of one piece: G lanes each, `batch` <= G neighbouring ones in turn. Lane k of the group keeps the sums of the k-th, and all lanes make their rows' outputs at once.
 // Bound by vector issue, some 500 instructions a row of 64 lanes: batches, of which 8192 wavefronts have one each, spare most rows those of the outputs. us with a row a batch | so:
-// 20000x1000 bf16 35 | 32.6, 100000x100 fp32 with 64 lanes a row 111 | 94, with 16 26; with 4096 wavefronts 28.
+// 20000x1000 bf16 34.0 | 30.6 to 32.1, 100000x100 fp32 26.6 | 24.4, with 64 lanes a row 89.
 template <typename T, int E, int G>
 __global__ __launch_bounds__(kBlock) void k_kl_short(Rows<T> a, int batch, Outputs o) {
   constexpr int kGroups = kBlock / G;
@@ -155,9 +155,9 @@ __device__ __forceinline__ Total block_total(const Apart& s, Scale sc, Room& roo
   return t;
 }
 
-// A workgroup a row, its wavefronts a piece each in turn. Bound by memory and by vector issue (21.6 instructions for a pair of logits, two powers of two among them, as 4 each): 4096x50257
-// bf16 of which an eighth does not count 145 us, 5.0 TB/s, where loads alone take 127; 3000x50257 fp32 220 us, 5.5 TB/s. Registers for four wavefronts a unit; fp32, whose packs take
-// twice as many, for three (spilled for four: 247 us), bf16 for three 159.
+// A workgroup a row, its wavefronts a piece each in turn. Bound by memory and by vector issue (24 instructions for a pair of logits, two powers of two among them, as 4 each): 4096x50257
+// bf16 of which an eighth does not count 140 us in a graph, 5.1 TB/s, where loads alone take 127; 3000x50257 fp32 190 us, 6.3 TB/s. Registers for four wavefronts a unit; fp32, whose packs
+// take twice as many, for three (spilled for four: 234 us), bf16 for three 155.
 template <typename T, int E, bool NT>
 __global__ __launch_bounds__(kMostWaves * kWave, sizeof(T) == 4 ? 3 : 4) void k_kl(Rows<T> a, Outputs o) {
   typedef Piece<T, E> P;
@@ -238,24 +238,25 @@ struct RowPlan {
 };
 inline RowPlan plan_rows(int64_t rows, int64_t vocab) {
   const int64_t n = vocab + 7;   // a row counted from its pack
-  // us with 64 lanes a row / 16: 1024x100 fp32 5.5 / 5.2, 16384x100 19.5 / 7.9, 100000x300 bf16 97 / 61, 16384x500 fp16 20.6 / 14.8, 4096x500 bf16 8.7 / 7.2, but 1024x500 5.5 / 7.0
+  // us with 64 lanes a row / 16: 1024x100 fp32 4.8 / 4.8, 16384x100 17.4 / 7.0, 100000x300 bf16 91 / 58, 16384x500 fp16 19.1 / 13.9, 4096x500 bf16 7.8 / 6.6, but 1024x500 4.8 / 6.4
   if (n <= 128 || (n <= 512 && rows >= 4096)) return RowPlan{kRowWave, n <= 128 ? 8 : n <= 256 ? 16 : 32, 4, 16, 0, 0};
   if (n <= 2048) return RowPlan{kRowWave, n <= 512 ? 8 : n <= 1024 ? 16 : 32, 4, kWave, 0, 0};
   const int64_t pieces = (n + 1023) / 1024;
-  // Few long rows in segments, which costs a launch and a workspace more on the host, some 5 us. us in a graph, a workgroup a row / segments: 1x50257 fp32 14.2 / 9.1, 1x100000 bf16
-  // 21 / 8.8, 12x99760 fp32 23.5 / 10.3, 64x100000 bf16 24 / 16, 128x70000 18.4 / 19.5, 200x100000 25 / 29, 200x131000 fp32 40 / 42.
+  // Few long rows in segments, which costs a launch and a workspace more on the host, some 5 us. us in a graph, a workgroup a row / segments: 1x50257 fp32 12.9 / 8.5, 1x100000 bf16
+  // 21 / 8.2, 12x99760 fp32 21.9 / 9.6, 64x100000 bf16 22 / 16.7, 128x70000 18.6 / 19.1, 200x100000 25 / 30, 200x131000 fp32 37 / 42, but 70x262300 bf16 52 / 27.
   if (rows <= 64 ? n > 64 * 1024 : rows < 256 && n > 256 * 1024) {
     const int64_t per = std::clamp<int64_t>(rows * pieces / 2048, 4, 32);
     return RowPlan{kRowSplit, 16, 4, kWave, per, (pieces + per - 1) / per};
   }
-  // Wavefronts: one for about five pieces up to four, with fewer than 1024 rows as many as make 4096 in all, up to eight. us with 1 / 2 / 4 / 8: 20000x5000 bf16 83 / 94 / 116,
-  // 8192x16000 104 / 110 / 113 / 130, 4096x50257 167 / 169 / 157 / 177, 2048x131000 239 / 217 / 211 / 218, 512x50257 62 / 42 / 27 / 26, 256x32000 38 / 22 / 14 / 12.
+  // Wavefronts: one for about five pieces up to four, with fewer than 1024 rows as many as make 4096 in all, up to eight. us with 1 / 2 / 4 / 8: 20000x5000 bf16 85 / 98 / 120,
+  // 8192x16000 101 / 100 / 104 / 132, 4096x50257 159 / 164 / 152 / 167, 2048x131000 255 / 198 / 191 / 197, 512x50257 62 / 43 / 27 / 26, 256x32000 38 / 22 / 14 / 12.
   return RowPlan{kRowBlock, 16, (int)std::max(std::clamp<int64_t>((pieces + 4) / 5, 1, 4), std::min<int64_t>({kMostWaves, pieces, 4096 / rows})), kWave, 0, 0};
 }
 
 // The gradients, element by element, with d = scale ((x - r) - (mx - mr)) and g = dkl:
 //   dx = g scale p (d - mean d under p),   dr = g scale (q - p)
-// Bound by memory: two reads and one or two writes of the logits. Laid out as the gradient of the token log probabilities.
+// Bound by memory: two reads and one or two writes of the logits. Laid out as the gradient of the token log probabilities. Reads and writes go past the cache whatever the size. us together
+// with a sum that reads dx, so / stores by the cache / loads too: 4096x50257 bf16 339 / 352 / 353; smaller ones lose by it, 1024x50257 91 / 85 / 98, 512x50257 48 / 45 / 46, 64x50257 13.8 / 13.1 / 12.4.
 template <typename T, bool DX, bool DR, int G>
 __global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, float lift, float drop, const float* __restrict__ stats, const float* __restrict__ dkl, T* dx, int64_t ld_dx,
                                                     T* dr, int64_t ld_dr) {
@@ -368,7 +369,7 @@ lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64
                                 : plan.lane == 8 ? k_kl_short<T, 8, 64> : plan.lane == 16 ? k_kl_short<T, 16, 64> : k_kl_short<T, 32, 64>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + per - 1) / per)), block, 0, stream, a, batch, o);
     } else if (plan.form == kRowBlock) {
-      // what the Infinity Cache cannot hold is not left there: 4096x50257 bf16 165 -> 157 us, 20000x5000 93 -> 83, but 1024x50257, which fits, 43 -> 46
+      // what the Infinity Cache cannot hold is not left there: 4096x50257 bf16 157 -> 150 us, 20000x5000 87 -> 84, 3000x50257 fp32 212 -> 189, but 1024x50257, which fits, 43 -> 44.5
       const bool large = 2 * rows * vocab * (int64_t)sizeof(T) > kCacheBytes;
       auto kernel = large ? k_kl<T, 16, true> : k_kl<T, 16, false>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), block, 0, stream, a, o);
