@@ -27,7 +27,7 @@ inline Scale scale_of(float c) {
   return Scale{c, unit, c * unit};
 }
 __device__ __forceinline__ Apart nothing() { return Apart{-FLT_MAX, -FLT_MAX, 0.f, 0.f, 0.f, 0.f, -INFINITY}; }
-__device__ __forceinline__ float shift_of(float mx, float mr, float c) { return fminf(c * (mx - mr), FLT_MAX); }
+__device__ __forceinline__ float shift_of(float mx, float mr, float c) { return __builtin_amdgcn_fmed3f(c * (mx - mr), -FLT_MAX, FLT_MAX); }
 // The same of a wavefront or more. Lanes add up some hundred terms each in 32 bits, whose roundings are many and independent; the sums over the lanes and what is made of them
 // are in 64, for KL is the small difference of its two terms (32 bits throughout: 1.6e-6 of the KL of 64 rows, so 2e-7).
 struct Total { double sx, sr, w, h; float mx, mr, most; };
@@ -52,8 +52,8 @@ constexpr float kNear = 64.f, kOffset = 32.f;
 template <typename V>
 __device__ __forceinline__ Move<V> move_of(float mx0, float mr0, float mx, float mr, Scale s) {
   const bool close_by = fabsf(mx0 - mr0) <= kOffset && fabsf(mx - mr) <= kOffset;
-  const float apart = __builtin_amdgcn_fmed3f((mx0 - mx) - (mr0 - mr), -FLT_MAX, FLT_MAX);
-  const float moved = close_by ? shift_of(mx0, mr0, s.c) - shift_of(mx, mr, s.c) : s.c * apart, held = close_by ? moved * s.unit : apart * s.step;
+  const float apart = (mx0 - mx) - (mr0 - mr);
+  const float moved = close_by ? shift_of(mx0, mr0, s.c) - shift_of(mx, mr, s.c) : s.c * apart, held = close_by ? moved * s.unit : __builtin_amdgcn_fmed3f(apart * s.step, -FLT_MAX, FLT_MAX);
   const float fx = __builtin_amdgcn_exp2f((mx0 - mx) * s.c), less = fabsf(moved) <= 4.f ? less_one(moved) : __builtin_amdgcn_exp2f(-moved) - 1.f;
   if (fabsf(moved) <= kNear && fx > 0.f) return Move<V>{fx, (V)fx + (V)fx * less, (V)fx * less, held};
   const float fr = __builtin_amdgcn_exp2f((mr0 - mr) * s.c);
@@ -129,7 +129,7 @@ __device__ __forceinline__ void add_far(Apart& a, const float (&x)[E], const flo
     a.sx += e;
     a.sr += f;
     a.w += f - e;
-    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d, -FLT_MAX, FLT_MAX) * s.step, a.h);   // that of a masked token is finite, for e is 0
+    a.h = __builtin_fmaf(e, __builtin_amdgcn_fmed3f(d * s.step, -FLT_MAX, FLT_MAX), a.h);   // that of a masked token is finite, for e is 0
   }
 }
 

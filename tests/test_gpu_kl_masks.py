@@ -3,7 +3,7 @@ Rows and tolerances: those of the arithmetic's CPU test and of the kernels' own.
 import numpy as np
 import pytest
 
-from tests.test_gpu_more_ops import check_kl, kl_exact, kl_tolerance
+from tests.test_gpu_more_ops import check_kl, kl_exact, kl_tolerance, logits_pair
 from tests.test_gpu_ops import TYPES, close, dev, host, ops, tt
 from tests.test_kl_sums_cpu import rows_that_x_masks, rows_with_unlikely_tokens_that_r_masks
 
@@ -95,3 +95,16 @@ def test_gradient_where_the_scale_takes_differences_beyond_the_type(vocab, kind)
         run = y == np.float64(lowest(kind))
         a = np.where(run, a.max() - 14.0 / scale - np.log(vocab) / scale, a)
         check_kl(a, np.where(run, lowest(kind), b), kind, scale, what=f"scale {scale}")
+
+
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_enormous_scales(vocab):
+    for scale in (1e20, 1e30):
+        s32 = float(np.float32(scale))
+        for x, y in (logits_pair(8, vocab, 1), logits_pair(8, vocab, 2, 0.3, 2.0), rows_that_x_masks(vocab, lowest("fp32"))):
+            (xt, xv), (yt, yv) = dev(x[:24], "fp32"), dev(y[:24], "fp32")
+            want = kl_exact(xv, yv, s32)
+            kl, stats = ops().token_kl_forward(xt, yt, scale=scale)
+            close(kl, want[0], kl_tolerance(xv, yv, s32, want)[0], f"kl {scale}")
+            dx = ops().token_kl_backward(xt, yt, stats, kl.new_zeros(kl.shape).fill_(1e-30), scale=scale)[0]
+            assert bool(dx.isfinite().all())

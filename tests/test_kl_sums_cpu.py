@@ -114,3 +114,15 @@ def test_unlikely_tokens_that_r_masks_by_the_lowest(probe, form, vocab, low):
         x, y = rows_with_unlikely_tokens_that_r_masks(vocab, low, masked)
         for scale in (1.0, 0.5, 2.0):
             assert np.isfinite(check(probe, form, x, y, scale, (scale, masked))[:, 0]).all()
+
+
+@pytest.mark.parametrize("form,vocab", FORMS)
+def test_enormous_scales(probe, form, vocab):
+    """Scales that make p one token's, from which the others are 1e20 and more away, masked ones beyond the type."""
+    for scale in (1e20, 1e30):
+        s32 = float(np.float32(scale))
+        for x, y in (logits_pair(8, vocab, 1), logits_pair(8, vocab, 2, 0.3, 2.0), rows_that_x_masks(vocab, -3.4028234663852886e38), rows_that_x_masks(vocab, -65504.0)):
+            check(probe, form, x, y, s32, scale)
+    x, _ = logits_pair(8, vocab, 3)
+    for y in (x, x + 1.0):
+        assert np.isfinite(probe(form, x, y, 1e38)).all()
