@@ -272,8 +272,8 @@ __global__ __launch_bounds__(kBlock) void k_kl_back(Rows<T> a, float lift, float
     const bool r_empty = mr == -INFINITY;
     const float A = zero ? 0.f : mean < INFINITY ? g * a.scale : NAN;   // an infinite mean or none makes the whole row NaN
     // d - mean under an unlikely token may be beyond the type where the token's gradient is not: for dx a power of two goes from the scale over to g
-    const bool lifted = fabsf(A * lift) < INFINITY;
-    const float Ax = lifted ? A * lift : A, scale_d = lifted ? a.scale * drop : a.scale, mean_d = lifted ? mean * drop : mean;
+    float Ax = A, scale_d = a.scale, mean_d = mean;
+    if (lift != 1.f && fabsf(A * lift) < INFINITY) Ax *= lift, scale_d *= drop, mean_d *= drop;
     // d by way of x - r, or of the maxima where a constant lies between the rows
     const bool close_by = fabsf(mx - mr) <= kOffset;
     const float ux = close_by ? 0.f : mx, ur = close_by ? 0.f : mr, dm = close_by ? mx - mr : 0.f;
