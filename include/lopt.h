@@ -366,7 +366,8 @@ lopt_status lopt_token_logprobs_backward(const void* logits, int64_t ld, const i
  * mask[rows]: 0 where a row does not count, whose kl and stats are 0 and whose logits are not read; null: every row counts.
  * A token of which both logits are -infinity counts nothing, nor does one that x alone masks; one that r alone masks makes kl +infinity, however unlikely it is.
  * A row that x masks whole has kl 0. A row with a NaN or +infinity in either has kl NaN. Finite masks, to the type's lowest value, are numbers; a kl beyond
- * 1e38 may come out as +infinity, as may one of rows whose own logits are 3.4e38 apart. scale > 0, finite. workspace: lopt_token_kl_workspace bytes, may be null where that is 0.
+ * 1e38 may come out as +infinity, as may one of rows whose own logits are 3.4e38 apart. A token of p < 2^-126 counts as one of p = 0.
+ * scale > 0, finite. workspace: lopt_token_kl_workspace bytes, may be null where that is 0.
  * Errors: LOPT_EINVAL, LOPT_ESHAPE (rows, vocab or ld out of range; vocab <= LOPT_VOCAB_MAX), LOPT_EHIP. */
 size_t lopt_token_kl_workspace(int64_t rows, int64_t vocab);
 lopt_status lopt_token_kl(const void* logits, int64_t ld, const void* ref, int64_t ld_ref, const uint8_t* mask, int64_t rows,

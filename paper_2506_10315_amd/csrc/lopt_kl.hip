@@ -402,7 +402,7 @@ lopt_status lopt_token_kl_backward(const void* logits, int64_t ld, const void* r
     using T = decltype(t);
     const Rows<T> a{(const T*)logits, (const T*)ref, ld, ld_ref, rows, (uint32_t)vocab, scale, scale_of(std::fmin(scale * kLog2e, FLT_MAX)), mask};
     const int64_t packs = (vocab + 2 * Pack<T>::n - 2) / Pack<T>::n;   // that a row may touch
-    const float lift = std::ldexp(1.f, std::clamp(std::ilogb(scale) + 1, 0, 16));
+    const float lift = scale > 1.f ? std::ldexp(1.f, std::min(std::ilogb(scale) + 1, 16)) : 1.f;
     auto launch = [&](auto g) {
       constexpr int G = decltype(g)::value, kSpan = 2 * G;
       const int64_t spans = (packs + kSpan - kSpan / 8) / kSpan;

@@ -19,8 +19,9 @@ namespace {
 // sums alone; by 2e-4 with the maxima's products rounded as in the token log probabilities, for e and f are not 1 at them). `most`: the largest d that was
 // not near; it is infinite where r masks a token that x does not (or where finite logits are 3.4e38 apart). A NaN makes the maximum and by it the sums NaN.
 struct Apart { float mx, mr, sx, sr, w, h, most; };
-// c, and a power of two by which it is 2^-26 to 2^-25. A lane whose tokens x masks all by a finite value has that value as its maximum and e = 1 for them, and r may have the type's lowest
-// there, c d being beyond the type: in this unit the sum of 2^25 of them is finite until the row's maxima take it away. (From c = 2^75 on the unit stays, and fewer are: rebase drops what is nothing beside the row's maxima even if it is infinite.)
+// c, and a power of two by which it is 2^-26 to 2^-25. A lane whose tokens x masks all by a finite value has that value as its maximum and e = 1 for them, and r may have the type's
+// lowest there, c d being beyond the type: in this unit the sum of 2^25 of them is finite until the row's maxima take it away. (From c = 2^75 on the unit stays, and fewer are: rebase
+// drops what is nothing beside the row's maxima even if it is infinite.)
 struct Scale { float c, unit, step; };   // step = c unit, which differences near the type's largest are multiplied by at once
 inline Scale scale_of(float c) {
   const float unit = std::ldexp(1.f, -std::clamp(std::ilogb(c) + 26, -100, 100));
